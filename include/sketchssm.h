@@ -275,6 +275,91 @@ int sketchssm_step_host(sketchssm_ctx* ctx, int op, int n_before, const void* ho
                         const void* host_v, const void* host_beta, const void* host_decay, void* host_out,
                         const sketchssm_staging* staging, uint32_t flags, void* stream);
 
+/* ---- The operators around the recurrence ------------------------------------------------------------------------------
+ * What a layer runs before and after the calls above: the short convolution and the gates that make the token tensors, the
+ * scan of a prompt that leaves the state a decode starts from, the norms, and the projections in 8 bits.  They obey the
+ * general rules (device pointers, 16-byte aligned; the caller's stream; nothing allocated, nothing synchronised; bounded
+ * waits reported through the status block, so the context must be bound), and take row strides in elements: the distance
+ * between the rows of two tokens, a multiple of 16 bytes and at least a row, so that column ranges of a wider matrix (a
+ * projection's output) go in as they are.  "io" is config.io_dtype.  Everything between input and output is fp32.
+ * Tensors of one call do not overlap unless a call's description says so. */
+
+/* A batch of prompts packed one behind another along the token axis.  Device arrays, read by the kernels (4-byte aligned). */
+typedef struct sketchssm_prompts {
+    int32_t sequences;      /* N >= 0 */
+    int32_t tokens;         /* T >= 0: rows of the packed tensors */
+    const int32_t* starts;  /* [N + 1] ascending: sequence i is the rows starts[i] .. starts[i + 1] - 1 (none, one or more); rows
+                               outside starts[0] .. starts[N] are neither read nor written */
+    const int32_t* slots;   /* [N]: the batch entry that keeps sequence i's state, or NULL: i.  The entries of one call are distinct.
+                               An entry outside 0..B-1: the sequence's state is not kept (its outputs are written) */
+    const int32_t* resume;  /* [N]: the batch entry whose stored state sequence i goes on from (its own, or another one that no
+                               sequence of the call writes), outside 0..B-1: it starts from zeros.  NULL: all start from zeros */
+} sketchssm_prompts;
+
+/* flags of sketchssm_causal_conv */
+#define SKETCHSSM_SILU 0x1u            /* out = y / (1 + exp(-y)) of the convolution's y */
+
+/* Short causal convolution of every channel over packed prompts:
+ *     y[t][c] = bias[c] + sum_{j < W} weight[c][j] x[t - (W - 1) + j][c]      within a sequence,
+ * where rows before a sequence's start come from the stored rows of its resume entry, or are zeros.  Afterwards the rows of its
+ * slot hold the last W - 1 rows of (stored rows, prompt).  Any kind of context.
+ *   width W      : 2..4;  channels: a multiple of 16 bytes of io
+ *   weight, bias : [channels][W], [channels] fp32 (bias may be NULL)
+ *   state        : [B][W - 1][channels] io, oldest row first
+ *   x, out       : [T][channels] io, strided */
+int sketchssm_causal_conv(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int channels, int width, const void* weight,
+                          const void* bias, void* state, const void* x, int64_t x_stride, void* out, int64_t out_stride,
+                          uint32_t flags, void* stream);
+
+/* The same for one token of every batch entry, with SiLU and the gates, written as the token tensors that the decode calls take
+ * (Mamba-2; channels in the order v [H][V], k [G][K], q [G][K], a group's k and q going to its H / G heads):
+ *     beta = softplus(dt + dt_bias),  decay = exp(a beta).
+ * The stored rows of every entry move on by one.  x [B][H V + 2 G K] io and dt [B][H] io strided (dt's stride is free of the
+ * 16-byte rule); a [H] fp32; dt_bias [H] fp32 or NULL; groups G divides H; q, k, v, beta, decay as in sketchssm_decode_step. */
+int sketchssm_conv_step(sketchssm_ctx* ctx, int groups, int width, const void* weight, const void* bias, void* state,
+                        const void* x, int64_t x_stride, const void* dt, int64_t dt_stride, const void* a,
+                        const void* dt_bias, void* q, void* k, void* v, void* beta, void* decay, void* stream);
+
+/* Bytes of `work` that sketchssm_prompt_scan needs for batches of at most this many sequences and tokens (may be 0).
+ * Host-only.  The scratch is transient; calls that overlap on the GPU need separate ones. */
+int sketchssm_prompt_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes);
+
+/* Selective scan over packed prompts (Mamba-2): per sequence and head, token by token
+ *     beta = softplus(dt + dt_bias),  S <- exp(a beta) S + beta k v^T,  out = S^T q + skip v,
+ * from the bound state of the sequence's resume entry (or zeros) into the bound state of its slot.  The sketch and the maps are
+ * not touched: a sketchssm_state_update without a token builds them before the first decode step.
+ *   q, k : [T][G][K] io strided, a group for H / G heads;  v : [T][H][V] io strided;  dt : [T][H] io (stride free of the 16-byte
+ *   rule);  a [H] fp32, <= 0;  dt_bias, skip [H] fp32 or NULL;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked
+ *   here, the call says it. */
+int sketchssm_prompt_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, const void* q, int64_t q_stride,
+                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* dt, int64_t dt_stride,
+                          const void* a, const void* dt_bias, const void* skip, void* out, int64_t out_stride, int out_dtype,
+                          void* work, size_t work_bytes, void* stream);
+
+/* Root-mean-square norm of rows, in groups of `group` elements (0: the row):
+ *     h = x;   with residual: h = x + residual, and residual_out = h (before rounding to io h goes on);
+ *              with gate:     h = (x + skip skip_weight) gate / (1 + exp(-gate))     (skip optional)
+ *     y = h / sqrt(mean(h^2) + eps) weight
+ * to out (io) and/or in 8 bits: for each block of 128 elements of a row scale = max|y| / 448 and out8 = e4m3(y 448 / max|y|), to
+ * nearest even (a block whose largest value is below 1e-30 is stored as zeros).
+ *   rows >= 0; width a multiple of 8, at most 16384; group: a divisor of width that is a multiple of 128
+ *   x [rows][width] of x_dtype strided; weight [width] fp32; residual, residual_out [rows][width] io, dense, both or none,
+ *   residual_out may be residual; gate, skip [rows][width] io strided; skip_weight [skip_heads] fp32, skip_heads divides width (element e uses
+ *   skip_weight[e / (width / skip_heads)]); out [rows][width] io dense; out8 [rows][width] bytes and scale
+ *   [rows][(width + 127) / 128] fp32, both or none.  residual and gate exclude one another. */
+int sketchssm_rms_norm(sketchssm_ctx* ctx, int rows, int width, int group, float eps, const void* x, int64_t x_stride,
+                       int x_dtype, const void* weight, const void* residual, void* residual_out, const void* gate,
+                       int64_t gate_stride, const void* skip, int64_t skip_stride, const void* skip_weight, int skip_heads,
+                       void* out, void* out8, void* scale, void* stream);
+
+/* Product of 8-bit matrices (e4m3) with a scale for each block of 128 along the inner axis, and of 128 x 128 for the weights:
+ *     out[m][n] = sum_b a_scale[m][b] w_scale[n / 128][b] sum_{k in block b} a[m][k] w[n][k]
+ *   rows >= 0, cols >= 1; inner >= 16, a multiple of 16; a [rows][inner], w [cols][inner] dense; a_scale [rows][(inner + 127) / 128],
+ *   w_scale [(cols + 127) / 128][(inner + 127) / 128] fp32 (4-byte aligned); out [rows][cols] of out_dtype, its stride at least cols, free of the 16-byte
+ *   rule.  Products inside a block are summed in fp32 by the tensor cores, blocks in fp32. */
+int sketchssm_scaled_matmul(sketchssm_ctx* ctx, int rows, int cols, int inner, const void* a, const void* a_scale,
+                            const void* w, const void* w_scale, void* out, int64_t out_stride, int out_dtype, void* stream);
+
 /* Copy the status word back (synchronises `stream`).  Returns SKETCHSSM_OK if no kernel
  * recorded a fault, SKETCHSSM_DEVICE_TIMEOUT otherwise; `detail`, if not NULL, receives the
  * four status ints. */

@@ -20,6 +20,7 @@ DTYPE = {"f32": 0, "bf16": 1}
 TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 NO_SKETCH = 0x1
 NO_APPEND = 0x1
+SILU = 0x1
 
 EXPORTED = (
     "sketchssm_create", "sketchssm_destroy", "sketchssm_query_sizes", "sketchssm_bind",
@@ -27,6 +28,8 @@ EXPORTED = (
     "sketchssm_read_status", "sketchssm_last_launch_count", "sketchssm_tune",
     "sketchssm_status_string", "sketchssm_version", "sketchssm_last_cuda_error", "sketchssm_step_host",
     "sketchssm_decode_step_static", "sketchssm_selftest_wait_timeout", "sketchssm_step_mixed",
+    "sketchssm_causal_conv", "sketchssm_conv_step", "sketchssm_prompt_work_bytes", "sketchssm_prompt_scan",
+    "sketchssm_rms_norm", "sketchssm_scaled_matmul",
 )
 OP_DECODE, OP_FULL_READ, OP_UPDATE = 0, 1, 2
 
@@ -52,6 +55,33 @@ class Buffers(ctypes.Structure):
 
 class Staging(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "beta", "decay", "out")]
+
+
+class PromptBatch(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int32), ("tokens", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in
+                                                                             ("starts", "slots", "resume")]
+
+
+class Prompts:
+    """Prompts packed one behind another along the token axis: sequence i is the rows starts[i] .. starts[i + 1] - 1 of `tokens`.
+
+    starts [N + 1], slots [N] (the batch entry that keeps a sequence's state; None: i) and resume [N] (the batch entry whose
+    state it goes on from, -1: none; None: no sequence does) are int32 tensors on the device, read when the kernels run."""
+
+    def __init__(self, starts: torch.Tensor, tokens: int, slots: Optional[torch.Tensor] = None,
+                 resume: Optional[torch.Tensor] = None):
+        self.sequences, self.tokens = starts.numel() - 1, int(tokens)
+        if self.sequences < 0 or self.tokens < 0:
+            raise ValueError("starts holds one row number more than there are sequences, and tokens is not negative")
+        for name, t, n in (("starts", starts, self.sequences + 1), ("slots", slots, self.sequences), ("resume", resume, self.sequences)):
+            if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
+                raise ValueError(f"{name} is a dense int32 tensor of {n} entries")
+        self.starts, self.slots, self.resume = starts, slots, resume
+        self.c = PromptBatch(self.sequences, self.tokens, _ptr(starts), _ptr(slots), _ptr(resume))
+        self.ref = ctypes.byref(self.c)
+
+    def on(self, device: torch.device) -> bool:
+        return all(t is None or t.device == device for t in (self.starts, self.slots, self.resume))
 
 
 class SketchSSMError(RuntimeError):
@@ -84,6 +114,16 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sketchssm_step_mixed.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, u32, vp]
     lib.sketchssm_step_host.argtypes = [vp, i32, i32, vp, vp, vp, vp, vp, vp, ctypes.POINTER(Staging), u32, vp]
     lib.sketchssm_selftest_wait_timeout.argtypes = [vp, i32, i32, vp]
+    i64 = ctypes.c_int64
+    pb = ctypes.POINTER(PromptBatch)
+    lib.sketchssm_causal_conv.argtypes = [vp, pb, i32, i32, vp, vp, vp, vp, i64, vp, i64, u32, vp]
+    lib.sketchssm_conv_step.argtypes = [vp, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sketchssm_prompt_work_bytes.argtypes = [vp, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sketchssm_prompt_scan.argtypes = [vp, pb, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, i32, vp,
+                                          ctypes.c_size_t, vp]
+    lib.sketchssm_rms_norm.argtypes = [vp, i32, i32, i32, ctypes.c_float, vp, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, i32,
+                                       vp, vp, vp, vp]
+    lib.sketchssm_scaled_matmul.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, i64, i32, vp]
     lib.sketchssm_read_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32 * 4), vp]
     lib.sketchssm_last_launch_count.argtypes = [vp]
     lib.sketchssm_tune.argtypes = [vp, ctypes.c_char_p, i32]
@@ -105,6 +145,10 @@ _RAW_STREAM, _DEVICE = getattr(torch._C, "_cuda_getCurrentRawStream", None), get
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()       # (the declared argument types make the C pointer of it)
+
+
+_CODE = {torch.float32: 0, torch.bfloat16: 1}
+_E4M3 = torch.float8_e4m3fn
 
 
 class SketchSSM:
@@ -271,6 +315,143 @@ class SketchSSM:
         if rc:
             self._check("sketchssm_step_host", rc)
         return host["out"]
+
+    # -- the operators around the recurrence ---------------------------------------------------
+    def _want(self, ok: bool, text: str):
+        if not ok:
+            raise ValueError(text)
+
+    def _rows(self, name: str, t: torch.Tensor, dtype: torch.dtype, *shape) -> int:
+        """Checks a tensor whose rows (first axis) may be strided; returns the row stride in elements."""
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device:
+            raise ValueError(f"{name} is a {dtype} tensor {tuple(shape)} on {self.device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
+        n = t.dim()
+        if n == 2:
+            inner = t.stride(1) == 1 or shape[1] == 1
+            row = shape[1]
+        else:
+            inner = (t.stride(2) == 1 or shape[2] == 1) and (t.stride(1) == shape[2] or shape[1] == 1)
+            row = shape[1] * shape[2]
+        if not inner:
+            raise ValueError(f"{name}: the elements of a row are dense")
+        return t.stride(0) if shape[0] > 1 else row
+
+    def _dense(self, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, *shape) -> Optional[int]:
+        """Checks a dense tensor (None passes); returns its address."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name} is a dense {dtype} tensor {tuple(shape)} on {self.device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def new_conv_state(self, channels: int, width: int) -> torch.Tensor:
+        """Zeroed stored rows [B, width - 1, channels] of the short convolution."""
+        return torch.zeros(self.B, width - 1, channels, dtype=TORCH_DTYPE[self.io], device=self.device)
+
+    def causal_conv(self, prompts: Prompts, x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
+                    state: torch.Tensor, out: torch.Tensor, silu: bool = True, stream=None) -> torch.Tensor:
+        """sketchssm_causal_conv: the short causal convolution of packed prompts x [T, C] into out; weight [C, W] f32, bias [C]
+        f32 or None, state [B, W - 1, C] holds the stored rows and is moved on."""
+        io, T = TORCH_DTYPE[self.io], prompts.tokens
+        self._want(prompts.on(self.device) and weight.dim() == 2, "prompts lie on the layer's device, and weight is [C, W]")
+        C, W = weight.shape
+        xs, os_ = self._rows("x", x, io, T, C), self._rows("out", out, io, T, C)
+        rc = self.lib.sketchssm_causal_conv(
+            self._ctx, prompts.ref, C, W, self._dense("weight", weight, torch.float32, C, W),
+            self._dense("bias", bias, torch.float32, C), self._dense("state", state, io, self.B, W - 1, C), x.data_ptr(), xs,
+            out.data_ptr(), os_, SILU if silu else 0, self._stream(stream))
+        if rc:
+            self._check("sketchssm_causal_conv", rc)
+        return out
+
+    def conv_step(self, x: torch.Tensor, dt: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
+                  state: torch.Tensor, a: torch.Tensor, dt_bias: Optional[torch.Tensor], token: dict, groups: int = 1,
+                  stream=None) -> dict:
+        """sketchssm_conv_step: one token of every batch entry, x [B, H V + 2 G K] and dt [B, H], into the q, k, v, beta, decay of
+        `token` (new_token_buffers), which the decode calls take."""
+        B, H, K, V = self.B, self.H, self.K, self.V
+        io, C, W = TORCH_DTYPE[self.io], H * V + 2 * groups * K, weight.shape[-1]
+        f32 = torch.float32
+        xs, ds = self._rows("x", x, io, B, C), self._rows("dt", dt, io, B, H)
+        rc = self.lib.sketchssm_conv_step(
+            self._ctx, groups, W, self._dense("weight", weight, f32, C, W), self._dense("bias", bias, f32, C),
+            self._dense("state", state, io, B, W - 1, C), x.data_ptr(), xs, dt.data_ptr(), ds, self._dense("a", a, f32, H),
+            self._dense("dt_bias", dt_bias, f32, H), self._dense("q", token["q"], io, B, H, K),
+            self._dense("k", token["k"], io, B, H, K), self._dense("v", token["v"], io, B, H, V),
+            self._dense("beta", token["beta"], f32, B, H), self._dense("decay", token["decay"], f32, B, H), self._stream(stream))
+        if rc:
+            self._check("sketchssm_conv_step", rc)
+        return token
+
+    def new_prompt_work(self, sequences: int, tokens: int) -> Optional[torch.Tensor]:
+        """Scratch of prompt_scan for batches of at most this many sequences and tokens (None: none is needed)."""
+        n = ctypes.c_size_t()
+        self._check("sketchssm_prompt_work_bytes", self.lib.sketchssm_prompt_work_bytes(self._ctx, sequences, tokens, ctypes.byref(n)))
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device) if n.value else None
+
+    def prompt_scan(self, prompts: Prompts, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, dt: torch.Tensor, a: torch.Tensor,
+                    out: torch.Tensor, dt_bias: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None,
+                    work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """sketchssm_prompt_scan: the selective scan of packed prompts, q, k [T, G, K], v [T, H, V], dt [T, H] in io, a [H] f32, into
+        out [T, H, V] (f32 or bf16) and the bound state.  work: new_prompt_work (allocated here if None)."""
+        io, T, H, f32 = TORCH_DTYPE[self.io], prompts.tokens, self.H, torch.float32
+        self._want(prompts.on(self.device) and q.dim() == 3 and out.dtype in _CODE,
+                   "prompts lie on the layer's device, q is [T, G, K], and out is f32 or bf16")
+        G = q.shape[1]
+        qs, ks = self._rows("q", q, io, T, G, self.K), self._rows("k", k, io, T, G, self.K)
+        vs, ds = self._rows("v", v, io, T, H, self.V), self._rows("dt", dt, io, T, H)
+        os_ = self._rows("out", out, out.dtype, T, H, self.V)
+        if work is None:
+            work = self.new_prompt_work(prompts.sequences, T)
+        self._want(work is None or (work.device == self.device and work.is_contiguous()), "work is a dense tensor on the layer's device")
+        rc = self.lib.sketchssm_prompt_scan(
+            self._ctx, prompts.ref, G, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dt.data_ptr(), ds,
+            self._dense("a", a, f32, H), self._dense("dt_bias", dt_bias, f32, H), self._dense("skip", skip, f32, H),
+            out.data_ptr(), os_, _CODE[out.dtype], _ptr(work), 0 if work is None else work.numel() * work.element_size(),
+            self._stream(stream))
+        if rc:
+            self._check("sketchssm_prompt_scan", rc)
+        return out
+
+    def rms_norm(self, x: torch.Tensor, weight: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 out8: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                 residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None,
+                 gate: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None,
+                 skip_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, group: int = 0, stream=None):
+        """sketchssm_rms_norm: the norm of x [T, D] (f32 or bf16) with the residual's addition, or the skip and the gate, before it;
+        into out (io) and/or out8 [T, D] e4m3 with scale [T, ceil(D / 128)]."""
+        io, f32 = TORCH_DTYPE[self.io], torch.float32
+        self._want(x.dim() == 2 and x.dtype in _CODE, "x is [T, D], f32 or bf16")
+        T, D = x.shape
+        xs = self._rows("x", x, x.dtype, T, D)
+        gs = self._rows("gate", gate, io, T, D) if gate is not None else 0
+        ss = self._rows("skip", skip, io, T, D) if skip is not None else 0
+        heads = skip_weight.numel() if skip_weight is not None else 0
+        rc = self.lib.sketchssm_rms_norm(
+            self._ctx, T, D, group, eps, x.data_ptr(), xs, _CODE[x.dtype], self._dense("weight", weight, f32, D),
+            self._dense("residual", residual, io, T, D), self._dense("residual_out", residual_out, io, T, D), _ptr(gate), gs,
+            _ptr(skip), ss, self._dense("skip_weight", skip_weight, f32, heads), heads, self._dense("out", out, io, T, D),
+            self._dense("out8", out8, _E4M3, T, D), self._dense("scale", scale, f32, T, -(-D // 128)), self._stream(stream))
+        if rc:
+            self._check("sketchssm_rms_norm", rc)
+        return out if out is not None else out8
+
+    def scaled_matmul(self, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torch.Tensor,
+                      stream=None) -> torch.Tensor:
+        """sketchssm_scaled_matmul: out [M, N] (f32 or bf16) = a [M, K] w [N, K]^T in e4m3, with a_scale [M, ceil(K / 128)] and
+        w_scale [ceil(N / 128), ceil(K / 128)]."""
+        f32 = torch.float32
+        self._want(a.dim() == 2 and w.dim() == 2 and out.dtype in _CODE, "a is [M, K], w [N, K], and out f32 or bf16")
+        (M, K), N = a.shape, w.shape[0]
+        kb = -(-K // 128)
+        os_ = self._rows("out", out, out.dtype, M, N)
+        rc = self.lib.sketchssm_scaled_matmul(
+            self._ctx, M, N, K, self._dense("a", a, _E4M3, M, K), self._dense("a_scale", a_scale, f32, M, kb),
+            self._dense("w", w, _E4M3, N, K), self._dense("w_scale", w_scale, f32, -(-N // 128), kb), out.data_ptr(), os_,
+            _CODE[out.dtype], self._stream(stream))
+        if rc:
+            self._check("sketchssm_scaled_matmul", rc)
+        return out
 
     def selftest_wait_timeout(self, poll_limit: int = 2048, where: int = 99, stream=None):
         """sketchssm_selftest_wait_timeout: one warp whose bounded wait runs out and reports through the status block."""

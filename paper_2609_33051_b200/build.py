@@ -10,14 +10,18 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsketchssm.so")
+# the operators around the recurrence
+LAYER_UNITS = ("api_layer.cu", "conv.cu", "prompt_scan.cu", "rms_norm.cu", "scaled_matmul.cu")
 # (source, object suffix, extra defines); the decodes are compiled once per (recurrence kind, I/O type)
 UNITS = [("api.cu", "", []), ("update.cu", "", []), ("update_cols.cu", "", []), ("update_tc.cu", "", []),
          ("update_tc_ws.cu", "", []), ("update_tc_ws_gdn.cu", "", []), ("update_tc_ws_kda.cu", "", []), ("decode_static.cu", "", []), ("selftest.cu", "", []), ("coef_map.cu", "", []), ("coef_map_pivot.cu", "", []),
          *[(src, f"_k{k}_io{io}", [f"-DSKETCHSSM_GROUP_KIND={k}", f"-DSKETCHSSM_GROUP_IO={io}"])
-           for src in ("decode.cu", "decode_split.cu") for k in range(3) for io in range(2)]]
+           for src in ("decode.cu", "decode_split.cu") for k in range(3) for io in range(2)],
+         *[(src, "", []) for src in LAYER_UNITS]]
 HEADERS = [os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "lanegroup.cuh"), os.path.join(CSRC, "tc_common.cuh"),
            os.path.join(CSRC, "state_rows.h"), os.path.join(CSRC, "operand_sets.h"), os.path.join(CSRC, "team_size.h"),
            os.path.join(ROOT, "include", "sketchssm.h")]
+LAYER_HEADERS = [os.path.join(CSRC, "layer.cuh")]      # of the operators around the recurrence alone
 
 
 def _nvcc() -> str:
@@ -48,7 +52,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         sp = os.path.join(CSRC, src)
         obj = os.path.join(objdir, src.replace(".cu", suffix + ".o"))
         objs.append(obj)
-        if force or _stale(obj, [sp] + HEADERS):
+        if force or _stale(obj, [sp] + HEADERS + (LAYER_HEADERS if src in LAYER_UNITS else [])):
             procs.append((src + suffix, subprocess.Popen([nvcc, *flags, *defs, "-c", sp, "-o", obj],
                                                 stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for src, pr in procs:

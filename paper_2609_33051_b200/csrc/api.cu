@@ -5,19 +5,7 @@
 
 using namespace sketchssm;
 
-struct sketchssm_ctx : public Ctx {
-    int tune_batches_per_cta;
-    int tune_stages;
-    int tune_warps_per_cta;
-    int tune_decode_impl;   // 0: two kernels (weights + output rows), 1: warp-per-head kernel
-    int tune_max_warps;
-    int tune_update_impl;
-    int tune_pdl;
-};
-
 namespace {
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 RingLayout ring_layout(const sketchssm_config& c, int io) {
     RingLayout r;
@@ -66,13 +54,6 @@ Params base_params(const sketchssm_ctx* ctx) {
     p.sketch_bf16 = ctx->cfg.sketch_dtype == SKETCHSSM_BF16;
     p.erase = ctx->cfg.erase_factors ? static_cast<float*>(ctx->bufs.erase) : nullptr;
     return p;
-}
-
-int set_device(const sketchssm_ctx* ctx) {
-    int cur = -1;
-    if (cudaGetDevice(&cur) != cudaSuccess) return SKETCHSSM_CUDA_ERROR;
-    if (cur != ctx->cfg.device && cudaSetDevice(ctx->cfg.device) != cudaSuccess) return SKETCHSSM_CUDA_ERROR;
-    return SKETCHSSM_OK;
 }
 
 // Argument checks shared by every decode entry point, then the parameter block of a decode launch.

@@ -115,6 +115,15 @@ int launch_update_tc_ws(Ctx* ctx, const Params& p, cudaStream_t stream); // same
 int launch_update_tc_ws_gdn(Ctx* ctx, const Params& p, cudaStream_t stream); // gated delta rule, warp-specialised, the state read once
 int launch_update_tc_ws_kda(Ctx* ctx, const Params& p, cudaStream_t stream); // delta rule with per-channel decay, warp-specialised, up to 32 tokens per pass
 
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+inline int set_device(const Ctx* ctx) {
+    int cur = -1;
+    if (cudaGetDevice(&cur) != cudaSuccess) return SKETCHSSM_CUDA_ERROR;
+    if (cur != ctx->cfg.device && cudaSetDevice(ctx->cfg.device) != cudaSuccess) return SKETCHSSM_CUDA_ERROR;
+    return SKETCHSSM_OK;
+}
+
 // ---------------------------------------------------------------------------------------------
 // device helpers
 // ---------------------------------------------------------------------------------------------
@@ -327,3 +336,14 @@ __device__ __forceinline__ void store_io(__nv_bfloat16* base, int idx, const flo
 #endif  // __CUDACC__
 
 }  // namespace sketchssm
+
+// The context behind the C ABI: what every kernel launch needs, and the launch tuning.
+struct sketchssm_ctx : public sketchssm::Ctx {
+    int tune_batches_per_cta;
+    int tune_stages;
+    int tune_warps_per_cta;
+    int tune_decode_impl;   // 0: two kernels (weights + output rows), 1: warp-per-head kernel
+    int tune_max_warps;
+    int tune_update_impl;
+    int tune_pdl;
+};
