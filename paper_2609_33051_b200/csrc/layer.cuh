@@ -97,17 +97,21 @@ inline int sm_count(Ctx* ctx) {
 // Launch with the programmatic-stream-serialization attribute.  The kernels wait for their predecessor before anything else and
 // only then let their successor start: a successor that reads ahead of its own wait never overtakes what came before them.
 template <typename P>
-inline int launch_layer(Ctx* ctx, void (*kern)(const P), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const P& p) {
+inline int launch_layer(Ctx* ctx, void (*kern)(const P), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const P& p,
+                        int cluster = 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = static_cast<sketchssm_ctx*>(ctx)->tune_pdl ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
     if (e != cudaSuccess) {
         ctx->last_cuda_error = e;

@@ -1,64 +1,286 @@
-// Product of e4m3 matrices with a scale for each block of 128 along the inner axis (and 128 rows of the weights).
+// Product of e4m3 matrices with a scale for each block of 128 along the inner axis (and 128 rows of the weights), on tcgen05.
 //
 //     out[m][n] = sum_b a_scale[m][b] w_scale[n / 128][b] sum_{k in block b} a[m][k] w[n][k]
-#include "layer.cuh"
-
-#include <cuda_fp8.h>
+//
+// The weights are the 128-row operand and the tokens the BN-column one: an accumulator lane is a weight row, a column a token.
+// So a few tokens cost a narrow accumulator instead of a mostly empty 128-row one, the weights' scale is one number per tile and
+// block, and a warp's stores of a token are 32 neighbouring elements of its row, whatever the row stride and the edges are.
+// Each block of 128 goes through the tensor cores into an accumulator of its own (fp32, in tensor memory); the epilogue warps
+// add it, times its scales, to sums in registers, two elements an instruction, while the next block is multiplied.
+//
+// Roles: one thread issues the copies (TMA, 128-byte swizzle: a row of a tile is exactly one block), one the products; two warps
+// fetch the token scales one block ahead and leave them, times the weights' scale, in shared memory; the other warps add.
+// With few tiles (a decode step) the blocks are split over a cluster of up to eight CTAs that add their sums through distributed
+// shared memory in the order of their ranks.
+#include "tma.cuh"
 
 namespace sketchssm {
 
 namespace {
 
-constexpr int kTile = 32;
+using namespace tc;
 
-__device__ __forceinline__ float e4m3(unsigned char x) {
-    const __half_raw h = __nv_cvt_fp8_to_halfraw(x, __NV_E4M3);
-    return __half2float(__half(h));
-}
+struct MatmulArgs {
+    CUtensorMap tw, ta;
+    MatmulParams p;
+    int ks, n_tiles, tiles;
+};
 
-__global__ void __launch_bounds__(256) scaled_matmul_kernel(const MatmulParams p) {
-    __shared__ float sa[kTile][kTile + 1], sw[kTile][kTile + 1];
+__device__ __forceinline__ void put(float* o, float y) { *o = y; }
+__device__ __forceinline__ void put(__nv_bfloat16* o, float y) { *o = __float2bfloat16_rn(y); }
+
+// AS accumulators of BN columns, NS stages of operand tiles, EW epilogue warps.
+template <int BN, int EW, int NS, int AS>
+struct MatmulSmem {
+    static constexpr uint32_t kW = 128u * 128u, kA = (uint32_t)BN * 128u, kStage = kW + kA;
+    static constexpr uint32_t kScales = NS * kStage;                       // [AS][BN] floats
+    static constexpr uint32_t kBars = kScales + AS * BN * 4u;
+    static constexpr uint32_t kTotal = kBars + (2 * NS + 3 * AS) * 8u + 16u;
+    static constexpr uint32_t kBytes = kTotal + 1024u;                     // (the tiles start on 1024 bytes)
+    static_assert(BN * 128u * 4u <= NS * kStage, "the sums of a split tile take the stages' place");
+};
+
+template <int BN, int EW, int NS, int AS, int MINB>
+__global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(const __grid_constant__ MatmulArgs g) {
+    using L = MatmulSmem<BN, EW, NS, AS>;
+    constexpr int CW = BN / (EW / 4);                  // accumulator columns of an epilogue warp
+    constexpr int CH = CW < 32 ? CW : 32;              // of one load
+    constexpr int TM = AS * BN < 32 ? 32 : AS * BN;
+    extern __shared__ unsigned char raw[];
+    unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    float* scales = reinterpret_cast<float*>(smem + L::kScales);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+    uint64_t *empty = full + NS, *acc_full = empty + NS, *acc_empty = acc_full + AS, *sc_full = acc_empty + AS;
+    uint32_t* slot = reinterpret_cast<uint32_t*>(sc_full + AS);
+    const MatmulParams& p = g.p;
+    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int i = 0; i < NS; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
+        for (int i = 0; i < AS; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, EW); mbar_init(sc_full + i, 2); }
+        mbar_fence_init();
+    }
+    if (warp == 1) tmem_alloc<TM>(slot);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
     grid_dep_wait();
     grid_dep_launch_dependents();
-    const int tid = (int)threadIdx.x, tn = tid & 31, tm = tid >> 5;
-    const int m0 = (int)blockIdx.y * kTile, n0 = (int)blockIdx.x * kTile;
-    float acc[4] = {};
-    for (int b = 0; b < p.KB; ++b) {
-        float part[4] = {};
-        for (int k0 = b * 128; k0 < min(p.K, b * 128 + 128); k0 += kTile) {
-            __syncthreads();
-            for (int i = tid; i < kTile * kTile; i += 256) {
-                const int r = i / kTile, k = k0 + i % kTile;
-                sa[r][i % kTile] = m0 + r < p.M && k < p.K ? e4m3(p.a[(size_t)(m0 + r) * p.K + k]) : 0.f;
-                sw[r][i % kTile] = n0 + r < p.N && k < p.K ? e4m3(p.w[(size_t)(n0 + r) * p.K + k]) : 0.f;
+    const uint32_t tmem = *slot;
+    const int rank = (int)blockIdx.x % g.ks, first = (int)blockIdx.x / g.ks, step = (int)gridDim.x / g.ks;
+    const int kb0 = p.KB * rank / g.ks, kb1 = p.KB * (rank + 1) / g.ks;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int tile = first; tile < g.tiles && ok; tile += step) {
+                const int n0 = tile % g.n_tiles * 128, m0 = tile / g.n_tiles * BN;
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % NS;
+                    if (it >= NS && !mbar_wait_bounded(empty + s, (it / NS - 1) & 1)) {
+                        record_fault(p.status, kFaultMatmulWait, 1);
+                        ok = false;
+                        break;
+                    }
+                    mbar_expect_tx(full + s, L::kStage);
+                    tma_load(smem + s * L::kStage, &g.tw, kb * 128, n0, full + s);
+                    tma_load(smem + s * L::kStage + L::kW, &g.ta, kb * 128, m0, full + s);
+                }
             }
-            __syncthreads();
-            for (int k = 0; k < kTile; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[i] = fmaf(sa[tm * 4 + i][k], sw[tn][k], part[i]);
+            // no copy may be under way when the CTA ends (after a fault; otherwise all of them have been waited for)
+            for (int i = it < NS ? 0 : it - NS; i < it; ++i) mbar_wait_bounded(full + i % NS, (i / NS) & 1);
         }
-        const int n = n0 + tn;
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);      // e4m3 x e4m3 -> fp32
+            int it = 0;
+            bool ok = true;
+            for (int tile = first; tile < g.tiles && ok; tile += step) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = it % NS, as = it % AS;
+                    ok = it < AS || mbar_wait_bounded(acc_empty + as, (it / AS - 1) & 1);
+                    ok = ok && mbar_wait_bounded(full + s, (it / NS) & 1);
+                    if (!ok) {
+                        record_fault(p.status, kFaultMatmulWait, 2);
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t base = smem_u32(smem) + (uint32_t)s * L::kStage;
+                    const uint64_t dw = swizzled_desc(base, 16u, 1024u), da = swizzled_desc(base + L::kW, 16u, 1024u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = m0 + tm * 4 + i;
-            if (m < p.M && n < p.N) acc[i] = fmaf(p.a_scale[(size_t)m * p.KB + b] * p.w_scale[(size_t)(n / 128) * p.KB + b], part[i], acc[i]);
+                    for (int j = 0; j < 4; ++j)        // 32 bytes of every row at a time
+                        asm volatile(
+                            "{\n\t.reg .pred p;\n\t"
+                            "setp.ne.b32 p, %4, 0;\n\t"
+                            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * BN)),
+                            "l"(dw + 2u * j), "l"(da + 2u * j), "r"(idesc), "r"((uint32_t)j)
+                            : "memory");
+                    tc_commit(empty + s);
+                    tc_commit(acc_full + as);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        constexpr int PT = (BN + 63) / 64;             // tokens of a thread
+        const int t = tid - 64;
+        int it = 0;
+        bool ok = true;
+        for (int tile = first; tile < g.tiles && ok; tile += step) {
+            const float* sw = p.w_scale + (size_t)(tile % g.n_tiles) * p.KB;
+            const int m0 = tile / g.n_tiles * BN;
+            auto fetch = [&](int kb, int i) {
+                const int m = m0 + t + 64 * i;
+                return t + 64 * i < BN && m < p.M ? p.a_scale[(size_t)m * p.KB + kb] * sw[kb] : 0.f;
+            };
+            float next[PT];
+#pragma unroll
+            for (int i = 0; i < PT; ++i) next[i] = fetch(kb0, i);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int as = it % AS;
+                ok = it < AS || mbar_wait_bounded(acc_empty + as, (it / AS - 1) & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) {
+                    if (lane == 0) record_fault(p.status, kFaultMatmulWait, 3);
+                    break;
+                }
+#pragma unroll
+                for (int i = 0; i < PT; ++i) {
+                    if (t + 64 * i < BN) scales[as * BN + t + 64 * i] = next[i];
+                    if (kb + 1 < kb1) next[i] = fetch(kb + 1, i);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(sc_full + as);
+            }
+        }
+    } else {
+        const int quad = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        int it = 0;
+        bool ok = true;
+        uint64_t acc[CW / 2];
+        for (int tile = first; tile < g.tiles && ok; tile += step) {
+#pragma unroll
+            for (int c = 0; c < CW / 2; ++c) acc[c] = 0ull;
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int as = it % AS;
+                ok = mbar_wait_bounded(sc_full + as, (it / AS) & 1) && mbar_wait_bounded(acc_full + as, (it / AS) & 1);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) {
+                    if (lane == 0) record_fault(p.status, kFaultMatmulWait, 4);
+                    break;
+                }
+                tc_fence_after();
+                const uint64_t* sc = reinterpret_cast<const uint64_t*>(scales + as * BN + half * CW);
+#pragma unroll
+                for (int c = 0; c < CW / CH; ++c) {
+                    float d[CH];
+                    const uint32_t at = tmem + (uint32_t)(as * BN + half * CW + c * CH) + lanes;
+                    if constexpr (CH == 32) tmem_ld32(at, d);
+                    else tmem_ld16(at, d);
+#pragma unroll
+                    for (int j = 0; j < CH / 2; ++j)
+                        acc[c * (CH / 2) + j] = fma2(pack2(d[2 * j], d[2 * j + 1]), sc[c * (CH / 2) + j], acc[c * (CH / 2) + j]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(acc_empty + as);
+            }
+            const int n = tile % g.n_tiles * 128 + quad * 32 + lane, m0 = tile / g.n_tiles * BN + half * CW;
+            if (g.ks == 1) {
+                if (n < p.N) {
+                    const int cols = min(CW, p.M - m0);
+                    auto store = [&](auto* out) {
+                        out += (size_t)m0 * p.out_stride + n;
+#pragma unroll
+                        for (int c = 0; c < CW; ++c) {
+                            float lo, hi;
+                            unpack2(acc[c / 2], lo, hi);
+                            if (c < cols) put(out, (c & 1) ? hi : lo);
+                            out += p.out_stride;
+                        }
+                    };
+                    if (p.out_bf16) store(static_cast<__nv_bfloat16*>(p.out));
+                    else store(static_cast<float*>(p.out));
+                }
+            } else {
+                // every product of this CTA has been waited for, so nothing reads or fills the stages any more
+                float* sums = reinterpret_cast<float*>(smem) + (size_t)(half * CW) * 128 + quad * 32 + lane;
+#pragma unroll
+                for (int c = 0; c < CW; ++c) {
+                    float lo, hi;
+                    unpack2(acc[c / 2], lo, hi);
+                    sums[c * 128] = (c & 1) ? hi : lo;
+                }
+            }
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = m0 + tm * 4 + i, n = n0 + tn;
-        if (m < p.M && n < p.N) {
-            if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[m * p.out_stride + n] = __float2bfloat16_rn(acc[i]);
-            else static_cast<float*>(p.out)[m * p.out_stride + n] = acc[i];
+    if (g.ks > 1) {                                    // a CTA of a cluster has one tile
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        const int m0 = first / g.n_tiles * BN, n0 = first % g.n_tiles * 128;
+        const int per = BN / g.ks, c0 = rank * per;
+        for (int i = tid; i < per * 128; i += 32 * (EW + 4)) {
+            const int c = c0 + i / 128, r = i % 128;
+            float y = 0.f;
+            for (int q = 0; q < g.ks; ++q) {
+                uint32_t at;
+                float f;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(smem) + (uint32_t)(c * 128 + r) * 4u), "r"(q));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at) : "memory");
+                y += f;
+            }
+            if (m0 + c < p.M && n0 + r < p.N) {
+                const size_t o = (size_t)(m0 + c) * p.out_stride + n0 + r;
+                if (p.out_bf16) put(static_cast<__nv_bfloat16*>(p.out) + o, y);
+                else put(static_cast<float*>(p.out) + o, y);
+            }
         }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_free<TM>(tmem);
+}
+
+template <int BN, int EW, int NS, int AS, int MINB>
+int launch_tiles(Ctx* ctx, const MatmulParams& p, int ks, cudaStream_t stream) {
+    MatmulArgs g;
+    g.p = p;
+    g.ks = ks;
+    g.n_tiles = (p.N + 127) / 128;
+    const long long tiles = (long long)g.n_tiles * ((p.M + BN - 1) / BN);
+    if (tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    g.tiles = (int)tiles;
+    if (!make_map(&g.tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, (uint64_t)p.K, (uint64_t)p.N, (uint64_t)p.K, 128) ||
+        !make_map(&g.ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.a, (uint64_t)p.K, (uint64_t)p.M, (uint64_t)p.K, BN)) {
+        ctx->last_cuda_error = cudaErrorInvalidValue;
+        return SKETCHSSM_CUDA_ERROR;
+    }
+    auto kern = scaled_matmul_kernel<BN, EW, NS, AS, MINB>;
+    const cudaError_t e = unlock_smem(ctx, kern);
+    if (e != cudaSuccess) { ctx->last_cuda_error = e; return SKETCHSSM_CUDA_ERROR; }
+    const int grid = ks > 1 ? (int)tiles * ks : (int)(tiles < (long long)sm_count(ctx) * MINB ? tiles : sm_count(ctx) * MINB);
+    return launch_layer<MatmulArgs>(ctx, kern, dim3((unsigned)grid), dim3(32 * (EW + 4)), MatmulSmem<BN, EW, NS, AS>::kBytes, stream, g, ks);
 }
 
 }  // namespace
 
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
-    if ((p.M + kTile - 1) / kTile > 65535) return SKETCHSSM_UNSUPPORTED_SHAPE;
-    return launch_layer(ctx, scaled_matmul_kernel, dim3((unsigned)((p.N + kTile - 1) / kTile), (unsigned)((p.M + kTile - 1) / kTile)), dim3(256), 0, stream, p);
+    const int sms = sm_count(ctx);
+    const long long nt = (p.N + 127) / 128;
+    // 256 tokens a tile once that gives every SM one; below it the narrowest tile that holds the tokens.
+    if (p.M > 128 && nt * ((p.M + 255) / 256) >= sms) return launch_tiles<256, 8, 4, 2, 1>(ctx, p, 1, stream);
+    const int bn = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
+    const long long tiles = nt * ((p.M + bn - 1) / bn);
+    // Few tiles: the blocks split over a cluster, while that leaves a CTA two blocks and the SMs one CTA (two of the narrow ones).
+    int ks = 1;
+    while (ks < 8 && tiles * ks * 2 <= (long long)sms * (bn == 128 ? 1 : 2) && p.KB >= ks * 4) ks *= 2;
+    if (bn == 16) return launch_tiles<16, 4, 6, 4, 2>(ctx, p, ks, stream);
+    if (bn == 32) return launch_tiles<32, 4, 5, 4, 2>(ctx, p, ks, stream);
+    if (bn == 64) return launch_tiles<64, 4, 4, 4, 2>(ctx, p, ks, stream);
+    return launch_tiles<128, 8, 6, 4, 1>(ctx, p, ks, stream);
 }
 
 }  // namespace sketchssm
