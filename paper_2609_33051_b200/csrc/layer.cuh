@@ -85,6 +85,7 @@ int launch_conv_step(Ctx* ctx, const ConvStepParams& p, bool bf16, cudaStream_t 
 int launch_prompt_scan(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
 int launch_rms_norm(Ctx* ctx, const NormParams& p, bool bf16, cudaStream_t stream);
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
+int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE for few tiles
 
 inline int sm_count(Ctx* ctx) {
     if (ctx->sm_count == 0 && cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, ctx->cfg.device) != cudaSuccess)

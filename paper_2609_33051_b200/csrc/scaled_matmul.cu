@@ -10,8 +10,8 @@
 //
 // Roles: one thread issues the copies (TMA, 128-byte swizzle: a row of a tile is exactly one block), one the products; two warps
 // fetch the token scales one block ahead and leave them, times the weights' scale, in shared memory; the other warps add.
-// With few tiles (a decode step) the blocks are split over a cluster of up to eight CTAs that add their sums through distributed
-// shared memory in the order of their ranks.
+// With few tiles (a decode step) the blocks are split over a cluster of up to eight CTAs; each of them adds up a share of the
+// columns, from the sums in every rank's shared memory in the order of the ranks.
 #include "tma.cuh"
 
 namespace sketchssm {
@@ -40,11 +40,56 @@ struct MatmulSmem {
     static_assert(BN * 128u * 4u <= NS * kStage, "the sums of a split tile take the stages' place");
 };
 
+// The sums of a tile's BN columns that the KS CTAs of a cluster hold, a share of the columns by each: four rows of a column at a
+// time, all loads of a thread under way together (a round trip to another SM's shared memory is about a thousand cycles).
+template <int BN, int THREADS, int KS>
+__device__ __forceinline__ void add_ranks(const MatmulArgs& g, unsigned char* smem, int tile, int rank) {
+    constexpr int kPer = BN / KS, kItems = kPer * 32, kRounds = (kItems + THREADS - 1) / THREADS;
+    const MatmulParams& p = g.p;
+    const int m0 = tile / g.n_tiles * BN + rank * kPer, n0 = tile % g.n_tiles * 128;
+    cluster_sync();
+    float4 f[kRounds][KS];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+        const int item = i * THREADS + (int)threadIdx.x;
+        if (kItems % THREADS == 0 || item < kItems) {
+#pragma unroll
+            for (int q = 0; q < KS; ++q)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[i][q].x), "=f"(f[i][q].y), "=f"(f[i][q].z), "=f"(f[i][q].w)
+                             : "r"(cluster_addr(smem + (uint32_t)(rank * kItems + item) * 16u, (uint32_t)q)) : "memory");
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+#pragma unroll
+        for (int q = 1; q < KS; ++q) {
+            f[i][0].x += f[i][q].x; f[i][0].y += f[i][q].y; f[i][0].z += f[i][q].z; f[i][0].w += f[i][q].w;
+        }
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // this CTA needs the others' sums no more
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+        const int item = i * THREADS + (int)threadIdx.x, m = m0 + item / 32, n = n0 + item % 32 * 4;
+        if ((kItems % THREADS == 0 || item < kItems) && m < p.M) {
+            const float y[4] = {f[i][0].x, f[i][0].y, f[i][0].z, f[i][0].w};
+            const size_t o = (size_t)m * p.out_stride + n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (n + j < p.N) {
+                    if (p.out_bf16) put(static_cast<__nv_bfloat16*>(p.out) + o + j, y[j]);
+                    else put(static_cast<float*>(p.out) + o + j, y[j]);
+                }
+            }
+        }
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // nobody reaches into a CTA that has ended
+}
+
 template <int BN, int EW, int NS, int AS, int MINB>
 __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(const __grid_constant__ MatmulArgs g) {
     using L = MatmulSmem<BN, EW, NS, AS>;
     constexpr int CW = BN / (EW / 4);                  // accumulator columns of an epilogue warp
-    constexpr int CH = CW < 32 ? CW : 32;              // of one load
+    constexpr int CH = 16;                             // of one load
     constexpr int TM = AS * BN < 32 ? 32 : AS * BN;
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
@@ -54,6 +99,7 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
     uint32_t* slot = reinterpret_cast<uint32_t*>(sc_full + AS);
     const MatmulParams& p = g.p;
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 32) { prefetch_map(&g.tw); prefetch_map(&g.ta); }
     if (tid == 0) {
         for (int i = 0; i < NS; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
         for (int i = 0; i < AS; ++i) { mbar_init(acc_full + i, 1); mbar_init(acc_empty + i, EW); mbar_init(sc_full + i, 2); }
@@ -130,14 +176,31 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
         for (int tile = first; tile < g.tiles && ok; tile += step) {
             const float* sw = p.w_scale + (size_t)(tile % g.n_tiles) * p.KB;
             const int m0 = tile / g.n_tiles * BN;
-            auto fetch = [&](int kb, int i) {
-                const int m = m0 + t + 64 * i;
-                return t + 64 * i < BN && m < p.M ? p.a_scale[(size_t)m * p.KB + kb] * sw[kb] : 0.f;
-            };
-            float next[PT];
+            // four blocks' scales at a time, one such group ahead of the one in use (nothing may be computed from them before
+            // that: the first use waits for the load)
+            auto fetch = [&](int kb, float (&f)[4][PT], float (&fw)[4]) {
 #pragma unroll
-            for (int i = 0; i < PT; ++i) next[i] = fetch(kb0, i);
+                for (int j = 0; j < 4; ++j) {
+                    fw[j] = kb + j < kb1 ? sw[kb + j] : 0.f;
+#pragma unroll
+                    for (int i = 0; i < PT; ++i) {
+                        const int m = m0 + t + 64 * i;
+                        f[j][i] = t + 64 * i < BN && m < p.M && kb + j < kb1 ? p.a_scale[(size_t)m * p.KB + kb + j] : 0.f;
+                    }
+                }
+            };
+            float now[4][PT], next[4][PT], now_w[4], next_w[4];
+            fetch(kb0, next, next_w);
             for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                if (((kb - kb0) & 3) == 0) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        now_w[j] = next_w[j];
+#pragma unroll
+                        for (int i = 0; i < PT; ++i) now[j][i] = next[j][i];
+                    }
+                    fetch(kb + 4, next, next_w);
+                }
                 const int as = it % AS;
                 ok = it < AS || mbar_wait_bounded(acc_empty + as, (it / AS - 1) & 1);
                 ok = __all_sync(0xffffffffu, ok);
@@ -147,9 +210,14 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
                 }
 #pragma unroll
                 for (int i = 0; i < PT; ++i) {
-                    if (t + 64 * i < BN) scales[as * BN + t + 64 * i] = next[i];
-                    if (kb + 1 < kb1) next[i] = fetch(kb + 1, i);
+                    if (t + 64 * i < BN) scales[as * BN + t + 64 * i] = now[0][i] * now_w[0];
+                    now[0][i] = now[1][i];
+                    now[1][i] = now[2][i];
+                    now[2][i] = now[3][i];
                 }
+                now_w[0] = now_w[1];
+                now_w[1] = now_w[2];
+                now_w[2] = now_w[3];
                 __syncwarp();
                 if (lane == 0) mbar_arrive_one(sc_full + as);
             }
@@ -172,16 +240,18 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
                     break;
                 }
                 tc_fence_after();
-                const uint64_t* sc = reinterpret_cast<const uint64_t*>(scales + as * BN + half * CW);
+                const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(scales + as * BN + half * CW);
 #pragma unroll
                 for (int c = 0; c < CW / CH; ++c) {
                     float d[CH];
-                    const uint32_t at = tmem + (uint32_t)(as * BN + half * CW + c * CH) + lanes;
-                    if constexpr (CH == 32) tmem_ld32(at, d);
-                    else tmem_ld16(at, d);
+                    tmem_ld16(tmem + (uint32_t)(as * BN + half * CW + c * CH) + lanes, d);
 #pragma unroll
-                    for (int j = 0; j < CH / 2; ++j)
-                        acc[c * (CH / 2) + j] = fma2(pack2(d[2 * j], d[2 * j + 1]), sc[c * (CH / 2) + j], acc[c * (CH / 2) + j]);
+                    for (int j = 0; j < CH / 4; ++j) {
+                        const ulonglong2 s4 = sc[c * (CH / 4) + j];
+                        uint64_t* a = acc + c * (CH / 2) + 2 * j;
+                        a[0] = fma2(pack2(d[4 * j], d[4 * j + 1]), s4.x, a[0]);
+                        a[1] = fma2(pack2(d[4 * j + 2], d[4 * j + 3]), s4.y, a[1]);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -216,28 +286,9 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
             }
         }
     }
-    if (g.ks > 1) {                                    // a CTA of a cluster has one tile
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        const int m0 = first / g.n_tiles * BN, n0 = first % g.n_tiles * 128;
-        const int per = BN / g.ks, c0 = rank * per;
-        for (int i = tid; i < per * 128; i += 32 * (EW + 4)) {
-            const int c = c0 + i / 128, r = i % 128;
-            float y = 0.f;
-            for (int q = 0; q < g.ks; ++q) {
-                uint32_t at;
-                float f;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(smem) + (uint32_t)(c * 128 + r) * 4u), "r"(q));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(f) : "r"(at) : "memory");
-                y += f;
-            }
-            if (m0 + c < p.M && n0 + r < p.N) {
-                const size_t o = (size_t)(m0 + c) * p.out_stride + n0 + r;
-                if (p.out_bf16) put(static_cast<__nv_bfloat16*>(p.out) + o, y);
-                else put(static_cast<float*>(p.out) + o, y);
-            }
-        }
-        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
+    if (g.ks == 2) add_ranks<BN, 32 * (EW + 4), 2>(g, smem, first, rank);      // a CTA of a cluster has one tile
+    if (g.ks == 4) add_ranks<BN, 32 * (EW + 4), 4>(g, smem, first, rank);
+    if (g.ks == 8) add_ranks<BN, 32 * (EW + 4), 8>(g, smem, first, rank);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -270,8 +321,11 @@ int launch_tiles(Ctx* ctx, const MatmulParams& p, int ks, cudaStream_t stream) {
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
     const int sms = sm_count(ctx);
     const long long nt = (p.N + 127) / 128;
-    // 256 tokens a tile once that gives every SM one; below it the narrowest tile that holds the tokens.
-    if (p.M > 128 && nt * ((p.M + 255) / 256) >= sms) return launch_tiles<256, 8, 4, 2, 1>(ctx, p, 1, stream);
+    if (p.M > 128) {
+        const int rc = launch_scaled_matmul_pair(ctx, p, stream);
+        if (rc != SKETCHSSM_UNSUPPORTED_SHAPE) return rc;
+    }
+    // The narrowest tile that holds the tokens.
     const int bn = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     const long long tiles = nt * ((p.M + bn - 1) / bn);
     // Few tiles: the blocks split over a cluster, while that leaves a CTA two blocks and the SMs one CTA (two of the narrow ones).

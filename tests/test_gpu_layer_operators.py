@@ -368,7 +368,9 @@ def quantised(gen, n, k, rows):
                                           (64, 513, 2048, "bf16", 8), (65, 200, 112, "bf16", 0), (129, 257, 400, "f32", 3),
                                           (128, 256, 384, "bf16", 0), (300, 520, 1040, "f32", 0), (1000, 1000, 512, "bf16", 24),
                                           (513, 2056, 272, "bf16", 0), (2049, 384, 640, "bf16", 0), (700, 4160, 1152, "f32", 0),
-                                          (16, 8512, 2048, "bf16", 0)])
+                                          (16, 8512, 2048, "bf16", 0), (130, 8512, 528, "bf16", 0), (2100, 2200, 272, "f32", 0),
+                                          (2100, 2201, 144, "bf16", 2), (1801, 2500, 912, "bf16", 4), (5000, 1030, 128, "f32", 1),
+                                          (4099, 4100, 16, "bf16", 4)])
 def test_matmul(M, N, K, od, pad):
     gen = torch.Generator().manual_seed(M + N + K)
     a, sa = quantised(gen, M, K, 1)
