@@ -83,6 +83,7 @@ struct MatmulParams {
 int launch_causal_conv(Ctx* ctx, const ConvParams& p, bool bf16, cudaStream_t stream);
 int launch_conv_step(Ctx* ctx, const ConvStepParams& p, bool bf16, cudaStream_t stream);
 int launch_prompt_scan(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
+int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);    // tcgen05; UNSUPPORTED_SHAPE outside its domain
 int launch_rms_norm(Ctx* ctx, const NormParams& p, bool bf16, cudaStream_t stream);
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
 int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE for few tiles

@@ -98,6 +98,8 @@ __global__ void __launch_bounds__(256) prompt_scan_kernel(const ScanParams p) {
 }  // namespace
 
 int launch_prompt_scan(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_t stream) {
+    const int rc = launch_prompt_scan_tc(ctx, p0, bf16, stream);
+    if (rc != SKETCHSSM_UNSUPPORTED_SHAPE) return rc;
     ScanParams p = p0;
     // 16 columns a CTA where 32 would leave SMs with less than two CTAs (V = 80 is five times 16)
     p.cols = p.V % 32 == 0 && (long long)p.pr.N * p.H * (p.V / 32) >= 2ll * sm_count(ctx) ? 32 : 16;

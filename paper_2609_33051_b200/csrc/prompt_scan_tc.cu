@@ -1,0 +1,687 @@
+// Selective scan of packed prompts on tcgen05 + TMEM: bf16 tensors, K = 128, value columns in blocks of 64.
+//
+// A sequence goes through in chunks of 128 tokens.  With c_t the sum of the chunk's log2 decays up to token t, per head:
+//     Y   = diag(2^c_t) Q S + P V,      P[t][s] = <q_t, k_s> beta_s 2^(c_t - c_s)  for s <= t, else 0        (outputs, + skip V)
+//     S  <- 2^c_end S + K^T W,          W[t] = beta_t 2^(c_end - c_t) v_t                                   (state)
+// A CTA (one per SM, persistent) takes two column blocks of one group at a time ("sets": two heads of 64 columns, or both halves of
+// one of 128), which share K, Q and the products Q K^T.
+//
+// Precision.  Q K^T is exact up to the fp32 sums.  The state is held in fp32 registers; W goes to the tensor cores in three bf16
+// parts, so that a term of S is off by less than 2^-25.  P goes in two parts (2^-17), S as an operand of Y in one (2^-9, half a
+// step of bf16: the outputs are rounded to bf16 by as much behind it).  Sums of decays run forward for c_t and backward for
+// c_end - c_t, so that what is small is exact.
+//
+// Roles: warp 0 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
+// warp 3 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, scale Q S there, add the skip and
+// store Y, and four ("B") make W, hold S and hand it on as an operand.  They meet through mbarriers alone; every wait is bounded.
+// Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64; the lower parts of P take the columns of Q K^T that
+// both sets have read.
+//
+// Few sequences and heads: a sequence is split into segments.  A first launch (OUTPUTS = false) leaves every segment's own state and
+// decay in the scratch, a second one starts each segment from the sum of those before it.
+#include "tma.cuh"
+
+namespace sketchssm {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kQ = 128;                                // tokens of a chunk
+constexpr uint32_t kTile = 16384u;                     // 128 rows of 128 bytes
+constexpr uint32_t kKOff = 0, kQOff = 4 * kTile, kVOff = 6 * kTile, kWOff = 10 * kTile;      // K in two buffers, Q in one, V in two
+constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 64 tokens in three parts, or S in one
+constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][4][128] floats: c, beta, beta 2^(c_end - c), 2^c
+constexpr uint32_t kGateSet = 4 * kQ, kGateBuf = 2 * kGateSet;
+constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
+constexpr int kThreads = 640;
+
+enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
+       bInter = 17, bP = 19, bY = 21, bYFree = 23, bW = 25, bProd = 27, bVRead = 29, bRead = 31, kBars = 35 };
+constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
+
+// columns of tensor memory
+constexpr uint32_t kDot = 0, kY = 128, kProd = 256, kP = 384;
+
+struct ScanArgs {
+    CUtensorMap tq, tk, tv;
+    ScanParams p;
+    int slabs, slabs_per_group, blocks_per_group;      // pairs of column blocks: all, per group; column blocks per group
+    long long units;
+};
+
+// One unit: a segment of a sequence for one pair of column blocks.
+struct Unit {
+    int t0, t1;            // rows of the segment
+    int seq, seg, group;
+    int block0, live1;     // first column block; whether the second set has one of its own
+    int last;              // this segment ends the sequence
+};
+
+__device__ __forceinline__ Unit decode_unit(const ScanArgs& g, long long u) {
+    Unit x;
+    const int slab = (int)(u % g.slabs);
+    const long long r = u / g.slabs;
+    x.seg = (int)(r % g.p.segments);
+    x.seq = (int)(r / g.p.segments);
+    x.group = slab / g.slabs_per_group;
+    const int i = slab % g.slabs_per_group * 2;
+    x.block0 = x.group * g.blocks_per_group + i;
+    x.live1 = i + 1 < g.blocks_per_group;
+    const int2 rows = seq_rows(g.p.pr, x.seq);
+    const int chunks = (rows.y - rows.x + kQ - 1) / kQ;
+    const int per = max(1, (chunks + g.p.segments - 1) / g.p.segments);
+    x.t0 = min(rows.y, rows.x + x.seg * per * kQ);
+    x.t1 = min(rows.y, x.t0 + per * kQ);
+    x.last = x.seg == (chunks > 0 ? (chunks - 1) / per : 0);
+    return x;
+}
+// The segment has work: tokens, or (a sequence without tokens) a state to hand on.
+__device__ __forceinline__ bool unit_runs(const Unit& x, bool outputs) { return outputs ? x.t1 > x.t0 || x.last : !x.last && x.t1 > x.t0; }
+
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) { tc_mma_bf16(d, a, b, idesc, acc ? 1u : 0u); }
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+        "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+
+// A warp's wait: false to all its lanes if it ran out.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity)); }
+
+// 32 rows of 128 bytes in shared memory (128-byte swizzle, this warp's) to or from rows of global memory `stride` bytes apart;
+// rows from `n` on are left out.
+template <bool STORE>
+__device__ __forceinline__ void copy_rows(unsigned char* tile, unsigned char* global, long long stride, int n) {
+    const int lane = (int)threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = i * 4 + lane / 8, c = lane % 8;
+        uint4* s = reinterpret_cast<uint4*>(tile + r * 128 + ((c ^ (r & 7)) * 16));
+        uint4* d = reinterpret_cast<uint4*>(global + r * stride + c * 16);
+        if (r < n) {
+            if constexpr (STORE) *d = *s;
+            else *s = *d;
+        }
+    }
+}
+
+template <bool OUTPUTS>
+__global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __grid_constant__ ScanArgs g) {
+    extern __shared__ unsigned char raw[];
+    unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    float* gates = reinterpret_cast<float*>(smem + kGateOff);
+    uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kBarOff);
+    uint32_t* slot = reinterpret_cast<uint32_t*>(bar + kBars);
+    const ScanParams& p = g.p;
+    const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per_head = p.V / 64;                     // column blocks of a head
+    if (tid == 32) { prefetch_map(&g.tq); prefetch_map(&g.tk); prefetch_map(&g.tv); }
+    if (tid == 0) {
+        for (int i = 0; i < kBars; ++i) {
+            int n = 1;                                  // copies and commits of products arrive once
+            if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;               // both product warps read K
+            if (i >= bEmptyV && i < bGate) n = 8;                               // A (without outputs: B) of both sets
+            if (i >= bGateFree && i < bDot) n = OUTPUTS ? 16 : 8;
+            if (i == bState || i == bState + 1 || (i >= bP && i < bY) || (i >= bYFree && i < bProd) || (i >= bVRead && i < bRead)) n = 4;
+            if (i >= bRead) n = 8;
+            mbar_init(bar + i, n);
+        }
+        mbar_fence_init();
+    }
+    if (warp == 1) tmem_alloc<512>(slot);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    grid_dep_wait();
+    grid_dep_launch_dependents();
+    const uint32_t tmem = *slot;
+    const uint32_t sbase = smem_u32(smem);
+    bool ok = true;
+    int n = 0;                                          // chunks so far, over all units of the CTA
+
+    if (warp == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (lane == 0) {
+            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+                const Unit x = decode_unit(g, u);
+                if (!unit_runs(x, OUTPUTS)) continue;
+                for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                    const int b = n & 1;
+                    ok = n < 2 || mbar_wait_bounded(bar + bEmptyK + b, (n / 2 - 1) & 1);
+                    if (ok) {
+                        mbar_expect_tx(bar + bFullK + b, 2 * kTile);
+                        tma_load(smem + kKOff + b * 2 * kTile, &g.tk, x.group * 128, t, bar + bFullK + b);
+                        tma_load(smem + kKOff + (b * 2 + 1) * kTile, &g.tk, x.group * 128 + 64, t, bar + bFullK + b);
+                    }
+                    ok = ok && (n < 2 || mbar_wait_bounded(bar + bEmptyV + b, (n / 2 - 1) & 1));
+                    if (ok) {
+                        mbar_expect_tx(bar + bFullV + b, 2 * kTile);
+                        tma_load(smem + kVOff + b * 2 * kTile, &g.tv, x.block0 * 64, t, bar + bFullV + b);
+                        tma_load(smem + kVOff + (b * 2 + 1) * kTile, &g.tv, (x.block0 + x.live1) * 64, t, bar + bFullV + b);
+                    }
+                    if constexpr (OUTPUTS) {
+                        ok = ok && (n < 1 || mbar_wait_bounded(bar + bEmptyQ, (n - 1) & 1));
+                        if (ok) {
+                            mbar_expect_tx(bar + bFullQ, 2 * kTile);
+                            tma_load(smem + kQOff, &g.tq, x.group * 128, t, bar + bFullQ);
+                            tma_load(smem + kQOff + kTile, &g.tq, x.group * 128 + 64, t, bar + bFullQ);
+                        }
+                    }
+                    if (!ok) {
+                        record_fault(p.status, kFaultScanWait, 1);
+                        break;
+                    }
+                }
+            }
+            if (!ok) {                                  // let the copies under way end (n chunks were asked for in full)
+                for (int i = max(0, n - 2); i < n; ++i) {
+                    mbar_wait_bounded(bar + bFullK + (i & 1), (i / 2) & 1, 1u << 16);
+                    mbar_wait_bounded(bar + bFullV + (i & 1), (i / 2) & 1, 1u << 16);
+                }
+                if (OUTPUTS && n > 0) mbar_wait_bounded(bar + bFullQ, (n - 1) & 1, 1u << 16);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (OUTPUTS && lane == 0) {
+            constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
+            constexpr uint32_t kDotDesc = kTypes | ((128u >> 3) << 17), kYDesc = kTypes | (1u << 16) | ((64u >> 3) << 17);
+            int m = 0;                                  // chunks with a state before them
+            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+                const Unit x = decode_unit(g, u);
+                if (!unit_runs(x, true)) continue;
+                const bool fresh0 = x.seg == 0 && seq_resume(p.pr, x.seq) < 0;
+                for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                    const int b = n & 1;
+                    const bool fresh = fresh0 && t == x.t0;                     // S is zero
+                    ok = mbar_wait_bounded(bar + bFullK + b, (n / 2) & 1) && mbar_wait_bounded(bar + bFullQ, n & 1);
+                    // the columns of Q K^T hold parts of P until the products with them are done
+                    ok = ok && (n < 1 || (mbar_wait_bounded(bar + bY, (n - 1) & 1) && mbar_wait_bounded(bar + bY + 1, (n - 1) & 1)));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t dq = swizzled_desc(sbase + kQOff, 16u, 1024u);
+                    {
+                        const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, 16u, 1024u);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t step = (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u;
+                            mma_ss(tmem + kDot, dq + step, dk + step, kDotDesc, i > 0);
+                        }
+                        tc_commit(bar + bDot);
+                        tc_commit(bar + bEmptyK + b);
+                    }
+                    for (int j = 0; j < 2 && ok; ++j) {
+                        ok = n < 1 || mbar_wait_bounded(bar + bYFree + j, (n - 1) & 1);
+                        if (fresh) continue;
+                        ok = ok && mbar_wait_bounded(bar + bState + j, m & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t ds = swizzled_desc(sbase + kWOff + j * kWBuf, 16u, 1024u);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            mma_ss(tmem + kY + j * 64, dq + (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u, ds + (uint32_t)i * 128u, kYDesc, i > 0);
+                        tc_commit(bar + bInter + j);
+                    }
+                    if (!ok) break;
+                    if (!fresh) ++m;
+                    tc_commit(bar + bEmptyQ);
+                    ok = mbar_wait_bounded(bar + bFullV + b, (n / 2) & 1);
+                    for (int j = 0; j < 2 && ok; ++j) {
+                        ok = mbar_wait_bounded(bar + bP + j, n & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t dv = swizzled_desc(sbase + kVOff + (b * 2 + j) * kTile, 16u, 1024u);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + i * 8, dv + (uint32_t)i * 128u, kYDesc, i > 0 || !fresh);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            mma_ts(tmem + kY + j * 64, tmem + kDot + (i / 2) * 32 + j * 16 + (i % 2) * 8, dv + (uint32_t)i * 128u, kYDesc, true);
+                        tc_commit(bar + bY + j);
+                    }
+                    if (!ok) break;
+                }
+            }
+            if (!ok) record_fault(p.status, kFaultScanWait, 2);
+        }
+        __syncwarp();
+    } else if (warp == 2) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (lane == 0) {
+            constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
+            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+                const Unit x = decode_unit(g, u);
+                if (!unit_runs(x, OUTPUTS)) continue;
+                for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
+                    const int b = n & 1;
+                    ok = mbar_wait_bounded(bar + bFullK + b, (n / 2) & 1);
+                    for (int hj = 0; hj < 4 && ok; ++hj) {                      // halves of 64 tokens, both sets
+                        const int h = hj >> 1, j = hj & 1;
+                        ok = mbar_wait_bounded(bar + bW + j, h);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile + h * 8192u, kTile, 1024u);
+#pragma unroll
+                        for (int i = 0; i < 12; ++i) {
+                            const uint64_t dw = swizzled_desc(sbase + kWOff + j * kWBuf + (i / 4) * 8192u, 16u, 1024u);
+                            mma_ss(tmem + kProd + j * 64, dk + (uint32_t)(i % 4) * 128u, dw + (uint32_t)(i % 4) * 128u, kDesc, i > 0 || h > 0);
+                        }
+                        tc_commit(bar + bProd + j);
+                    }
+                    if (ok) tc_commit(bar + bEmptyK + b);
+                }
+            }
+            if (!ok) record_fault(p.status, kFaultScanWait, 3);
+        }
+        __syncwarp();
+    } else if (warp == 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // gates: four neighbouring tokens a lane
+        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            const Unit x = decode_unit(g, u);
+            if (!unit_runs(x, OUTPUTS)) continue;
+            const int h0 = x.block0 / per_head, h1 = (x.block0 + x.live1) / per_head;
+            float a2[2], bias[2], next[2][4];
+            a2[0] = p.a[h0] * 1.4426950408889634f; a2[1] = p.a[h1] * 1.4426950408889634f;
+            bias[0] = p.dt_bias != nullptr ? p.dt_bias[h0] : 0.f; bias[1] = p.dt_bias != nullptr ? p.dt_bias[h1] : 0.f;
+            auto fetch = [&](int t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = t + lane * 4 + i;
+                    const __nv_bfloat16* dt = static_cast<const __nv_bfloat16*>(p.dt) + (long long)r * p.dt_stride;
+                    next[0][i] = r < x.t1 ? __bfloat162float(dt[h0]) : 0.f;
+                    next[1][i] = r < x.t1 ? __bfloat162float(dt[h1]) : 0.f;
+                }
+            };
+            fetch(x.t0);
+            for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                const int b = n & 1;
+                float beta[2][4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) beta[j][i] = t + lane * 4 + i < x.t1 ? softplus(next[j][i] + bias[j]) : 0.f;
+                if (t + kQ < x.t1) fetch(t + kQ);
+                ok = n < 2 || warp_wait(bar + bGateFree + b, (n / 2 - 1) & 1);
+                if (!ok) break;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float l[4], pre[4], suf[4];
+                    // (2^-256 is zero in fp32 anyway; the bound keeps differences of sums finite)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l[i] = t + lane * 4 + i < x.t1 ? fmaxf(a2[j] * beta[j][i], -256.f) : 0.f;
+                    pre[0] = l[0];
+#pragma unroll
+                    for (int i = 1; i < 4; ++i) pre[i] = pre[i - 1] + l[i];
+                    suf[3] = 0.f;
+#pragma unroll
+                    for (int i = 2; i >= 0; --i) suf[i] = suf[i + 1] + l[i + 1];
+                    const float all = pre[3];
+                    float before = all, after = all;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const float up = __shfl_up_sync(0xffffffffu, before, o), down = __shfl_down_sync(0xffffffffu, after, o);
+                        if (lane >= o) before += up;
+                        if (lane + o < 32) after += down;
+                    }
+                    before = __shfl_up_sync(0xffffffffu, before, 1);
+                    after = __shfl_down_sync(0xffffffffu, after, 1);
+                    if (lane == 0) before = 0.f;
+                    if (lane == 31) after = 0.f;
+                    float4 c, be, w, e;
+                    float *pc = &c.x, *pb = &be.x, *pw = &w.x, *pe = &e.x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        pc[i] = before + pre[i];
+                        pb[i] = beta[j][i];
+                        pw[i] = beta[j][i] * exp2f(after + suf[i]);
+                        pe[i] = exp2f(pc[i]);
+                    }
+                    float4* o = reinterpret_cast<float4*>(gates + b * kGateBuf + j * kGateSet) + lane;
+                    o[0] = c; o[32] = be; o[64] = w; o[96] = e;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(bar + bGate + b);
+            }
+        }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 4);
+    } else if (warp < 12) {
+        if constexpr (OUTPUTS) {
+            // A: token row `row` of set j
+            const int j = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
+            const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+            const uint32_t tp = tmem + lanes + kP + j * 64, td = tmem + lanes + kDot, ty = tmem + lanes + kY + j * 64;
+            int m = 0;
+            {
+                uint32_t z[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = 0u;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_st16u(tp + c * 16, z);          // above the diagonal P stays zero
+                tmem_st_wait();
+            }
+            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+                const Unit x = decode_unit(g, u);
+                if (!unit_runs(x, true)) continue;
+                const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
+                const bool live = j == 0 || x.live1, fresh0 = x.seg == 0 && seq_resume(p.pr, x.seq) < 0;
+                const float skip = p.skip != nullptr ? p.skip[head] : 0.f;
+                for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                    const int b = n & 1, valid = min(kQ, x.t1 - t);
+                    const bool fresh = fresh0 && t == x.t0;
+                    const float* gt = gates + b * kGateBuf + j * kGateSet;
+                    unsigned char* v = smem + kVOff + (b * 2 + j) * kTile;
+                    unsigned char* mine = v + row * 128;
+                    ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bDot, n & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const float ct = gt[row];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t hi[16], lo[16];
+                        uint32_t d[32];
+                        if (c <= quad) {
+                            tmem_ld32_async(td + c * 32, d);
+                            tmem_ld_wait();
+                        }
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_one(bar + bRead + c);
+                        if (c <= quad) {
+                            const float4 *c4 = reinterpret_cast<const float4*>(gt + c * 32), *b4 = reinterpret_cast<const float4*>(gt + kQ + c * 32);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float4 cs = c4[i], be = b4[i];
+                                float f[4] = {__uint_as_float(d[4 * i]) * be.x * ex2(ct - cs.x), __uint_as_float(d[4 * i + 1]) * be.y * ex2(ct - cs.y),
+                                              __uint_as_float(d[4 * i + 2]) * be.z * ex2(ct - cs.z), __uint_as_float(d[4 * i + 3]) * be.w * ex2(ct - cs.w)};
+                                if (c == quad) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        if (4 * i + e > lane) f[e] = 0.f;
+                                }
+                                split_bf16x2(f[0], f[1], hi[2 * i], lo[2 * i]);
+                                split_bf16x2(f[2], f[3], hi[2 * i + 1], lo[2 * i + 1]);
+                            }
+                            tmem_st16u(tp + c * 16, hi);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) lo[i] = 0u;
+                        }
+                        ok = ok && warp_wait(bar + bRead + c, n & 1);            // both sets have read these columns
+                        if (!ok) break;
+                        tc_fence_after();
+                        tmem_st16u(td + c * 32 + j * 16, lo);
+                    }
+                    if (!ok) break;
+                    ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
+                    if (ok && row >= valid) {                                    // rows of the next sequence are no part of this one
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    if (valid < kQ) proxy_fence();
+                    if (!fresh) {
+                        ok = ok && warp_wait(bar + bInter + j, m & 1);
+                        ++m;
+                        if (!ok) break;
+                        tc_fence_after();
+                        const float ec = gt[3 * kQ + row];
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t d[32];
+                            tmem_ld32_async(ty + c * 32, d);
+                            tmem_ld_wait();
+                            float f[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(d[i]) * ec;
+                            tmem_st16(ty + c * 32, f);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(d[16 + i]) * ec;
+                            tmem_st16(ty + c * 32 + 16, f);
+                        }
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive_one(bar + bP + j);
+                        mbar_arrive_one(bar + bGateFree + b);
+                    }
+                    // Y: what the products left, and the skip; v's row becomes y's, then the warp stores its rows
+                    ok = ok && warp_wait(bar + bY + j, n & 1) && warp_wait(bar + bVRead + j, n & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t d[2][32];
+                    tmem_ld32_async(ty, d[0]);
+                    tmem_ld32_async(ty + 32, d[1]);
+                    tmem_ld_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bYFree + j);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint4* at = reinterpret_cast<uint4*>(mine + ((c ^ (row & 7)) * 16));
+                        float f[8];
+                        Vec16<__nv_bfloat16>::unpack(*at, f);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = fmaf(skip, f[i], __uint_as_float(d[c / 4][c % 4 * 8 + i]));
+                        *at = Vec16<__nv_bfloat16>::pack(f);
+                    }
+                    __syncwarp();
+                    if (live)
+                        copy_rows<true>(v + quad * 4096, static_cast<unsigned char*>(p.out) + ((long long)(t + quad * 32) * p.out_stride + block * 64) * 2,
+                                        p.out_stride * 2, valid - quad * 32);
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bEmptyV + b);
+                }
+            }
+            if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 5);
+        }
+    } else {
+        // B: state row `row` of set j (640 threads start with 96 registers: 128 x 56 + 256 x 96 + 256 x 112 of 61440)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        const int j = (warp - 12) >> 2, quad = warp & 3, row = quad * 32 + lane, bt = (tid - 384) & 127;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        unsigned char* buf = smem + kWOff + j * kWBuf;
+        unsigned char* rows = buf + quad * 4096;        // this warp's 32 rows of 128 bytes
+        float S[64];
+        int m = 0;                                      // chunks with a state before them
+        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            const Unit x = decode_unit(g, u);
+            if (!unit_runs(x, OUTPUTS)) continue;
+            const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
+            const bool live = j == 0 || x.live1;
+            const int src = seq_resume(p.pr, x.seq), dst = seq_slot(p.pr, x.seq);
+            const size_t at = (size_t)head * 128 * p.V + (size_t)quad * 32 * p.V + (block % per_head) * 64, entry = (size_t)p.H * 128 * p.V;
+            // scratch: per sequence `segments` states (that before segment 0, those left by segments 0, 1, ..) and as many decays a head
+            float* scratch = p.work + (size_t)x.seq * p.segments * entry + at;
+            float* decays = p.work + (size_t)p.pr.N * p.segments * entry + (size_t)x.seq * p.segments * p.H + head;
+            auto load = [&](const float* from, float keep) {                     // S <- keep S + rows of global memory
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    copy_rows<false>(rows, reinterpret_cast<unsigned char*>(const_cast<float*>(from + c * 32)), (long long)p.V * 4, 32);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 f = *reinterpret_cast<const float4*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16));
+                        S[c * 32 + 4 * i] = fmaf(keep, S[c * 32 + 4 * i], f.x);
+                        S[c * 32 + 4 * i + 1] = fmaf(keep, S[c * 32 + 4 * i + 1], f.y);
+                        S[c * 32 + 4 * i + 2] = fmaf(keep, S[c * 32 + 4 * i + 2], f.z);
+                        S[c * 32 + 4 * i + 3] = fmaf(keep, S[c * 32 + 4 * i + 3], f.w);
+                    }
+                    __syncwarp();
+                }
+            };
+            auto store = [&](float* to) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        *reinterpret_cast<float4*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16)) =
+                            make_float4(S[c * 32 + 4 * i], S[c * 32 + 4 * i + 1], S[c * 32 + 4 * i + 2], S[c * 32 + 4 * i + 3]);
+                    __syncwarp();
+                    copy_rows<true>(rows, reinterpret_cast<unsigned char*>(to + c * 32), (long long)p.V * 4, 32);
+                    __syncwarp();
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < 64; ++i) S[i] = 0.f;
+            if (x.seg == 0) {
+                // (a later segment's CTA may have written the entry already: the first launch kept a copy)
+                if (src >= 0) load(OUTPUTS && !x.last ? scratch : p.state + src * entry + at, 0.f);
+                if (!OUTPUTS && live) store(scratch);
+            } else if (OUTPUTS) {
+                for (int i = 1; i <= x.seg; ++i) load(scratch + (size_t)i * entry, i == 1 ? 0.f : decays[(size_t)i * p.H]);
+            }
+            const bool fresh0 = x.seg == 0 && src < 0;
+            float total = 1.f;
+            for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                const int b = n & 1, valid = min(kQ, x.t1 - t);
+                const bool fresh = fresh0 && t == x.t0;
+                if (OUTPUTS && !fresh) {                 // S as an operand: row n of 64 columns
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        float f[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = S[c * 8 + i];
+                        *reinterpret_cast<uint4*>(buf + row * 128 + ((c ^ (row & 7)) * 16)) = Vec16<__nv_bfloat16>::pack(f);
+                    }
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bState + j);
+                }
+                ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bFullV + b, (n / 2) & 1) && warp_wait(bar + bFullK + b, (n / 2) & 1);
+                if (!ok) break;
+                if (valid < kQ && j == 0 && row >= valid) {                      // rows of the next sequence are no part of this one
+                    unsigned char* k = smem + kKOff + b * 2 * kTile + row * 128;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        reinterpret_cast<uint4*>(k)[i] = make_uint4(0u, 0u, 0u, 0u);
+                        reinterpret_cast<uint4*>(k + kTile)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                if (OUTPUTS && !fresh) {                 // the buffer's S has been read
+                    ok = warp_wait(bar + bInter + j, m & 1);
+                    ++m;
+                    if (!ok) break;
+                }
+                const float* w = gates + b * kGateBuf + j * kGateSet + 2 * kQ;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) {
+                        ok = warp_wait(bar + bProd + j, 0);
+                        if (!ok) break;
+                    }
+                    const int tt = bt >> 1, t64 = h * 64 + tt;                   // two threads a token
+                    const float wt = w[t64];
+                    const unsigned char* v = smem + kVOff + (b * 2 + j) * kTile + t64 * 128;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t off = (uint32_t)((((bt & 1) * 4 + c) ^ (tt & 7)) * 16);
+                        float f[8];
+                        Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(v + off), f);
+                        uint32_t q[3][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float a0 = t64 < valid ? f[2 * i] * wt : 0.f, a1 = t64 < valid ? f[2 * i + 1] * wt : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 3; ++e) {
+                                q[e][i] = bf16x2(a0, a1);
+                                a0 -= __uint_as_float(q[e][i] << 16);
+                                a1 -= __uint_as_float(q[e][i] & 0xffff0000u);
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            *reinterpret_cast<uint4*>(buf + e * 8192 + tt * 128 + off) = make_uint4(q[e][0], q[e][1], q[e][2], q[e][3]);
+                    }
+                    proxy_fence();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive_one(bar + bW + j);
+                        if (h == 1) mbar_arrive_one(OUTPUTS ? bar + bVRead + j : bar + bEmptyV + b);
+                    }
+                }
+                if (!ok) break;
+                const float keep = ex2(gates[b * kGateBuf + j * kGateSet + kQ - 1]);
+                total *= keep;
+                ok = warp_wait(bar + bProd + j, 1);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float d[16];
+                    tmem_ld16(tmem + lanes + kProd + j * 64 + c * 16, d);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) S[c * 16 + i] = fmaf(keep, S[c * 16 + i], d[i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(bar + bGateFree + b);
+            }
+            if (!ok) break;
+            if (live) {
+                if (!OUTPUTS) {
+                    store(scratch + (size_t)(x.seg + 1) * entry);
+                    if (row == 0 && block % per_head == 0) decays[(size_t)(x.seg + 1) * p.H] = total;
+                } else if (x.last && dst >= 0) {
+                    store(p.state + dst * entry + at);
+                }
+            }
+        }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 6);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_free<512>(tmem);
+}
+
+}  // namespace
+
+int prompt_scan_tc_segments(int sms, int sequences, int tokens, int heads, int groups, int V) {
+    return 1;
+}
+
+int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_t stream) {
+    ScanParams p = p0;
+    if (!bf16 || !p.out_bf16 || p.K != 128 || p.V % 64 != 0 || p.pr.T == 0) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    ScanArgs g;
+    p.segments = 1;
+    g.p = p;
+    g.blocks_per_group = p.H / p.G * (p.V / 64);
+    g.slabs_per_group = (g.blocks_per_group + 1) / 2;
+    g.slabs = g.slabs_per_group * p.G;
+    g.units = (long long)p.pr.N * p.segments * g.slabs;
+    if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
+        !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ) ||
+        !make_map(&g.tv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.v, (uint64_t)p.H * p.V, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2, kQ)) {
+        ctx->last_cuda_error = cudaErrorInvalidValue;
+        return SKETCHSSM_CUDA_ERROR;
+    }
+    const cudaError_t e = unlock_smem(ctx, prompt_scan_tc_kernel<true>);
+    if (e != cudaSuccess) { ctx->last_cuda_error = e; return SKETCHSSM_CUDA_ERROR; }
+    const unsigned grid = (unsigned)(g.units < sm_count(ctx) ? g.units : sm_count(ctx));
+    return launch_layer<ScanArgs>(ctx, prompt_scan_tc_kernel<true>, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
+}
+
+}  // namespace sketchssm
