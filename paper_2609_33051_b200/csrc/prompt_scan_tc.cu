@@ -37,7 +37,7 @@ constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
 constexpr int kThreads = 640;
 
 enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
-       bInter = 17, bP = 19, bY = 21, bYFree = 23, bW = 25, bProd = 27, bVRead = 29, bRead = 31, kBars = 35 };
+       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 23, bVRead = 24, bRead = 28, kBars = 32 };
 constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
 
 // columns of tensor memory
@@ -94,6 +94,13 @@ __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[1
         "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+// One lane of a converged warp.  (The product warps run their loops with all lanes and elect one for each product: the operands then
+// stay in uniform registers, and an instruction is issued every 30 to 60 cycles; from a branch that one lane takes it was 95.)
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -138,11 +145,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
             int n = 1;                                  // copies and commits of products arrive once
-            if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;               // both product warps read K
+            if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;                // both product warps read K
             if (i >= bEmptyV && i < bGate) n = 8;                               // A (without outputs: B) of both sets
             if (i >= bGateFree && i < bDot) n = OUTPUTS ? 16 : 8;
-            if (i == bState || i == bState + 1 || (i >= bP && i < bY) || (i >= bYFree && i < bProd) || (i >= bVRead && i < bRead)) n = 4;
-            if (i >= bRead) n = 8;
+            if (i == bState || i == bYFree || i == bW || i >= bRead) n = 8;     // the warps of both sets
+            if ((i >= bP && i < bY) || (i >= bVRead && i < bRead)) n = 4;       // of one
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -203,9 +210,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         __syncwarp();
     } else if (warp == 1) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (OUTPUTS && lane == 0) {
+        if constexpr (OUTPUTS) {
             constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
-            constexpr uint32_t kDotDesc = kTypes | ((128u >> 3) << 17), kYDesc = kTypes | (1u << 16) | ((64u >> 3) << 17);
+            constexpr uint32_t kDotDesc = kTypes | ((128u >> 3) << 17), kInterDesc = kDotDesc | (1u << 16);
+            constexpr uint32_t kPDesc = kTypes | (1u << 16) | ((64u >> 3) << 17);
+            const uint64_t dq = swizzled_desc(sbase + kQOff, 16u, 1024u), ds = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
             int m = 0;                                  // chunks with a state before them
             for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
                 const Unit x = decode_unit(g, u);
@@ -214,84 +223,85 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 for (int t = x.t0; t < x.t1; t += kQ, ++n) {
                     const int b = n & 1;
                     const bool fresh = fresh0 && t == x.t0;                     // S is zero
-                    ok = mbar_wait_bounded(bar + bFullK + b, (n / 2) & 1) && mbar_wait_bounded(bar + bFullQ, n & 1);
+                    ok = warp_wait(bar + bFullK + b, (n / 2) & 1) && warp_wait(bar + bFullQ, n & 1);
                     // the columns of Q K^T hold parts of P until the products with them are done
-                    ok = ok && (n < 1 || (mbar_wait_bounded(bar + bY, (n - 1) & 1) && mbar_wait_bounded(bar + bY + 1, (n - 1) & 1)));
+                    ok = ok && (n < 1 || (warp_wait(bar + bY, (n - 1) & 1) && warp_wait(bar + bY + 1, (n - 1) & 1)));
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t dq = swizzled_desc(sbase + kQOff, 16u, 1024u);
-                    {
-                        const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, 16u, 1024u);
+                    const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, 16u, 1024u);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const uint32_t step = (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u;
-                            mma_ss(tmem + kDot, dq + step, dk + step, kDotDesc, i > 0);
-                        }
-                        tc_commit(bar + bDot);
-                        tc_commit(bar + bEmptyK + b);
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t step = (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u;
+                        if (elect()) mma_ss(tmem + kDot, dq + step, dk + step, kDotDesc, i > 0);
                     }
-                    for (int j = 0; j < 2 && ok; ++j) {
-                        ok = n < 1 || mbar_wait_bounded(bar + bYFree + j, (n - 1) & 1);
-                        if (fresh) continue;
-                        ok = ok && mbar_wait_bounded(bar + bState + j, m & 1);
+                    if (elect()) { tc_commit(bar + bDot); tc_commit(bar + bEmptyK + b); }
+                    __syncwarp();
+                    ok = n < 1 || warp_wait(bar + bYFree, (n - 1) & 1);
+                    if (!fresh) {
+                        ok = ok && warp_wait(bar + bState, m & 1);
                         if (!ok) break;
+                        ++m;
                         tc_fence_after();
-                        const uint64_t ds = swizzled_desc(sbase + kWOff + j * kWBuf, 16u, 1024u);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            mma_ss(tmem + kY + j * 64, dq + (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u, ds + (uint32_t)i * 128u, kYDesc, i > 0);
-                        tc_commit(bar + bInter + j);
+                            if (elect())
+                                mma_ss(tmem + kY, dq + (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u, ds + (uint32_t)i * 128u, kInterDesc, i > 0);
+                        if (elect()) tc_commit(bar + bInter);
                     }
-                    if (!ok) break;
-                    if (!fresh) ++m;
-                    tc_commit(bar + bEmptyQ);
-                    ok = mbar_wait_bounded(bar + bFullV + b, (n / 2) & 1);
-                    for (int j = 0; j < 2 && ok; ++j) {
-                        ok = mbar_wait_bounded(bar + bP + j, n & 1);
+                    if (elect()) tc_commit(bar + bEmptyQ);
+                    __syncwarp();
+                    ok = ok && warp_wait(bar + bFullV + b, (n / 2) & 1);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        ok = ok && warp_wait(bar + bP + j, n & 1);
                         if (!ok) break;
                         tc_fence_after();
                         const uint64_t dv = swizzled_desc(sbase + kVOff + (b * 2 + j) * kTile, 16u, 1024u);
+                        if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64, dv, kPDesc, !fresh);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + i * 8, dv + (uint32_t)i * 128u, kYDesc, i > 0 || !fresh);
+                        for (int i = 1; i < 8; ++i)
+                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + i * 8, dv + (uint32_t)i * 128u, kPDesc, true);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            mma_ts(tmem + kY + j * 64, tmem + kDot + (i / 2) * 32 + j * 16 + (i % 2) * 8, dv + (uint32_t)i * 128u, kYDesc, true);
-                        tc_commit(bar + bY + j);
+                            if (elect())
+                                mma_ts(tmem + kY + j * 64, tmem + kDot + (i / 2) * 32 + j * 16 + (i % 2) * 8, dv + (uint32_t)i * 128u, kPDesc, true);
+                        if (elect()) tc_commit(bar + bY + j);
+                        __syncwarp();
                     }
                     if (!ok) break;
                 }
             }
-            if (!ok) record_fault(p.status, kFaultScanWait, 2);
+            if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 2);
         }
         __syncwarp();
     } else if (warp == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (lane == 0) {
-            constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((64u >> 3) << 17) | ((128u >> 4) << 24);
-            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
-                const Unit x = decode_unit(g, u);
-                if (!unit_runs(x, OUTPUTS)) continue;
-                for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
-                    const int b = n & 1;
-                    ok = mbar_wait_bounded(bar + bFullK + b, (n / 2) & 1);
-                    for (int hj = 0; hj < 4 && ok; ++hj) {                      // halves of 64 tokens, both sets
-                        const int h = hj >> 1, j = hj & 1;
-                        ok = mbar_wait_bounded(bar + bW + j, h);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile + h * 8192u, kTile, 1024u);
+        constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+        const uint64_t dw = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
+        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            const Unit x = decode_unit(g, u);
+            if (!unit_runs(x, OUTPUTS)) continue;
+            for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
+                const int b = n & 1;
+                ok = warp_wait(bar + bFullK + b, (n / 2) & 1);
+                const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, kTile, 1024u);
 #pragma unroll
-                        for (int i = 0; i < 12; ++i) {
-                            const uint64_t dw = swizzled_desc(sbase + kWOff + j * kWBuf + (i / 4) * 8192u, 16u, 1024u);
-                            mma_ss(tmem + kProd + j * 64, dk + (uint32_t)(i % 4) * 128u, dw + (uint32_t)(i % 4) * 128u, kDesc, i > 0 || h > 0);
-                        }
-                        tc_commit(bar + bProd + j);
-                    }
-                    if (ok) tc_commit(bar + bEmptyK + b);
+                for (int h = 0; h < 2; ++h) {                                   // halves of 64 tokens, both sets' columns
+                    ok = ok && warp_wait(bar + bW, h);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 12; ++i)
+                        if (elect())
+                            mma_ss(tmem + kProd, dk + (uint32_t)(h * 4 + i % 4) * 128u, dw + (uint32_t)(i / 4) * 512u + (uint32_t)(i % 4) * 128u, kDesc, i > 0 || h > 0);
+                    if (elect()) tc_commit(bar + bProd);
+                    __syncwarp();
                 }
+                if (ok && elect()) tc_commit(bar + bEmptyK + b);
+                __syncwarp();
             }
-            if (!ok) record_fault(p.status, kFaultScanWait, 3);
         }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 3);
         __syncwarp();
     } else if (warp == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -439,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                     if (valid < kQ) proxy_fence();
                     if (!fresh) {
-                        ok = ok && warp_wait(bar + bInter + j, m & 1);
+                        ok = ok && warp_wait(bar + bInter, m & 1);
                         ++m;
                         if (!ok) break;
                         tc_fence_after();
@@ -466,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         mbar_arrive_one(bar + bGateFree + b);
                     }
                     // Y: what the products left, and the skip; v's row becomes y's, then the warp stores its rows
-                    ok = ok && warp_wait(bar + bY + j, n & 1) && warp_wait(bar + bVRead + j, n & 1);
+                    ok = ok && warp_wait(bar + bY + j, n & 1) && warp_wait(bar + bVRead + j * 2 + b, (n / 2) & 1);
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t d[2][32];
@@ -475,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     tmem_ld_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_one(bar + bYFree + j);
+                    if (lane == 0) mbar_arrive_one(bar + bYFree);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         uint4* at = reinterpret_cast<uint4*>(mine + ((c ^ (row & 7)) * 16));
@@ -567,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                     proxy_fence();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_one(bar + bState + j);
+                    if (lane == 0) mbar_arrive_one(bar + bState);
                 }
                 ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bFullV + b, (n / 2) & 1) && warp_wait(bar + bFullK + b, (n / 2) & 1);
                 if (!ok) break;
@@ -580,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                 }
                 if (OUTPUTS && !fresh) {                 // the buffer's S has been read
-                    ok = warp_wait(bar + bInter + j, m & 1);
+                    ok = warp_wait(bar + bInter, m & 1);
                     ++m;
                     if (!ok) break;
                 }
@@ -588,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (h == 1) {
-                        ok = warp_wait(bar + bProd + j, 0);
+                        ok = warp_wait(bar + bProd, 0);
                         if (!ok) break;
                     }
                     const int tt = bt >> 1, t64 = h * 64 + tt;                   // two threads a token
@@ -617,14 +627,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive_one(bar + bW + j);
-                        if (h == 1) mbar_arrive_one(OUTPUTS ? bar + bVRead + j : bar + bEmptyV + b);
+                        mbar_arrive_one(bar + bW);
+                        if (h == 1) mbar_arrive_one(OUTPUTS ? bar + bVRead + j * 2 + b : bar + bEmptyV + b);
                     }
                 }
                 if (!ok) break;
                 const float keep = ex2(gates[b * kGateBuf + j * kGateSet + kQ - 1]);
                 total *= keep;
-                ok = warp_wait(bar + bProd + j, 1);
+                ok = warp_wait(bar + bProd, 1);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
