@@ -7,15 +7,15 @@
 // one of 128), which share K, Q and the products Q K^T.
 //
 // Precision.  Q K^T is exact up to the fp32 sums.  The state is held in fp32 registers; W goes to the tensor cores in three bf16
-// parts, so that a term of S is off by less than 2^-25.  P goes in two parts (2^-17), S as an operand of Y in one (2^-9, half a
-// step of bf16: the outputs are rounded to bf16 by as much behind it).  Sums of decays run forward for c_t and backward for
-// c_end - c_t, so that what is small is exact.
+// parts, so that a term of S is off by less than 2^-22.  P, and S as an operand of Y, are rounded to bf16 once: the outputs are rounded
+// by as much behind them, so an output's error is sqrt(2) times that of its own rounding, at most.  (P in two parts, which cuts half
+// of that, took 16.6 products of 128 x 64 x 128 a pair of heads instead of 12.1 and was 60 % slower.)  Sums of decays run forward for
+// c_t and backward for c_end - c_t, so that what is small is exact.
 //
 // Roles: warp 0 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
 // warp 3 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, scale Q S there, add the skip and
 // store Y, and four ("B") make W, hold S and hand it on as an operand.  They meet through mbarriers alone; every wait is bounded.
-// Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64; the lower parts of P take the columns of Q K^T that
-// both sets have read.
+// Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64.
 //
 // Few sequences and heads: a sequence is split into segments.  A first launch (OUTPUTS = false) leaves every segment's own state and
 // decay in the scratch, a second one starts each segment from the sum of those before it.
@@ -31,13 +31,13 @@ constexpr int kQ = 128;                                // tokens of a chunk
 constexpr uint32_t kTile = 16384u;                     // 128 rows of 128 bytes
 constexpr uint32_t kKOff = 0, kQOff = 4 * kTile, kVOff = 6 * kTile, kWOff = 10 * kTile;      // K in two buffers, Q in one, V in two
 constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 64 tokens in three parts, or S in one
-constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][4][128] floats: c, beta, beta 2^(c_end - c), 2^c
+constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][4][128] floats: c, log2(beta) - c, beta 2^(c_end - c), 2^c
 constexpr uint32_t kGateSet = 4 * kQ, kGateBuf = 2 * kGateSet;
 constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
 constexpr int kThreads = 640;
 
 enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
-       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 23, bVRead = 24, bRead = 28, kBars = 32 };
+       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 23, bVRead = 24, kBars = 28 };
 constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
 
 // columns of tensor memory
@@ -148,8 +148,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;                // both product warps read K
             if (i >= bEmptyV && i < bGate) n = 8;                               // A (without outputs: B) of both sets
             if (i >= bGateFree && i < bDot) n = OUTPUTS ? 16 : 8;
-            if (i == bState || i == bYFree || i == bW || i >= bRead) n = 8;     // the warps of both sets
-            if ((i >= bP && i < bY) || (i >= bVRead && i < bRead)) n = 4;       // of one
+            if (i == bState || i == bYFree || i == bW) n = 8;     // the warps of both sets
+            if ((i >= bP && i < bY) || i >= bVRead) n = 4;       // of one
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -224,9 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     const int b = n & 1;
                     const bool fresh = fresh0 && t == x.t0;                     // S is zero
                     ok = warp_wait(bar + bFullK + b, (n / 2) & 1) && warp_wait(bar + bFullQ, n & 1);
-                    // the columns of Q K^T hold parts of P until the products with them are done
-                    ok = ok && (n < 1 || (warp_wait(bar + bY, (n - 1) & 1) && warp_wait(bar + bY + 1, (n - 1) & 1)));
-                    if (!ok) break;
+                    if (!ok) break;                                             // (P of the chunk before is made: its Q K^T has been read)
                     tc_fence_after();
                     const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, 16u, 1024u);
 #pragma unroll
@@ -261,10 +259,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                         for (int i = 1; i < 8; ++i)
                             if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + i * 8, dv + (uint32_t)i * 128u, kPDesc, true);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (elect())
-                                mma_ts(tmem + kY + j * 64, tmem + kDot + (i / 2) * 32 + j * 16 + (i % 2) * 8, dv + (uint32_t)i * 128u, kPDesc, true);
                         if (elect()) tc_commit(bar + bY + j);
                         __syncwarp();
                     }
@@ -336,9 +330,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float l[4], pre[4], suf[4];
-                    // (2^-256 is zero in fp32 anyway; the bound keeps differences of sums finite)
+                    // (2^-160 is zero in fp32; the bound keeps the sums finite, and a difference of two exact to 2^-10)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) l[i] = t + lane * 4 + i < x.t1 ? fmaxf(a2[j] * beta[j][i], -256.f) : 0.f;
+                    for (int i = 0; i < 4; ++i) l[i] = t + lane * 4 + i < x.t1 ? fmaxf(a2[j] * beta[j][i], -160.f) : 0.f;
                     pre[0] = l[0];
 #pragma unroll
                     for (int i = 1; i < 4; ++i) pre[i] = pre[i - 1] + l[i];
@@ -362,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         pc[i] = before + pre[i];
-                        pb[i] = beta[j][i];
+                        pb[i] = __log2f(beta[j][i]) - pc[i];
                         pw[i] = beta[j][i] * exp2f(after + suf[i]);
                         pe[i] = exp2f(pc[i]);
                     }
@@ -404,44 +398,30 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bDot, n & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const float ct = gt[row];
+                    const uint64_t ct = pack2(gt[row], gt[row]);
+#pragma unroll 1
+                    for (int c = 0; c <= quad; ++c) {
+                        uint32_t d[32], f[16];
+                        tmem_ld32_async(td + c * 32, d);
+                        tmem_ld_wait();
+                        const ulonglong2* e4 = reinterpret_cast<const ulonglong2*>(gt + kQ + c * 32);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t hi[16], lo[16];
-                        uint32_t d[32];
-                        if (c <= quad) {
-                            tmem_ld32_async(td + c * 32, d);
-                            tmem_ld_wait();
+                        for (int i = 0; i < 8; ++i) {
+                            const ulonglong2 e = e4[i];
+                            float x0, x1, x2, x3;
+                            unpack2(add2(ct, e.x), x0, x1);
+                            unpack2(add2(ct, e.y), x2, x3);
+                            unpack2(mul2(pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), pack2(ex2(x0), ex2(x1))), x0, x1);
+                            unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), pack2(ex2(x2), ex2(x3))), x2, x3);
+                            f[2 * i] = bf16x2(x0, x1);
+                            f[2 * i + 1] = bf16x2(x2, x3);
                         }
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_one(bar + bRead + c);
-                        if (c <= quad) {
-                            const float4 *c4 = reinterpret_cast<const float4*>(gt + c * 32), *b4 = reinterpret_cast<const float4*>(gt + kQ + c * 32);
+                        if (c == quad) {                                         // the diagonal: column 2 i + e of the 32 is there up to row `lane`
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float4 cs = c4[i], be = b4[i];
-                                float f[4] = {__uint_as_float(d[4 * i]) * be.x * ex2(ct - cs.x), __uint_as_float(d[4 * i + 1]) * be.y * ex2(ct - cs.y),
-                                              __uint_as_float(d[4 * i + 2]) * be.z * ex2(ct - cs.z), __uint_as_float(d[4 * i + 3]) * be.w * ex2(ct - cs.w)};
-                                if (c == quad) {
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e)
-                                        if (4 * i + e > lane) f[e] = 0.f;
-                                }
-                                split_bf16x2(f[0], f[1], hi[2 * i], lo[2 * i]);
-                                split_bf16x2(f[2], f[3], hi[2 * i + 1], lo[2 * i + 1]);
-                            }
-                            tmem_st16u(tp + c * 16, hi);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) lo[i] = 0u;
+                            for (int i = 0; i < 16; ++i) f[i] &= (2 * i <= lane ? 0xffffu : 0u) | (2 * i + 1 <= lane ? 0xffff0000u : 0u);
                         }
-                        ok = ok && warp_wait(bar + bRead + c, n & 1);            // both sets have read these columns
-                        if (!ok) break;
-                        tc_fence_after();
-                        tmem_st16u(td + c * 32 + j * 16, lo);
+                        tmem_st16u(tp + c * 16, f);
                     }
-                    if (!ok) break;
                     ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
                     if (ok && row >= valid) {                                    // rows of the next sequence are no part of this one
 #pragma unroll
@@ -456,16 +436,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         const float ec = gt[3 * kQ + row];
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            uint32_t d[32];
-                            tmem_ld32_async(ty + c * 32, d);
+                            uint32_t d[2][16];
+                            tmem_ld16_async(ty + c * 32, d[0]);
+                            tmem_ld16_async(ty + c * 32 + 16, d[1]);
                             tmem_ld_wait();
-                            float f[16];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(d[i]) * ec;
-                            tmem_st16(ty + c * 32, f);
+                            for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(d[16 + i]) * ec;
-                            tmem_st16(ty + c * 32 + 16, f);
+                                for (int i = 0; i < 16; ++i) d[e][i] = __float_as_uint(__uint_as_float(d[e][i]) * ec);
+                                tmem_st16u(ty + c * 32 + e * 16, d[e]);
+                            }
                         }
                     }
                     tmem_st_wait();
@@ -513,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         unsigned char* buf = smem + kWOff + j * kWBuf;
         unsigned char* rows = buf + quad * 4096;        // this warp's 32 rows of 128 bytes
-        float S[64];
+        uint64_t S[32];                                 // pairs of columns
         int m = 0;                                      // chunks with a state before them
         for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
             const Unit x = decode_unit(g, u);
@@ -532,11 +512,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const float4 f = *reinterpret_cast<const float4*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16));
-                        S[c * 32 + 4 * i] = fmaf(keep, S[c * 32 + 4 * i], f.x);
-                        S[c * 32 + 4 * i + 1] = fmaf(keep, S[c * 32 + 4 * i + 1], f.y);
-                        S[c * 32 + 4 * i + 2] = fmaf(keep, S[c * 32 + 4 * i + 2], f.z);
-                        S[c * 32 + 4 * i + 3] = fmaf(keep, S[c * 32 + 4 * i + 3], f.w);
+                        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16));
+                        S[c * 16 + 2 * i] = fma2(pack2(keep, keep), S[c * 16 + 2 * i], f.x);
+                        S[c * 16 + 2 * i + 1] = fma2(pack2(keep, keep), S[c * 16 + 2 * i + 1], f.y);
                     }
                     __syncwarp();
                 }
@@ -546,15 +524,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 for (int c = 0; c < 2; ++c) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<float4*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16)) =
-                            make_float4(S[c * 32 + 4 * i], S[c * 32 + 4 * i + 1], S[c * 32 + 4 * i + 2], S[c * 32 + 4 * i + 3]);
+                        *reinterpret_cast<ulonglong2*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16)) = make_ulonglong2(S[c * 16 + 2 * i], S[c * 16 + 2 * i + 1]);
                     __syncwarp();
                     copy_rows<true>(rows, reinterpret_cast<unsigned char*>(to + c * 32), (long long)p.V * 4, 32);
                     __syncwarp();
                 }
             };
 #pragma unroll
-            for (int i = 0; i < 64; ++i) S[i] = 0.f;
+            for (int i = 0; i < 32; ++i) S[i] = 0ull;
             if (x.seg == 0) {
                 // (a later segment's CTA may have written the entry already: the first launch kept a copy)
                 if (src >= 0) load(OUTPUTS && !x.last ? scratch : p.state + src * entry + at, 0.f);
@@ -572,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     for (int c = 0; c < 8; ++c) {
                         float f[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = S[c * 8 + i];
+                        for (int i = 0; i < 4; ++i) unpack2(S[c * 4 + i], f[2 * i], f[2 * i + 1]);
                         *reinterpret_cast<uint4*>(buf + row * 128 + ((c ^ (row & 7)) * 16)) = Vec16<__nv_bfloat16>::pack(f);
                     }
                     proxy_fence();
@@ -595,30 +572,35 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     if (!ok) break;
                 }
                 const float* w = gates + b * kGateBuf + j * kGateSet + 2 * kQ;
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     if (h == 1) {
                         ok = warp_wait(bar + bProd, 0);
                         if (!ok) break;
                     }
                     const int tt = bt >> 1, t64 = h * 64 + tt;                   // two threads a token
-                    const float wt = w[t64];
+                    const uint64_t wt = pack2(w[t64], w[t64]), minus = pack2(-1.f, -1.f);
+                    const uint32_t keep_rows = t64 < valid ? 0xffffffffu : 0u;
                     const unsigned char* v = smem + kVOff + (b * 2 + j) * kTile + t64 * 128;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const uint32_t off = (uint32_t)((((bt & 1) * 4 + c) ^ (tt & 7)) * 16);
-                        float f[8];
-                        Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(v + off), f);
+                        const uint4 vv = *reinterpret_cast<const uint4*>(v + off);
+                        const uint32_t v4[4] = {vv.x & keep_rows, vv.y & keep_rows, vv.z & keep_rows, vv.w & keep_rows};
                         uint32_t q[3][4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            float a0 = t64 < valid ? f[2 * i] * wt : 0.f, a1 = t64 < valid ? f[2 * i + 1] * wt : 0.f;
+                            // the upper 16 bits of what is left, twice, and the rest rounded: 8 + 8 + 8 bits
+                            uint64_t r = mul2(pack2(__uint_as_float(v4[i] << 16), __uint_as_float(v4[i] & 0xffff0000u)), wt);
 #pragma unroll
-                            for (int e = 0; e < 3; ++e) {
-                                q[e][i] = bf16x2(a0, a1);
-                                a0 -= __uint_as_float(q[e][i] << 16);
-                                a1 -= __uint_as_float(q[e][i] & 0xffff0000u);
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t lo = (uint32_t)r & 0xffff0000u, hi = (uint32_t)(r >> 32) & 0xffff0000u;
+                                q[e][i] = __byte_perm(lo, hi, 0x7632);
+                                r = fma2(pack2(__uint_as_float(lo), __uint_as_float(hi)), minus, r);
                             }
+                            float r0, r1;
+                            unpack2(r, r0, r1);
+                            q[2][i] = bf16x2(r0, r1);
                         }
 #pragma unroll
                         for (int e = 0; e < 3; ++e)
@@ -637,12 +619,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 ok = warp_wait(bar + bProd, 1);
                 if (!ok) break;
                 tc_fence_after();
+                const uint64_t keep2 = pack2(keep, keep);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float d[16];
-                    tmem_ld16(tmem + lanes + kProd + j * 64 + c * 16, d);
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t d[2][16];
+                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + c * 32, d[0]);
+                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + c * 32 + 16, d[1]);
+                    tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) S[c * 16 + i] = fmaf(keep, S[c * 16 + i], d[i]);
+                    for (int i = 0; i < 16; ++i)
+                        S[c * 16 + i] = fma2(keep2, S[c * 16 + i], pack2(__uint_as_float(d[i / 8][2 * i % 16]), __uint_as_float(d[i / 8][2 * i % 16 + 1])));
                 }
                 tc_fence_before();
                 __syncwarp();
