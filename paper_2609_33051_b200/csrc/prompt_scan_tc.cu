@@ -30,14 +30,14 @@ using namespace tc;
 constexpr int kQ = 128;                                // tokens of a chunk
 constexpr uint32_t kTile = 16384u;                     // 128 rows of 128 bytes
 constexpr uint32_t kKOff = 0, kQOff = 4 * kTile, kVOff = 6 * kTile, kWOff = 10 * kTile;      // K in two buffers, Q in one, V in two
-constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 64 tokens in three parts, or S in one
-constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][4][128] floats: c, log2(beta) - c, beta 2^(c_end - c), 2^c
-constexpr uint32_t kGateSet = 4 * kQ, kGateBuf = 2 * kGateSet;
+constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 32 tokens in three parts, twice, or S in one
+constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][5][128] floats: see gates
+constexpr uint32_t kGateSet = 5 * kQ, kGateBuf = 2 * kGateSet;
 constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
 constexpr int kThreads = 640;
 
 enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
-       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 23, bVRead = 24, kBars = 28 };
+       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 24, bVRead = 26, kBars = 30 };
 constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
 
 // columns of tensor memory
@@ -47,7 +47,7 @@ struct ScanArgs {
     CUtensorMap tq, tk, tv;
     ScanParams p;
     int slabs, slabs_per_group, blocks_per_group;      // pairs of column blocks: all, per group; column blocks per group
-    long long units;
+    int units;
 };
 
 // One unit: a segment of a sequence for one pair of column blocks.
@@ -58,12 +58,11 @@ struct Unit {
     int last;              // this segment ends the sequence
 };
 
-__device__ __forceinline__ Unit decode_unit(const ScanArgs& g, long long u) {
+__device__ __forceinline__ Unit decode_unit(const ScanArgs& g, int u) {
     Unit x;
-    const int slab = (int)(u % g.slabs);
-    const long long r = u / g.slabs;
-    x.seg = (int)(r % g.p.segments);
-    x.seq = (int)(r / g.p.segments);
+    const int slab = u % g.slabs, r = u / g.slabs;
+    x.seg = r % g.p.segments;
+    x.seq = r / g.p.segments;
     x.group = slab / g.slabs_per_group;
     const int i = slab % g.slabs_per_group * 2;
     x.block0 = x.group * g.blocks_per_group + i;
@@ -119,7 +118,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { retu
 template <bool STORE>
 __device__ __forceinline__ void copy_rows(unsigned char* tile, unsigned char* global, long long stride, int n) {
     const int lane = (int)threadIdx.x & 31;
-#pragma unroll
+#pragma unroll 2
     for (int i = 0; i < 8; ++i) {
         const int r = i * 4 + lane / 8, c = lane % 8;
         uint4* s = reinterpret_cast<uint4*>(tile + r * 128 + ((c ^ (r & 7)) * 16));
@@ -148,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;                // both product warps read K
             if (i >= bEmptyV && i < bGate) n = 8;                               // A (without outputs: B) of both sets
             if (i >= bGateFree && i < bDot) n = OUTPUTS ? 16 : 8;
-            if (i == bState || i == bYFree || i == bW) n = 8;     // the warps of both sets
+            if (i == bState || i == bYFree || i == bW || i == bW + 1) n = 8;     // the warps of both sets
             if ((i >= bP && i < bY) || i >= bVRead) n = 4;       // of one
             mbar_init(bar + i, n);
         }
@@ -168,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (lane == 0) {
-            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
                 const Unit x = decode_unit(g, u);
                 if (!unit_runs(x, OUTPUTS)) continue;
                 for (int t = x.t0; t < x.t1; t += kQ, ++n) {
@@ -216,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             constexpr uint32_t kPDesc = kTypes | (1u << 16) | ((64u >> 3) << 17);
             const uint64_t dq = swizzled_desc(sbase + kQOff, 16u, 1024u), ds = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
             int m = 0;                                  // chunks with a state before them
-            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
                 const Unit x = decode_unit(g, u);
                 if (!unit_runs(x, true)) continue;
                 const bool fresh0 = x.seg == 0 && seq_resume(p.pr, x.seq) < 0;
@@ -272,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
         const uint64_t dw = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
-        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const Unit x = decode_unit(g, u);
             if (!unit_runs(x, OUTPUTS)) continue;
             for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
@@ -280,15 +279,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 ok = warp_wait(bar + bFullK + b, (n / 2) & 1);
                 const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, kTile, 1024u);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {                                   // halves of 64 tokens, both sets' columns
-                    ok = ok && warp_wait(bar + bW, h);
+                for (int h = 0; h < 4; ++h) {                                   // 32 tokens at a time, both sets' columns
+                    ok = ok && warp_wait(bar + bW + (h & 1), h >> 1);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int i = 0; i < 12; ++i)
+                    for (int i = 0; i < 6; ++i)
                         if (elect())
-                            mma_ss(tmem + kProd, dk + (uint32_t)(h * 4 + i % 4) * 128u, dw + (uint32_t)(i / 4) * 512u + (uint32_t)(i % 4) * 128u, kDesc, i > 0 || h > 0);
-                    if (elect()) tc_commit(bar + bProd);
+                            mma_ss(tmem + kProd, dk + (uint32_t)(h * 2 + i % 2) * 128u, dw + (uint32_t)(h & 1) * 768u + (uint32_t)(i / 2) * 256u + (uint32_t)(i % 2) * 128u,
+                                   kDesc, i > 0 || h > 0);
+                    if (elect()) tc_commit(bar + bProd + (h & 1));
                     __syncwarp();
                 }
                 if (ok && elect()) tc_commit(bar + bEmptyK + b);
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     } else if (warp == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // gates: four neighbouring tokens a lane
-        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const Unit x = decode_unit(g, u);
             if (!unit_runs(x, OUTPUTS)) continue;
             const int h0 = x.block0 / per_head, h1 = (x.block0 + x.live1) / per_head;
@@ -351,17 +351,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     after = __shfl_down_sync(0xffffffffu, after, 1);
                     if (lane == 0) before = 0.f;
                     if (lane == 31) after = 0.f;
-                    float4 c, be, w, e;
-                    float *pc = &c.x, *pb = &be.x, *pw = &w.x, *pe = &e.x;
+                    float c[4], lb[4], w[4], e[4], f[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[i] = before + pre[i];
+                    const float end = __shfl_sync(0xffffffffu, c[3], lane | 7);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        pc[i] = before + pre[i];
-                        pb[i] = __log2f(beta[j][i]) - pc[i];
-                        pw[i] = beta[j][i] * exp2f(after + suf[i]);
-                        pe[i] = exp2f(pc[i]);
+                        lb[i] = __log2f(beta[j][i]) - c[i];
+                        w[i] = beta[j][i] * exp2f(after + suf[i]);
+                        e[i] = exp2f(c[i]);
+                        f[i] = beta[j][i] * ex2(end - c[i]);
                     }
                     float4* o = reinterpret_cast<float4*>(gates + b * kGateBuf + j * kGateSet) + lane;
-                    o[0] = c; o[32] = be; o[64] = w; o[96] = e;
+                    o[0] = make_float4(c[0], c[1], c[2], c[3]);                  // c
+                    o[32] = make_float4(lb[0], lb[1], lb[2], lb[3]);             // log2(beta) - c
+                    o[64] = make_float4(w[0], w[1], w[2], w[3]);                 // beta 2^(c at the chunk's end - c)
+                    o[96] = make_float4(e[0], e[1], e[2], e[3]);                 // 2^c
+                    o[128] = make_float4(f[0], f[1], f[2], f[3]);                // beta 2^(c at the end of the 32 tokens - c)
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive_one(bar + bGate + b);
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 for (int c = 0; c < 4; ++c) tmem_st16u(tp + c * 16, z);          // above the diagonal P stays zero
                 tmem_st_wait();
             }
-            for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+            for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
                 const Unit x = decode_unit(g, u);
                 if (!unit_runs(x, true)) continue;
                 const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
@@ -398,29 +404,49 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bDot, n & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t ct = pack2(gt[row], gt[row]);
+                    // P: below the diagonal's 32 x 32 blocks its weight is 2^(c_t - c at the end of the columns' 32) times a factor of
+                    // the column, both at most 1 (but for beta); in them it is one exponential an element
+                    const float ct = gt[row];
 #pragma unroll 1
-                    for (int c = 0; c <= quad; ++c) {
+                    for (int c = 0; c < quad; ++c) {
                         uint32_t d[32], f[16];
                         tmem_ld32_async(td + c * 32, d);
+                        const float r = ex2(ct - gt[c * 32 + 31]);
+                        const uint64_t r2 = pack2(r, r);
+                        const ulonglong2* f4 = reinterpret_cast<const ulonglong2*>(gt + 4 * kQ + c * 32);
                         tmem_ld_wait();
-                        const ulonglong2* e4 = reinterpret_cast<const ulonglong2*>(gt + kQ + c * 32);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const ulonglong2 w = f4[i];
+                            float x0, x1, x2, x3;
+                            unpack2(mul2(pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), mul2(r2, w.x)), x0, x1);
+                            unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), mul2(r2, w.y)), x2, x3);
+                            f[2 * i] = bf16x2(x0, x1);
+                            f[2 * i + 1] = bf16x2(x2, x3);
+                        }
+                        tmem_st16u(tp + c * 16, f);
+                    }
+                    {
+                        uint32_t d[32], f[16];
+                        tmem_ld32_async(td + quad * 32, d);
+                        const uint64_t ct2 = pack2(ct, ct);
+                        const ulonglong2* e4 = reinterpret_cast<const ulonglong2*>(gt + kQ + quad * 32);
+                        tmem_ld_wait();
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const ulonglong2 e = e4[i];
                             float x0, x1, x2, x3;
-                            unpack2(add2(ct, e.x), x0, x1);
-                            unpack2(add2(ct, e.y), x2, x3);
+                            unpack2(add2(ct2, e.x), x0, x1);
+                            unpack2(add2(ct2, e.y), x2, x3);
                             unpack2(mul2(pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), pack2(ex2(x0), ex2(x1))), x0, x1);
                             unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), pack2(ex2(x2), ex2(x3))), x2, x3);
                             f[2 * i] = bf16x2(x0, x1);
                             f[2 * i + 1] = bf16x2(x2, x3);
                         }
-                        if (c == quad) {                                         // the diagonal: column 2 i + e of the 32 is there up to row `lane`
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) f[i] &= (2 * i <= lane ? 0xffffu : 0u) | (2 * i + 1 <= lane ? 0xffff0000u : 0u);
-                        }
-                        tmem_st16u(tp + c * 16, f);
+                        for (int i = 0; i < 16; ++i)            // column 2 i + e of the 32 is there up to row `lane`
+                            f[i] &= (2 * i <= lane ? 0xffffu : 0u) | (2 * i + 1 <= lane ? 0xffff0000u : 0u);
+                        tmem_st16u(tp + quad * 16, f);
                     }
                     ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
                     if (ok && row >= valid) {                                    // rows of the next sequence are no part of this one
@@ -495,16 +521,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         unsigned char* rows = buf + quad * 4096;        // this warp's 32 rows of 128 bytes
         uint64_t S[32];                                 // pairs of columns
         int m = 0;                                      // chunks with a state before them
-        for (long long u = blockIdx.x; u < g.units && ok; u += gridDim.x) {
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const Unit x = decode_unit(g, u);
             if (!unit_runs(x, OUTPUTS)) continue;
-            const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
+            const int block = x.block0 + (j ? x.live1 : 0);
             const bool live = j == 0 || x.live1;
-            const int src = seq_resume(p.pr, x.seq), dst = seq_slot(p.pr, x.seq);
-            const size_t at = (size_t)head * 128 * p.V + (size_t)quad * 32 * p.V + (block % per_head) * 64, entry = (size_t)p.H * 128 * p.V;
-            // scratch: per sequence `segments` states (that before segment 0, those left by segments 0, 1, ..) and as many decays a head
-            float* scratch = p.work + (size_t)x.seq * p.segments * entry + at;
-            float* decays = p.work + (size_t)p.pr.N * p.segments * entry + (size_t)x.seq * p.segments * p.H + head;
+            const int src = seq_resume(p.pr, x.seq);
+            // The block's first row of this warp in a state; and in the scratch: per sequence `segments` states (that before segment 0,
+            // those left by segments 0, 1, ..) and behind them as many decays a head.  (Worked out where they are used, from a
+            // number that the compiler cannot see through: kept over the chunks they cost the registers of the state.)
+            auto at = [&](int row0) {
+                int k = block;
+                asm volatile("" : "+r"(k));
+                return ((size_t)row0 * p.H + k / per_head) * 128 * p.V + (size_t)quad * 32 * p.V + (k % per_head) * 64;
+            };
+            auto decay = [&](int i) {
+                int k = block;
+                asm volatile("" : "+r"(k));
+                return p.work + (size_t)p.pr.N * p.segments * p.H * 128 * p.V + ((size_t)x.seq * p.segments + i) * p.H + k / per_head;
+            };
             auto load = [&](const float* from, float keep) {                     // S <- keep S + rows of global memory
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -534,10 +569,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             for (int i = 0; i < 32; ++i) S[i] = 0ull;
             if (x.seg == 0) {
                 // (a later segment's CTA may have written the entry already: the first launch kept a copy)
-                if (src >= 0) load(OUTPUTS && !x.last ? scratch : p.state + src * entry + at, 0.f);
-                if (!OUTPUTS && live) store(scratch);
+                if (src >= 0) load(OUTPUTS && !x.last ? p.work + at(x.seq * p.segments) : p.state + at(src), 0.f);
+                if (!OUTPUTS && live) store(p.work + at(x.seq * p.segments));
             } else if (OUTPUTS) {
-                for (int i = 1; i <= x.seg; ++i) load(scratch + (size_t)i * entry, i == 1 ? 0.f : decays[(size_t)i * p.H]);
+                for (int i = 1; i <= x.seg; ++i) load(p.work + at(x.seq * p.segments + i), i == 1 ? 0.f : *decay(i));
             }
             const bool fresh0 = x.seg == 0 && src < 0;
             float total = 1.f;
@@ -572,21 +607,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     if (!ok) break;
                 }
                 const float* w = gates + b * kGateBuf + j * kGateSet + 2 * kQ;
+                const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll 1
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) {
-                        ok = warp_wait(bar + bProd, 0);
+                for (int h = 0; h < 4; ++h) {
+                    if (h >= 2) {
+                        ok = warp_wait(bar + bProd + (h & 1), 0);
                         if (!ok) break;
                     }
-                    const int tt = bt >> 1, t64 = h * 64 + tt;                   // two threads a token
-                    const uint64_t wt = pack2(w[t64], w[t64]), minus = pack2(-1.f, -1.f);
-                    const uint32_t keep_rows = t64 < valid ? 0xffffffffu : 0u;
-                    const unsigned char* v = smem + kVOff + (b * 2 + j) * kTile + t64 * 128;
+                    const int tt = bt >> 2, t32 = h * 32 + tt;                   // four threads a token, 16 columns each
+                    const uint64_t wt = pack2(w[t32], w[t32]);
+                    const uint32_t inside = t32 < valid ? 0xffffffffu : 0u;
+                    const unsigned char* v = smem + kVOff + (b * 2 + j) * kTile + t32 * 128;
+                    unsigned char* to = buf + (h & 1) * 12288 + tt * 128;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const uint32_t off = (uint32_t)((((bt & 1) * 4 + c) ^ (tt & 7)) * 16);
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t off = (uint32_t)((((bt & 3) * 2 + c) ^ (tt & 7)) * 16);
                         const uint4 vv = *reinterpret_cast<const uint4*>(v + off);
-                        const uint32_t v4[4] = {vv.x & keep_rows, vv.y & keep_rows, vv.z & keep_rows, vv.w & keep_rows};
+                        const uint32_t v4[4] = {vv.x & inside, vv.y & inside, vv.z & inside, vv.w & inside};
                         uint32_t q[3][4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -604,19 +641,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         }
 #pragma unroll
                         for (int e = 0; e < 3; ++e)
-                            *reinterpret_cast<uint4*>(buf + e * 8192 + tt * 128 + off) = make_uint4(q[e][0], q[e][1], q[e][2], q[e][3]);
+                            *reinterpret_cast<uint4*>(to + e * 4096 + off) = make_uint4(q[e][0], q[e][1], q[e][2], q[e][3]);
                     }
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) {
-                        mbar_arrive_one(bar + bW);
-                        if (h == 1) mbar_arrive_one(OUTPUTS ? bar + bVRead + j * 2 + b : bar + bEmptyV + b);
+                        mbar_arrive_one(bar + bW + (h & 1));
+                        if (h == 3) mbar_arrive_one(OUTPUTS ? bar + bVRead + j * 2 + b : bar + bEmptyV + b);
                     }
                 }
                 if (!ok) break;
                 const float keep = ex2(gates[b * kGateBuf + j * kGateSet + kQ - 1]);
                 total *= keep;
-                ok = warp_wait(bar + bProd, 1);
+                ok = warp_wait(bar + bProd + 1, 1);
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t keep2 = pack2(keep, keep);
@@ -636,11 +673,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             }
             if (!ok) break;
             if (live) {
-                if (!OUTPUTS) {
-                    store(scratch + (size_t)(x.seg + 1) * entry);
-                    if (row == 0 && block % per_head == 0) decays[(size_t)(x.seg + 1) * p.H] = total;
-                } else if (x.last && dst >= 0) {
-                    store(p.state + dst * entry + at);
+                if constexpr (!OUTPUTS) {
+                    store(p.work + at(x.seq * p.segments + x.seg + 1));
+                    if (row == 0 && block % per_head == 0) *decay(x.seg + 1) = total;
+                } else if (x.last) {
+                    const int dst = seq_slot(p.pr, x.seq);
+                    if (dst >= 0) store(p.state + at(dst));
                 }
             }
         }
@@ -667,7 +705,9 @@ int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_
     g.blocks_per_group = p.H / p.G * (p.V / 64);
     g.slabs_per_group = (g.blocks_per_group + 1) / 2;
     g.slabs = g.slabs_per_group * p.G;
-    g.units = (long long)p.pr.N * p.segments * g.slabs;
+    const long long units = (long long)p.pr.N * p.segments * g.slabs;
+    if (units > (1 << 30)) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    g.units = (int)units;
     if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
         !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ) ||
         !make_map(&g.tv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.v, (uint64_t)p.H * p.V, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2, kQ)) {
