@@ -88,7 +88,9 @@ int sketchssm_conv_step(sketchssm_ctx* ctx, int groups, int width, const void* w
 
 int sketchssm_prompt_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes) {
     if (ctx == nullptr || bytes == nullptr || sequences < 0 || tokens < 0) return SKETCHSSM_INVALID_ARG;
-    *bytes = 0;
+    const sketchssm_config& c = ctx->cfg;
+    const size_t states = sequences > 0 ? (size_t)scan_segment_states(c, tokens) : 0;
+    *bytes = (states * c.heads * ((size_t)c.dk * c.dv + 1) * 4 + 15) & ~(size_t)15;
     return SKETCHSSM_OK;
 }
 

@@ -84,9 +84,19 @@ int launch_causal_conv(Ctx* ctx, const ConvParams& p, bool bf16, cudaStream_t st
 int launch_conv_step(Ctx* ctx, const ConvStepParams& p, bool bf16, cudaStream_t stream);
 int launch_prompt_scan(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
 int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);    // tcgen05; UNSUPPORTED_SHAPE outside its domain
+int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens);     // parts that a sequence is split into
 int launch_rms_norm(Ctx* ctx, const NormParams& p, bool bf16, cudaStream_t stream);
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
 int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE for few tiles
+
+// Prompt scan on tensor cores: at most this many segments (of all sequences of a batch together) keep a state in the scratch.  A unit
+// of work is a segment for two blocks of 64 value columns; segments are made until 148 SMs have one, of at least four chunks of
+// 128 tokens on the average.
+inline long long scan_segment_states(const sketchssm_config& c, long long tokens) {
+    if (c.kind != SKETCHSSM_MAMBA2 || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv % 64 != 0) return 0;
+    const long long slabs = ((long long)c.heads * (c.dv / 64) + 1) / 2, n = 148 / slabs, most = tokens / 512;
+    return (n < most ? n : most) < 2 ? 0 : n < most ? n : most;
+}
 
 inline int sm_count(Ctx* ctx) {
     if (ctx->sm_count == 0 && cudaDeviceGetAttribute(&ctx->sm_count, cudaDevAttrMultiProcessorCount, ctx->cfg.device) != cudaSuccess)

@@ -113,20 +113,14 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
 // A warp's wait: false to all its lanes if it ran out.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity)); }
 
-// 32 rows of 128 bytes in shared memory (128-byte swizzle, this warp's) to or from rows of global memory `stride` bytes apart;
-// rows from `n` on are left out.
-template <bool STORE>
-__device__ __forceinline__ void copy_rows(unsigned char* tile, unsigned char* global, long long stride, int n) {
+// 32 rows of 128 bytes in shared memory (128-byte swizzle, this warp's) to rows of global memory `stride` bytes apart; rows from `n` on
+// are left out.
+__device__ __forceinline__ void store_rows(const unsigned char* tile, unsigned char* global, long long stride, int n) {
     const int lane = (int)threadIdx.x & 31;
-#pragma unroll 2
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = i * 4 + lane / 8, c = lane % 8;
-        uint4* s = reinterpret_cast<uint4*>(tile + r * 128 + ((c ^ (r & 7)) * 16));
-        uint4* d = reinterpret_cast<uint4*>(global + r * stride + c * 16);
-        if (r < n) {
-            if constexpr (STORE) *d = *s;
-            else *s = *d;
-        }
+        if (r < n) *reinterpret_cast<uint4*>(global + r * stride + c * 16) = *reinterpret_cast<const uint4*>(tile + r * 128 + ((c ^ (r & 7)) * 16));
     }
 }
 
@@ -503,8 +497,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                     __syncwarp();
                     if (live)
-                        copy_rows<true>(v + quad * 4096, static_cast<unsigned char*>(p.out) + ((long long)(t + quad * 32) * p.out_stride + block * 64) * 2,
-                                        p.out_stride * 2, valid - quad * 32);
+                        store_rows(v + quad * 4096, static_cast<unsigned char*>(p.out) + ((long long)(t + quad * 32) * p.out_stride + block * 64) * 2,
+                                   p.out_stride * 2, valid - quad * 32);
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bEmptyV + b);
@@ -518,7 +512,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         const int j = (warp - 12) >> 2, quad = warp & 3, row = quad * 32 + lane, bt = (tid - 384) & 127;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         unsigned char* buf = smem + kWOff + j * kWBuf;
-        unsigned char* rows = buf + quad * 4096;        // this warp's 32 rows of 128 bytes
         uint64_t S[32];                                 // pairs of columns
         int m = 0;                                      // chunks with a state before them
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
@@ -527,52 +520,52 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             const int block = x.block0 + (j ? x.live1 : 0);
             const bool live = j == 0 || x.live1;
             const int src = seq_resume(p.pr, x.seq);
-            // The block's first row of this warp in a state; and in the scratch: per sequence `segments` states (that before segment 0,
+            // The block's row of this thread in a state; and in the scratch: per sequence `segments` states (that before segment 0,
             // those left by segments 0, 1, ..) and behind them as many decays a head.  (Worked out where they are used, from a
             // number that the compiler cannot see through: kept over the chunks they cost the registers of the state.)
             auto at = [&](int row0) {
                 int k = block;
                 asm volatile("" : "+r"(k));
-                return ((size_t)row0 * p.H + k / per_head) * 128 * p.V + (size_t)quad * 32 * p.V + (k % per_head) * 64;
+                return ((size_t)row0 * p.H + k / per_head) * 128 * p.V + (size_t)row * p.V + (k % per_head) * 64;
             };
             auto decay = [&](int i) {
                 int k = block;
                 asm volatile("" : "+r"(k));
                 return p.work + (size_t)p.pr.N * p.segments * p.H * 128 * p.V + ((size_t)x.seq * p.segments + i) * p.H + k / per_head;
             };
-            auto load = [&](const float* from, float keep) {                     // S <- keep S + rows of global memory
+            // A row is 256 bytes of a state, all of it asked for before the first use: a round trip a state.
+            auto load = [&](const float* from) {
+                const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    copy_rows<false>(rows, reinterpret_cast<unsigned char*>(const_cast<float*>(from + c * 32)), (long long)p.V * 4, 32);
-                    __syncwarp();
+                for (int i = 0; i < 16; ++i) {
+                    const ulonglong2 v = f[i];
+                    S[2 * i] = v.x;
+                    S[2 * i + 1] = v.y;
+                }
+            };
+            auto add = [&](const float* from, float keep) {                      // S <- keep S + a state
+                const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
+                const uint64_t keep2 = pack2(keep, keep);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16));
-                        S[c * 16 + 2 * i] = fma2(pack2(keep, keep), S[c * 16 + 2 * i], f.x);
-                        S[c * 16 + 2 * i + 1] = fma2(pack2(keep, keep), S[c * 16 + 2 * i + 1], f.y);
-                    }
-                    __syncwarp();
+                for (int i = 0; i < 16; ++i) {
+                    const ulonglong2 v = f[i];
+                    S[2 * i] = fma2(keep2, S[2 * i], v.x);
+                    S[2 * i + 1] = fma2(keep2, S[2 * i + 1], v.y);
                 }
             };
             auto store = [&](float* to) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        *reinterpret_cast<ulonglong2*>(rows + lane * 128 + ((i ^ (lane & 7)) * 16)) = make_ulonglong2(S[c * 16 + 2 * i], S[c * 16 + 2 * i + 1]);
-                    __syncwarp();
-                    copy_rows<true>(rows, reinterpret_cast<unsigned char*>(to + c * 32), (long long)p.V * 4, 32);
-                    __syncwarp();
-                }
+                for (int i = 0; i < 16; ++i) reinterpret_cast<ulonglong2*>(to)[i] = make_ulonglong2(S[2 * i], S[2 * i + 1]);
             };
 #pragma unroll
             for (int i = 0; i < 32; ++i) S[i] = 0ull;
             if (x.seg == 0) {
                 // (a later segment's CTA may have written the entry already: the first launch kept a copy)
-                if (src >= 0) load(OUTPUTS && !x.last ? p.work + at(x.seq * p.segments) : p.state + at(src), 0.f);
+                if (src >= 0) load(OUTPUTS && !x.last ? p.work + at(x.seq * p.segments) : p.state + at(src));
                 if (!OUTPUTS && live) store(p.work + at(x.seq * p.segments));
             } else if (OUTPUTS) {
-                for (int i = 1; i <= x.seg; ++i) load(p.work + at(x.seq * p.segments + i), i == 1 ? 0.f : *decay(i));
+                load(p.work + at(x.seq * p.segments + 1));
+                for (int i = 2; i <= x.seg; ++i) add(p.work + at(x.seq * p.segments + i), *decay(i));
             }
             const bool fresh0 = x.seg == 0 && src < 0;
             float total = 1.f;
@@ -692,15 +685,19 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 
 }  // namespace
 
-int prompt_scan_tc_segments(int sms, int sequences, int tokens, int heads, int groups, int V) {
-    return 1;
+// Segments of a sequence, from what the host knows of the lengths.
+int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens) {
+    const sketchssm_config& c = ctx->cfg;
+    const long long slabs = (long long)groups * ((c.heads / groups * (c.dv / 64) + 1) / 2);
+    const long long all = scan_segment_states(c, tokens), n = (all < 148 / slabs ? all : 148 / slabs) / sequences;
+    return n < 2 ? 1 : n > 16 ? 16 : (int)n;
 }
 
 int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_t stream) {
     ScanParams p = p0;
     if (!bf16 || !p.out_bf16 || p.K != 128 || p.V % 64 != 0 || p.pr.T == 0) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    p.segments = prompt_scan_tc_segments(ctx, p.G, p.pr.N, p.pr.T);
     ScanArgs g;
-    p.segments = 1;
     g.p = p;
     g.blocks_per_group = p.H / p.G * (p.V / 64);
     g.slabs_per_group = (g.blocks_per_group + 1) / 2;
@@ -714,9 +711,14 @@ int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_
         ctx->last_cuda_error = cudaErrorInvalidValue;
         return SKETCHSSM_CUDA_ERROR;
     }
-    const cudaError_t e = unlock_smem(ctx, prompt_scan_tc_kernel<true>);
+    cudaError_t e = unlock_smem(ctx, prompt_scan_tc_kernel<true>);
+    if (e == cudaSuccess && p.segments > 1) e = unlock_smem(ctx, prompt_scan_tc_kernel<false>);
     if (e != cudaSuccess) { ctx->last_cuda_error = e; return SKETCHSSM_CUDA_ERROR; }
-    const unsigned grid = (unsigned)(g.units < sm_count(ctx) ? g.units : sm_count(ctx));
+    const unsigned grid = (unsigned)(units < sm_count(ctx) ? units : sm_count(ctx));
+    if (p.segments > 1) {
+        const int rc = launch_layer<ScanArgs>(ctx, prompt_scan_tc_kernel<false>, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
+        if (rc != SKETCHSSM_OK) return rc;
+    }
     return launch_layer<ScanArgs>(ctx, prompt_scan_tc_kernel<true>, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
 }
 

@@ -144,6 +144,13 @@ SCAN = [
     ([300, 5], 2, 2, 128, 128, "bf16", "f32", None, [6, 7], 0, 7),
     ([300], 3, 3, 128, 80, "bf16", "bf16", None, [6], 0, 7),
     ([1100], 1, 1, 64, 64, "bf16", "bf16", None, None, 0, 0),
+    # sequences split into segments: one from a stored state into the same entry, ragged ones with an empty one among them, two groups
+    # of three heads, halves of 128 columns
+    ([2100], 2, 1, 128, 64, "bf16", "bf16", [4], [4], 0, 3),
+    ([1500, 0, 90, 1025], 3, 1, 128, 64, "bf16", "bf16", [0, 1, 2, 3], [-1, 6, 2, 3], 2, 0),
+    ([1111, 1000], 6, 2, 128, 64, "bf16", "bf16", [3, 2], [2, -1], 0, 0),
+    ([1200], 2, 2, 128, 128, "bf16", "bf16", None, [0], 0, 0),
+    ([200] * 40, 8, 1, 128, 64, "bf16", "bf16", [-1] * 35 + [0, 1, 2, 3, 4], [i % 3 + 5 if i % 4 else -1 for i in range(40)], 0, 0),
 ]
 # How many half steps 2^-8 of bfloat16 the products may be off by, measured by A, for the type of the output.  With bf16 outputs a term
 # goes into its product either by way of the scores or by way of the state, and either is rounded once: one half step; the log2 of a

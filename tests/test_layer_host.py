@@ -96,6 +96,16 @@ def test_scan_scratch(lib):
     assert lib.sketchssm_prompt_work_bytes(ctx, 1, 1, None) == INVALID
     assert lib.sketchssm_prompt_work_bytes(ctx, -1, 1, ctypes.byref(n)) == INVALID
     assert lib.sketchssm_prompt_work_bytes(ctx, 0, 0, ctypes.byref(n)) == OK and n.value == 0
+    assert lib.sketchssm_prompt_work_bytes(ctx, 1, 1000, ctypes.byref(n)) == OK and n.value == 0          # too short to split
+    # 8 heads of 64 columns: four pairs, so up to 37 segments fill 148 SMs; 4096 tokens make 8 of 512
+    assert lib.sketchssm_prompt_work_bytes(ctx, 3, 4096, ctypes.byref(n)) == OK and n.value == 8 * 8 * (128 * 64 + 1) * 4
+    assert lib.sketchssm_prompt_work_bytes(ctx, 1, 1 << 20, ctypes.byref(n)) == OK and n.value == 37 * 8 * (128 * 64 + 1) * 4
+    for other in (context(lib, io_dtype=0), context(lib, heads=200), context(lib, dv=80), context(lib, dk=64)):
+        assert lib.sketchssm_prompt_work_bytes(other, 1, 1 << 20, ctypes.byref(n)) == OK and n.value == 0
+    assert scan(lib, ctx, pr=prompts(tokens=4096), wb=0, work=None) == OK                                # no sequences: no scratch
+    assert scan(lib, ctx, pr=prompts(sequences=1, tokens=4096), wb=8 * 8 * (128 * 64 + 1) * 4 - 1) == INVALID
+    assert scan(lib, ctx, pr=prompts(sequences=1, tokens=4096), work=Q) == INVALID
+    assert scan(lib, ctx, pr=prompts(sequences=1, tokens=4096), work=None) == INVALID
 
 
 def norm(lib, ctx, rows=0, width=256, group=0, eps=1e-5, x=P, xs=256, xd=1, weight=P, res=None, res_out=None, gate=None, gs=256,
