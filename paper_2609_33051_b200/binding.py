@@ -8,6 +8,7 @@ library is missing or CUDA is unavailable the calls fail.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 from typing import Optional
 
@@ -78,10 +79,12 @@ class Prompts:
                 raise ValueError(f"{name} is a dense int32 tensor of {n} entries")
         self.starts, self.slots, self.resume = starts, slots, resume
         self.c = PromptBatch(self.sequences, self.tokens, _ptr(starts), _ptr(slots), _ptr(resume))
-        self.ref = ctypes.byref(self.c)
+        self.address, self.device = ctypes.addressof(self.c), starts.device
+        if any(t is not None and t.device != starts.device for t in (slots, resume)):
+            raise ValueError("starts, slots and resume lie on one device")
 
     def on(self, device: torch.device) -> bool:
-        return all(t is None or t.device == device for t in (self.starts, self.slots, self.resume))
+        return self.device == device
 
 
 class SketchSSMError(RuntimeError):
@@ -91,6 +94,7 @@ class SketchSSMError(RuntimeError):
 
 
 _LIB = None
+_CALLS = None       # the extension module that checks tensors and calls the library for the operators around the recurrence
 
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
@@ -137,6 +141,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             getattr(lib, name).restype = ctypes.c_int
     if path == _build.LIB_PATH:
         _LIB = lib
+    global _CALLS
+    if _CALLS is None:
+        _CALLS = importlib.import_module("._layer_calls", __package__)
     return lib
 
 
@@ -145,10 +152,6 @@ _RAW_STREAM, _DEVICE = getattr(torch._C, "_cuda_getCurrentRawStream", None), get
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()       # (the declared argument types make the C pointer of it)
-
-
-_CODE = {torch.float32: 0, torch.bfloat16: 1}
-_E4M3 = torch.float8_e4m3fn
 
 
 class SketchSSM:
@@ -179,6 +182,7 @@ class SketchSSM:
         self.sizes = Sizes()
         self._check("sketchssm_query_sizes", self.lib.sketchssm_query_sizes(self._ctx, ctypes.byref(self.sizes)))
         self.state = self.sketch = self.ring = self.omega = self.coef = self.status = self.work = self.erase = None
+        self._heads()
         self.head_rank = None        # optional int32 [H] device tensor: per-head sketch rank (0 = full-state read); set, then bind()
         if allocate:
             self.allocate()
@@ -208,10 +212,20 @@ class SketchSSM:
                     self.erase.data_ptr() if self.erase is not None else None)
         self._check("sketchssm_bind", self.lib.sketchssm_bind(self._ctx, ctypes.byref(b)))
 
+    def _heads(self):
+        """What the calls of _layer_calls begin with: the C function, the context, the device and the layer's sizes."""
+        def head(fn):
+            return (ctypes.cast(fn, ctypes.c_void_p).value, self._ctx.value or 0, self.device.index or 0, self.B, self.H, self.K,
+                    self.V, DTYPE[self.io])
+        lib = self.lib
+        self._conv, self._step, self._scan = (head(f) for f in (lib.sketchssm_causal_conv, lib.sketchssm_conv_step, lib.sketchssm_prompt_scan))
+        self._norm, self._matmul = head(lib.sketchssm_rms_norm), head(lib.sketchssm_scaled_matmul)
+
     def close(self):
         if self._ctx:
             self.lib.sketchssm_destroy(self._ctx)
             self._ctx = ctypes.c_void_p()
+            self._heads()
 
     def __del__(self):
         try:
@@ -317,33 +331,6 @@ class SketchSSM:
         return host["out"]
 
     # -- the operators around the recurrence ---------------------------------------------------
-    def _want(self, ok: bool, text: str):
-        if not ok:
-            raise ValueError(text)
-
-    def _rows(self, name: str, t: torch.Tensor, dtype: torch.dtype, *shape) -> int:
-        """Checks a tensor whose rows (first axis) may be strided; returns the row stride in elements."""
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device:
-            raise ValueError(f"{name} is a {dtype} tensor {tuple(shape)} on {self.device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
-        n = t.dim()
-        if n == 2:
-            inner = t.stride(1) == 1 or shape[1] == 1
-            row = shape[1]
-        else:
-            inner = (t.stride(2) == 1 or shape[2] == 1) and (t.stride(1) == shape[2] or shape[1] == 1)
-            row = shape[1] * shape[2]
-        if not inner:
-            raise ValueError(f"{name}: the elements of a row are dense")
-        return t.stride(0) if shape[0] > 1 else row
-
-    def _dense(self, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, *shape) -> Optional[int]:
-        """Checks a dense tensor (None passes); returns its address."""
-        if t is None:
-            return None
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
-            raise ValueError(f"{name} is a dense {dtype} tensor {tuple(shape)} on {self.device}: got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return t.data_ptr()
-
     def new_conv_state(self, channels: int, width: int) -> torch.Tensor:
         """Zeroed stored rows [B, width - 1, channels] of the short convolution."""
         return torch.zeros(self.B, width - 1, channels, dtype=TORCH_DTYPE[self.io], device=self.device)
@@ -352,14 +339,10 @@ class SketchSSM:
                     state: torch.Tensor, out: torch.Tensor, silu: bool = True, stream=None) -> torch.Tensor:
         """sketchssm_causal_conv: the short causal convolution of packed prompts x [T, C] into out; weight [C, W] f32, bias [C]
         f32 or None, state [B, W - 1, C] holds the stored rows and is moved on."""
-        io, T = TORCH_DTYPE[self.io], prompts.tokens
-        self._want(prompts.on(self.device) and weight.dim() == 2, "prompts lie on the layer's device, and weight is [C, W]")
-        C, W = weight.shape
-        xs, os_ = self._rows("x", x, io, T, C), self._rows("out", out, io, T, C)
-        rc = self.lib.sketchssm_causal_conv(
-            self._ctx, prompts.ref, C, W, self._dense("weight", weight, torch.float32, C, W),
-            self._dense("bias", bias, torch.float32, C), self._dense("state", state, io, self.B, W - 1, C), x.data_ptr(), xs,
-            out.data_ptr(), os_, SILU if silu else 0, self._stream(stream))
+        if not prompts.on(self.device):
+            raise ValueError("prompts lie on the layer's device")
+        rc = _CALLS.causal_conv(*self._conv, prompts.address, prompts.tokens, x, weight, bias, state, out, SILU if silu else 0,
+                                self._stream(stream))
         if rc:
             self._check("sketchssm_causal_conv", rc)
         return out
@@ -369,16 +352,8 @@ class SketchSSM:
                   stream=None) -> dict:
         """sketchssm_conv_step: one token of every batch entry, x [B, H V + 2 G K] and dt [B, H], into the q, k, v, beta, decay of
         `token` (new_token_buffers), which the decode calls take."""
-        B, H, K, V = self.B, self.H, self.K, self.V
-        io, C, W = TORCH_DTYPE[self.io], H * V + 2 * groups * K, weight.shape[-1]
-        f32 = torch.float32
-        xs, ds = self._rows("x", x, io, B, C), self._rows("dt", dt, io, B, H)
-        rc = self.lib.sketchssm_conv_step(
-            self._ctx, groups, W, self._dense("weight", weight, f32, C, W), self._dense("bias", bias, f32, C),
-            self._dense("state", state, io, B, W - 1, C), x.data_ptr(), xs, dt.data_ptr(), ds, self._dense("a", a, f32, H),
-            self._dense("dt_bias", dt_bias, f32, H), self._dense("q", token["q"], io, B, H, K),
-            self._dense("k", token["k"], io, B, H, K), self._dense("v", token["v"], io, B, H, V),
-            self._dense("beta", token["beta"], f32, B, H), self._dense("decay", token["decay"], f32, B, H), self._stream(stream))
+        rc = _CALLS.conv_step(*self._step, x, dt, weight, bias, state, a, dt_bias, token["q"], token["k"], token["v"], token["beta"],
+                              token["decay"], groups, self._stream(stream))
         if rc:
             self._check("sketchssm_conv_step", rc)
         return token
@@ -394,21 +369,11 @@ class SketchSSM:
                     work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """sketchssm_prompt_scan: the selective scan of packed prompts, q, k [T, G, K], v [T, H, V], dt [T, H] in io, a [H] f32, into
         out [T, H, V] (f32 or bf16) and the bound state.  work: new_prompt_work (allocated here if None)."""
-        io, T, H, f32 = TORCH_DTYPE[self.io], prompts.tokens, self.H, torch.float32
-        self._want(prompts.on(self.device) and q.dim() == 3 and out.dtype in _CODE,
-                   "prompts lie on the layer's device, q is [T, G, K], and out is f32 or bf16")
-        G = q.shape[1]
-        qs, ks = self._rows("q", q, io, T, G, self.K), self._rows("k", k, io, T, G, self.K)
-        vs, ds = self._rows("v", v, io, T, H, self.V), self._rows("dt", dt, io, T, H)
-        os_ = self._rows("out", out, out.dtype, T, H, self.V)
+        if not prompts.on(self.device):
+            raise ValueError("prompts lie on the layer's device")
         if work is None:
-            work = self.new_prompt_work(prompts.sequences, T)
-        self._want(work is None or (work.device == self.device and work.is_contiguous()), "work is a dense tensor on the layer's device")
-        rc = self.lib.sketchssm_prompt_scan(
-            self._ctx, prompts.ref, G, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dt.data_ptr(), ds,
-            self._dense("a", a, f32, H), self._dense("dt_bias", dt_bias, f32, H), self._dense("skip", skip, f32, H),
-            out.data_ptr(), os_, _CODE[out.dtype], _ptr(work), 0 if work is None else work.numel() * work.element_size(),
-            self._stream(stream))
+            work = self.new_prompt_work(prompts.sequences, prompts.tokens)
+        rc = _CALLS.prompt_scan(*self._scan, prompts.address, prompts.tokens, q, k, v, dt, a, out, dt_bias, skip, work, self._stream(stream))
         if rc:
             self._check("sketchssm_prompt_scan", rc)
         return out
@@ -420,18 +385,8 @@ class SketchSSM:
                  skip_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, group: int = 0, stream=None):
         """sketchssm_rms_norm: the norm of x [T, D] (f32 or bf16) with the residual's addition, or the skip and the gate, before it;
         into out (io) and/or out8 [T, D] e4m3 with scale [T, ceil(D / 128)]."""
-        io, f32 = TORCH_DTYPE[self.io], torch.float32
-        self._want(x.dim() == 2 and x.dtype in _CODE, "x is [T, D], f32 or bf16")
-        T, D = x.shape
-        xs = self._rows("x", x, x.dtype, T, D)
-        gs = self._rows("gate", gate, io, T, D) if gate is not None else 0
-        ss = self._rows("skip", skip, io, T, D) if skip is not None else 0
-        heads = skip_weight.numel() if skip_weight is not None else 0
-        rc = self.lib.sketchssm_rms_norm(
-            self._ctx, T, D, group, eps, x.data_ptr(), xs, _CODE[x.dtype], self._dense("weight", weight, f32, D),
-            self._dense("residual", residual, io, T, D), self._dense("residual_out", residual_out, io, T, D), _ptr(gate), gs,
-            _ptr(skip), ss, self._dense("skip_weight", skip_weight, f32, heads), heads, self._dense("out", out, io, T, D),
-            self._dense("out8", out8, _E4M3, T, D), self._dense("scale", scale, f32, T, -(-D // 128)), self._stream(stream))
+        rc = _CALLS.rms_norm(*self._norm, x, weight, out, out8, scale, residual, residual_out, gate, skip, skip_weight, eps, group,
+                             self._stream(stream))
         if rc:
             self._check("sketchssm_rms_norm", rc)
         return out if out is not None else out8
@@ -440,15 +395,7 @@ class SketchSSM:
                       stream=None) -> torch.Tensor:
         """sketchssm_scaled_matmul: out [M, N] (f32 or bf16) = a [M, K] w [N, K]^T in e4m3, with a_scale [M, ceil(K / 128)] and
         w_scale [ceil(N / 128), ceil(K / 128)]."""
-        f32 = torch.float32
-        self._want(a.dim() == 2 and w.dim() == 2 and out.dtype in _CODE, "a is [M, K], w [N, K], and out f32 or bf16")
-        (M, K), N = a.shape, w.shape[0]
-        kb = -(-K // 128)
-        os_ = self._rows("out", out, out.dtype, M, N)
-        rc = self.lib.sketchssm_scaled_matmul(
-            self._ctx, M, N, K, self._dense("a", a, _E4M3, M, K), self._dense("a_scale", a_scale, f32, M, kb),
-            self._dense("w", w, _E4M3, N, K), self._dense("w_scale", w_scale, f32, -(-N // 128), kb), out.data_ptr(), os_,
-            _CODE[out.dtype], self._stream(stream))
+        rc = _CALLS.scaled_matmul(*self._matmul, a, a_scale, w, w_scale, out, self._stream(stream))
         if rc:
             self._check("sketchssm_scaled_matmul", rc)
         return out

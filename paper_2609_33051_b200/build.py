@@ -5,6 +5,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
@@ -24,6 +25,11 @@ HEADERS = [os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "lanegroup.cuh
 LAYER_HEADERS = [os.path.join(CSRC, "layer.cuh"), os.path.join(CSRC, "tma.cuh")]      # of the operators around the recurrence alone
 
 
+# the extension module that checks tensors and calls the library for the operators around the recurrence
+CALLS_SRC = os.path.join(CSRC, "layer_calls.cpp")
+CALLS_PATH = os.path.join(PKG_DIR, "_layer_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
 def _nvcc() -> str:
     for cand in (os.environ.get("NVCC"), shutil.which("nvcc"), "/usr/local/cuda/bin/nvcc"):
         if cand and os.path.exists(cand):
@@ -38,6 +44,15 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _calls_command() -> list:
+    import torch
+    home = os.path.dirname(torch.__file__)
+    lib, inc = os.path.join(home, "lib"), os.path.join(home, "include")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            *[f"-I{d}" for d in (inc, os.path.join(inc, "torch", "csrc", "api", "include"), sysconfig.get_path("include"), os.path.join(ROOT, "include"))],
+            CALLS_SRC, "-o", CALLS_PATH, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", f"-Wl,-rpath,{lib}"]
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu to an object (parallel-friendly, incremental) and link the shared library."""
     nvcc = _nvcc()
@@ -48,6 +63,8 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         flags += ["-Xptxas", "-v"]
     procs, objs = [], []
+    if force or _stale(CALLS_PATH, [CALLS_SRC, os.path.join(ROOT, "include", "sketchssm.h")]):
+        procs.append(("layer_calls.cpp", subprocess.Popen(_calls_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for src, suffix, defs in UNITS:
         sp = os.path.join(CSRC, src)
         obj = os.path.join(objdir, src.replace(".cu", suffix + ".o"))
@@ -60,7 +77,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if verbose or pr.returncode != 0:
             sys.stderr.write(out)
         if pr.returncode != 0:
-            raise RuntimeError(f"nvcc failed on {src}")
+            raise RuntimeError(f"compilation failed: {src}")
     if force or procs or _stale(LIB_PATH, objs):
         subprocess.check_call([nvcc, "-shared", "-o", LIB_PATH, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
     return LIB_PATH

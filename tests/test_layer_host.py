@@ -157,3 +157,37 @@ def test_prompts_of_the_binding():
                      ((i(0, 3), 3), dict(resume=i())), ((i(0, 1, 2, 3)[::3], 3), {})):
         with pytest.raises(ValueError):
             binding.Prompts(*args, **kw)
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    """The extension module's checks come before the library's, and before any CUDA call: a CPU tensor is refused by name."""
+    build.build()
+    m = binding.SketchSSM("mamba2", 2, 4, 128, 64, 8, 4, device=0, allocate=False)
+
+    class Stream:
+        cuda_stream = 0
+
+    x = torch.zeros(3, 256, dtype=torch.bfloat16)
+    w = torch.ones(256)
+    pr = binding.Prompts(torch.tensor([0, 3], dtype=torch.int32), 3)
+    with pytest.raises(ValueError, match=r"x is a BFloat16 tensor \(3, 256, \) on cuda:0"):
+        m.rms_norm(x, w, out=x, stream=Stream)
+    with pytest.raises(ValueError, match="x is f32 or bf16"):
+        m.rms_norm(x.half(), w, out=x, stream=Stream)
+    with pytest.raises(ValueError, match="x has 2 axes"):
+        m.rms_norm(x[0], w, out=x, stream=Stream)
+    with pytest.raises(ValueError, match="x is a tensor"):
+        m.rms_norm(None, w, out=x, stream=Stream)
+    with pytest.raises(ValueError, match="prompts lie on the layer's device"):
+        m.causal_conv(pr, x, torch.ones(256, 4), None, x, x, stream=Stream)
+    with pytest.raises(ValueError, match="prompts lie on the layer's device"):
+        m.prompt_scan(pr, x, x, x, x, w, x, stream=Stream)
+    with pytest.raises(ValueError, match="weight has 2 axes"):
+        m.conv_step(x, x, w, None, x, w, None, {n: x for n in ("q", "k", "v", "beta", "decay")}, stream=Stream)
+    a = torch.zeros(3, 256, dtype=torch.float8_e4m3fn)
+    with pytest.raises(ValueError, match="out is a Float tensor"):
+        m.scaled_matmul(a, w, a, w, torch.zeros(3, 3), stream=Stream)
+    with pytest.raises(ValueError, match="out is f32 or bf16"):
+        m.scaled_matmul(a, w, a, w, a, stream=Stream)
+    m.close()
+    assert m._norm[1] == 0                     # a closed layer's context is not handed on
