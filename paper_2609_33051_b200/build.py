@@ -22,7 +22,7 @@ UNITS = [("api.cu", "", []), ("update.cu", "", []), ("update_cols.cu", "", []), 
 HEADERS = [os.path.join(CSRC, "internal.cuh"), os.path.join(CSRC, "lanegroup.cuh"), os.path.join(CSRC, "tc_common.cuh"),
            os.path.join(CSRC, "state_rows.h"), os.path.join(CSRC, "operand_sets.h"), os.path.join(CSRC, "team_size.h"),
            os.path.join(ROOT, "include", "sketchssm.h")]
-LAYER_HEADERS = [os.path.join(CSRC, "layer.cuh"), os.path.join(CSRC, "tma.cuh")]      # of the operators around the recurrence alone
+LAYER_HEADERS = [os.path.join(CSRC, "layer.cuh"), os.path.join(CSRC, "tma.cuh"), os.path.join(CSRC, "pairs.cuh")]      # of the operators around the recurrence alone
 
 
 # the extension module that checks tensors and calls the library for the operators around the recurrence

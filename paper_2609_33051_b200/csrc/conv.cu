@@ -7,7 +7,7 @@
 // Ragged sequences: a run takes the rows of its R whose window lies inside their sequence, and of every sequence that starts
 // in it at least the first W - 1 rows, over its own end if need be.  So one run alone reads a sequence's stored rows, and it
 // writes the new ones afterwards: the slot may be the resume entry, without a second launch.
-#include "layer.cuh"
+#include "pairs.cuh"
 
 namespace sketchssm {
 
@@ -40,53 +40,95 @@ __device__ __forceinline__ void load_taps(const float* weight, const float* bias
 template <typename T, int W, int R>
 __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
     using V = Vec16<T>;
-    constexpr int N = V::N, U = 8;                     // rows requested together
+    constexpr int N = V::N, U = 4;
     grid_dep_wait();
     grid_dep_launch_dependents();
     const PromptsDev& pr = p.pr;
     const int t0 = (int)blockIdx.x * R;
     const bool last = blockIdx.x == gridDim.x - 1;
+    // The whole run is on its way to L2 while the sequences are looked up and the taps fetched.
+    const int c0 = (int)blockIdx.y * 64 * N;
+    for (int r = (int)threadIdx.x; r < R && t0 + r < pr.T; r += 64)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const T*>(p.x) + (long long)(t0 + r) * p.x_stride + c0),
+                     "r"((uint32_t)(min(64 * N, p.C - c0) * (int)sizeof(T)))
+                     : "memory");
     const int i0 = starts_before(pr, t0);              // by whole warps, before any thread leaves
     const int c = ((int)blockIdx.y * 64 + (int)threadIdx.x) * N;
     if (c >= p.C) return;
     const T* x = static_cast<const T*>(p.x) + c;
     T* out = static_cast<T*>(p.out) + c;
     T* state = static_cast<T*>(p.state) + c;
-    float w[W][N], b[N];
-    load_taps<W, N>(p.weight, p.bias, c, w, b);
-    uint4 win[W - 1];                                  // the rows before the next one, oldest first
+    uint64_t w[W][N / 2], b[N / 2];                    // pairs of channels
+    {
+        float wf[W][N], bf[N];
+        load_taps<W, N>(p.weight, p.bias, c, wf, bf);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+            b[e] = pack2(bf[2 * e], bf[2 * e + 1]);
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j][e] = pack2(wf[j][2 * e], wf[j][2 * e + 1]);
+        }
+    }
+    uint64_t win[W - 1][N / 2];                        // the rows before the next one, oldest first
+    auto open = [&](const uint4& u, uint64_t (&f)[N / 2]) {
+        float g[N];
+        V::unpack(u, g);
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) f[e] = pack2(g[2 * e], g[2 * e + 1]);
+    };
+    auto row = [&](const uint4& u, T* to) {
+        uint64_t f[N / 2];
+        open(u, f);
+        float y[N];
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+            uint64_t s = b[e];
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) s = fma2(w[j][e], win[j][e], s);
+            unpack2(fma2(w[W - 1][e], f[e], s), y[2 * e], y[2 * e + 1]);
+        }
+        if (p.silu) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = silu<T>(y[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < N / 2; ++e) {
+#pragma unroll
+            for (int j = 0; j + 1 < W - 1; ++j) win[j][e] = win[j + 1][e];
+            win[W - 2][e] = f[e];
+        }
+        *reinterpret_cast<uint4*>(to) = V::pack(y);
+    };
+    // Rows t .. end - 1, U at a time; the next U are under way while these are worked on.
     auto walk = [&](int t, int end) {
-        while (t < end) {
-            const int n = min(U, end - t);
-            uint4 in[U];
+        const T* from = x + (long long)t * p.x_stride;
+        T* to = out + (long long)t * p.out_stride;
+        uint4 in[U], next[U];
+        if (t + U <= end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (u < n) in[u] = *reinterpret_cast<const uint4*>(x + (long long)(t + u) * p.x_stride);
+            for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const uint4*>(from + u * p.x_stride);
+#pragma unroll 1
+            while (t + U <= end) {
+                from += U * p.x_stride;
+                t += U;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (u < n) {
-                    float y[N], f[N];
+                for (int u = 0; u < U; ++u) in[u] = next[u];
+                if (t + U <= end) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) y[e] = b[e];
+                    for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const uint4*>(from + u * p.x_stride);
+                }
 #pragma unroll
-                    for (int j = 0; j < W - 1; ++j) {
-                        V::unpack(win[j], f);
-#pragma unroll
-                        for (int e = 0; e < N; ++e) y[e] = fmaf(w[j][e], f[e], y[e]);
-                    }
-                    V::unpack(in[u], f);
-#pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        y[e] = fmaf(w[W - 1][e], f[e], y[e]);
-                        if (p.silu) y[e] = silu<T>(y[e]);
-                    }
-#pragma unroll
-                    for (int j = 0; j + 1 < W - 1; ++j) win[j] = win[j + 1];
-                    win[W - 2] = in[u];
-                    *reinterpret_cast<uint4*>(out + (long long)(t + u) * p.out_stride) = V::pack(y);
+                for (int u = 0; u < U; ++u) {
+                    row(in[u], to);
+                    to += p.out_stride;
                 }
             }
-            t += n;
+        }
+#pragma unroll 1
+        for (; t < end; ++t) {
+            row(*reinterpret_cast<const uint4*>(from), to);
+            from += p.x_stride;
+            to += p.out_stride;
         }
     };
     if (i0 > 0) {                                      // the sequence that began before this run
@@ -94,7 +136,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         const int t = max(t0, r.x + W - 1), end = min(r.y, t0 + R);
         if (t < end) {
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) win[j] = *reinterpret_cast<const uint4*>(x + (long long)(t - (W - 1) + j) * p.x_stride);
+            for (int j = 0; j < W - 1; ++j) open(*reinterpret_cast<const uint4*>(x + (long long)(t - (W - 1) + j) * p.x_stride), win[j]);
             walk(t, end);
         }
     }
@@ -107,7 +149,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         for (int j = 0; j < W - 1; ++j) {
             old[j] = make_uint4(0u, 0u, 0u, 0u);
             if (src >= 0) old[j] = *reinterpret_cast<const uint4*>(state + ((size_t)src * (W - 1) + j) * p.C);
-            win[j] = old[j];
+            open(old[j], win[j]);
         }
         walk(r.x, min(r.y, max(t0 + R, r.x + W - 1)));
         if (dst >= 0) {
@@ -130,52 +172,89 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
     }
 }
 
-// One token: a thread per 16 bytes of channels convolves, moves the stored rows on and writes the value, or the key or query to
-// every head of its group; the last block of a batch entry makes the gates.
+// One token.  Values: a thread convolves 16 bytes of channels for four batch entries with the taps in registers (read for
+// every entry they are as many bytes as everything else), moves the stored rows on and writes.  Keys and queries go to every head of
+// their group, which is most of what the call writes: a block convolves 32 pieces of 16 bytes into shared memory and all its threads
+// copy them to the heads.  The last block of a batch entry makes the gates.
+constexpr int kEntries = 4, kPieces = 32;
+
 template <typename T, int W>
-__global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) {
+__device__ __forceinline__ void token_rows(const ConvStepParams& p, int b, int c, int C, uint4 (&in)[W]) {
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) in[j] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.state) + ((size_t)b * (W - 1) + j) * C + c);
+    in[W - 1] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (long long)b * p.x_stride + c);
+}
+template <typename T, int W>
+__device__ __forceinline__ uint4 conv_token(const ConvStepParams& p, int b, int c, int C, const uint4 (&in)[W], const float (&w)[W][Vec16<T>::N],
+                                            const float (&bias)[Vec16<T>::N]) {
     using V = Vec16<T>;
     constexpr int N = V::N;
-    grid_dep_wait();
-    grid_dep_launch_dependents();
-    const int b = (int)blockIdx.x, hv = p.H * p.V, gk = p.G * p.K, C = hv + 2 * gk;
-    if (blockIdx.y == gridDim.y - 1) {
-        const T* dt = static_cast<const T*>(p.dt) + (long long)b * p.dt_stride;
-        for (int h = (int)threadIdx.x; h < p.H; h += 128) {
-            const float beta = softplus((float)dt[h] + (p.dt_bias != nullptr ? p.dt_bias[h] : 0.f));
-            p.beta[(size_t)b * p.H + h] = beta;
-            p.decay[(size_t)b * p.H + h] = expf(p.a[h] * beta);
-        }
-        return;
-    }
-    const int c = ((int)blockIdx.y * 128 + (int)threadIdx.x) * N;
-    if (c >= C) return;
-    const T* x = static_cast<const T*>(p.x) + (long long)b * p.x_stride + c;
-    T* state = static_cast<T*>(p.state) + (size_t)b * (W - 1) * C + c;
-    uint4 in[W];
+    float y[N], f[N];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) in[j] = *reinterpret_cast<const uint4*>(state + (size_t)j * C);
-    in[W - 1] = *reinterpret_cast<const uint4*>(x);
-    float y[N], f[N], w[W][N];
-    load_taps<W, N>(p.weight, p.bias, c, w, y);
+    for (int e = 0; e < N; ++e) y[e] = bias[e];
 #pragma unroll
     for (int j = 0; j < W; ++j) {
         V::unpack(in[j], f);
 #pragma unroll
         for (int e = 0; e < N; ++e) y[e] = fmaf(w[j][e], f[e], y[e]);
-        if (j > 0) *reinterpret_cast<uint4*>(state + (size_t)(j - 1) * C) = in[j];
+        if (j > 0) *reinterpret_cast<uint4*>(static_cast<T*>(p.state) + ((size_t)b * (W - 1) + j - 1) * C + c) = in[j];
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = silu<T>(y[e]);
-    const uint4 r = V::pack(y);
-    if (c < hv) {
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.v) + (size_t)b * hv + c) = r;
+    return V::pack(y);
+}
+
+template <typename T, int W>
+__global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) {
+    constexpr int N = Vec16<T>::N;
+    __shared__ uint4 piece[kPieces];
+    grid_dep_wait();
+    grid_dep_launch_dependents();
+    const int tid = (int)threadIdx.x, hv = p.H * p.V, gk = p.G * p.K, C = hv + 2 * gk;
+    const int v_blocks = (hv / N + 127) / 128 * ((p.B + kEntries - 1) / kEntries), k_blocks = (2 * gk / N + kPieces - 1) / kPieces * p.B;
+    int i = (int)blockIdx.x;
+    if (i < k_blocks) {
+        const int b = i % p.B, first = hv + i / p.B * kPieces * N, n = min(kPieces, (C - first) / N), per = p.H / p.G;
+        if (tid < n) {
+            float w[W][N], bias[N];
+            uint4 in[W];
+            token_rows<T, W>(p, b, first + tid * N, C, in);
+            load_taps<W, N>(p.weight, p.bias, first + tid * N, w, bias);
+            piece[tid] = conv_token<T, W>(p, b, first + tid * N, C, in, w, bias);
+        }
+        __syncthreads();
+        const int at = tid % kPieces, c = first - hv + at * N;
+        if (at >= n) return;
+        const bool key = c < gk;
+        const int e = key ? c : c - gk;
+        const uint4 r = piece[at];
+        T* dst = static_cast<T*>(key ? p.k : p.q) + ((size_t)b * p.H + (size_t)(e / p.K) * per) * p.K + e % p.K;
+        for (int h = tid / kPieces; h < per; h += 128 / kPieces) *reinterpret_cast<uint4*>(dst + (size_t)h * p.K) = r;
         return;
     }
-    const bool key = c < hv + gk;
-    const int e = c - hv - (key ? 0 : gk), per = p.H / p.G;
-    T* dst = static_cast<T*>(key ? p.k : p.q) + ((size_t)b * p.H + (size_t)(e / p.K) * per) * p.K + e % p.K;
-    for (int h = 0; h < per; ++h) *reinterpret_cast<uint4*>(dst + (size_t)h * p.K) = r;
+    i -= k_blocks;
+    if (i < v_blocks) {
+        const int groups = (p.B + kEntries - 1) / kEntries, b0 = i % groups * kEntries, c = (i / groups * 128 + tid) * N;
+        if (c >= hv) return;
+        float w[W][N], bias[N];
+        uint4 in[kEntries][W];
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+            if (b0 + k < p.B) token_rows<T, W>(p, b0 + k, c, C, in[k]);
+        load_taps<W, N>(p.weight, p.bias, c, w, bias);
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+            if (b0 + k < p.B) *reinterpret_cast<uint4*>(static_cast<T*>(p.v) + (size_t)(b0 + k) * hv + c) = conv_token<T, W>(p, b0 + k, c, C, in[k], w, bias);
+        return;
+    }
+    i = (i - v_blocks) * 128 + tid;
+    if (i < p.B * p.H) {
+        const int b = i / p.H, h = i % p.H;
+        const T* dt = static_cast<const T*>(p.dt) + (long long)b * p.dt_stride;
+        const float beta = softplus((float)dt[h] + (p.dt_bias != nullptr ? p.dt_bias[h] : 0.f));
+        p.beta[i] = beta;
+        p.decay[i] = expf(p.a[h] * beta);
+    }
 }
 
 template <typename T, int W>
@@ -191,8 +270,11 @@ int conv_width(Ctx* ctx, const ConvParams& p, cudaStream_t stream) {
 
 template <typename T, int W>
 int step_width(Ctx* ctx, const ConvStepParams& p, cudaStream_t stream) {
-    const int vecs = (p.H * p.V + 2 * p.G * p.K) / Vec16<T>::N;
-    return launch_layer(ctx, conv_step_kernel<T, W>, dim3((unsigned)p.B, (unsigned)((vecs + 127) / 128 + 1)), dim3(128), 0, stream, p);
+    constexpr int N = Vec16<T>::N;
+    const long long values = (long long)((p.H * p.V / N + 127) / 128) * ((p.B + kEntries - 1) / kEntries);
+    const long long others = (long long)((2 * p.G * p.K / N + kPieces - 1) / kPieces) * p.B, gates = ((long long)p.B * p.H + 127) / 128;
+    if (values + others + gates > 0x7fffffff) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    return launch_layer(ctx, conv_step_kernel<T, W>, dim3((unsigned)(values + others + gates)), dim3(128), 0, stream, p);
 }
 
 }  // namespace

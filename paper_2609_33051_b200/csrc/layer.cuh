@@ -197,12 +197,23 @@ struct Vec16<__nv_bfloat16> {
     }
 };
 
-// y / (1 + exp(-y)); where the result is rounded to bfloat16 the exponential and the division are the fast ones (a few parts
-// in 10^7, the rounding is 2^-9).
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// y / (1 + exp(-y)); where the result is rounded to bfloat16 the exponential and the reciprocal are the fast ones (a few parts
+// in 10^7, the rounding is 2^-9; with denormals flushed, which costs nothing here and saves half of their instructions).
 template <typename T>
 __device__ __forceinline__ float silu(float y) {
-    if constexpr (sizeof(T) == 2) return __fdividef(y, 1.f + __expf(-y));
-    else return y / (1.f + expf(-y));
+    if constexpr (sizeof(T) == 2) {
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-1.4426950408889634f * y)));
+        return y * r;
+    } else {
+        return y / (1.f + expf(-y));
+    }
 }
 
 #endif  // __CUDACC__

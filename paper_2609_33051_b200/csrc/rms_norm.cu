@@ -52,6 +52,19 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const NormParams p) {
     const int g0 = live ? (int)(unit - row * p.groups) * p.group : 0;
     float h[NV][8];
     float sq = 0.f;
+    // Short rows: the weights are asked for with the row, not a round trip behind it.
+    constexpr bool kAhead = NV <= 2;
+    float4 ahead[kAhead ? NV : 1][2];
+    if constexpr (kAhead) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int i = (v * nt + tx) * 8;
+            if (live && i < p.group) {
+                ahead[v][0] = *reinterpret_cast<const float4*>(p.weight + g0 + i);
+                ahead[v][1] = *reinterpret_cast<const float4*>(p.weight + g0 + i + 4);
+            }
+        }
+    }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int i = (v * nt + tx) * 8;                // inside the group
@@ -104,7 +117,14 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const NormParams p) {
         const int e = g0 + i;
         float top = 0.f;
         if (in) {
-            const float4 w0 = *reinterpret_cast<const float4*>(p.weight + e), w1 = *reinterpret_cast<const float4*>(p.weight + e + 4);
+            float4 w0, w1;
+            if constexpr (kAhead) {
+                w0 = ahead[v][0];
+                w1 = ahead[v][1];
+            } else {
+                w0 = *reinterpret_cast<const float4*>(p.weight + e);
+                w1 = *reinterpret_cast<const float4*>(p.weight + e + 4);
+            }
             const float w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
