@@ -13,6 +13,32 @@ namespace sketchssm {
 
 namespace {
 
+// What a thread of the prompt kernel reads of a row: four channels.  (Sixteen bytes of bf16, eight channels, took 153 registers: 12 warps
+// an SM and 66 us for 16384 x 4352.)
+template <typename T>
+struct Four;
+template <>
+struct Four<float> {
+    using Raw = uint4;
+    static __device__ __forceinline__ void open(const uint4& u, uint64_t (&f)[2]) {
+        f[0] = (uint64_t)u.y << 32 | u.x;
+        f[1] = (uint64_t)u.w << 32 | u.z;
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&f)[4]) { return Vec16<float>::pack(f); }
+};
+template <>
+struct Four<__nv_bfloat16> {
+    using Raw = uint2;
+    static __device__ __forceinline__ void open(const uint2& u, uint64_t (&f)[2]) {
+        f[0] = pack2(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u));
+        f[1] = pack2(__uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint2 pack(const float (&f)[4]) {
+        __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+        return make_uint2(*reinterpret_cast<uint32_t*>(&a), *reinterpret_cast<uint32_t*>(&b));
+    }
+};
+
 // The taps and the bias of N channels.
 template <int W, int N>
 __device__ __forceinline__ void load_taps(const float* weight, const float* bias, int c, float (&w)[W][N], float (&b)[N]) {
@@ -38,22 +64,23 @@ __device__ __forceinline__ void load_taps(const float* weight, const float* bias
 }
 
 template <typename T, int W, int R>
-__global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
-    using V = Vec16<T>;
-    constexpr int N = V::N, U = 4;
+__global__ void __launch_bounds__(128) causal_conv_kernel(const ConvParams p) {
+    using V = Four<T>;
+    using Raw = typename V::Raw;
+    constexpr int N = 4, U = 4, kBlock = 128;
     grid_dep_wait();
     grid_dep_launch_dependents();
     const PromptsDev& pr = p.pr;
     const int t0 = (int)blockIdx.x * R;
     const bool last = blockIdx.x == gridDim.x - 1;
     // The whole run is on its way to L2 while the sequences are looked up and the taps fetched.
-    const int c0 = (int)blockIdx.y * 64 * N;
-    for (int r = (int)threadIdx.x; r < R && t0 + r < pr.T; r += 64)
+    const int c0 = (int)blockIdx.y * kBlock * N;
+    for (int r = (int)threadIdx.x; r < R && t0 + r < pr.T; r += kBlock)
         asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(static_cast<const T*>(p.x) + (long long)(t0 + r) * p.x_stride + c0),
-                     "r"((uint32_t)(min(64 * N, p.C - c0) * (int)sizeof(T)))
+                     "r"((uint32_t)(min(kBlock * N, p.C - c0) * (int)sizeof(T)))
                      : "memory");
     const int i0 = starts_before(pr, t0);              // by whole warps, before any thread leaves
-    const int c = ((int)blockIdx.y * 64 + (int)threadIdx.x) * N;
+    const int c = ((int)blockIdx.y * kBlock + (int)threadIdx.x) * N;
     if (c >= p.C) return;
     const T* x = static_cast<const T*>(p.x) + c;
     T* out = static_cast<T*>(p.out) + c;
@@ -70,15 +97,9 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         }
     }
     uint64_t win[W - 1][N / 2];                        // the rows before the next one, oldest first
-    auto open = [&](const uint4& u, uint64_t (&f)[N / 2]) {
-        float g[N];
-        V::unpack(u, g);
-#pragma unroll
-        for (int e = 0; e < N / 2; ++e) f[e] = pack2(g[2 * e], g[2 * e + 1]);
-    };
-    auto row = [&](const uint4& u, T* to) {
+    auto row = [&](const Raw& u, T* to) {
         uint64_t f[N / 2];
-        open(u, f);
+        V::open(u, f);
         float y[N];
 #pragma unroll
         for (int e = 0; e < N / 2; ++e) {
@@ -97,16 +118,16 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
             for (int j = 0; j + 1 < W - 1; ++j) win[j][e] = win[j + 1][e];
             win[W - 2][e] = f[e];
         }
-        *reinterpret_cast<uint4*>(to) = V::pack(y);
+        *reinterpret_cast<Raw*>(to) = V::pack(y);
     };
     // Rows t .. end - 1, U at a time; the next U are under way while these are worked on.
     auto walk = [&](int t, int end) {
         const T* from = x + (long long)t * p.x_stride;
         T* to = out + (long long)t * p.out_stride;
-        uint4 in[U], next[U];
+        Raw in[U], next[U];
         if (t + U <= end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const uint4*>(from + u * p.x_stride);
+            for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const Raw*>(from + u * p.x_stride);
 #pragma unroll 1
             while (t + U <= end) {
                 from += U * p.x_stride;
@@ -115,7 +136,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
                 for (int u = 0; u < U; ++u) in[u] = next[u];
                 if (t + U <= end) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const uint4*>(from + u * p.x_stride);
+                    for (int u = 0; u < U; ++u) next[u] = *reinterpret_cast<const Raw*>(from + u * p.x_stride);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -126,7 +147,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         }
 #pragma unroll 1
         for (; t < end; ++t) {
-            row(*reinterpret_cast<const uint4*>(from), to);
+            row(*reinterpret_cast<const Raw*>(from), to);
             from += p.x_stride;
             to += p.out_stride;
         }
@@ -136,7 +157,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         const int t = max(t0, r.x + W - 1), end = min(r.y, t0 + R);
         if (t < end) {
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) open(*reinterpret_cast<const uint4*>(x + (long long)(t - (W - 1) + j) * p.x_stride), win[j]);
+            for (int j = 0; j < W - 1; ++j) V::open(*reinterpret_cast<const Raw*>(x + (long long)(t - (W - 1) + j) * p.x_stride), win[j]);
             walk(t, end);
         }
     }
@@ -144,22 +165,22 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
         const int2 r = seq_rows(pr, i);
         if (r.x >= t0 + R && !last) break;
         const int src = seq_resume(pr, i), dst = seq_slot(pr, i);
-        uint4 old[W - 1];
+        Raw old[W - 1];
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
-            old[j] = make_uint4(0u, 0u, 0u, 0u);
-            if (src >= 0) old[j] = *reinterpret_cast<const uint4*>(state + ((size_t)src * (W - 1) + j) * p.C);
-            open(old[j], win[j]);
+            old[j] = Raw{};
+            if (src >= 0) old[j] = *reinterpret_cast<const Raw*>(state + ((size_t)src * (W - 1) + j) * p.C);
+            V::open(old[j], win[j]);
         }
         walk(r.x, min(r.y, max(t0 + R, r.x + W - 1)));
         if (dst >= 0) {
             const int len = r.y - r.x;
-            uint4 nw[W - 1];
+            Raw nw[W - 1];
 #pragma unroll
             for (int j = 0; j < W - 1; ++j) {          // row len + j of (stored rows, prompt)
-                nw[j] = make_uint4(0u, 0u, 0u, 0u);
+                nw[j] = Raw{};
                 if (len + j >= W - 1) {
-                    nw[j] = *reinterpret_cast<const uint4*>(x + (long long)(r.y - (W - 1) + j) * p.x_stride);
+                    nw[j] = *reinterpret_cast<const Raw*>(x + (long long)(r.y - (W - 1) + j) * p.x_stride);
                 } else {
 #pragma unroll
                     for (int m = 0; m < W - 1; ++m)
@@ -167,7 +188,7 @@ __global__ void __launch_bounds__(64) causal_conv_kernel(const ConvParams p) {
                 }
             }
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) *reinterpret_cast<uint4*>(state + ((size_t)dst * (W - 1) + j) * p.C) = nw[j];
+            for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Raw*>(state + ((size_t)dst * (W - 1) + j) * p.C) = nw[j];
         }
     }
 }
@@ -259,13 +280,13 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) 
 
 template <typename T, int W>
 int conv_width(Ctx* ctx, const ConvParams& p, cudaStream_t stream) {
-    const int vecs = p.C / Vec16<T>::N, bx = (vecs + 63) / 64;
+    const int bx = (p.C / 4 + 127) / 128;
     // Runs of 32 rows where they give every SM work, of 8 below that (short calls are latency: fewer rows in a row).
     const long long blocks32 = (long long)bx * ((p.pr.T + 31) / 32);
     const int r = blocks32 >= 4ll * sm_count(ctx) ? 32 : 8;
     const dim3 grid((unsigned)max(1, (p.pr.T + r - 1) / r), (unsigned)bx);
-    return r == 32 ? launch_layer(ctx, causal_conv_kernel<T, W, 32>, grid, dim3(64), 0, stream, p)
-                   : launch_layer(ctx, causal_conv_kernel<T, W, 8>, grid, dim3(64), 0, stream, p);
+    return r == 32 ? launch_layer(ctx, causal_conv_kernel<T, W, 32>, grid, dim3(128), 0, stream, p)
+                   : launch_layer(ctx, causal_conv_kernel<T, W, 8>, grid, dim3(128), 0, stream, p);
 }
 
 template <typename T, int W>
