@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const NormParams p) {
     float h[NV][8];
     float sq = 0.f;
     // Short rows: the weights are asked for with the row, not a round trip behind it.
-    constexpr bool kAhead = NV <= 2;
+    constexpr bool kAhead = NV == 1;
     float4 ahead[kAhead ? NV : 1][2];
     if constexpr (kAhead) {
 #pragma unroll
@@ -163,8 +163,9 @@ template <typename T, typename X>
 int norm_types(Ctx* ctx, const NormParams& p, cudaStream_t stream) {
     const int vecs = (p.group + 7) / 8;                 // of the longest part that threads share
     const long long units = (long long)p.rows * p.groups;
-    // Enough threads that a row is at most four vectors for each; with few rows one vector each, for a short chain.
-    int nv = units * vecs >= (long long)sm_count(ctx) * 1024 ? 4 : 1;
+    // Two vectors a thread (16384 rows of 2048: 46 us; four 50, eight in a warp without a barrier 74), with few rows one, for a short
+    // chain; long rows as many as 512 threads leave.
+    int nv = units * vecs >= (long long)sm_count(ctx) * 1024 ? 2 : 1;
     while (nv < 4 && (vecs + nv - 1) / nv > 512) nv *= 2;
     const int tx = ((vecs + nv - 1) / nv + 31) / 32 * 32;
     const int rows_per_cta = tx == 32 ? 4 : 1;
