@@ -13,8 +13,8 @@
 // c_t and backward for c_end - c_t, so that what is small is exact.
 //
 // Roles: warp 0 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
-// warp 3 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, scale Q S there, add the skip and
-// store Y, and four ("B") make W, hold S and hand it on as an operand.  They meet through mbarriers alone; every wait is bounded.
+// warp 3 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
+// ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
 // Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64.
 //
 // Few sequences and heads: a sequence is split into segments.  A first launch (OUTPUTS = false) leaves every segment's own state and
@@ -34,10 +34,10 @@ constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 32 toke
 constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][5][128] floats: see gates
 constexpr uint32_t kGateSet = 5 * kQ, kGateBuf = 2 * kGateSet;
 constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
-constexpr int kThreads = 640;
+constexpr int kThreads = 896;
 
 enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
-       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 24, bVRead = 26, kBars = 30 };
+       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 24, bVRead = 26, bScaled = 30, kBars = 32 };
 constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
 
 // columns of tensor memory
@@ -108,17 +108,6 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
 // A warp's wait: false to all its lanes if it ran out.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity)); }
 
-// 32 rows of 128 bytes in shared memory (128-byte swizzle, this warp's) to rows of global memory `stride` bytes apart; rows from `n` on
-// are left out.
-__device__ __forceinline__ void store_rows(const unsigned char* tile, unsigned char* global, long long stride, int n) {
-    const int lane = (int)threadIdx.x & 31;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 4 + lane / 8, c = lane % 8;
-        if (r < n) *reinterpret_cast<uint4*>(global + r * stride + c * 16) = *reinterpret_cast<const uint4*>(tile + r * 128 + ((c ^ (r & 7)) * 16));
-    }
-}
-
 template <bool OUTPUTS>
 __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __grid_constant__ ScanArgs g) {
     extern __shared__ unsigned char raw[];
@@ -134,10 +123,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         for (int i = 0; i < kBars; ++i) {
             int n = 1;                                  // copies and commits of products arrive once
             if (i >= bEmptyK && i < bFullQ) n = OUTPUTS ? 2 : 1;                // both product warps read K
-            if (i >= bEmptyV && i < bGate) n = 8;                               // A (without outputs: B) of both sets
-            if (i >= bGateFree && i < bDot) n = OUTPUTS ? 16 : 8;
-            if (i == bState || i == bYFree || i == bW || i == bW + 1) n = 8;     // the warps of both sets
-            if ((i >= bP && i < bY) || i >= bVRead) n = 4;       // of one
+            if (i >= bEmptyV && i < bGate) n = OUTPUTS ? 8 : 16;                               // A (without outputs: B) of both sets
+            if (i >= bGateFree && i < bDot) n = OUTPUTS ? 24 : 16;
+            if (i == bYFree) n = 8;                                             // the warps of both sets
+            if (i == bState || i == bW || i == bW + 1) n = 16;
+            if (i >= bP && i < bY) n = 4;                                       // of one
+            if (i >= bVRead) n = 8;                                              // (B)
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -154,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     int n = 0;                                          // chunks so far, over all units of the CTA
 
     if (warp == 0) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (lane == 0) {
             for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
                 const Unit x = decode_unit(g, u);
@@ -197,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         }
         __syncwarp();
     } else if (warp == 1) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if constexpr (OUTPUTS) {
             constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
             constexpr uint32_t kDotDesc = kTypes | ((128u >> 3) << 17), kInterDesc = kDotDesc | (1u << 16);
@@ -239,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     ok = ok && warp_wait(bar + bFullV + b, (n / 2) & 1);
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        ok = ok && warp_wait(bar + bP + j, n & 1);
+                        ok = ok && warp_wait(bar + bP + j, n & 1) && (fresh || warp_wait(bar + bScaled + j, (m - 1) & 1));
                         if (!ok) break;
                         tc_fence_after();
                         const uint64_t dv = swizzled_desc(sbase + kVOff + (b * 2 + j) * kTile, 16u, 1024u);
@@ -257,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         }
         __syncwarp();
     } else if (warp == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         constexpr uint32_t kDesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
         const uint64_t dw = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
@@ -287,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 3);
         __syncwarp();
     } else if (warp == 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         // gates: four neighbouring tokens a lane
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const Unit x = decode_unit(g, u);
@@ -366,10 +357,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     } else if (warp < 12) {
         if constexpr (OUTPUTS) {
             // A: token row `row` of set j
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
             const int j = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
             const uint32_t lanes = (uint32_t)(quad * 32) << 16;
             const uint32_t tp = tmem + lanes + kP + j * 64, td = tmem + lanes + kDot, ty = tmem + lanes + kY + j * 64;
-            int m = 0;
             {
                 uint32_t z[16];
 #pragma unroll
@@ -382,11 +373,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 const Unit x = decode_unit(g, u);
                 if (!unit_runs(x, true)) continue;
                 const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
-                const bool live = j == 0 || x.live1, fresh0 = x.seg == 0 && seq_resume(p.pr, x.seq) < 0;
+                const bool live = j == 0 || x.live1;
                 const float skip = p.skip != nullptr ? p.skip[head] : 0.f;
+                const uint64_t skip2 = pack2(skip, skip);
                 for (int t = x.t0; t < x.t1; t += kQ, ++n) {
                     const int b = n & 1, valid = min(kQ, x.t1 - t);
-                    const bool fresh = fresh0 && t == x.t0;
                     const float* gt = gates + b * kGateBuf + j * kGateSet;
                     unsigned char* v = smem + kVOff + (b * 2 + j) * kTile;
                     unsigned char* mine = v + row * 128;
@@ -396,10 +387,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     // P: below the diagonal's 32 x 32 blocks its weight is 2^(c_t - c at the end of the columns' 32) times a factor of
                     // the column, both at most 1 (but for beta); in them it is one exponential an element
                     const float ct = gt[row];
+                    uint32_t d[32], f[16];
+                    tmem_ld32_async(td, d);
 #pragma unroll 1
                     for (int c = 0; c < quad; ++c) {
-                        uint32_t d[32], f[16];
-                        tmem_ld32_async(td + c * 32, d);
                         const float r = ex2(ct - gt[c * 32 + 31]);
                         const uint64_t r2 = pack2(r, r);
                         const ulonglong2* f4 = reinterpret_cast<const ulonglong2*>(gt + 4 * kQ + c * 32);
@@ -413,11 +404,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                             f[2 * i] = bf16x2(x0, x1);
                             f[2 * i + 1] = bf16x2(x2, x3);
                         }
+                        tmem_ld32_async(td + (c + 1) * 32, d);
                         tmem_st16u(tp + c * 16, f);
                     }
                     {
-                        uint32_t d[32], f[16];
-                        tmem_ld32_async(td + quad * 32, d);
                         const uint64_t ct2 = pack2(ct, ct);
                         const ulonglong2* e4 = reinterpret_cast<const ulonglong2*>(gt + kQ + quad * 32);
                         tmem_ld_wait();
@@ -433,8 +423,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                             f[2 * i + 1] = bf16x2(x2, x3);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)            // column 2 i + e of the 32 is there up to row `lane`
-                            f[i] &= (2 * i <= lane ? 0xffffu : 0u) | (2 * i + 1 <= lane ? 0xffff0000u : 0u);
+                        for (int i = 0; i < 16; ++i) {           // column 2 i + e of the 32 is there up to row `lane`
+                            if (lane < 2 * i) f[i] = 0u;
+                            if (lane == 2 * i) f[i] &= 0xffffu;
+                        }
                         tmem_st16u(tp + quad * 16, f);
                     }
                     ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
@@ -443,26 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0u, 0u, 0u, 0u);
                     }
                     if (valid < kQ) proxy_fence();
-                    if (!fresh) {
-                        ok = ok && warp_wait(bar + bInter, m & 1);
-                        ++m;
-                        if (!ok) break;
-                        tc_fence_after();
-                        const float ec = gt[3 * kQ + row];
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t d[2][16];
-                            tmem_ld16_async(ty + c * 32, d[0]);
-                            tmem_ld16_async(ty + c * 32 + 16, d[1]);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) d[e][i] = __float_as_uint(__uint_as_float(d[e][i]) * ec);
-                                tmem_st16u(ty + c * 32 + e * 16, d[e]);
-                            }
-                        }
-                    }
+                    if (!ok) break;
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -474,9 +447,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     ok = ok && warp_wait(bar + bY + j, n & 1) && warp_wait(bar + bVRead + j * 2 + b, (n / 2) & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    uint32_t d[2][32];
-                    tmem_ld32_async(ty, d[0]);
-                    tmem_ld32_async(ty + 32, d[1]);
+                    uint32_t o[2][32];
+                    tmem_ld32_async(ty, o[0]);
+                    tmem_ld32_async(ty + 32, o[1]);
                     tmem_ld_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -484,30 +457,50 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         uint4* at = reinterpret_cast<uint4*>(mine + ((c ^ (row & 7)) * 16));
-                        float f[8];
-                        Vec16<__nv_bfloat16>::unpack(*at, f);
+                        const uint4 u = *at;
+                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                        uint32_t z[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = fmaf(skip, f[i], __uint_as_float(d[c / 4][c % 4 * 8 + i]));
-                        *at = Vec16<__nv_bfloat16>::pack(f);
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = c % 4 * 8 + 2 * i;
+                            float lo, hi;
+                            unpack2(fma2(skip2, pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)),
+                                         pack2(__uint_as_float(o[c / 4][e]), __uint_as_float(o[c / 4][e + 1]))), lo, hi);
+                            z[i] = bf16x2(lo, hi);
+                        }
+                        *at = make_uint4(z[0], z[1], z[2], z[3]);
                     }
                     __syncwarp();
-                    if (live)
-                        store_rows(v + quad * 4096, static_cast<unsigned char*>(p.out) + ((long long)(t + quad * 32) * p.out_stride + block * 64) * 2,
-                                   p.out_stride * 2, valid - quad * 32);
+                    // a warp's 32 rows of 128 bytes, eight lanes a row; the buffer is free before the stores are made
+                    uint4 y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int r = i * 4 + lane / 8;
+                        y[i] = *reinterpret_cast<const uint4*>(v + quad * 4096 + r * 128 + (((lane % 8) ^ (r & 7)) * 16));
+                    }
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bEmptyV + b);
+                    if (live) {
+                        unsigned char* out = static_cast<unsigned char*>(p.out) +
+                                             ((long long)(t + quad * 32 + lane / 8) * p.out_stride + block * 64 + lane % 8 * 8) * 2;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (i * 4 + lane / 8 < valid - quad * 32) *reinterpret_cast<uint4*>(out) = y[i];
+                            out += p.out_stride * 8;
+                        }
+                    }
                 }
             }
             if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 5);
         }
     } else {
-        // B: state row `row` of set j (640 threads start with 96 registers: 128 x 56 + 256 x 96 + 256 x 112 of 61440)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-        const int j = (warp - 12) >> 2, quad = warp & 3, row = quad * 32 + lane, bt = (tid - 384) & 127;
+        // B: state row `row` of set j (896 threads start with 72 registers: 128 x 48 + 256 x 96 + 512 x 64 of 64512)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        const int j = (warp - 12) >> 3, quad = warp & 3, row = quad * 32 + lane, bt = (tid - 384) & 255, half = bt >> 7;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         unsigned char* buf = smem + kWOff + j * kWBuf;
-        uint64_t S[32];                                 // pairs of columns
+        uint64_t S[16];                                 // pairs of columns: half `half` of the 64
         int m = 0;                                      // chunks with a state before them
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const Unit x = decode_unit(g, u);
@@ -521,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             auto at = [&](int row0) {
                 int k = block;
                 asm volatile("" : "+r"(k));
-                return ((size_t)row0 * p.H + k / per_head) * 128 * p.V + (size_t)row * p.V + (k % per_head) * 64;
+                return ((size_t)row0 * p.H + k / per_head) * 128 * p.V + (size_t)row * p.V + (k % per_head) * 64 + half * 32;
             };
             auto decay = [&](int i) {
                 int k = block;
@@ -532,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             auto load = [&](const float* from) {
                 const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     const ulonglong2 v = f[i];
                     S[2 * i] = v.x;
                     S[2 * i + 1] = v.y;
@@ -542,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 const ulonglong2* f = reinterpret_cast<const ulonglong2*>(from);
                 const uint64_t keep2 = pack2(keep, keep);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     const ulonglong2 v = f[i];
                     S[2 * i] = fma2(keep2, S[2 * i], v.x);
                     S[2 * i + 1] = fma2(keep2, S[2 * i + 1], v.y);
@@ -550,10 +543,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             };
             auto store = [&](float* to) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) reinterpret_cast<ulonglong2*>(to)[i] = make_ulonglong2(S[2 * i], S[2 * i + 1]);
+                for (int i = 0; i < 8; ++i) reinterpret_cast<ulonglong2*>(to)[i] = make_ulonglong2(S[2 * i], S[2 * i + 1]);
             };
 #pragma unroll
-            for (int i = 0; i < 32; ++i) S[i] = 0ull;
+            for (int i = 0; i < 16; ++i) S[i] = 0ull;
             if (x.seg == 0) {
                 // (a later segment's CTA may have written the entry already: the first launch kept a copy)
                 if (src >= 0) load(OUTPUTS && !x.last ? p.work + at(x.seq * p.segments) : p.state + at(src));
@@ -569,11 +562,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 const bool fresh = fresh0 && t == x.t0;
                 if (OUTPUTS && !fresh) {                 // S as an operand: row n of 64 columns
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < 4; ++c) {
                         float f[8];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) unpack2(S[c * 4 + i], f[2 * i], f[2 * i + 1]);
-                        *reinterpret_cast<uint4*>(buf + row * 128 + ((c ^ (row & 7)) * 16)) = Vec16<__nv_bfloat16>::pack(f);
+                        *reinterpret_cast<uint4*>(buf + row * 128 + (((half * 4 + c) ^ (row & 7)) * 16)) = Vec16<__nv_bfloat16>::pack(f);
                     }
                     proxy_fence();
                     __syncwarp();
@@ -581,7 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 }
                 ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bFullV + b, (n / 2) & 1) && warp_wait(bar + bFullK + b, (n / 2) & 1);
                 if (!ok) break;
-                if (valid < kQ && j == 0 && row >= valid) {                      // rows of the next sequence are no part of this one
+                if (valid < kQ && j == 0 && half == 0 && row >= valid) {                      // rows of the next sequence are no part of this one
                     unsigned char* k = smem + kKOff + b * 2 * kTile + row * 128;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
@@ -589,10 +582,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         reinterpret_cast<uint4*>(k + kTile)[i] = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
-                if (OUTPUTS && !fresh) {                 // the buffer's S has been read
+                if (OUTPUTS && !fresh) {                 // Q S is there (and the buffer's S has been read): its rows times 2^c
                     ok = warp_wait(bar + bInter, m & 1);
                     ++m;
                     if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t ty = tmem + lanes + kY + j * 64 + half * 32;
+                    const float ec = gates[b * kGateBuf + j * kGateSet + 3 * kQ + row];
+                    const uint64_t ec2 = pack2(ec, ec);
+                    uint32_t d[16];
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_ld16_async(ty + c * 16, d);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint64_t y = mul2(ec2, pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1])));
+                            d[2 * i] = (uint32_t)y;
+                            d[2 * i + 1] = (uint32_t)(y >> 32);
+                        }
+                        tmem_st16u(ty + c * 16, d);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bScaled + j);
                 }
                 const float* w = gates + b * kGateBuf + j * kGateSet + 2 * kQ;
                 const uint64_t minus = pack2(-1.f, -1.f);
@@ -602,14 +616,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         ok = warp_wait(bar + bProd + (h & 1), 0);
                         if (!ok) break;
                     }
-                    const int tt = bt >> 2, t32 = h * 32 + tt;                   // four threads a token, 16 columns each
+                    const int tt = bt >> 3, t32 = h * 32 + tt;                   // eight threads a token, 8 columns each
                     const uint64_t wt = pack2(w[t32], w[t32]);
                     const uint32_t inside = t32 < valid ? 0xffffffffu : 0u;
                     const unsigned char* v = smem + kVOff + (b * 2 + j) * kTile + t32 * 128;
                     unsigned char* to = buf + (h & 1) * 12288 + tt * 128;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t off = (uint32_t)((((bt & 3) * 2 + c) ^ (tt & 7)) * 16);
+                    {
+                        const uint32_t off = (uint32_t)(((bt & 7) ^ (tt & 7)) * 16);
                         const uint4 vv = *reinterpret_cast<const uint4*>(v + off);
                         const uint32_t v4[4] = {vv.x & inside, vv.y & inside, vv.z & inside, vv.w & inside};
                         uint32_t q[3][4];
@@ -645,15 +658,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t keep2 = pack2(keep, keep);
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                {
                     uint32_t d[2][16];
-                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + c * 32, d[0]);
-                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + c * 32 + 16, d[1]);
+                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + half * 32, d[0]);
+                    tmem_ld16_async(tmem + lanes + kProd + j * 64 + half * 32 + 16, d[1]);
                     tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        S[c * 16 + i] = fma2(keep2, S[c * 16 + i], pack2(__uint_as_float(d[i / 8][2 * i % 16]), __uint_as_float(d[i / 8][2 * i % 16 + 1])));
+                        S[i] = fma2(keep2, S[i], pack2(__uint_as_float(d[i / 8][2 * i % 16]), __uint_as_float(d[i / 8][2 * i % 16 + 1])));
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -663,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             if (live) {
                 if constexpr (!OUTPUTS) {
                     store(p.work + at(x.seq * p.segments + x.seg + 1));
-                    if (row == 0 && block % per_head == 0) *decay(x.seg + 1) = total;
+                    if (row == 0 && half == 0 && block % per_head == 0) *decay(x.seg + 1) = total;
                 } else if (x.last) {
                     const int dst = seq_slot(p.pr, x.seq);
                     if (dst >= 0) store(p.state + at(dst));
