@@ -12,8 +12,8 @@
 // of that, took 16.6 products of 128 x 64 x 128 a pair of heads instead of 12.1 and was 60 % slower.)  Sums of decays run forward for
 // c_t and backward for c_end - c_t, so that what is small is exact.
 //
-// Roles: warp 0 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
-// warp 3 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
+// Roles: warp 3 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
+// warp 0 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
 // ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
 // Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64.
 //
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     bool ok = true;
     int n = 0;                                          // chunks so far, over all units of the CTA
 
-    if (warp == 0) {
+    if (warp == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (lane == 0) {
             for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 3);
         __syncwarp();
-    } else if (warp == 3) {
+    } else if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         // gates: four neighbouring tokens a lane
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
