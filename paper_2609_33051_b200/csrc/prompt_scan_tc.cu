@@ -93,20 +93,10 @@ __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[1
         "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// One lane of a converged warp.  (The product warps run their loops with all lanes and elect one for each product: the operands then
-// stay in uniform registers, and an instruction is issued every 30 to 60 cycles; from a branch that one lane takes it was 95.)
-__device__ __forceinline__ bool elect() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t*>(&h);
 }
-
-// A warp's wait: false to all its lanes if it ran out.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity)); }
 
 template <bool OUTPUTS>
 __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __grid_constant__ ScanArgs g) {

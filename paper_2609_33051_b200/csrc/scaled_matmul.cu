@@ -138,36 +138,37 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);      // e4m3 x e4m3 -> fp32
-            int it = 0;
-            bool ok = true;
-            for (int tile = first; tile < g.tiles && ok; tile += step) {
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = it % NS, as = it % AS;
-                    ok = it < AS || mbar_wait_bounded(acc_empty + as, (it / AS - 1) & 1);
-                    ok = ok && mbar_wait_bounded(full + s, (it / NS) & 1);
-                    if (!ok) {
-                        record_fault(p.status, kFaultMatmulWait, 2);
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t base = smem_u32(smem) + (uint32_t)s * L::kStage;
-                    const uint64_t dw = swizzled_desc(base, 16u, 1024u), da = swizzled_desc(base + L::kW, 16u, 1024u);
+        constexpr uint32_t idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((128u >> 4) << 24);      // e4m3 x e4m3 -> fp32
+        int it = 0;
+        bool ok = true;
+        for (int tile = first; tile < g.tiles && ok; tile += step) {
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int s = it % NS, as = it % AS;
+                ok = it < AS || warp_wait(acc_empty + as, (it / AS - 1) & 1);
+                ok = ok && warp_wait(full + s, (it / NS) & 1);
+                if (!ok) {
+                    if (lane == 0) record_fault(p.status, kFaultMatmulWait, 2);
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t base = smem_u32(smem) + (uint32_t)s * L::kStage;
+                const uint64_t dw = swizzled_desc(base, 16u, 1024u), da = swizzled_desc(base + L::kW, 16u, 1024u);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)        // 32 bytes of every row at a time
+                for (int j = 0; j < 4; ++j)            // 32 bytes of every row at a time
+                    if (elect())
                         asm volatile(
                             "{\n\t.reg .pred p;\n\t"
                             "setp.ne.b32 p, %4, 0;\n\t"
                             "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * BN)),
                             "l"(dw + 2u * j), "l"(da + 2u * j), "r"(idesc), "r"((uint32_t)j)
                             : "memory");
+                if (elect()) {
                     tc_commit(empty + s);
                     tc_commit(acc_full + as);
                 }
+                __syncwarp();
             }
         }
-        __syncwarp();
     } else if (warp < 4) {
         constexpr int PT = (BN + 63) / 64;             // tokens of a thread
         const int t = tid - 64;

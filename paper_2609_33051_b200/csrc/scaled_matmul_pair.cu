@@ -6,9 +6,12 @@
 // accumulator's lanes, the weights its columns (the other way round than for few tokens): a thread's scale is one number a block,
 // where scales read per column from shared memory, which the operands keep busy, made the sums 1700 cycles a block.
 //
-// Roles per CTA: one thread issues the copies of its half (they report to the leader's barrier), one thread of the leader the
-// products; two warps fetch scales, eight blocks at a time; sixteen warps add a block's accumulator (32 lanes, 64 columns each), times its scale, to sums in registers and at
-// the end store them through shared memory (TMA), or directly where a row or the row stride is no multiple of 16 bytes.
+// Roles per CTA: one thread issues the copies of its half (they report to the leader's barrier), one warp of the leader the products
+// (an elected lane of the converged warp: from a branch that one lane takes, an issue takes 95 cycles and a block 600); two warps
+// fetch scales, eight blocks at a time; sixteen warps add a block's accumulator (32 lanes, 64 columns each), times its scale, to
+// sums in registers and at the end store them through shared memory (TMA), or directly where a row or the row stride is no
+// multiple of 16 bytes.  They release an accumulator with an arrival at the leader's barrier of the default (CTA) scope: reads of
+// tensor memory are ordered by the tcgen05 fences, and a release of cluster scope waited 900 cycles for the stores before it.
 #include "tma.cuh"
 
 namespace sketchssm {
@@ -17,7 +20,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kStages = 4, kEpiWarps = 8, kThreads = 32 * (4 + kEpiWarps);
+constexpr int kStages = 4, kEpiWarps = 16, kThreads = 32 * (4 + kEpiWarps);
 constexpr int kScaleBlocks = 8;                        // blocks whose scales are fetched together, in two buffers
 constexpr uint32_t kHalf = 128u * 128u, kStageBytes = 2u * kHalf;
 constexpr uint32_t kOut = kStages * kStageBytes, kScales = kOut + kEpiWarps * 4096u;
@@ -75,6 +78,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
     const uint32_t tmem = *slot;
 
     if (warp == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (lane == 0) {
             int it = 0;
             bool ok = true;
@@ -100,17 +104,18 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (rank == 0) {
             constexpr uint32_t idesc = (1u << 4) | ((256u >> 3) << 17) | ((256u >> 4) << 24);      // e4m3 x e4m3 -> fp32
             int it = 0;
             bool ok = true;
             for (int tile = first; tile < g.tiles && ok; tile += step) {
                 for (int kb = 0; kb < p.KB; ++kb, ++it) {
                     const int s = it % kStages, as = it & 1;
-                    ok = it < 2 || mbar_wait_bounded(acc_empty + as, (it / 2 - 1) & 1);
-                    ok = ok && mbar_wait_bounded(full + s, (it / kStages) & 1);
+                    ok = it < 2 || warp_wait(acc_empty + as, (it / 2 - 1) & 1);
+                    ok = ok && warp_wait(full + s, (it / kStages) & 1);
                     if (!ok) {
-                        record_fault(p.status, kFaultMatmulWait, 12);
+                        if (lane == 0) record_fault(p.status, kFaultMatmulWait, 12);
                         break;
                     }
                     tc_fence_after();
@@ -118,19 +123,24 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
                     const uint64_t da = swizzled_desc(base, 16u, 1024u), dw = swizzled_desc(base + kHalf, 16u, 1024u);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)        // 32 bytes of every row at a time
-                        asm volatile(
-                            "{\n\t.reg .pred p;\n\t"
-                            "setp.ne.b32 p, %4, 0;\n\t"
-                            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * 256)),
-                            "l"(da + 2u * j), "l"(dw + 2u * j), "r"(idesc), "r"((uint32_t)j)
-                            : "memory");
-                    commit_pair(empty + s);
-                    commit_pair(acc_full + as);
+                        if (elect())
+                            asm volatile(
+                                "{\n\t.reg .pred p;\n\t"
+                                "setp.ne.b32 p, %4, 0;\n\t"
+                                "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * 256)),
+                                "l"(da + 2u * j), "l"(dw + 2u * j), "r"(idesc), "r"((uint32_t)j)
+                                : "memory");
+                    if (elect()) {
+                        commit_pair(empty + s);
+                        commit_pair(acc_full + as);
+                    }
+                    __syncwarp();
                 }
             }
         }
         __syncwarp();
     } else if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // Scales: eight blocks of 128 tokens and two column blocks, all loads of a group under way together.
         constexpr int kEach = kScaleBlocks * 128 / 64;
         const int t = tid - 64;
@@ -163,16 +173,18 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
             }
         }
     } else {
-        const int quad = warp & 3, part = (warp - 4) >> 2;             // 32 lanes, 128 columns
-        const uint32_t at0 = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * 128);
+        // (640 threads start with 96 registers: 128 x 56 + 512 x 104 of 61440)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int quad = warp & 3, part = (warp - 4) >> 2;             // 32 lanes, 64 columns
+        const uint32_t at0 = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * 64);
         unsigned char* stage = smem + kOut + (uint32_t)(warp - 4) * 4096u;
         const uint32_t release = cluster_addr(acc_empty, 0);
         int it = 0, group = 0;
         bool ok = true;
-        uint64_t acc[64];
+        uint64_t acc[32];
         for (int tile = first; tile < g.tiles && ok; tile += step) {
 #pragma unroll
-            for (int c = 0; c < 64; ++c) acc[c] = 0ull;
+            for (int c = 0; c < 32; ++c) acc[c] = 0ull;
             for (int kb = 0; kb < p.KB; ++kb, ++it) {
                 if (kb % kScaleBlocks == 0) {
                     ok = mbar_wait_bounded(sc_full + (group & 1), (group >> 1) & 1);
@@ -187,17 +199,16 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
                     break;
                 }
                 tc_fence_after();
-                const float s = sc[quad * 32 + lane] * sc[128 + part];
+                const float s = sc[quad * 32 + lane] * sc[128 + (part >> 1)];
                 const uint64_t s2 = pack2(s, s);
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    uint32_t d[2][32];
-                    tmem_ld32_async(at0 + (uint32_t)(as * 256 + c * 64), d[0]);
-                    tmem_ld32_async(at0 + (uint32_t)(as * 256 + c * 64 + 32), d[1]);
+                    uint32_t d[32];
+                    tmem_ld32_async(at0 + (uint32_t)(as * 256 + c * 32), d);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        acc[c * 32 + j] = fma2(pack2(__uint_as_float(d[j / 16][2 * j % 32]), __uint_as_float(d[j / 16][2 * j % 32 + 1])), s2, acc[c * 32 + j]);
+                    for (int j = 0; j < 16; ++j)
+                        acc[c * 16 + j] = fma2(pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])), s2, acc[c * 16 + j]);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -206,12 +217,12 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
                     if (kb % kScaleBlocks == kScaleBlocks - 1 || kb == p.KB - 1) mbar_arrive_one(sc_empty + ((group - 1) & 1));
                 }
             }
-            const int m0 = tile / g.n_tiles * 256 + rank * 128 + quad * 32, n0 = tile % g.n_tiles * 256 + part * 128;
+            const int m0 = tile / g.n_tiles * 256 + rank * 128 + quad * 32, n0 = tile % g.n_tiles * 256 + part * 64;
             // through shared memory, 128 bytes of a row at a time: 64 elements, or 32
             const int per = p.out_bf16 ? 64 : 32;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if (p.out_bf16 && r >= 2) break;
+            for (int r = 0; r < 2; ++r) {
+                if (p.out_bf16 && r >= 1) break;
                 if (lane == 0) tma_store_read();
                 __syncwarp();
 #pragma unroll
@@ -220,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
                     if (p.out_bf16) {
                         float f[8];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) unpack2(acc[(r & 1) * 32 + c * 4 + j], f[2 * j], f[2 * j + 1]);
+                        for (int j = 0; j < 4; ++j) unpack2(acc[c * 4 + j], f[2 * j], f[2 * j + 1]);
                         u = Vec16<__nv_bfloat16>::pack(f);
                     } else {
                         const uint64_t lo = acc[r * 16 + c * 2], hi = acc[r * 16 + c * 2 + 1];

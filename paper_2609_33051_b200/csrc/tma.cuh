@@ -52,6 +52,16 @@ __device__ __forceinline__ void mbar_arrive_one(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// A warp's wait: false to all its lanes if it ran out.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity)); }
+
+// One lane of a converged warp.  (The product warps run their loops with all lanes and elect one for each product: the operands then
+// stay in uniform registers, and an instruction is issued every 30 to 60 cycles; from a branch that one lane takes it was 95.)
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 // Descriptor of an operand in the 128-byte swizzle: rows of 128 bytes, groups of eight of them 1024 bytes apart (`sbo`); for
 // operands whose contiguous axis is not the inner one `lbo` is the distance of the next 128 bytes along it.
 __device__ __forceinline__ uint64_t swizzled_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
