@@ -5,4 +5,4 @@ Nothing here computes on the CPU: without the CUDA library the calls fail.
 """
 from . import synth  # noqa: F401
 
-__all__ = ["synth", "binding", "build", "calibrate"]
+__all__ = ["synth", "binding", "build", "calibrate", "layer"]
