@@ -288,8 +288,8 @@ int sketchssm_step_host(sketchssm_ctx* ctx, int op, int n_before, const void* ho
 typedef struct sketchssm_prompts {
     int32_t sequences;      /* N >= 0 */
     int32_t tokens;         /* T >= 0: rows of the packed tensors */
-    const int32_t* starts;  /* [N + 1] ascending: sequence i is the rows starts[i] .. starts[i + 1] - 1 (none, one or more); rows
-                               outside starts[0] .. starts[N] are neither read nor written */
+    const int32_t* starts;  /* [N + 1] ascending: sequence i is the rows starts[i] .. starts[i + 1] - 1 (none, one or more); what
+                               rows outside starts[0] .. starts[N] hold changes nothing, and they are not written */
     const int32_t* slots;   /* [N]: the batch entry that keeps sequence i's state, or NULL: i.  The entries of one call are distinct.
                                An entry outside 0..B-1: the sequence's state is not kept (its outputs are written) */
     const int32_t* resume;  /* [N]: the batch entry whose stored state sequence i goes on from (its own, or another one that no

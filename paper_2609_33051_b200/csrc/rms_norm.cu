@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(512) rms_norm_kernel(const NormParams p) {
                 }
                 load8(static_cast<const T*>(p.gate) + row * p.gate_stride + e, f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[v][j] *= silu<float>(f[j]);
+                for (int j = 0; j < 8; ++j) h[v][j] *= silu<T>(f[j]);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sq = fmaf(h[v][j], h[v][j], sq);

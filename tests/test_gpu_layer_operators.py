@@ -238,6 +238,39 @@ def test_scan_keeps_what_is_not_finite_to_its_own_sequence_and_head():
     assert ((st - new).abs() - (6 * 150 + 144) * U * new_mag)[keep].max() <= 0
 
 
+@pytest.mark.parametrize("od", ["bf16", "f32"])
+def test_what_rows_outside_the_sequences_hold_changes_nothing(od):
+    """NaN before, behind and in the rows of a batch that belong to no sequence; none of them is written."""
+    lens, first, tail = [130, 0, 60], 5, 40
+    x = scan_inputs(lens, 4, 1, 128, 64, "bf16", 8, first, tail)
+    starts, pr = batch_of(lens, None, [3, 4, 5], first, tail)
+    clean = check_scan(layer(8, 4, 128, 64), x, starts, pr, None, [3, 4, 5], od)
+    for n in ("q", "k", "v", "dt"):
+        x[n][:first] = x[n][starts[-1]:] = float("nan")
+    assert torch.equal(check_scan(layer(8, 4, 128, 64), x, starts, pr, None, [3, 4, 5], od)[first:-tail], clean[first:-tail])
+    m, st = layer(8), torch.zeros(8, 3, 256, dtype=torch.bfloat16, device=DEV)
+    w, out = rand(torch.Generator().manual_seed(1), 256, 4).to(DEV), torch.full((pr.tokens, 256), 7.0, dtype=torch.bfloat16, device=DEV)
+    m.causal_conv(pr, x["v"].flatten(1).to(DEV), w, None, st, out)
+    assert torch.isfinite(out).all() and (out[:first] == 7).all() and (out[starts[-1]:] == 7).all() and torch.isfinite(st).all()
+
+
+def test_norm_keeps_what_is_not_finite_to_its_row():
+    gen = torch.Generator().manual_seed(3)
+    x, w = rand(gen, 600, 512), torch.ones(512)
+    m = layer(1, io="f32")
+    outs = []
+    for bad in (False, True):
+        if bad:
+            x[5, 7], x[100, 0] = float("nan"), float("inf")
+        out8, scale, out = torch.empty(600, 512, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(600, 4, device=DEV), torch.empty(600, 512, device=DEV)
+        m.rms_norm(x.to(DEV), w.to(DEV), out=out, out8=out8, scale=scale)
+        outs.append((out8.view(torch.uint8), scale, out))
+    rest = [i for i in range(600) if i not in (5, 100)]
+    for a, b in zip(*outs):
+        assert torch.equal(a[rest], b[rest])
+    assert torch.isnan(outs[1][2][5]).all()
+
+
 def test_scan_in_pieces_is_the_whole():
     """A prompt in three calls that go on from the stored state, on another stream, equals the prompt in one."""
     x = scan_inputs([450], 4, 1, 128, 64, "bf16", 8, seed=9)
@@ -313,6 +346,8 @@ NORM = [
     (257, 5128, 0, "bf16", "bf16", "residual", 0),
     (1300, 1928, 0, "bf16", "bf16", "gated", 0),
     (1025, 248, 0, "bf16", "f32", "gated", 31),
+    (130, 512, 128, "f32", "f32", "gated", 8),
+    (700, 16384, 8192, "bf16", "bf16", "gated", 128),
 ]
 
 
