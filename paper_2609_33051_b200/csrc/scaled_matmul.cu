@@ -109,11 +109,12 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    int rank = (int)blockIdx.x % g.ks, first = (int)blockIdx.x / g.ks, step = (int)gridDim.x / g.ks;
+    int kb0 = p.KB * rank / g.ks, kb1 = p.KB * (rank + 1) / g.ks;
+    asm volatile("" : "+r"(rank), "+r"(first), "+r"(step), "+r"(kb0), "+r"(kb1));      // (worked out while the predecessor still runs)
     grid_dep_wait();
     grid_dep_launch_dependents();
     const uint32_t tmem = *slot;
-    const int rank = (int)blockIdx.x % g.ks, first = (int)blockIdx.x / g.ks, step = (int)gridDim.x / g.ks;
-    const int kb0 = p.KB * rank / g.ks, kb1 = p.KB * (rank + 1) / g.ks;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -329,12 +330,14 @@ int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
     // The narrowest tile that holds the tokens.
     const int bn = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     const long long tiles = nt * ((p.M + bn - 1) / bn);
-    // Few tiles: the blocks split over a cluster, while that leaves a CTA two blocks and the SMs one CTA (two of the narrow ones).
+    // Few tiles: the blocks split over a cluster, while that leaves a CTA two blocks and every SM one CTA.  (Two CTAs an SM: 9.3 us for
+    // 64 x 8512 x 2048 against 8.3; the sums' way through distributed shared memory, some 10 bytes a cycle and SM, is what grows.)
     int ks = 1;
-    while (ks < 8 && tiles * ks * 2 <= (long long)sms * (bn == 128 ? 1 : 2) && p.KB >= ks * 4) ks *= 2;
+    while (ks < 8 && tiles * ks * 2 <= (long long)sms && p.KB >= ks * 4) ks *= 2;
     if (bn == 16) return launch_tiles<16, 4, 6, 4, 2>(ctx, p, ks, stream);
     if (bn == 32) return launch_tiles<32, 4, 5, 4, 2>(ctx, p, ks, stream);
-    if (bn == 64) return launch_tiles<64, 4, 4, 4, 2>(ctx, p, ks, stream);
+    // (eight stages where a CTA has an SM to itself; clusters of four and eight find their place more easily with half of them)
+    if (bn == 64) return ks <= 2 ? launch_tiles<64, 4, 8, 4, 1>(ctx, p, ks, stream) : launch_tiles<64, 4, 4, 4, 2>(ctx, p, ks, stream);
     return launch_tiles<128, 8, 6, 4, 1>(ctx, p, ks, stream);
 }
 
