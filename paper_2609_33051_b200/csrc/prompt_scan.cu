@@ -2,12 +2,13 @@
 //
 //     S <- exp(a beta) S + beta k v^T,   out = S^T q + skip v,   token by token, S in fp32 registers.
 //
-// A CTA takes `cols` value columns of one head of one sequence.  A thread holds eight rows (K = 128: two runs of four; four with K = 64) of four
-// columns, sixteen neighbouring lanes share the columns: a token is 48 two-element operations a thread and five loads of 16 bytes from shared memory.
-// The sums over the lanes are made for four tokens and columns together: every step halves what a lane still has to add, and nothing
-// waits for a token's own chain of shuffles (which took 400 cycles a token).  Tokens come through shared memory, 32 of them while
-// the 32 before are worked on.  Bound by fp32 issue (three multiply-adds for an element of the state and a token), and with few heads by the chain of
-// a token, about 250 cycles.
+// A CTA takes `cols` value columns of one head of one sequence.  A thread holds eight rows (K = 128: two runs of four; four with
+// K = 64) of four columns, sixteen neighbouring lanes share the columns: a token is 48 two-element operations a thread and five loads
+// of 16 bytes from shared memory.  The sums over the lanes are made for four tokens and columns together: every step halves what a
+// lane still has to add, and nothing waits for a token's own chain of shuffles (which took 400 cycles a token).  Tokens come through
+// shared memory, 32 of them while the 32 before are worked on.  Bound by fp32 issue (three multiply-adds for an element of the state and a
+// token), and with few heads by the chain of a token, about 300 cycles.  2000 fp32 tokens of 24 heads of 80 columns, seven ragged
+// sequences: 152 us (split in time for more CTAs: 208; the states and a second reading cost more than the longest sequence's tail).
 #include "pairs.cuh"
 
 namespace sketchssm {

@@ -8,10 +8,14 @@
 // Each block of 128 goes through the tensor cores into an accumulator of its own (fp32, in tensor memory); the epilogue warps
 // add it, times its scales, to sums in registers, two elements an instruction, while the next block is multiplied.
 //
-// Roles: one thread issues the copies (TMA, 128-byte swizzle: a row of a tile is exactly one block), one the products; two warps
-// fetch the token scales one block ahead and leave them, times the weights' scale, in shared memory; the other warps add.
+// Roles: one thread issues the copies (TMA, 128-byte swizzle: a row of a tile is exactly one block), one warp the products (an elected
+// lane of the converged warp); two warps fetch the token scales, four blocks at a time and one such group ahead, and leave them, times
+// the weights' scale, in shared memory; the other warps add.
 // With few tiles (a decode step) the blocks are split over a cluster of up to eight CTAs; each of them adds up a share of the
 // columns, from the sums in every rank's shared memory in the order of the ranks.
+//
+// What bounds it: 64 x 8512 x 2048 takes 8.3 us, of which the weights' bytes are 2.7 at the rate of HBM; the first tile arrives 3400
+// cycles after the start, the eight blocks of a CTA take another 2500, the sums' way to the other CTA and out 4000.
 #include "tma.cuh"
 
 namespace sketchssm {
