@@ -172,13 +172,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                 }
             }
-            if (!ok) {                                  // let the copies under way end (n chunks were asked for in full)
-                for (int i = max(0, n - 2); i < n; ++i) {
-                    mbar_wait_bounded(bar + bFullK + (i & 1), (i / 2) & 1, 1u << 16);
-                    mbar_wait_bounded(bar + bFullV + (i & 1), (i / 2) & 1, 1u << 16);
-                }
-                if (OUTPUTS && n > 0) mbar_wait_bounded(bar + bFullQ, (n - 1) & 1, 1u << 16);
+            // Before the CTA ends the copies under way have ended (after a fault; otherwise they have been waited for), and the products'
+            // last arrivals at the buffers' barriers are in.
+            for (int i = max(0, n - 2); i < n; ++i) {
+                if (!ok) mbar_wait_bounded(bar + bFullK + (i & 1), (i / 2) & 1, 1u << 16);
+                if (!ok) mbar_wait_bounded(bar + bFullV + (i & 1), (i / 2) & 1, 1u << 16);
+                if (ok) mbar_wait_bounded(bar + bEmptyK + (i & 1), (i / 2) & 1);
             }
+            if (OUTPUTS && n > 0) mbar_wait_bounded(bar + (ok ? bEmptyQ : bFullQ), (n - 1) & 1, 1u << 16);
         }
         __syncwarp();
     } else if (warp == 1) {

@@ -138,8 +138,9 @@ __global__ void __launch_bounds__(32 * (EW + 4), MINB) scaled_matmul_kernel(cons
                     tma_load(smem + s * L::kStage + L::kW, &g.ta, kb * 128, m0, full + s);
                 }
             }
-            // no copy may be under way when the CTA ends (after a fault; otherwise all of them have been waited for)
-            for (int i = it < NS ? 0 : it - NS; i < it; ++i) mbar_wait_bounded(full + i % NS, (i / NS) & 1);
+            // before the CTA ends: no copy is under way (after a fault; otherwise all of them have been waited for), and the products'
+            // last arrivals at the stages' barriers are in
+            for (int i = it < NS ? 0 : it - NS; i < it; ++i) mbar_wait_bounded((ok ? empty : full) + i % NS, (i / NS) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {

@@ -98,9 +98,12 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
                     tma_load_pair(dst + kHalf, &g.tw, kb * 128, n, bar);
                 }
             }
-            // no copy may be under way when the CTAs end (after a fault; otherwise all of them have been waited for)
-            if (rank == 0)
-                for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) mbar_wait_bounded(full + i % kStages, (i / kStages) & 1);
+            // before the CTAs end: no copy is under way (after a fault; otherwise all of them have been waited for), and the products'
+            // last arrivals at the stages' barriers are in
+            for (int i = it < kStages ? 0 : it - kStages; i < it; ++i) {
+                if (ok) mbar_wait_bounded(empty + i % kStages, (i / kStages) & 1);
+                else if (rank == 0) mbar_wait_bounded(full + i % kStages, (i / kStages) & 1);
+            }
         }
         __syncwarp();
     } else if (warp == 1) {
