@@ -7,15 +7,17 @@
 // one of 128), which share K, Q and the products Q K^T.
 //
 // Precision.  Q K^T is exact up to the fp32 sums.  The state is held in fp32 registers; W goes to the tensor cores in three bf16
-// parts, so that a term of S is off by less than 2^-22.  P, and S as an operand of Y, are rounded to bf16 once: the outputs are rounded
-// by as much behind them, so an output's error is sqrt(2) times that of its own rounding, at most (measured 2.3e-3 against 1.7e-3 in
-// the square mean).  Two parts of P as well cost a pair of heads 16 more products of 128 x 64 x 16 a chunk, and a third as much
-// arithmetic on CUDA cores as the rest of P.  Sums of decays run forward for c_t and backward for c_end - c_t, so that what is small
-// is exact.
+// parts, so that a term of S is off by less than 2^-22.  P below its diagonal, and S as an operand of Y, are rounded to bf16 once: the
+// outputs are rounded by as much behind them, so an output's error is sqrt(2) times that of its own rounding, at most.  The diagonal, a
+// token's own and mostly largest weight, stays in fp32 and goes with the skip (error in the square mean 1.9e-3, 2.3e-3 with the
+// diagonal in bf16, 1.7e-3 of the outputs' rounding alone; it costs one chunk 0.4 us and long prompts nothing).  Two parts of P as well
+// cost a pair of heads 16 more products of 128 x 64 x 16 a chunk, and a third as much arithmetic on CUDA cores as the rest of P.
+// Sums of decays run forward for c_t and backward for c_end - c_t, so that what is small is exact.
 //
 // What bounds it: a chunk of a pair of heads is about 8800 cycles, of which the tensor cores work 3100 and HBM would need 2800.  It is
 // 20,000 warp instructions, a third of them the three parts of W, issued at 2.3 a cycle; the chain from one state to the next (S as an
-// operand, Q S, W in four quarters, S) is about as long.  16384 tokens of 64 heads in one prompt: 262 us (1.07 TB/s), in 48: 295 us (1.54 TB/s).
+// operand, Q S, W in four quarters, S) is about as long.  16384 tokens of 64 heads in one prompt: 263 us (1.07 TB/s), in
+// 48: 296 us (1.54 TB/s).
 // Roles: warp 3 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
 // warp 0 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
 // ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
@@ -370,7 +372,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 const int block = x.block0 + (j ? x.live1 : 0), head = block / per_head;
                 const bool live = j == 0 || x.live1;
                 const float skip = p.skip != nullptr ? p.skip[head] : 0.f;
-                const uint64_t skip2 = pack2(skip, skip);
                 for (int t = x.t0; t < x.t1; t += kQ, ++n) {
                     const int b = n & 1, valid = min(kQ, x.t1 - t);
                     const float* gt = gates + b * kGateBuf + j * kGateSet;
@@ -382,6 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     // P: below the diagonal's 32 x 32 blocks its weight is 2^(c_t - c at the end of the columns' 32) times a factor of
                     // the column, both at most 1 (but for beta); in them it is one exponential an element
                     const float ct = gt[row];
+                    float own;
                     uint32_t d[32], f[16];
                     tmem_ld32_async(td, d);
 #pragma unroll 1
@@ -416,12 +418,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                             unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), pack2(ex2(x2), ex2(x3))), x2, x3);
                             f[2 * i] = bf16x2(x0, x1);
                             f[2 * i + 1] = bf16x2(x2, x3);
+                            d[4 * i] = __float_as_uint(x0);
+                            d[4 * i + 1] = __float_as_uint(x1);
+                            d[4 * i + 2] = __float_as_uint(x2);
+                            d[4 * i + 3] = __float_as_uint(x3);
                         }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {           // column 2 i + e of the 32 is there up to row `lane`
-                            if (lane < 2 * i) f[i] = 0u;
-                            if (lane == 2 * i) f[i] &= 0xffffu;
+                        for (int i = 0; i < 16; ++i) {           // column 2 i + e of the 32 is there up to the row before `lane`
+                            if (lane <= 2 * i) f[i] = 0u;
+                            if (lane == 2 * i + 1) f[i] &= 0xffffu;
                         }
+                        // the token's own weight stays in fp32: it goes with the skip
+#pragma unroll
+                        for (int s = 16; s > 0; s >>= 1) {
+#pragma unroll
+                            for (int i = 0; i < s; ++i) d[i] = (lane & s) ? d[i + s] : d[i];
+                        }
+                        own = __uint_as_float(d[0]);
                         tmem_st16u(tp + quad * 16, f);
                     }
                     ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
@@ -449,6 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bYFree);
+                    const uint64_t skip2 = pack2(skip + own, skip + own);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         uint4* at = reinterpret_cast<uint4*>(mine + ((c ^ (row & 7)) * 16));
