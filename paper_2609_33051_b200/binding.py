@@ -7,6 +7,7 @@ library is missing or CUDA is unavailable the calls fail.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -85,6 +86,12 @@ class Prompts:
 
     def on(self, device: torch.device) -> bool:
         return self.device == device
+
+
+def on_stream(stream):
+    """Tensors made under it may be dropped as soon as what uses them is in `stream`'s queue (None: the current stream, as always):
+    their memory is then given only to later work of that stream."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class SketchSSMError(RuntimeError):
@@ -372,7 +379,8 @@ class SketchSSM:
         if not prompts.on(self.device):
             raise ValueError("prompts lie on the layer's device")
         if work is None:
-            work = self.new_prompt_work(prompts.sequences, prompts.tokens)
+            with on_stream(stream):
+                work = self.new_prompt_work(prompts.sequences, prompts.tokens)
         rc = _CALLS.prompt_scan(*self._scan, prompts.address, prompts.tokens, q, k, v, dt, a, out, dt_bias, skip, work, self._stream(stream))
         if rc:
             self._check("sketchssm_prompt_scan", rc)

@@ -31,7 +31,8 @@ def quantise_weight(w: torch.Tensor):
 class Mamba2Layer:
     """One layer of `width` channels for `batch` sequences.  Tensors between layers are bf16; weights come in as floats:
     norm [width], w_in [2 H V + 2 G K + H, width] (rows: gate, values, keys, queries, step sizes), conv_weight [C, W] and conv_bias [C]
-    with C = H V + 2 G K, a [H] (negative), dt_bias and skip [H], gate_norm [H V], w_out [width, H V]."""
+    with C = H V + 2 G K, a [H] (negative), dt_bias and skip [H], gate_norm [H V], w_out [width, H V].
+    stream (None: the current one): what runs, and what it allocates, the results among it, belongs to that stream."""
 
     def __init__(self, batch: int, heads: int, dk: int, dv: int, groups: int, rank: int, buf_len: int, norm, w_in, conv_weight,
                  conv_bias, a, dt_bias, skip, gate_norm, w_out, eps: float = 1e-5, device: int = 0, **kw):
@@ -69,6 +70,10 @@ class Mamba2Layer:
     def prompt(self, prompts: binding.Prompts, x: torch.Tensor, residual: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The layer over packed prompts x [T, width]; leaves the states and the convolution's rows of the prompts' slots.  Before the
         first decode step of a window begin_window builds the sketch."""
+        with binding.on_stream(stream):
+            return self._prompt(prompts, x, residual, stream)
+
+    def _prompt(self, prompts, x, residual, stream):
         m, h, k = self.m, self.m.H, self.m.K
         gate, xbc, dt = self._project_in(x, residual, stream)
         t = x.shape[0]
@@ -87,6 +92,10 @@ class Mamba2Layer:
     def step(self, n_before: int, x: torch.Tensor, residual: Optional[torch.Tensor] = None, exact: bool = False, stream=None) -> torch.Tensor:
         """One token of every sequence, x [B, width], with n_before tokens in the ring: a decode step, and at the end of the window the
         state update, after which the ring is empty.  exact: the full state is read instead of the sketch."""
+        with binding.on_stream(stream):
+            return self._step(n_before, x, residual, exact, stream)
+
+    def _step(self, n_before, x, residual, exact, stream):
         m = self.m
         gate, xbc, dt = self._project_in(x, residual, stream)
         t = m.conv_step(xbc, dt, self.conv_weight, self.conv_bias, self.conv_state, self.a, self.dt_bias, self.token, groups=self.groups,

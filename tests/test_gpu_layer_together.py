@@ -147,3 +147,39 @@ def test_a_layers_token_in_a_graph():
     want = b.step(0, x)
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(a.conv_state, b.conv_state)
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(monkeypatch):
+    """Tensors that a call makes and drops are made on the stream that the caller named: their memory would otherwise go to the current
+    stream's next tensors while the kernels still use it."""
+    H, G, K, V, W, width, B = 4, 1, 128, 64, 4, 256, 3
+    gen = torch.Generator().manual_seed(6)
+    w = weights(gen, width, H, G, K, V, W)
+    a, b = (layer.Mamba2Layer(B, H, K, V, G, 8, 4, **w) for _ in range(2))
+    lens = [0, 1100, 1103, 1110]
+    x, tok = rand(gen, lens[-1], width, dtype=torch.bfloat16).to(DEV), rand(gen, B, width, dtype=torch.bfloat16).to(DEV)
+    pr = prompts(lens)
+    want = a.prompt(pr, x)
+    a.begin_window()
+    want_tok = a.step(0, tok)
+    args = [torch.zeros(lens[-1], *d, dtype=torch.bfloat16, device=DEV) for d in ((G, K), (G, K), (H, V), (H,))]
+    y = torch.zeros(lens[-1], H, V, device=DEV)
+    torch.cuda.synchronize()
+    side, seen, empty = torch.cuda.Stream(), [], torch.empty
+
+    def watched(*args, **kw):
+        seen.append(torch.cuda.current_stream())
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch, "empty", watched)
+    out = b.prompt(pr, x, stream=side)
+    b.begin_window(stream=side)
+    out_tok = b.step(0, tok, stream=side)
+    assert len(seen) > 9 and all(s == side for s in seen)
+    assert torch.cuda.current_stream() != side
+    del seen[:]
+    b.m.prompt_scan(pr, *args, a.a, y, stream=side)
+    assert seen == [side]                      # the scan's scratch
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(out_tok, want_tok)
