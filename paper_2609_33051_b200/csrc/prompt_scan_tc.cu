@@ -307,9 +307,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float l[4], pre[4], suf[4];
-                    // (2^-160 is zero in fp32; the bound keeps the sums finite, and a difference of two exact to 2^-10)
+                    // (2^-160 is zero in fp32; the bound keeps the sums finite, and a difference of two exact to 2^-10; NaN passes it)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) l[i] = t + lane * 4 + i < x.t1 ? fmaxf(a2[j] * beta[j][i], -160.f) : 0.f;
+                    for (int i = 0; i < 4; ++i) {
+                        const float x2 = a2[j] * beta[j][i];
+                        l[i] = t + lane * 4 + i < x.t1 ? (x2 < -160.f ? -160.f : x2) : 0.f;
+                    }
                     pre[0] = l[0];
 #pragma unroll
                     for (int i = 1; i < 4; ++i) pre[i] = pre[i - 1] + l[i];

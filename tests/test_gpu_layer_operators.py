@@ -212,6 +212,26 @@ def test_scan_with_extreme_gates(dt, a):
     check_scan(layer(8, 2, 128, 64), x, starts, pr, None, [1], "f32")
 
 
+@pytest.mark.parametrize("lengths", [[140, 150, 40], [1, 5, 1], [60, 2300]])
+def test_scan_hands_on_a_nan_of_the_gates(lengths):
+    """Rates and step sizes that are NaN: the head is NaN from that token on, in outputs and state, and nothing else is."""
+    x = scan_inputs(lengths, 4, 2, 128, 64, "bf16", 4, seed=5)
+    starts, pr = batch_of(lengths)
+    T, at = sum(lengths), lengths[0] + lengths[1] // 2
+    x["a"][2] = float("nan")
+    x["dt"][at, 0] = float("nan")                 # sequence 1, head 0
+    m = layer(4, 4, 128, 64)
+    out = torch.zeros(T, 4, 64, dtype=torch.bfloat16, device=DEV)
+    m.prompt_scan(pr, *(x[n].to(DEV) for n in ("q", "k", "v", "dt", "a")), out, dt_bias=x["bias"].to(DEV), skip=x["skip"].to(DEV))
+    m.check_status()
+    bad = torch.zeros(T, 4, dtype=torch.bool)
+    bad[:, 2] = bad[at:lengths[0] + lengths[1], 0] = True
+    assert torch.equal(torch.isnan(out).all(2).cpu(), bad) and torch.equal(torch.isnan(out).any(2).cpu(), bad)
+    state = torch.zeros(4, 4, dtype=torch.bool)
+    state[:len(lengths), 2] = state[1, 0] = True
+    assert torch.equal(torch.isnan(m.state).all(3).all(2).cpu(), state) and torch.equal(torch.isnan(m.state).any(3).any(2).cpu(), state)
+
+
 def test_scan_keeps_what_is_not_finite_to_its_own_sequence_and_head():
     x = scan_inputs([140, 150, 40], 4, 2, 128, 64, "bf16", 8, seed=3)
     starts, pr = batch_of([140, 150, 40], None, [3, 4, 5])
