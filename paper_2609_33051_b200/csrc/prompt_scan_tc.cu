@@ -10,14 +10,14 @@
 // parts, so that a term of S is off by less than 2^-22.  P below its diagonal, and S as an operand of Y, are rounded to bf16 once: the
 // outputs are rounded by as much behind them, so an output's error is sqrt(2) times that of its own rounding, at most.  The diagonal, a
 // token's own and mostly largest weight, stays in fp32 and goes with the skip (error in the square mean 1.9e-3, 2.3e-3 with the
-// diagonal in bf16, 1.7e-3 of the outputs' rounding alone; it costs one chunk 0.4 us and long prompts nothing).  Two parts of P as well
+// diagonal in bf16, 1.7e-3 of the outputs' rounding alone; it costs one chunk 0.4 us of 13 and long prompts nothing).  Two parts of P as well
 // cost a pair of heads 16 more products of 128 x 64 x 16 a chunk, and a third as much arithmetic on CUDA cores as the rest of P.
 // Sums of decays run forward for c_t and backward for c_end - c_t, so that what is small is exact.
 //
 // What bounds it: a chunk of a pair of heads is about 8800 cycles, of which the tensor cores work 3100 and HBM would need 2800.  It is
 // 20,000 warp instructions, a third of them the three parts of W, issued at 2.3 a cycle; the chain from one state to the next (S as an
-// operand, Q S, W in four quarters, S) is about as long.  16384 tokens of 64 heads in one prompt: 263 us (1.07 TB/s), in
-// 48: 296 us (1.54 TB/s).
+// operand, Q S, W in four quarters, S) is about as long.  16384 tokens of 64 heads in one prompt: 269 us (1.05 TB/s), in
+// 48: 295 us (1.54 TB/s).
 // Roles: warp 3 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
 // warp 0 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
 // ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
@@ -44,7 +44,9 @@ constexpr int kThreads = 896;
 
 enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
        bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 24, bVRead = 26, bScaled = 30, kBars = 32 };
-constexpr uint32_t kSmemTc = kBarOff + kBars * 8u + 16u + 1024u;
+constexpr uint32_t kMarkOff = kBarOff + kBars * 8u + 16u;       // [2 buffers][2 sets][65]: see mark_of
+constexpr uint32_t kMarks = 65;
+constexpr uint32_t kSmemTc = kMarkOff + 4u * kMarks * 4u + 1024u;
 
 // columns of tensor memory
 constexpr uint32_t kDot = 0, kY = 128, kProd = 256, kP = 384;
@@ -99,6 +101,20 @@ __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[1
         "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+
+// The products take every value of a chunk into every row, and a zero weight times NaN or infinity is NaN: values that are not finite go
+// to the products as zeros, and a column's rows from the first of them on become NaN afterwards.  A mark of chunk n holds that row; the
+// largest of several is the first row of the latest chunk, so that marks need no clearing.  (The 65th: of any column.)
+// Looking for them costs one long prompt 2 % (269 us, 263), many short ones 0.6 %.
+__device__ __forceinline__ uint32_t mark_of(int n, int row) { return ((uint32_t)n << 8) + (uint32_t)(kQ - row); }
+
+// Adds products of the eight values, two by two, to two sums: not finite if one of the values is not (or if a product overflows: then
+// for nothing).  Half as many instructions as a sum for each value.
+__device__ __forceinline__ void odd_values(const uint4& v, uint32_t& a, uint32_t& b) {
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(a) : "r"(v.x), "r"(v.y));
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(b) : "r"(v.z), "r"(v.w));
+}
+
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t*>(&h);
@@ -129,6 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
         }
         mbar_fence_init();
     }
+    if (OUTPUTS && tid < 4 * (int)kMarks) reinterpret_cast<uint32_t*>(smem + kMarkOff)[tid] = 0u;
     if (warp == 1) tmem_alloc<512>(slot);
     tc_fence_before();
     __syncthreads();
@@ -380,6 +397,21 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     const float* gt = gates + b * kGateBuf + j * kGateSet;
                     unsigned char* v = smem + kVOff + (b * 2 + j) * kTile;
                     unsigned char* mine = v + row * 128;
+                    ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
+                    if (ok && row >= valid) {                                    // rows of the next sequence are no part of this one
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    if (valid < kQ) proxy_fence();
+                    if (!ok) break;
+                    uint32_t odd = 0u;
+                    {
+                        uint32_t a = 0u;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) odd_values(*reinterpret_cast<const uint4*>(mine + ((i ^ (row & 7)) * 16)), odd, a);
+                        asm("{ .reg .b32 z; mov.b32 z, 0; fma.rn.bf16x2 %0, %0, z, z; fma.rn.bf16x2 %0, %1, z, %0; }" : "+r"(odd) : "r"(a));
+                    }
+                    const bool odd_row = (odd & 0x7fff7fffu) != 0u;
                     ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bDot, n & 1);
                     if (!ok) break;
                     tc_fence_after();
@@ -440,13 +472,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         own = __uint_as_float(d[0]);
                         tmem_st16u(tp + quad * 16, f);
                     }
-                    ok = warp_wait(bar + bFullV + b, (n / 2) & 1);
-                    if (ok && row >= valid) {                                    // rows of the next sequence are no part of this one
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(mine)[i] = make_uint4(0u, 0u, 0u, 0u);
+                    uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kMarkOff) + (b * 2 + j) * kMarks;
+                    if (__any_sync(0xffffffffu, odd_row)) {
+                        ok = warp_wait(bar + bVRead + j * 2 + b, (n / 2) & 1);       // (the state takes the values as they are)
+                        if (!ok) break;
+                        if (odd_row) {
+                            atomicMax(marks + 64, mark_of(n, row));
+#pragma unroll 1
+                            for (int e = 0; e < 64; ++e) {
+                                unsigned short* at = reinterpret_cast<unsigned short*>(mine + (((e >> 3) ^ (row & 7)) * 16)) + (e & 7);
+                                if ((*at & 0x7f80u) == 0x7f80u) {
+                                    *at = 0;
+                                    atomicMax(marks + e, mark_of(n, row));
+                                }
+                            }
+                        }
+                        proxy_fence();
                     }
-                    if (valid < kQ) proxy_fence();
-                    if (!ok) break;
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -465,6 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bYFree);
+                    const bool nan_here = reinterpret_cast<const volatile uint32_t*>(marks)[64] >= mark_of(n, row);
                     const uint64_t skip2 = pack2(skip + own, skip + own);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
@@ -481,6 +524,12 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                             z[i] = bf16x2(lo, hi);
                         }
                         *at = make_uint4(z[0], z[1], z[2], z[3]);
+                    }
+                    if (nan_here) {
+#pragma unroll 1
+                        for (int e = 0; e < 64; ++e)
+                            if (reinterpret_cast<const volatile uint32_t*>(marks)[e] >= mark_of(n, row))
+                                reinterpret_cast<unsigned short*>(mine + (((e >> 3) ^ (row & 7)) * 16))[e & 7] = 0x7fff;
                     }
                     __syncwarp();
                     // a warp's 32 rows of 128 bytes, eight lanes a row; the buffer is free before the stores are made

@@ -232,6 +232,30 @@ def test_scan_hands_on_a_nan_of_the_gates(lengths):
     assert torch.equal(torch.isnan(m.state).all(3).all(2).cpu(), state) and torch.equal(torch.isnan(m.state).any(3).any(2).cpu(), state)
 
 
+@pytest.mark.parametrize("lengths,H,G,V", [([300, 7, 0, 141, 1], 3, 1, 64), ([140, 2, 128], 4, 2, 128), ([1400], 2, 1, 64)])
+def test_scan_in_chunks_does_not_look_ahead(lengths, H, G, V):
+    """bf16 outputs, which are made 128 tokens at a time: what is not finite changes no output of a token before it, of another
+    column (values) or head (keys, queries); everything else is as in the test of the same sizes."""
+    x = scan_inputs(lengths, H, G, 128, V, "bf16", 8, seed=9)
+    T, nan, inf = sum(lengths), float("nan"), float("inf")
+    for t, h, c, value in ((0, H - 1, 3, nan), (1, 0, 0, nan), (70, 0, 63, inf), (70, 0, 10, -inf), (127, 1, 5, inf), (100, 1, 5, nan), (131, 1, V - 1, nan),
+                           (T - 1, 0, 7, nan), (T - 2, 1, 31, -inf)):
+        x["v"][t, h, c] = value
+    x["k"][135, 0, 3], x["q"][20, 0, 0] = nan, inf
+    starts, pr = batch_of(lengths)
+    m = layer(8, H, 128, V)
+    m.state.copy_(x["state"])
+    want, mag, new, new_mag = ref.scan(starts, None, None, *(x[n] for n in ("q", "k", "v", "dt", "a", "bias", "skip", "state")), m.B)
+    out = torch.zeros(T, H, V, dtype=torch.bfloat16, device=DEV)
+    m.prompt_scan(pr, *(x[n].to(DEV) for n in ("q", "k", "v", "dt", "a")), out, dt_bias=x["bias"].to(DEV), skip=x["skip"].to(DEV))
+    m.check_status()
+    rel = (6 * max(lengths) + 144) * U
+    for got, exp, tol in ((out, want, ref.half_step(torch.bfloat16) * want.abs() + (rel + TERMS["bf16"] * 2.0 ** -8) * mag), (m.state, new, rel * new_mag)):
+        there = torch.isfinite(exp)
+        assert torch.equal(torch.isfinite(got.cpu()), there)
+        ref.close(ref.f64(got)[there], exp[there], tol[there], "finite ones")
+
+
 def test_scan_keeps_what_is_not_finite_to_its_own_sequence_and_head():
     x = scan_inputs([140, 150, 40], 4, 2, 128, 64, "bf16", 8, seed=3)
     starts, pr = batch_of([140, 150, 40], None, [3, 4, 5])
