@@ -73,8 +73,8 @@ class Prompts:
     def __init__(self, starts: torch.Tensor, tokens: int, slots: Optional[torch.Tensor] = None,
                  resume: Optional[torch.Tensor] = None):
         self.sequences, self.tokens = starts.numel() - 1, int(tokens)
-        if self.sequences < 0 or self.tokens < 0:
-            raise ValueError("starts holds one row number more than there are sequences, and tokens is not negative")
+        if self.sequences < 0 or not 0 <= self.tokens < 2 ** 31:
+            raise ValueError("starts holds one row number more than there are sequences, and tokens is not negative (and an int32)")
         for name, t, n in (("starts", starts, self.sequences + 1), ("slots", slots, self.sequences), ("resume", resume, self.sequences)):
             if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous()):
                 raise ValueError(f"{name} is a dense int32 tensor of {n} entries")

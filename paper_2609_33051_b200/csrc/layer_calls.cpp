@@ -90,9 +90,16 @@ at::ScalarType f32_or_bf16(const at::Tensor& t, const char* name) {
 }
 int code(at::ScalarType t) { return t == kBF16 ? SKETCHSSM_BF16 : SKETCHSSM_F32; }
 
+// An axis' size, which the C ABI takes as an int.
 int64_t size_of(const at::Tensor& t, int64_t dim, int64_t axes, const char* name) {
     if (t.dim() != axes) throw Bad(std::string(name) + " has " + std::to_string(axes) + " axes");
+    if (t.size(dim) > 0x7fffffff) throw Bad(std::string(name) + ": an axis is longer than 2^31 - 1");
     return t.size(dim);
+}
+int small(PyObject* o, const char* name) {
+    const long long v = number(o);
+    if (v < -0x7fffffffll || v > 0x7fffffffll) throw Bad(std::string(name) + " is out of range");
+    return (int)v;
 }
 
 // (function, context, device, B, H, K, V, io): the first eight arguments of every call
@@ -122,7 +129,7 @@ PyObject* call(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F&& f) {
 // prompts (address), T, x, weight, bias, state, out, flags, stream
 PyObject* causal_conv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(a, n, 9, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
-        const int64_t T = number(v[1]), C = size_of(tensor(v[3], "weight"), 0, 2, "weight"), W = tensor(v[3], "weight").size(1);
+        const int64_t T = number(v[1]), C = size_of(tensor(v[3], "weight"), 0, 2, "weight"), W = size_of(tensor(v[3], "weight"), 1, 2, "weight");
         const Rows x = rows(v[2], "x", l, l.io, {T, C}), out = rows(v[6], "out", l, l.io, {T, C});
         return reinterpret_cast<decltype(&sketchssm_causal_conv)>(address(fn))(
             l.ctx, static_cast<const sketchssm_prompts*>(address(v[0])), (int)C, (int)W, dense(v[3], "weight", l, kF32, {C, W}),
@@ -134,7 +141,7 @@ PyObject* causal_conv(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // x, dt, weight, bias, state, a, dt_bias, q, k, v, beta, decay, groups, stream
 PyObject* conv_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(a, n, 14, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
-        const int64_t G = number(v[12]), C = (int64_t)l.H * l.V + 2 * G * l.K, W = size_of(tensor(v[2], "weight"), 1, 2, "weight");
+        const int64_t G = small(v[12], "groups"), C = (int64_t)l.H * l.V + 2 * G * l.K, W = size_of(tensor(v[2], "weight"), 1, 2, "weight");
         const Rows x = rows(v[0], "x", l, l.io, {l.B, C}), dt = rows(v[1], "dt", l, l.io, {l.B, l.H});
         return reinterpret_cast<decltype(&sketchssm_conv_step)>(address(fn))(
             l.ctx, (int)G, (int)W, dense(v[2], "weight", l, kF32, {C, W}), dense(v[3], "bias", l, kF32, {C}),
@@ -171,18 +178,18 @@ PyObject* prompt_scan(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(a, n, 13, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
         const at::Tensor& xt = tensor(v[0], "x");
-        const int64_t T = size_of(xt, 0, 2, "x"), D = xt.size(1);
+        const int64_t T = size_of(xt, 0, 2, "x"), D = size_of(xt, 1, 2, "x");
         const at::ScalarType xd = f32_or_bf16(xt, "x");
         const Rows x = rows(v[0], "x", l, xd, {T, D}), none = {nullptr, 0};
         const Rows gate = v[7] == Py_None ? none : rows(v[7], "gate", l, l.io, {T, D}), skip = v[8] == Py_None ? none : rows(v[8], "skip", l, l.io, {T, D});
-        const int64_t heads = v[9] == Py_None ? 0 : tensor(v[9], "skip_weight").numel();
+        const int64_t heads = v[9] == Py_None ? 0 : size_of(tensor(v[9], "skip_weight"), 0, 1, "skip_weight");
         const double eps = PyFloat_AsDouble(v[10]);
         if (eps == -1.0 && PyErr_Occurred()) {
             PyErr_Clear();
             throw Bad("eps is no number");
         }
         return reinterpret_cast<decltype(&sketchssm_rms_norm)>(address(fn))(
-            l.ctx, (int)T, (int)D, (int)number(v[11]), (float)eps, x.p, x.stride, code(xd), dense(v[1], "weight", l, kF32, {D}),
+            l.ctx, (int)T, (int)D, small(v[11], "group"), (float)eps, x.p, x.stride, code(xd), dense(v[1], "weight", l, kF32, {D}),
             dense(v[5], "residual", l, l.io, {T, D}), dense(v[6], "residual_out", l, l.io, {T, D}), gate.p, gate.stride, skip.p, skip.stride,
             dense(v[9], "skip_weight", l, kF32, {heads}), (int)heads, dense(v[2], "out", l, l.io, {T, D}), dense(v[3], "out8", l, kE4M3, {T, D}),
             dense(v[4], "scale", l, kF32, {T, (D + 127) / 128}), address(v[12]));
@@ -192,7 +199,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // a, a_scale, w, w_scale, out, stream
 PyObject* scaled_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call(a, n, 6, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
-        const int64_t M = size_of(tensor(v[0], "a"), 0, 2, "a"), K = tensor(v[0], "a").size(1), N = size_of(tensor(v[2], "w"), 0, 2, "w"), kb = (K + 127) / 128;
+        const int64_t M = size_of(tensor(v[0], "a"), 0, 2, "a"), K = size_of(tensor(v[0], "a"), 1, 2, "a"), N = size_of(tensor(v[2], "w"), 0, 2, "w"), kb = (K + 127) / 128;
         const at::ScalarType od = f32_or_bf16(tensor(v[4], "out"), "out");
         const Rows out = rows(v[4], "out", l, od, {M, N});
         return reinterpret_cast<decltype(&sketchssm_scaled_matmul)>(address(fn))(

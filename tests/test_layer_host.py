@@ -191,3 +191,30 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         m.scaled_matmul(a, w, a, w, a, stream=Stream)
     m.close()
     assert m._norm[1] == 0                     # a closed layer's context is not handed on
+
+
+def test_the_binding_refuses_sizes_beyond_the_librarys_numbers():
+    """The library takes sizes as ints: longer axes are refused before they are cut (views of one element: nothing is allocated)."""
+    build.build()
+    m = binding.SketchSSM("mamba2", 2, 4, 128, 64, 8, 4, device=0, allocate=False)
+
+    class Stream:
+        cuda_stream = 0
+
+    long = 2 ** 32 + 4
+    w = torch.ones(16)
+    for t in (torch.bfloat16, torch.float32):
+        x = torch.zeros(1, dtype=t)
+        for size in ((long, 16), (3, long)):
+            with pytest.raises(ValueError, match="longer than"):
+                m.rms_norm(x.expand(*size), w, out=x, stream=Stream)
+    a = torch.zeros(1, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    for a_size, w_size in (((long, 16), (8, 16)), ((3, long), (8, long)), ((3, 16), (long, 16))):
+        with pytest.raises(ValueError, match="longer than"):
+            m.scaled_matmul(a.expand(*a_size), w, a.expand(*w_size), w, torch.zeros(3, 8), stream=Stream)
+    x = torch.zeros(3, 16, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="groups is out of range"):
+        m.conv_step(x, x, torch.ones(16, 4), None, x, w, None, {n: x for n in ("q", "k", "v", "beta", "decay")}, groups=2 ** 32 + 1, stream=Stream)
+    m.close()
+    with pytest.raises(ValueError, match="tokens"):
+        binding.Prompts(torch.tensor([0, 3], dtype=torch.int32), long)
