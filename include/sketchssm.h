@@ -354,7 +354,7 @@ int sketchssm_rms_norm(sketchssm_ctx* ctx, int rows, int width, int group, float
 
 /* Product of 8-bit matrices (e4m3) with a scale for each block of 128 along the inner axis, and of 128 x 128 for the weights:
  *     out[m][n] = sum_b a_scale[m][b] w_scale[n / 128][b] sum_{k in block b} a[m][k] w[n][k]
- *   rows >= 0, cols >= 1; inner >= 16, a multiple of 16; a [rows][inner], w [cols][inner] dense; a_scale [rows][(inner + 127) / 128],
+ *   rows >= 0, cols >= 1; inner >= 16, a multiple of 16 (each at most 2^30); a [rows][inner], w [cols][inner] dense; a_scale [rows][(inner + 127) / 128],
  *   w_scale [(cols + 127) / 128][(inner + 127) / 128] fp32 (4-byte aligned); out [rows][cols] of out_dtype, its stride at least cols, free of the 16-byte
  *   rule.  Products inside a block are summed in fp32 by the tensor cores, blocks in fp32. */
 int sketchssm_scaled_matmul(sketchssm_ctx* ctx, int rows, int cols, int inner, const void* a, const void* a_scale,

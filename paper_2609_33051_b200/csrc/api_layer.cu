@@ -181,7 +181,8 @@ int sketchssm_scaled_matmul(sketchssm_ctx* ctx, int rows, int cols, int inner, c
     int rc = begin_call(ctx);
     if (rc != SKETCHSSM_OK) return rc;
     if (rows < 0 || cols < 1 || inner < 1 || !dtype_ok(out_dtype)) return SKETCHSSM_INVALID_ARG;
-    if (inner % 16 != 0) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    // rows and columns are numbered in 32 bits, with room for a tile behind the last one
+    if (inner % 16 != 0 || rows > (1 << 30) || cols > (1 << 30) || inner > (1 << 30)) return SKETCHSSM_UNSUPPORTED_SHAPE;
     if (out_stride < cols) return SKETCHSSM_INVALID_ARG;
     if (!good(w) || w_scale == nullptr || !aligned_to(w_scale, 4)) return SKETCHSSM_INVALID_ARG;
     if (rows == 0) return SKETCHSSM_OK;

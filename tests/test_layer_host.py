@@ -148,6 +148,13 @@ def test_matmul_refusals(lib):
         assert matmul(lib, ctx, M=1, **bad) == INVALID, bad
 
 
+def test_matmul_refuses_rows_that_a_tile_could_number_past_32_bits(lib):
+    ctx = context(lib)
+    for bad in (dict(M=2 ** 30 + 1), dict(M=2 ** 31 - 1), dict(N=2 ** 30 + 1, os=2 ** 30 + 1), dict(K=2 ** 30 + 16)):
+        assert matmul(lib, ctx, **bad) == SHAPE, bad
+    assert matmul(lib, ctx, N=2 ** 30, os=2 ** 30) == OK and matmul(lib, ctx, K=2 ** 30) == OK
+
+
 def test_prompts_of_the_binding():
     i = lambda *v: torch.tensor(v, dtype=torch.int32)  # noqa: E731
     p = binding.Prompts(i(0, 3, 3, 9), 9, slots=i(2, 0, 1), resume=i(-1, 5, -1))
