@@ -6,22 +6,22 @@
 // A CTA (one per SM, persistent) takes two column blocks of one group at a time ("sets": two heads of 64 columns, or both halves of
 // one of 128), which share K, Q and the products Q K^T.
 //
-// Precision.  Q K^T is exact up to the fp32 sums.  The state is held in fp32 registers; W goes to the tensor cores in three bf16
-// parts, so that a term of S is off by less than 2^-22.  P below its diagonal, and S as an operand of Y, are rounded to bf16 once: the
-// outputs are rounded by as much behind them, so an output's error is sqrt(2) times that of its own rounding, at most.  The diagonal, a
-// token's own and mostly largest weight, stays in fp32 and goes with the skip (error in the square mean 1.9e-3, 2.3e-3 with the
-// diagonal in bf16, 1.7e-3 of the outputs' rounding alone; it costs one chunk 0.4 us of 13 and long prompts nothing).  Two parts of P as well
-// cost a pair of heads 16 more products of 128 x 64 x 16 a chunk, and a third as much arithmetic on CUDA cores as the rest of P.
-// Sums of decays run forward for c_t and backward for c_end - c_t, so that what is small is exact.
+// Precision.  Outputs are sums of fp32 accuracy, rounded once to bf16, and states are fp32.  Q K^T is exact up to the fp32 sums.  The
+// state is held in fp32 registers; W goes to the tensor cores in three bf16 parts, so that a term of S is off by less than 2^-22.  P below
+// its diagonal, and S as an operand of Y, go there in two parts, off by 2^-16 of a term at most, where an output's own rounding is 2^-8 of
+// their sum (in one part: outputs 1.3e-3 in the square mean from those of fp32 sums, now 5e-5; one prompt of 16384 tokens of 64 heads
+// 269 us then, 323 now).  The diagonal, a token's own weight beta, is no part of P: it goes with the skip, in fp32.
+// Sums of log2 decays run backward for c_end - c_t, so that what is small is exact; forward sums are kept as whole numbers, which are
+// exact, and a rest of up to 64 in size, so that c_t - c_s is off by less than 2^-14.7 whatever was decayed before s.
 //
-// What bounds it: a chunk of a pair of heads is about 8800 cycles, of which the tensor cores work 3100 and HBM would need 2800.  It is
-// 20,000 warp instructions, a third of them the three parts of W, issued at 2.3 a cycle; the chain from one state to the next (S as an
-// operand, Q S, W in four quarters, S) is about as long.  16384 tokens of 64 heads in one prompt: 269 us (1.05 TB/s), in
-// 48: 295 us (1.54 TB/s).
+// What bounds it: a chunk of a pair of heads is about 10,500 cycles, of which the tensor cores work 4100 and HBM would need 2800.  It is
+// 26,000 warp instructions (7000 on the scheduler of the longest rows of P), many of them of pipes that take one every other cycle, and
+// the chain Q K^T, P, P V is about as long: Q K^T of the next chunk waits for P V, as P's second parts lie in its columns.  16384
+// tokens of 64 heads in one prompt: 323 us (0.87 TB/s), in 48: 368 us (1.24 TB/s).
 // Roles: warp 3 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
 // warp 0 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
 // ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
-// Tensor memory: Q K^T 128 columns, Y 2 x 64, state products 2 x 64, P 2 x 64.
+// Tensor memory: Q K^T and then P's second parts 128 columns, Y 2 x 64, state products 2 x 64, P's first parts 2 x 64.
 //
 // Few sequences and heads: a sequence is split into segments.  A first launch (OUTPUTS = false) leaves every segment's own state and
 // decay in the scratch, a second one starts each segment from the sum of those before it.
@@ -35,18 +35,20 @@ using namespace tc;
 
 constexpr int kQ = 128;                                // tokens of a chunk
 constexpr uint32_t kTile = 16384u;                     // 128 rows of 128 bytes
-constexpr uint32_t kKOff = 0, kQOff = 4 * kTile, kVOff = 6 * kTile, kWOff = 10 * kTile;      // K in two buffers, Q in one, V in two
-constexpr uint32_t kWBuf = 24576u;                     // of a set: W of 32 tokens in three parts, twice, or S in one
-constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][5][128] floats: see gates
-constexpr uint32_t kGateSet = 5 * kQ, kGateBuf = 2 * kGateSet;
+constexpr uint32_t kKOff = 0, kQOff = 3 * kTile, kVOff = 5 * kTile, kWOff = 9 * kTile;       // K of 64 tokens in three buffers, Q in one, V in two
+constexpr uint32_t kKHalf = kTile / 2;                 // 64 of the 128 columns of such a K
+constexpr uint32_t kWBuf = 32768u;                     // of a set: S in two parts, or W of 32 tokens in three, twice
+constexpr uint32_t kGateOff = kWOff + 2 * kWBuf;       // [2 buffers][2 sets][6][128] floats and one more: see gates
+constexpr uint32_t kGateSet = 6 * kQ + 4, kGateBuf = 2 * kGateSet;
 constexpr uint32_t kBarOff = kGateOff + 2 * kGateBuf * 4;
 constexpr int kThreads = 896;
 
-enum { bFullK = 0, bEmptyK = 2, bFullQ = 4, bEmptyQ = 5, bFullV = 6, bEmptyV = 8, bGate = 10, bGateFree = 12, bDot = 14, bState = 15,
-       bInter = 16, bP = 17, bY = 19, bYFree = 21, bW = 22, bProd = 24, bVRead = 26, bScaled = 30, kBars = 32 };
+enum { bFullK = 0, bEmptyK = 3, bFullQ = 6, bEmptyQ = 7, bFullV = 8, bEmptyV = 10, bGate = 12, bGateFree = 14, bDot = 16, bState = 17,
+       bInter = 18, bP = 19, bY = 23, bYFree = 25, bW = 26, bProd = 28, bVRead = 30, bScaled = 34, kBars = 36 };
 constexpr uint32_t kMarkOff = kBarOff + kBars * 8u + 16u;       // [2 buffers][2 sets][65]: see mark_of
 constexpr uint32_t kMarks = 65;
-constexpr uint32_t kSmemTc = kMarkOff + 4u * kMarks * 4u + 1024u;
+constexpr uint32_t kOwnOff = kMarkOff + 4u * kMarks * 4u;       // [2 buffers][128]: <q_t, k_t>
+constexpr uint32_t kSmemTc = kOwnOff + 2u * kQ * 4u + 1024u;
 
 // columns of tensor memory
 constexpr uint32_t kDot = 0, kY = 128, kProd = 256, kP = 384;
@@ -102,6 +104,12 @@ __device__ __forceinline__ void tmem_st16u(uint32_t taddr, const uint32_t (&r)[1
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
 // The products take every value of a chunk into every row, and a zero weight times NaN or infinity is NaN: values that are not finite go
 // to the products as zeros, and a column's rows from the first of them on become NaN afterwards.  A mark of chunk n holds that row; the
 // largest of several is the first row of the latest chunk, so that marks need no clearing.  (The 65th: of any column.)
@@ -119,6 +127,17 @@ __device__ __forceinline__ uint32_t bf16x2(float a, float b) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t*>(&h);
 }
+// Two floats as two parts of bfloat16 each: what the first leaves, rounded, is the second.
+__device__ __forceinline__ void two_parts(uint64_t x, uint32_t& hi, uint32_t& lo) {
+    float a, b;
+    unpack2(x, a, b);
+    hi = bf16x2(a, b);
+    unpack2(fma2(pack2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), pack2(-1.f, -1.f), x), a, b);
+    lo = bf16x2(a, b);
+}
+// Buffer of K's half `half` (64 tokens) of chunk n, and its barriers' parity.
+__device__ __forceinline__ uint32_t k_slot(int n, int half) { return (uint32_t)(2 * n + half) % 3u; }
+__device__ __forceinline__ uint32_t k_phase(int n, int half) { return ((uint32_t)(2 * n + half) / 3u) & 1u; }
 
 template <bool OUTPUTS>
 __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __grid_constant__ ScanArgs g) {
@@ -139,8 +158,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             if (i >= bGateFree && i < bDot) n = OUTPUTS ? 24 : 16;
             if (i == bYFree) n = 8;                                             // the warps of both sets
             if (i == bState || i == bW || i == bW + 1) n = 16;
-            if (i >= bP && i < bY) n = 4;                                       // of one
-            if (i >= bVRead) n = 8;                                              // (B)
+            if (i >= bP && i < bY) n = 8;                                       // (A)
+            if (i >= bVRead) n = 8;                                              // (B) of one set
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -160,52 +179,56 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
     if (warp == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (lane == 0) {
+            int nk = 0, nv = 0, nq = 0;                 // copies issued: halves of K, V, Q
+            auto load_k = [&](const Unit& x, int t) {
+                const uint32_t slot = (uint32_t)nk % 3u;
+                ok = ok && (nk < 3 || mbar_wait_bounded(bar + bEmptyK + slot, ((uint32_t)nk / 3u - 1u) & 1u));
+                if (ok) {
+                    mbar_expect_tx(bar + bFullK + slot, kTile);
+                    tma_load(smem + kKOff + slot * kTile, &g.tk, x.group * 128, t, bar + bFullK + slot);
+                    tma_load(smem + kKOff + slot * kTile + kKHalf, &g.tk, x.group * 128 + 64, t, bar + bFullK + slot);
+                    ++nk;
+                }
+            };
             for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
                 const Unit x = decode_unit(g, u);
                 if (!unit_runs(x, OUTPUTS)) continue;
-                for (int t = x.t0; t < x.t1; t += kQ, ++n) {
-                    const int b = n & 1;
-                    ok = n < 2 || mbar_wait_bounded(bar + bEmptyK + b, (n / 2 - 1) & 1);
-                    if (ok) {
-                        mbar_expect_tx(bar + bFullK + b, 2 * kTile);
-                        tma_load(smem + kKOff + b * 2 * kTile, &g.tk, x.group * 128, t, bar + bFullK + b);
-                        tma_load(smem + kKOff + (b * 2 + 1) * kTile, &g.tk, x.group * 128 + 64, t, bar + bFullK + b);
-                    }
-                    ok = ok && (n < 2 || mbar_wait_bounded(bar + bEmptyV + b, (n / 2 - 1) & 1));
+                for (int t = x.t0; t < x.t1 && ok; t += kQ) {
+                    load_k(x, t);
+                    const int b = nv & 1;
+                    ok = ok && (nv < 2 || mbar_wait_bounded(bar + bEmptyV + b, (nv / 2 - 1) & 1));
                     if (ok) {
                         mbar_expect_tx(bar + bFullV + b, 2 * kTile);
                         tma_load(smem + kVOff + b * 2 * kTile, &g.tv, x.block0 * 64, t, bar + bFullV + b);
                         tma_load(smem + kVOff + (b * 2 + 1) * kTile, &g.tv, (x.block0 + x.live1) * 64, t, bar + bFullV + b);
+                        ++nv;
                     }
                     if constexpr (OUTPUTS) {
-                        ok = ok && (n < 1 || mbar_wait_bounded(bar + bEmptyQ, (n - 1) & 1));
+                        ok = ok && (nq < 1 || mbar_wait_bounded(bar + bEmptyQ, (nq - 1) & 1));
                         if (ok) {
                             mbar_expect_tx(bar + bFullQ, 2 * kTile);
                             tma_load(smem + kQOff, &g.tq, x.group * 128, t, bar + bFullQ);
                             tma_load(smem + kQOff + kTile, &g.tq, x.group * 128 + 64, t, bar + bFullQ);
+                            ++nq;
                         }
                     }
-                    if (!ok) {
-                        record_fault(p.status, kFaultScanWait, 1);
-                        break;
-                    }
+                    load_k(x, t + 64);                  // (last: its buffer is free when half of the chunk before has gone to the state)
                 }
             }
+            if (!ok) record_fault(p.status, kFaultScanWait, 1);
             // Before the CTA ends the copies under way have ended (after a fault; otherwise they have been waited for), and the products'
             // last arrivals at the buffers' barriers are in.
-            for (int i = max(0, n - 2); i < n; ++i) {
-                if (!ok) mbar_wait_bounded(bar + bFullK + (i & 1), (i / 2) & 1, 1u << 16);
-                if (!ok) mbar_wait_bounded(bar + bFullV + (i & 1), (i / 2) & 1, 1u << 16);
-                if (ok) mbar_wait_bounded(bar + bEmptyK + (i & 1), (i / 2) & 1);
-            }
-            if (OUTPUTS && n > 0) mbar_wait_bounded(bar + (ok ? bEmptyQ : bFullQ), (n - 1) & 1, 1u << 16);
+            for (int i = max(0, nk - 3); i < nk; ++i)
+                mbar_wait_bounded(bar + (ok ? bEmptyK : bFullK) + i % 3, (i / 3) & 1, ok ? 1u << 22 : 1u << 16);
+            for (int i = max(0, nv - 2); i < nv && !ok; ++i) mbar_wait_bounded(bar + bFullV + (i & 1), (i / 2) & 1, 1u << 16);
+            if (nq > 0) mbar_wait_bounded(bar + (ok ? bEmptyQ : bFullQ), (nq - 1) & 1, 1u << 16);
         }
         __syncwarp();
     } else if (warp == 1) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if constexpr (OUTPUTS) {
             constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
-            constexpr uint32_t kDotDesc = kTypes | ((128u >> 3) << 17), kInterDesc = kDotDesc | (1u << 16);
+            constexpr uint32_t kDotDesc = kTypes | ((64u >> 3) << 17), kInterDesc = kTypes | (1u << 16) | ((128u >> 3) << 17);
             constexpr uint32_t kPDesc = kTypes | (1u << 16) | ((64u >> 3) << 17);
             const uint64_t dq = swizzled_desc(sbase + kQOff, 16u, 1024u), ds = swizzled_desc(sbase + kWOff, kWBuf, 1024u);
             int m = 0;                                  // chunks with a state before them
@@ -216,16 +239,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 for (int t = x.t0; t < x.t1; t += kQ, ++n) {
                     const int b = n & 1;
                     const bool fresh = fresh0 && t == x.t0;                     // S is zero
-                    ok = warp_wait(bar + bFullK + b, (n / 2) & 1) && warp_wait(bar + bFullQ, n & 1);
-                    if (!ok) break;                                             // (P of the chunk before is made: its Q K^T has been read)
-                    tc_fence_after();
-                    const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, 16u, 1024u);
+                    // (P of the chunk before is made and used: its Q K^T, and the second parts of P in that one's place, are needed no more)
+                    ok = (n < 1 || (warp_wait(bar + bY, (n - 1) & 1) && warp_wait(bar + bY + 1, (n - 1) & 1))) && warp_wait(bar + bFullQ, n & 1);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t step = (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u;
-                        if (elect()) mma_ss(tmem + kDot, dq + step, dk + step, kDotDesc, i > 0);
+                    for (int half = 0; half < 2; ++half) {                      // 64 tokens of K, 64 columns
+                        const uint32_t slot = k_slot(n, half);
+                        ok = ok && warp_wait(bar + bFullK + slot, k_phase(n, half));
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t dk = swizzled_desc(sbase + kKOff + slot * kTile, 16u, 1024u);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const uint32_t in = (uint32_t)(i % 4) * 2u;
+                            if (elect())
+                                mma_ss(tmem + kDot + half * 64, dq + (uint32_t)(i / 4) * (kTile >> 4) + in, dk + (uint32_t)(i / 4) * (kKHalf >> 4) + in, kDotDesc, i > 0);
+                        }
+                        if (elect()) tc_commit(bar + bEmptyK + slot);
+                        __syncwarp();
                     }
-                    if (elect()) { tc_commit(bar + bDot); tc_commit(bar + bEmptyK + b); }
+                    if (!ok) break;
+                    if (elect()) tc_commit(bar + bDot);
                     __syncwarp();
                     ok = n < 1 || warp_wait(bar + bYFree, (n - 1) & 1);
                     if (!fresh) {
@@ -234,26 +267,31 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         ++m;
                         tc_fence_after();
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
+                        for (int i = 0; i < 16; ++i)                             // S in two parts
                             if (elect())
-                                mma_ss(tmem + kY, dq + (uint32_t)(i / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u, ds + (uint32_t)i * 128u, kInterDesc, i > 0);
+                                mma_ss(tmem + kY, dq + (uint32_t)(i % 8 / 4) * (kTile >> 4) + (uint32_t)(i % 4) * 2u,
+                                       ds + (uint32_t)(i / 8) * (kTile >> 4) + (uint32_t)(i % 8) * 128u, kInterDesc, i > 0);
                         if (elect()) tc_commit(bar + bInter);
                     }
                     if (elect()) tc_commit(bar + bEmptyQ);
                     __syncwarp();
                     ok = ok && warp_wait(bar + bFullV + b, (n / 2) & 1);
+                    const uint64_t dv = swizzled_desc(sbase + kVOff + b * 2 * kTile, 16u, 1024u);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        ok = ok && warp_wait(bar + bP + j, n & 1) && (fresh || warp_wait(bar + bScaled + j, (m - 1) & 1));
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint64_t dv = swizzled_desc(sbase + kVOff + (b * 2 + j) * kTile, 16u, 1024u);
-                        if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64, dv, kPDesc, !fresh);
+                    for (int c = 0; c < 4; ++c) {                               // 32 columns of P at a time, as they are made
 #pragma unroll
-                        for (int i = 1; i < 8; ++i)
-                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + i * 8, dv + (uint32_t)i * 128u, kPDesc, true);
-                        if (elect()) tc_commit(bar + bY + j);
-                        __syncwarp();
+                        for (int j = 0; j < 2; ++j) {
+                            ok = ok && (j > 0 || warp_wait(bar + bP + c, n & 1)) && (fresh || c > 0 || warp_wait(bar + bScaled + j, (m - 1) & 1));
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint64_t v = dv + (uint32_t)j * (kTile >> 4) + (uint32_t)c * 256u;
+                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + c * 16, v, kPDesc, c > 0 || !fresh);
+                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kP + j * 64 + c * 16 + 8, v + 128u, kPDesc, true);
+                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kDot + c * 32 + j * 16, v, kPDesc, true);
+                            if (elect()) mma_ts(tmem + kY + j * 64, tmem + kDot + c * 32 + j * 16 + 8, v + 128u, kPDesc, true);
+                            if (c == 3 && elect()) tc_commit(bar + bY + j);
+                            __syncwarp();
+                        }
                     }
                     if (!ok) break;
                 }
@@ -269,24 +307,36 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             const Unit x = decode_unit(g, u);
             if (!unit_runs(x, OUTPUTS)) continue;
             for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
-                const int b = n & 1;
-                ok = warp_wait(bar + bFullK + b, (n / 2) & 1);
-                const uint64_t dk = swizzled_desc(sbase + kKOff + b * 2 * kTile, kTile, 1024u);
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {                                   // 32 tokens at a time, both sets' columns
+                    const uint32_t slot = k_slot(n, h >> 1);
+                    if ((h & 1) == 0) {
+                        ok = ok && warp_wait(bar + bFullK + slot, k_phase(n, h >> 1));
+                        const int valid = max(0, x.t1 - t - h * 32);
+                        if (ok && valid < 64) {          // rows of the next sequence are no part of this one
+                            for (int r = valid + lane / 8; r < 64; r += 4) {
+                                unsigned char* k = smem + kKOff + slot * kTile + r * 128 + lane % 8 * 16;
+                                *reinterpret_cast<uint4*>(k) = *reinterpret_cast<uint4*>(k + kKHalf) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                            proxy_fence();
+                            __syncwarp();
+                        }
+                    }
                     ok = ok && warp_wait(bar + bW + (h & 1), h >> 1);
                     if (!ok) break;
                     tc_fence_after();
+                    const uint64_t dk = swizzled_desc(sbase + kKOff + slot * kTile, kKHalf, 1024u);
 #pragma unroll
                     for (int i = 0; i < 6; ++i)
                         if (elect())
-                            mma_ss(tmem + kProd, dk + (uint32_t)(h * 2 + i % 2) * 128u, dw + (uint32_t)(h & 1) * 768u + (uint32_t)(i / 2) * 256u + (uint32_t)(i % 2) * 128u,
+                            mma_ss(tmem + kProd, dk + (uint32_t)((h & 1) * 2 + i % 2) * 128u, dw + (uint32_t)(h & 1) * 768u + (uint32_t)(i / 2) * 256u + (uint32_t)(i % 2) * 128u,
                                    kDesc, i > 0 || h > 0);
-                    if (elect()) tc_commit(bar + bProd + (h & 1));
+                    if (elect()) {
+                        tc_commit(bar + bProd + (h & 1));
+                        if (h & 1) tc_commit(bar + bEmptyK + slot);
+                    }
                     __syncwarp();
                 }
-                if (ok && elect()) tc_commit(bar + bEmptyK + b);
-                __syncwarp();
             }
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 3);
@@ -323,48 +373,70 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 if (!ok) break;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float l[4], pre[4], suf[4];
-                    // (2^-160 is zero in fp32; the bound keeps the sums finite, and a difference of two exact to 2^-10; NaN passes it)
+                    // (2^-160 is zero in fp32; the bound keeps the sums finite; NaN passes it)
+                    float l[4], suf[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float x2 = a2[j] * beta[j][i];
                         l[i] = t + lane * 4 + i < x.t1 ? (x2 < -160.f ? -160.f : x2) : 0.f;
                     }
-                    pre[0] = l[0];
-#pragma unroll
-                    for (int i = 1; i < 4; ++i) pre[i] = pre[i - 1] + l[i];
                     suf[3] = 0.f;
 #pragma unroll
                     for (int i = 2; i >= 0; --i) suf[i] = suf[i + 1] + l[i + 1];
-                    const float all = pre[3];
-                    float before = all, after = all;
+                    float after = suf[0] + l[0];
 #pragma unroll
                     for (int o = 1; o < 32; o <<= 1) {
-                        const float up = __shfl_up_sync(0xffffffffu, before, o), down = __shfl_down_sync(0xffffffffu, after, o);
-                        if (lane >= o) before += up;
+                        const float down = __shfl_down_sync(0xffffffffu, after, o);
                         if (lane + o < 32) after += down;
                     }
-                    before = __shfl_up_sync(0xffffffffu, before, 1);
+                    const float all = after;             // (in lane 0: of the chunk)
                     after = __shfl_down_sync(0xffffffffu, after, 1);
-                    if (lane == 0) before = 0.f;
                     if (lane == 31) after = 0.f;
-                    float c[4], lb[4], w[4], e[4], f[4];
+                    float w[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) c[i] = before + pre[i];
-                    const float end = __shfl_sync(0xffffffffu, c[3], lane | 7);
+                    for (int i = 0; i < 4; ++i) w[i] = beta[j][i] * exp2f(after + suf[i]);
+                    float* set = gates + b * kGateBuf + j * kGateSet;
+                    float4* o = reinterpret_cast<float4*>(set) + lane;
+                    o[0] = make_float4(w[0], w[1], w[2], w[3]);                  // beta 2^(c at the chunk's end - c)
+                    if (lane == 0) set[6 * kQ] = exp2f(all);                     // 2^(c at the chunk's end)
+                    if constexpr (OUTPUTS) {
+                        // Forward sums of whole numbers and of what is left, at most a half each: the first are exact, the second at most 64
+                        // in size, so that a difference of two sums is that of the tokens between them, whatever stands before them.
+                        float whole[4], part[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        lb[i] = __log2f(beta[j][i]) - c[i];
-                        w[i] = beta[j][i] * exp2f(after + suf[i]);
-                        e[i] = exp2f(c[i]);
-                        f[i] = beta[j][i] * ex2(end - c[i]);
+                        for (int i = 0; i < 4; ++i) {
+                            const float r = rintf(l[i]);
+                            whole[i] = i > 0 ? whole[i - 1] + r : r;
+                            part[i] = i > 0 ? part[i - 1] + (l[i] - r) : l[i] - r;
+                        }
+                        float whole0 = whole[3], part0 = part[3];
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) {
+                            const float up = __shfl_up_sync(0xffffffffu, whole0, o), up2 = __shfl_up_sync(0xffffffffu, part0, o);
+                            if (lane >= o) { whole0 += up; part0 += up2; }
+                        }
+                        whole0 = __shfl_up_sync(0xffffffffu, whole0, 1);
+                        part0 = __shfl_up_sync(0xffffffffu, part0, 1);
+                        if (lane == 0) whole0 = part0 = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            whole[i] += whole0;
+                            part[i] += part0;
+                        }
+                        const float end = __shfl_sync(0xffffffffu, whole[3], lane | 7), end2 = __shfl_sync(0xffffffffu, part[3], lane | 7);
+                        float e[4], f[4], own[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            e[i] = exp2f(whole[i] + part[i]);
+                            f[i] = beta[j][i] * ex2((end - whole[i]) + (end2 - part[i]));
+                            own[i] = beta[j][i] + (l[i] - l[i]);                 // (NaN where the decay is: it would reach a state of zeros too)
+                        }
+                        o[32] = make_float4(e[0], e[1], e[2], e[3]);             // 2^c
+                        o[64] = make_float4(whole[0], whole[1], whole[2], whole[3]);     // c, whole numbers
+                        o[96] = make_float4(part[0], part[1], part[2], part[3]);         // c, the rest
+                        o[128] = make_float4(f[0], f[1], f[2], f[3]);            // beta 2^(c at the end of the 32 tokens - c)
+                        o[160] = make_float4(own[0], own[1], own[2], own[3]);    // beta
                     }
-                    float4* o = reinterpret_cast<float4*>(gates + b * kGateBuf + j * kGateSet) + lane;
-                    o[0] = make_float4(c[0], c[1], c[2], c[3]);                  // c
-                    o[32] = make_float4(lb[0], lb[1], lb[2], lb[3]);             // log2(beta) - c
-                    o[64] = make_float4(w[0], w[1], w[2], w[3]);                 // beta 2^(c at the chunk's end - c)
-                    o[96] = make_float4(e[0], e[1], e[2], e[3]);                 // 2^c
-                    o[128] = make_float4(f[0], f[1], f[2], f[3]);                // beta 2^(c at the end of the 32 tokens - c)
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive_one(bar + bGate + b);
@@ -377,13 +449,13 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
             asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
             const int j = (warp - 4) >> 2, quad = warp & 3, row = quad * 32 + lane;
             const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-            const uint32_t tp = tmem + lanes + kP + j * 64, td = tmem + lanes + kDot, ty = tmem + lanes + kY + j * 64;
+            const uint32_t tp = tmem + lanes + kP, td = tmem + lanes + kDot, ty = tmem + lanes + kY + j * 64;
             {
                 uint32_t z[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[i] = 0u;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_st16u(tp + c * 16, z);          // above the diagonal P stays zero
+                for (int c = 0; c < 4; ++c) tmem_st16u(tp + j * 64 + c * 16, z);  // above the diagonal P stays zero
                 tmem_st_wait();
             }
             for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
@@ -415,63 +487,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bDot, n & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    // P: below the diagonal's 32 x 32 blocks its weight is 2^(c_t - c at the end of the columns' 32) times a factor of
-                    // the column, both at most 1 (but for beta); in them it is one exponential an element
-                    const float ct = gt[row];
-                    float own;
-                    uint32_t d[32], f[16];
-                    tmem_ld32_async(td, d);
-#pragma unroll 1
-                    for (int c = 0; c < quad; ++c) {
-                        const float r = ex2(ct - gt[c * 32 + 31]);
-                        const uint64_t r2 = pack2(r, r);
-                        const ulonglong2* f4 = reinterpret_cast<const ulonglong2*>(gt + 4 * kQ + c * 32);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const ulonglong2 w = f4[i];
-                            float x0, x1, x2, x3;
-                            unpack2(mul2(pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), mul2(r2, w.x)), x0, x1);
-                            unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), mul2(r2, w.y)), x2, x3);
-                            f[2 * i] = bf16x2(x0, x1);
-                            f[2 * i + 1] = bf16x2(x2, x3);
-                        }
-                        tmem_ld32_async(td + (c + 1) * 32, d);
-                        tmem_st16u(tp + c * 16, f);
-                    }
-                    {
-                        const uint64_t ct2 = pack2(ct, ct);
-                        const ulonglong2* e4 = reinterpret_cast<const ulonglong2*>(gt + kQ + quad * 32);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const ulonglong2 e = e4[i];
-                            float x0, x1, x2, x3;
-                            unpack2(add2(ct2, e.x), x0, x1);
-                            unpack2(add2(ct2, e.y), x2, x3);
-                            unpack2(mul2(pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), pack2(ex2(x0), ex2(x1))), x0, x1);
-                            unpack2(mul2(pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), pack2(ex2(x2), ex2(x3))), x2, x3);
-                            f[2 * i] = bf16x2(x0, x1);
-                            f[2 * i + 1] = bf16x2(x2, x3);
-                            d[4 * i] = __float_as_uint(x0);
-                            d[4 * i + 1] = __float_as_uint(x1);
-                            d[4 * i + 2] = __float_as_uint(x2);
-                            d[4 * i + 3] = __float_as_uint(x3);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {           // column 2 i + e of the 32 is there up to the row before `lane`
-                            if (lane <= 2 * i) f[i] = 0u;
-                            if (lane == 2 * i + 1) f[i] &= 0xffffu;
-                        }
-                        // the token's own weight stays in fp32: it goes with the skip
-#pragma unroll
-                        for (int s = 16; s > 0; s >>= 1) {
-#pragma unroll
-                            for (int i = 0; i < s; ++i) d[i] = (lane & s) ? d[i + s] : d[i];
-                        }
-                        own = __uint_as_float(d[0]);
-                        tmem_st16u(tp + quad * 16, f);
-                    }
                     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kMarkOff) + (b * 2 + j) * kMarks;
                     if (__any_sync(0xffffffffu, odd_row)) {
                         ok = warp_wait(bar + bVRead + j * 2 + b, (n / 2) & 1);       // (the state takes the values as they are)
@@ -489,13 +504,101 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                         }
                         proxy_fence();
                     }
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive_one(bar + bP + j);
-                        mbar_arrive_one(bar + bGateFree + b);
+                    // P: below the diagonal's 32 x 32 blocks its weight is 2^(c_t - c at the end of the columns' 32) times a factor of
+                    // the column, both at most 1 (but for beta); in them it is one exponential an element.  A block is one warp's, for both
+                    // sets (set 0's warps take those below the diagonal, set 1's those on it), so that the second parts can take the place of
+                    // the Q K^T that they are made of, 16 columns a set.
+                    auto made = [&](int c0, int c1) {    // this warp's part in blocks c0 .. c1 - 1, and its row of V, are there
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0)
+                            for (int c = c0; c < c1; ++c) mbar_arrive_one(bar + bP + c);
+                    };
+                    const float beta = gt[5 * kQ + row];
+                    const float* g2 = gates + b * kGateBuf;
+                    uint32_t d[32], f[8], f2[8];
+                    if (j == 0) {
+#pragma unroll 1
+                        for (int c = quad + 1; c < 4; ++c) {
+                            uint32_t z[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) z[i] = 0u;
+                            tmem_st16u(td + c * 32, z);          // (the second parts above the diagonal)
+                            tmem_st16u(td + c * 32 + 16, z);
+                        }
+                        made(quad, 4);
+                        if (quad > 0) tmem_ld32_async(td, d);
+#pragma unroll 1
+                        for (int c = 0; c < quad; ++c) {
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {                        // sets
+                                const float* g1 = g2 + q * kGateSet;
+                                const float r = ex2((g1[2 * kQ + row] - g1[2 * kQ + c * 32 + 31]) + (g1[3 * kQ + row] - g1[3 * kQ + c * 32 + 31]));
+                                const uint64_t r2 = pack2(r, r);
+                                const ulonglong2* f4 = reinterpret_cast<const ulonglong2*>(g1 + 4 * kQ + c * 32);
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const ulonglong2 w = f4[4 * h + i];
+                                        const uint32_t* u = d + 16 * h + 4 * i;
+                                        two_parts(mul2(pack2(__uint_as_float(u[0]), __uint_as_float(u[1])), mul2(r2, w.x)), f[2 * i], f2[2 * i]);
+                                        two_parts(mul2(pack2(__uint_as_float(u[2]), __uint_as_float(u[3])), mul2(r2, w.y)), f[2 * i + 1], f2[2 * i + 1]);
+                                    }
+                                    tmem_st8u(tp + q * 64 + c * 16 + h * 8, f);
+                                    tmem_st8u(td + c * 32 + q * 16 + h * 8, f2);
+                                }
+                            }
+                            if (c + 1 < quad) tmem_ld32_async(td + (c + 1) * 32, d);
+                            made(c, c + 1);
+                        }
+                    } else {
+                        tmem_ld32_async(td + quad * 32, d);
+                        made(0, quad);
+                        made(quad + 1, 4);
+                        tmem_ld_wait();
+                        {
+                            uint32_t o[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = (lane & 16) ? d[i + 16] : d[i];
+#pragma unroll
+                            for (int s = 8; s > 0; s >>= 1) {
+#pragma unroll
+                                for (int i = 0; i < s; ++i) o[i] = (lane & s) ? o[i + s] : o[i];
+                            }
+                            reinterpret_cast<uint32_t*>(smem + kOwnOff)[b * kQ + row] = o[0];
+                        }
+                        const uint64_t minus = pack2(-1.f, -1.f);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {                            // sets
+                            const float* g1 = g2 + q * kGateSet + 2 * kQ;
+                            const uint64_t ct = pack2(g1[row], g1[row]), part = pack2(g1[kQ + row], g1[kQ + row]);
+                            const ulonglong2* c4 = reinterpret_cast<const ulonglong2*>(g1 + quad * 32);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const ulonglong2 a = c4[4 * h + i], a2 = c4[32 + 4 * h + i], bt = c4[96 + 4 * h + i];
+                                    const uint32_t* u = d + 16 * h + 4 * i;
+                                    float x0, x1, x2, x3;
+                                    unpack2(add2(fma2(a.x, minus, ct), fma2(a2.x, minus, part)), x0, x1);
+                                    unpack2(add2(fma2(a.y, minus, ct), fma2(a2.y, minus, part)), x2, x3);
+                                    unpack2(mul2(mul2(pack2(__uint_as_float(u[0]), __uint_as_float(u[1])), bt.x), pack2(ex2(x0), ex2(x1))), x0, x1);
+                                    unpack2(mul2(mul2(pack2(__uint_as_float(u[2]), __uint_as_float(u[3])), bt.y), pack2(ex2(x2), ex2(x3))), x2, x3);
+                                    const int e = 16 * h + 4 * i;        // column e of the 32 is there up to the row before `lane`
+                                    two_parts(pack2(lane > e ? x0 : 0.f, lane > e + 1 ? x1 : 0.f), f[2 * i], f2[2 * i]);
+                                    two_parts(pack2(lane > e + 2 ? x2 : 0.f, lane > e + 3 ? x3 : 0.f), f[2 * i + 1], f2[2 * i + 1]);
+                                }
+                                tmem_st8u(tp + q * 64 + quad * 16 + h * 8, f);
+                                tmem_st8u(td + quad * 32 + q * 16 + h * 8, f2);
+                            }
+                        }
+                        made(quad, quad + 1);
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bGateFree + b);
                     // Y: what the products left, and the skip; v's row becomes y's, then the warp stores its rows
                     ok = ok && warp_wait(bar + bY + j, n & 1) && warp_wait(bar + bVRead + j * 2 + b, (n / 2) & 1);
                     if (!ok) break;
@@ -506,24 +609,30 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     tmem_ld_wait();
                     tc_fence_before();
                     __syncwarp();
+                    const float own = reinterpret_cast<const volatile float*>(smem + kOwnOff)[b * kQ + row] * beta;
+                    __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bYFree);
                     const bool nan_here = reinterpret_cast<const volatile uint32_t*>(marks)[64] >= mark_of(n, row);
                     const uint64_t skip2 = pack2(skip + own, skip + own);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        uint4* at = reinterpret_cast<uint4*>(mine + ((c ^ (row & 7)) * 16));
-                        const uint4 u = *at;
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                        uint32_t z[4];
+                    for (int c0 = 0; c0 < 8; c0 += 4) {
+                        uint4 u[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = c % 4 * 8 + 2 * i;
-                            float lo, hi;
-                            unpack2(fma2(skip2, pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)),
-                                         pack2(__uint_as_float(o[c / 4][e]), __uint_as_float(o[c / 4][e + 1]))), lo, hi);
-                            z[i] = bf16x2(lo, hi);
+                        for (int c = 0; c < 4; ++c) u[c] = *reinterpret_cast<const uint4*>(mine + (((c0 + c) ^ (row & 7)) * 16));
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t w[4] = {u[c].x, u[c].y, u[c].z, u[c].w};
+                            uint32_t z[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int e = (c0 + c) % 4 * 8 + 2 * i;
+                                float lo, hi;
+                                unpack2(fma2(skip2, pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)),
+                                             pack2(__uint_as_float(o[(c0 + c) / 4][e]), __uint_as_float(o[(c0 + c) / 4][e + 1]))), lo, hi);
+                                z[i] = bf16x2(lo, hi);
+                            }
+                            *reinterpret_cast<uint4*>(mine + (((c0 + c) ^ (row & 7)) * 16)) = make_uint4(z[0], z[1], z[2], z[3]);
                         }
-                        *at = make_uint4(z[0], z[1], z[2], z[3]);
                     }
                     if (nan_here) {
 #pragma unroll 1
@@ -624,32 +733,26 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                 if (OUTPUTS && !fresh) {                 // S as an operand: row n of 64 columns
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        float f[8];
+                        uint32_t hi[4], lo[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) unpack2(S[c * 4 + i], f[2 * i], f[2 * i + 1]);
-                        *reinterpret_cast<uint4*>(buf + row * 128 + (((half * 4 + c) ^ (row & 7)) * 16)) = Vec16<__nv_bfloat16>::pack(f);
+                        for (int i = 0; i < 4; ++i) two_parts(S[c * 4 + i], hi[i], lo[i]);
+                        unsigned char* to = buf + row * 128 + (((half * 4 + c) ^ (row & 7)) * 16);
+                        *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *reinterpret_cast<uint4*>(to + kTile) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                     }
                     proxy_fence();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bState);
                 }
-                ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bFullV + b, (n / 2) & 1) && warp_wait(bar + bFullK + b, (n / 2) & 1);
+                ok = warp_wait(bar + bGate + b, (n / 2) & 1) && warp_wait(bar + bFullV + b, (n / 2) & 1);
                 if (!ok) break;
-                if (valid < kQ && j == 0 && half == 0 && row >= valid) {                      // rows of the next sequence are no part of this one
-                    unsigned char* k = smem + kKOff + b * 2 * kTile + row * 128;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        reinterpret_cast<uint4*>(k)[i] = make_uint4(0u, 0u, 0u, 0u);
-                        reinterpret_cast<uint4*>(k + kTile)[i] = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                }
                 if (OUTPUTS && !fresh) {                 // Q S is there (and the buffer's S has been read): its rows times 2^c
                     ok = warp_wait(bar + bInter, m & 1);
                     ++m;
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t ty = tmem + lanes + kY + j * 64 + half * 32;
-                    const float ec = gates[b * kGateBuf + j * kGateSet + 3 * kQ + row];
+                    const float ec = gates[b * kGateBuf + j * kGateSet + kQ + row];
                     const uint64_t ec2 = pack2(ec, ec);
                     uint32_t d[16];
 #pragma unroll 1
@@ -669,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bScaled + j);
                 }
-                const float* w = gates + b * kGateBuf + j * kGateSet + 2 * kQ;
+                const float* w = gates + b * kGateBuf + j * kGateSet;
                 const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll 1
                 for (int h = 0; h < 4; ++h) {
@@ -713,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                     }
                 }
                 if (!ok) break;
-                const float keep = ex2(gates[b * kGateBuf + j * kGateSet + kQ - 1]);
+                const float keep = w[6 * kQ];
                 total *= keep;
                 ok = warp_wait(bar + bProd + 1, 1);
                 if (!ok) break;
@@ -774,7 +877,7 @@ int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_
     if (units > (1 << 30)) return SKETCHSSM_UNSUPPORTED_SHAPE;
     g.units = (int)units;
     if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
-        !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ) ||
+        !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ / 2) ||
         !make_map(&g.tv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.v, (uint64_t)p.H * p.V, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2, kQ)) {
         ctx->last_cuda_error = cudaErrorInvalidValue;
         return SKETCHSSM_CUDA_ERROR;
