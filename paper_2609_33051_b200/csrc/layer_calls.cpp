@@ -47,12 +47,19 @@ bool same(const at::Tensor& t, at::ScalarType type, std::initializer_list<int64_
     return t.scalar_type() == type && t.is_cuda() && t.get_device() == device && t.sizes().equals(at::IntArrayRef(size.begin(), size.size()));
 }
 
+// A tensor's address; where it has no elements some address that is not null, as the C ABI takes a null pointer for an absent tensor
+// (and reads or writes none of it).
+void* place(const at::Tensor& t) {
+    alignas(16) static char nothing[16];
+    return t.numel() > 0 ? t.data_ptr() : nothing;
+}
+
 // A dense tensor's address (None: a null pointer).
 void* dense(PyObject* o, const char* name, const Layer& l, at::ScalarType type, std::initializer_list<int64_t> size) {
     if (o == Py_None) return nullptr;
     const at::Tensor& t = tensor(o, name);
     if (!same(t, type, size, l.device) || !t.is_contiguous()) refuse(name, "dense ", type, size.begin(), size.size(), l.device, t);
-    return t.data_ptr();
+    return place(t);
 }
 
 struct Rows {
@@ -69,7 +76,7 @@ Rows rows(PyObject* o, const char* name, const Layer& l, at::ScalarType type, st
         if (t.size(d) != 1 && t.stride(d) != row) throw Bad(std::string(name) + ": the elements of a row are dense");
         row *= t.size(d);
     }
-    return {t.data_ptr(), t.size(0) > 1 ? t.stride(0) : row};
+    return {place(t), t.size(0) > 1 ? t.stride(0) : row};
 }
 
 long long number(PyObject* o) {
