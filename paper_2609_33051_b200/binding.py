@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
-import importlib
+import importlib.util
 import os
 from typing import Optional
 
@@ -148,10 +148,22 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             getattr(lib, name).restype = ctypes.c_int
     if path == _build.LIB_PATH:
         _LIB = lib
+    return lib
+
+
+def _calls():
+    """The extension module, loaded with the first call that needs it: the decode calls do without."""
     global _CALLS
     if _CALLS is None:
-        _CALLS = importlib.import_module("._layer_calls", __package__)
-    return lib
+        path = _build.calls_path()
+        if not os.path.exists(path):
+            raise FileNotFoundError(
+                f"{path} not found: build it with `python -m paper_2609_33051_b200.build` (needs a C++ compiler and torch's headers)")
+        spec = importlib.util.spec_from_file_location(__package__ + "._layer_calls", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _CALLS = module
+    return _CALLS
 
 
 _RAW_STREAM, _DEVICE = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
@@ -348,7 +360,7 @@ class SketchSSM:
         f32 or None, state [B, W - 1, C] holds the stored rows and is moved on."""
         if not prompts.on(self.device):
             raise ValueError("prompts lie on the layer's device")
-        rc = _CALLS.causal_conv(*self._conv, prompts.address, prompts.tokens, x, weight, bias, state, out, SILU if silu else 0,
+        rc = (_CALLS or _calls()).causal_conv(*self._conv, prompts.address, prompts.tokens, x, weight, bias, state, out, SILU if silu else 0,
                                 self._stream(stream))
         if rc:
             self._check("sketchssm_causal_conv", rc)
@@ -359,7 +371,7 @@ class SketchSSM:
                   stream=None) -> dict:
         """sketchssm_conv_step: one token of every batch entry, x [B, H V + 2 G K] and dt [B, H], into the q, k, v, beta, decay of
         `token` (new_token_buffers), which the decode calls take."""
-        rc = _CALLS.conv_step(*self._step, x, dt, weight, bias, state, a, dt_bias, token["q"], token["k"], token["v"], token["beta"],
+        rc = (_CALLS or _calls()).conv_step(*self._step, x, dt, weight, bias, state, a, dt_bias, token["q"], token["k"], token["v"], token["beta"],
                               token["decay"], groups, self._stream(stream))
         if rc:
             self._check("sketchssm_conv_step", rc)
@@ -381,7 +393,7 @@ class SketchSSM:
         if work is None:
             with on_stream(stream):
                 work = self.new_prompt_work(prompts.sequences, prompts.tokens)
-        rc = _CALLS.prompt_scan(*self._scan, prompts.address, prompts.tokens, q, k, v, dt, a, out, dt_bias, skip, work, self._stream(stream))
+        rc = (_CALLS or _calls()).prompt_scan(*self._scan, prompts.address, prompts.tokens, q, k, v, dt, a, out, dt_bias, skip, work, self._stream(stream))
         if rc:
             self._check("sketchssm_prompt_scan", rc)
         return out
@@ -393,7 +405,7 @@ class SketchSSM:
                  skip_weight: Optional[torch.Tensor] = None, eps: float = 1e-5, group: int = 0, stream=None):
         """sketchssm_rms_norm: the norm of x [T, D] (f32 or bf16) with the residual's addition, or the skip and the gate, before it;
         into out (io) and/or out8 [T, D] e4m3 with scale [T, ceil(D / 128)]."""
-        rc = _CALLS.rms_norm(*self._norm, x, weight, out, out8, scale, residual, residual_out, gate, skip, skip_weight, eps, group,
+        rc = (_CALLS or _calls()).rms_norm(*self._norm, x, weight, out, out8, scale, residual, residual_out, gate, skip, skip_weight, eps, group,
                              self._stream(stream))
         if rc:
             self._check("sketchssm_rms_norm", rc)
@@ -403,7 +415,7 @@ class SketchSSM:
                       stream=None) -> torch.Tensor:
         """sketchssm_scaled_matmul: out [M, N] (f32 or bf16) = a [M, K] w [N, K]^T in e4m3, with a_scale [M, ceil(K / 128)] and
         w_scale [ceil(N / 128), ceil(K / 128)]."""
-        rc = _CALLS.scaled_matmul(*self._matmul, a, a_scale, w, w_scale, out, self._stream(stream))
+        rc = (_CALLS or _calls()).scaled_matmul(*self._matmul, a, a_scale, w, w_scale, out, self._stream(stream))
         if rc:
             self._check("sketchssm_scaled_matmul", rc)
         return out

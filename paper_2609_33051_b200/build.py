@@ -27,7 +27,12 @@ LAYER_HEADERS = [os.path.join(CSRC, "layer.cuh"), os.path.join(CSRC, "tma.cuh"),
 
 # the extension module that checks tensors and calls the library for the operators around the recurrence
 CALLS_SRC = os.path.join(CSRC, "layer_calls.cpp")
-CALLS_PATH = os.path.join(PKG_DIR, "_layer_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def calls_path() -> str:
+    """The extension module's file.  It holds for one Python and one torch, which its name says: another one's is never taken for it."""
+    import torch
+    return os.path.join(PKG_DIR, f"_layer_calls.torch-{torch.__version__}-abi{int(torch.compiled_with_cxx11_abi())}" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 
 def _nvcc() -> str:
@@ -50,7 +55,7 @@ def _calls_command() -> list:
     lib, inc = os.path.join(home, "lib"), os.path.join(home, "include")
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
             *[f"-I{d}" for d in (inc, os.path.join(inc, "torch", "csrc", "api", "include"), sysconfig.get_path("include"), os.path.join(ROOT, "include"))],
-            CALLS_SRC, "-o", CALLS_PATH, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", f"-Wl,-rpath,{lib}"]
+            CALLS_SRC, "-o", calls_path(), f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", f"-Wl,-rpath,{lib}"]
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -63,7 +68,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if verbose:
         flags += ["-Xptxas", "-v"]
     procs, objs = [], []
-    if force or _stale(CALLS_PATH, [CALLS_SRC, os.path.join(ROOT, "include", "sketchssm.h")]):
+    if force or _stale(calls_path(), [CALLS_SRC, os.path.join(ROOT, "include", "sketchssm.h")]):
         procs.append(("layer_calls.cpp", subprocess.Popen(_calls_command(), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for src, suffix, defs in UNITS:
         sp = os.path.join(CSRC, src)
@@ -72,14 +77,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if force or _stale(obj, [sp] + HEADERS + (LAYER_HEADERS if src in LAYER_UNITS else [])):
             procs.append((src + suffix, subprocess.Popen([nvcc, *flags, *defs, "-c", sp, "-o", obj],
                                                 stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    failed = []
     for src, pr in procs:
         out, _ = pr.communicate()
         if verbose or pr.returncode != 0:
             sys.stderr.write(out)
         if pr.returncode != 0:
-            raise RuntimeError(f"compilation failed: {src}")
+            failed.append(src)
+    if any(src != "layer_calls.cpp" for src in failed):
+        raise RuntimeError(f"compilation failed: {', '.join(failed)}")
     if force or procs or _stale(LIB_PATH, objs):
         subprocess.check_call([nvcc, "-shared", "-o", LIB_PATH, *objs, "-gencode", "arch=compute_100a,code=sm_100a"])
+    if failed:                                          # (the library itself, which decode alone needs, is there)
+        raise RuntimeError(f"compilation failed: {', '.join(failed)}")
     return LIB_PATH
 
 
