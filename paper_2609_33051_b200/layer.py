@@ -32,14 +32,17 @@ class Mamba2Layer:
     """One layer of `width` channels for `batch` sequences.  Tensors between layers are bf16; weights come in as floats:
     norm [width], w_in [2 H V + 2 G K + H, width] (rows: gate, values, keys, queries, step sizes), conv_weight [C, W] and conv_bias [C]
     with C = H V + 2 G K, a [H] (negative), dt_bias and skip [H], gate_norm [H V], w_out [width, H V].
+    norm_group: how many of the H V inner elements the gated norm takes together, a multiple of 128 (0: all of them; models with several groups
+    of heads mostly norm each group's H V / G by itself).
     stream (None: the current one): what runs, and what it allocates, the results among it, belongs to that stream."""
 
     def __init__(self, batch: int, heads: int, dk: int, dv: int, groups: int, rank: int, buf_len: int, norm, w_in, conv_weight,
-                 conv_bias, a, dt_bias, skip, gate_norm, w_out, eps: float = 1e-5, device: int = 0, **kw):
+                 conv_bias, a, dt_bias, skip, gate_norm, w_out, eps: float = 1e-5, device: int = 0,
+                 norm_group: int = 0, **kw):
         self.m = binding.SketchSSM("mamba2", batch, heads, dk, dv, rank, buf_len, io="bf16", out="f32", device=device, **kw)
         dev = self.m.device
         f32 = lambda t: t.to(device=dev, dtype=torch.float32).contiguous()  # noqa: E731
-        self.groups, self.eps, self.inner = groups, eps, heads * dv
+        self.groups, self.eps, self.inner, self.norm_group = groups, eps, heads * dv, norm_group
         self.channels = self.inner + 2 * groups * dk
         self.norm, self.conv_weight, self.conv_bias = f32(norm), f32(conv_weight), f32(conv_bias)
         self.a, self.dt_bias, self.skip, self.gate_norm = f32(a), f32(dt_bias), f32(skip), f32(gate_norm)
@@ -64,7 +67,8 @@ class Mamba2Layer:
     def _project_out(self, y: torch.Tensor, gate: torch.Tensor, stream, **kw) -> torch.Tensor:
         t = y.shape[0]
         y8, scale = self._new(t, self.inner, _E4M3), self._new(t, -(-self.inner // 128), torch.float32)
-        self.m.rms_norm(y, self.gate_norm, out8=y8, scale=scale, gate=gate, eps=self.eps, stream=stream, **kw)
+        self.m.rms_norm(y, self.gate_norm, out8=y8, scale=scale, gate=gate, eps=self.eps, group=self.norm_group, stream=stream,
+                        **kw)
         return self.m.scaled_matmul(y8, scale, self.w_out, self.w_out_scale, self._new(t, self.w_out.shape[0]), stream=stream)
 
     def prompt(self, prompts: binding.Prompts, x: torch.Tensor, residual: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
