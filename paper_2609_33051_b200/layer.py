@@ -34,6 +34,8 @@ class Mamba2Layer:
     with C = H V + 2 G K, a [H] (negative), dt_bias and skip [H], gate_norm [H V], w_out [width, H V].
     norm_group: how many of the H V inner elements the gated norm takes together, a multiple of 128 (0: all of them; models with several groups
     of heads mostly norm each group's H V / G by itself).
+    The whole batch is at one phase of the decode window: a step takes a token of every sequence, and prompts are taken in while the ring is
+    empty (end_window).
     stream (None: the current one): what runs, and what it allocates, the results among it, belongs to that stream."""
 
     def __init__(self, batch: int, heads: int, dk: int, dv: int, groups: int, rank: int, buf_len: int, norm, w_in, conv_weight,
@@ -73,7 +75,8 @@ class Mamba2Layer:
 
     def prompt(self, prompts: binding.Prompts, x: torch.Tensor, residual: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """The layer over packed prompts x [T, width]; leaves the states and the convolution's rows of the prompts' slots.  Before the
-        first decode step of a window begin_window builds the sketch."""
+        first decode step of a window begin_window builds the sketch.  After decode steps end_window comes first: tokens that are still in
+        the ring are no part of the states that prompts go on from, and begin_window forgets them."""
         with binding.on_stream(stream):
             return self._prompt(prompts, x, residual, stream)
 
@@ -90,8 +93,13 @@ class Mamba2Layer:
         return self._project_out(y, gate, stream)
 
     def begin_window(self, stream=None):
-        """The sketch (and the maps) of the states as they are: after prompts, before decode steps."""
+        """The sketch (and the maps) of the states as they are: after prompts, before decode steps.  The ring is empty afterwards."""
         self.m.state_update(0, stream=stream)
+
+    def end_window(self, n_before: int, stream=None):
+        """The n_before tokens in the ring go into the states, and the ring is empty: before prompts that come between the steps of a window
+        (begin_window follows them, for the next step)."""
+        self.m.state_update(n_before, flags=binding.NO_SKETCH, stream=stream)
 
     def step(self, n_before: int, x: torch.Tensor, residual: Optional[torch.Tensor] = None, exact: bool = False, stream=None) -> torch.Tensor:
         """One token of every sequence, x [B, width], with n_before tokens in the ring: a decode step, and at the end of the window the

@@ -1,4 +1,4 @@
-"""A layer's gated norm in groups."""
+"""A layer's prompts between decode steps, and its gated norm in groups."""
 import pytest
 import torch
 
@@ -16,6 +16,52 @@ def make(seed=3, B=2, **kw):
 
 def one_prompt(n, slot):
     return binding.Prompts(torch.tensor([0, n], dtype=torch.int32, device=DEV), n, slots=torch.tensor([slot], dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("before", [1, 2, 3])
+def test_a_prompt_between_decode_steps(before):
+    """A sequence decodes `before` tokens of a window; another one's prompt is taken in; both decode on.  The first has the states of a layer
+    that never stopped, the second those of a layer that held it alone: sums of the same terms in another order, the flushes' in two parts of
+    bf16 (2^-16 of a term; far below 2^-12 of the state's norm)."""
+    gen, after = torch.Generator().manual_seed(before), 3
+    first, second = (rand(gen, n, WIDTH, dtype=torch.bfloat16).to(DEV) for n in (30, 20))
+    tokens = [rand(gen, 2, WIDTH, dtype=torch.bfloat16).to(DEV) for _ in range(before + after)]
+    lay, alone, other = make(), make(), make()
+    for a in (lay, alone):
+        a.prompt(one_prompt(30, 0), first)
+        a.begin_window()
+    for i in range(before):
+        lay.step(i, tokens[i], exact=True)
+    lay.end_window(before)
+    lay.prompt(one_prompt(20, 1), second)
+    lay.begin_window()
+    other.prompt(one_prompt(20, 1), second)
+    other.begin_window()
+    for i in range(after):
+        lay.step(i, tokens[before + i], exact=True)
+        other.step(i, tokens[before + i], exact=True)
+    for i in range(before + after):
+        alone.step(i % L, tokens[i], exact=True)
+    lay.end_window(after), other.end_window(after), alone.end_window((before + after) % L)
+    off = lambda a, b: float((a - b).norm() / b.norm())  # noqa: E731
+    assert off(lay.m.state[0], alone.m.state[0]) <= 2.0 ** -12 and off(lay.m.state[1], other.m.state[1]) <= 2.0 ** -12
+    assert torch.equal(lay.conv_state[0], alone.conv_state[0]) and torch.equal(lay.conv_state[1], other.conv_state[1])
+    assert off(lay.m.state[0], make().m.state[0] + 1) > 0.1                   # (there is a state)
+    lay.m.check_status()
+
+
+def test_the_ring_of_an_ended_window_is_empty():
+    """What the steps left in the ring is in the states: a window that ends early and one that goes on have the same."""
+    a, b = make(), make()
+    x = [rand(torch.Generator().manual_seed(i), 2, WIDTH, dtype=torch.bfloat16).to(DEV) for i in range(L)]
+    for i in range(L):
+        a.step(i, x[i])
+        b.step(i, x[i]) if i < 2 else b.step(i - 2, x[i])
+        if i == 1:
+            b.end_window(2)
+            b.begin_window()
+    b.end_window(2)
+    assert float((a.m.state - b.m.state).norm() / a.m.state.norm()) <= 2.0 ** -12
 
 
 @pytest.mark.parametrize("group", [0, 128])
