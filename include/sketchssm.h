@@ -281,7 +281,8 @@ int sketchssm_step_host(sketchssm_ctx* ctx, int op, int n_before, const void* ho
  * general rules (device pointers, 16-byte aligned; the caller's stream; nothing allocated, nothing synchronised; bounded
  * waits reported through the status block, so the context must be bound), and take row strides in elements: the distance
  * between the rows of two tokens, a multiple of 16 bytes and at least a row, so that column ranges of a wider matrix (a
- * projection's output) go in as they are.  "io" is config.io_dtype.  Everything between input and output is fp32.
+ * projection's output) go in as they are.  "io" is config.io_dtype.  Sums, statistics and states are fp32; the prompt scan's description
+ * says where products go to the tensor cores in parts of bfloat16.
  * Tensors of one call do not overlap unless a call's description says so. */
 
 /* A batch of prompts packed one behind another along the token axis.  Device arrays, read by the kernels (4-byte aligned). */
@@ -330,7 +331,11 @@ int sketchssm_prompt_work_bytes(const sketchssm_ctx* ctx, int sequences, int tok
  * not touched: a sketchssm_state_update without a token builds them before the first decode step.
  *   q, k : [T][G][K] io strided, a group for H / G heads;  v : [T][H][V] io strided;  dt : [T][H] io (stride free of the 16-byte
  *   rule);  a [H] fp32, <= 0;  dt_bias, skip [H] fp32 or NULL;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked
- *   here, the call says it. */
+ *   here, the call says it.
+ * With bf16 io and out_dtype, K = 128 and V a multiple of 64 the sums are made by the tensor cores, 128 tokens at a time: weights of earlier
+ * tokens and the state enter the products for `out` in two parts of bfloat16 (a term is off by up to 2^-16 of itself), those for the state in
+ * three (2^-22); sums are fp32, and `out` is rounded once.  There what is infinite in q, k, v or a state gives NaN in the outputs and
+ * states that depend on it, also where the formula leaves infinity.  All other types and shapes are summed in fp32, token by token. */
 int sketchssm_prompt_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, const void* q, int64_t q_stride,
                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* dt, int64_t dt_stride,
                           const void* a, const void* dt_bias, const void* skip, void* out, int64_t out_stride, int out_dtype,
