@@ -180,7 +180,9 @@ int launch_prompt_scan(Ctx* ctx, const ScanParams& p0, bool bf16, cudaStream_t s
     const int rc = launch_prompt_scan_tc(ctx, p0, bf16, stream);
     if (rc != SKETCHSSM_UNSUPPORTED_SHAPE) return rc;
     ScanParams p = p0;
-    // As many columns of a head in a CTA (keys and queries are then fetched once for them) as leave every SM four CTAs.
+    // As many columns of a head in a CTA (keys and queries are then fetched once for them) as leave every SM four CTAs.  (16 fp32 heads of 64
+    // columns, sequences of 50 tokens: 24 of them 45 us in blocks of 32, 53 in 16, 50 in 64; 74 of them 106 in 64, 135 in 16; 10 of them 30 in
+    // 16, 27 in 32.)
     const long long heads = (long long)p.pr.N * p.H;
     p.cols = 16;
     for (int c : {p.V, p.V / 2, 32})

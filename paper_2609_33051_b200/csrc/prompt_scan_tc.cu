@@ -396,8 +396,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
 #pragma unroll
                     for (int i = 0; i < 4; ++i) w[i] = beta[j][i] * exp2f(after + suf[i]);
                     float* set = gates + b * kGateBuf + j * kGateSet;
-                    float4* o = reinterpret_cast<float4*>(set) + lane;
-                    o[0] = make_float4(w[0], w[1], w[2], w[3]);                  // beta 2^(c at the chunk's end - c)
+                    float4* to = reinterpret_cast<float4*>(set) + lane;
+                    to[0] = make_float4(w[0], w[1], w[2], w[3]);                  // beta 2^(c at the chunk's end - c)
                     if (lane == 0) set[6 * kQ] = exp2f(all);                     // 2^(c at the chunk's end)
                     if constexpr (OUTPUTS) {
                         // Forward sums of whole numbers and of what is left, at most a half each: the first are exact, the second at most 64
@@ -431,11 +431,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_scan_tc_kernel(const __gri
                             f[i] = beta[j][i] * ex2((end - whole[i]) + (end2 - part[i]));
                             own[i] = beta[j][i] + (l[i] - l[i]);                 // (NaN where the decay is: it would reach a state of zeros too)
                         }
-                        o[32] = make_float4(e[0], e[1], e[2], e[3]);             // 2^c
-                        o[64] = make_float4(whole[0], whole[1], whole[2], whole[3]);     // c, whole numbers
-                        o[96] = make_float4(part[0], part[1], part[2], part[3]);         // c, the rest
-                        o[128] = make_float4(f[0], f[1], f[2], f[3]);            // beta 2^(c at the end of the 32 tokens - c)
-                        o[160] = make_float4(own[0], own[1], own[2], own[3]);    // beta
+                        to[32] = make_float4(e[0], e[1], e[2], e[3]);             // 2^c
+                        to[64] = make_float4(whole[0], whole[1], whole[2], whole[3]);     // c, whole numbers
+                        to[96] = make_float4(part[0], part[1], part[2], part[3]);         // c, the rest
+                        to[128] = make_float4(f[0], f[1], f[2], f[3]);            // beta 2^(c at the end of the 32 tokens - c)
+                        to[160] = make_float4(own[0], own[1], own[2], own[3]);    // beta
                     }
                 }
                 __syncwarp();

@@ -341,7 +341,8 @@ int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
     while (ks < 8 && tiles * ks * 2 <= (long long)sms && p.KB >= ks * 4) ks *= 2;
     if (bn == 16) return launch_tiles<16, 4, 6, 4, 2>(ctx, p, ks, stream);
     if (bn == 32) return launch_tiles<32, 4, 5, 4, 2>(ctx, p, ks, stream);
-    // (eight stages where a CTA has an SM to itself; clusters of four and eight find their place more easily with half of them)
+    // (Eight stages where a CTA has an SM to itself: 64 x 8512 x 2048 in 8.3 us, 8.7 with four.  With four stages two CTAs fit on an SM, and
+    // clusters of four and eight find their place more easily: 64 x 2048 x 4096 in 8.5 us, 11.4 with eight.)
     if (bn == 64) return ks <= 2 ? launch_tiles<64, 4, 8, 4, 1>(ctx, p, ks, stream) : launch_tiles<64, 4, 4, 4, 2>(ctx, p, ks, stream);
     return launch_tiles<128, 8, 6, 4, 1>(ctx, p, ks, stream);
 }
