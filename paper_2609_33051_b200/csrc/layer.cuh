@@ -87,7 +87,7 @@ int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t
 int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens);     // parts that a sequence is split into
 int launch_rms_norm(Ctx* ctx, const NormParams& p, bool bf16, cudaStream_t stream);
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
-int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE for few tiles
+int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE where a 128 x 128 tile an SM is enough
 
 // Prompt scan on tensor cores: at most this many segments (of all sequences of a batch together) keep a state in the scratch.  A unit
 // of work is a segment for two blocks of 64 value columns; segments are made until 148 SMs have one, of at least four chunks of

@@ -281,8 +281,11 @@ __global__ void __launch_bounds__(kThreads, 1) scaled_matmul_pair_kernel(const _
 int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
     const long long nt = (p.N + 255) / 256, tiles = nt * ((p.M + 255) / 256);
     const int pairs = sm_count(ctx) / 2;
-    // (from two thirds of the pairs on: below that the 128-column tiles of the other kernel use more SMs)
-    if (tiles * 3 < (long long)pairs * 2 || tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    // From where the other kernel's 128 x 128 tiles are more than the SMs, so that some of them would take two.  (Inner axis 2048: 256 x 9472,
+    // 148 such tiles, 11.5 us there and 12.8 here; 256 x 11264, 176 of them, 18.6 and 13.2; 1024 x 2304, 144, 11.3 and 12.9; 1024 x 3328,
+    // 208, 19.0 and 13.4.)
+    const long long small = (long long)((p.N + 127) / 128) * ((p.M + 127) / 128);
+    if (small <= sm_count(ctx) || tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
     PairArgs g;
     g.p = p;
     g.n_tiles = (int)nt;

@@ -51,3 +51,15 @@ def test_scan_on_cuda_cores(N, H, K, V, io, od):
     rel = (6 * 40 + K + 16) * U
     ref.close(out, want, ref.half_step(TYPE[od]) * want.abs() + rel * mag, "out")
     ref.close(m.state, new, rel * new_mag, "state")
+
+
+@pytest.mark.parametrize("M,N,K", [(256, 9472, 272), (256, 9473, 272), (257, 9472, 144), (1153, 2176, 272), (1100, 2100, 1040), (300, 11264, 400)])
+def test_matmul_around_a_tile_for_every_sm(M, N, K):
+    """As many tiles of 128 x 128 as the card has SMs, a few more and half as many again: where one kernel hands over to the other."""
+    gen = torch.Generator().manual_seed(M + N)
+    (a, sa), (w, sw) = quantised(gen, M, K, 1), quantised(gen, N, K, 128)
+    m, out = layer(1), torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    m.scaled_matmul(a.to(DEV), sa.to(DEV), w.to(DEV), sw.to(DEV), out)
+    m.check_status()
+    want, mag = ref.matmul(a, sa, w, sw)
+    ref.close(out, want, 2.0 ** -8 * want.abs() + K * 2.0 ** -23 * mag, "out")
