@@ -8,7 +8,8 @@
 // lane still has to add, and nothing waits for a token's own chain of shuffles (which took 400 cycles a token).  Tokens come through
 // shared memory, 32 of them while the 32 before are worked on.  Bound by fp32 issue (three multiply-adds for an element of the state and a
 // token), and with few heads by the chain of a token, about 300 cycles.  2000 fp32 tokens of 24 heads of 80 columns, seven ragged
-// sequences: 152 us (split in time for more CTAs: 208; the states and a second reading cost more than the longest sequence's tail).
+// sequences: 150 to 220 us, what the longest of them takes (lengths that took 152 us took 208 split in time for more CTAs: the states and a
+// second reading cost more than the longest sequence's tail).
 #include "pairs.cuh"
 
 namespace sketchssm {

@@ -10,14 +10,16 @@
 // state is held in fp32 registers; W goes to the tensor cores in three bf16 parts, so that a term of S is off by less than 2^-22.  P below
 // its diagonal, and S as an operand of Y, go there in two parts, off by 2^-16 of a term at most, where an output's own rounding is 2^-8 of
 // their sum (in one part: outputs 1.3e-3 in the square mean from those of fp32 sums, now 5e-5; one prompt of 16384 tokens of 64 heads
-// 269 us then, 323 now).  The diagonal, a token's own weight beta, is no part of P: it goes with the skip, in fp32.
+// 268 us then, 327 now).  The diagonal, a token's own weight beta, is no part of P: it goes with the skip, in fp32.
 // Sums of log2 decays run backward for c_end - c_t, so that what is small is exact; forward sums are kept as whole numbers, which are
 // exact, and a rest of up to 64 in size, so that c_t - c_s is off by less than 2^-14.7 whatever was decayed before s.
 //
-// What bounds it: a chunk of a pair of heads is about 10,500 cycles, of which the tensor cores work 4100 and HBM would need 2800.  It is
-// 26,000 warp instructions (7000 on the scheduler of the longest rows of P), many of them of pipes that take one every other cycle, and
-// the chain Q K^T, P, P V is about as long: Q K^T of the next chunk waits for P V, as P's second parts lie in its columns.  16384
-// tokens of 64 heads in one prompt: 323 us (0.87 TB/s), in 48: 368 us (1.24 TB/s).
+// What bounds it: a chunk of a pair of heads takes about 10,500 cycles, and no unit is busy throughout: the tensor cores work a quarter of
+// them, HBM would need 2800, the schedulers issue in half (the one with the longest rows of P in two thirds).  Two chains of about that
+// length go round: Q K^T, P, P V, Y (the next Q K^T waits for P V, as P's second parts lie in its columns), and S as an operand, Q S, W in four
+// quarters, their products, S.  16384 tokens of 64 heads in one prompt: 327 us (0.86 TB/s), in 48 ragged ones: 400 to 430 us by their
+// lengths (1.1 TB/s); 100 tokens 13 us.
+//
 // Roles: warp 3 issues the copies (TMA, 128-byte swizzle), warp 1 the products of Y (Q K^T, Q S, P V), warp 2 those of the state,
 // warp 0 makes the gates of a chunk; per set four warps ("A") turn Q K^T into P in tensor memory, add the skip and store Y, and eight
 // ("B") make W, hold S, hand it on as an operand and scale Q S.  They meet through mbarriers alone; every wait is bounded.
@@ -113,7 +115,7 @@ __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t (&r)[8]
 // The products take every value of a chunk into every row, and a zero weight times NaN or infinity is NaN: values that are not finite go
 // to the products as zeros, and a column's rows from the first of them on become NaN afterwards.  A mark of chunk n holds that row; the
 // largest of several is the first row of the latest chunk, so that marks need no clearing.  (The 65th: of any column.)
-// Looking for them costs one long prompt 2 % (269 us, 263), many short ones 0.6 %.
+// Looking for them cost one long prompt 2 % (269 us, 263, with P in one part), many short ones 0.6 %.
 __device__ __forceinline__ uint32_t mark_of(int n, int row) { return ((uint32_t)n << 8) + (uint32_t)(kQ - row); }
 
 // Adds products of the eight values, two by two, to two sums: not finite if one of the values is not (or if a product overflows: then
