@@ -245,7 +245,7 @@ def _own_token(s):
 
 def _own_norm(s):
     c = s["case"]
-    s["m"].norm_int8(s["x"], s["w"], s["out8"], s["scale"], residual=s.get("residual"), residual_out=s.get("residual_out"),
+    s["m"].integer_norm(s["x"], s["w"], s["out8"], s["scale"], residual=s.get("residual"), residual_out=s.get("residual_out"),
                      gate=s.get("gate"), act=c["act"], eps=_EPS)
     return _norm_result(s, s["out8"], s["scale"])
 
@@ -258,7 +258,7 @@ def _norm_result(s, out8, scale):
 
 
 def _own_matmul(s):
-    s["m"].int8_matmul(s["a"], s["a_scale"], s["w"], s["w_scale"], s["out"])
+    s["m"].integer_matmul(s["a"], s["a_scale"], s["w"], s["w_scale"], s["out"])
     return dict(out=s["out"])
 
 
