@@ -365,6 +365,65 @@ int sketchssm_rms_norm(sketchssm_ctx* ctx, int rows, int width, int group, float
 int sketchssm_scaled_matmul(sketchssm_ctx* ctx, int rows, int cols, int inner, const void* a, const void* a_scale,
                             const void* w, const void* w_scale, void* out, int64_t out_stride, int out_dtype, void* stream);
 
+/* ---- The delta rule's layer, and 8-bit integers -----------------------------------------------------------------------
+ * The same for GDN and KDA contexts, by the same rules: a token's gates and norms, the scan of a prompt, and (any kind of context) the
+ * norm and the product of a projection in 8-bit integers with a scale for each token and each channel. */
+
+/* One token of every batch entry (GDN, KDA): the convolution with SiLU, every group's key and query brought to unit length, and the gates,
+ * written as the token tensors that the decode calls take (channels in the order v [H][V], k [G][K], q [G][K], a group's k and q going to its
+ * H / G heads):
+ *     k = k' / sqrt(|k'|^2 + eps),  q = q_scale q' / sqrt(|q'|^2 + eps),  beta = 1 / (1 + exp(-b)),  decay = exp(a softplus(dt + dt_bias)),
+ * each rounded once, where it is stored.  The stored rows of every entry move on by one.  x [B][H V + 2 G K] io strided; b [B][H] io strided
+ * (free of the 16-byte rule); dt [B][H] io strided (free of it; GDN) or [B][H][K] io strided (KDA); a [H] fp32; dt_bias [H] (GDN) or
+ * [H][K] (KDA) fp32, or NULL; eps > 0; groups G divides H; weight, bias, state as in sketchssm_causal_conv; q, k, v, beta, decay as in
+ * sketchssm_decode_step. */
+int sketchssm_delta_step(sketchssm_ctx* ctx, int groups, int width, float eps, float q_scale, const void* weight, const void* bias, void* state,
+                         const void* x, int64_t x_stride, const void* b, int64_t b_stride, const void* dt, int64_t dt_stride, const void* a,
+                         const void* dt_bias, void* q, void* k, void* v, void* beta, void* decay, void* stream);
+
+/* Bytes of `work` that sketchssm_delta_scan needs for batches of at most this many sequences and tokens (may be 0).
+ * Host-only.  The scratch is transient; calls that overlap on the GPU need separate ones. */
+int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes);
+
+/* Gated delta rule over packed prompts (GDN, KDA): per sequence and head, token by token, with k, q, beta and the decay D (a number, or a
+ * diagonal) of a token as in sketchssm_delta_step (not rounded)
+ *     S <- D S,  S <- S + beta k (v - S^T k)^T,  out = S^T q,
+ * from the bound state of the sequence's resume entry (or zeros) into the bound state of its slot.  The sketch and the maps are
+ * not touched: a sketchssm_state_update without a token builds them before the first decode step.
+ *   q, k : [T][G][K] io strided, a group for H / G heads;  v : [T][H][V] io strided;  b : [T][H] io (stride free of the 16-byte rule);
+ *   dt : [T][H] io (stride free of it; GDN) or [T][H][K] io strided (KDA);  a [H] fp32, <= 0;  dt_bias [H] or [H][K] fp32, or NULL;
+ *   eps > 0;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked here, the call says it. */
+int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, float eps, float q_scale, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* b, int64_t b_stride, const void* dt,
+                         int64_t dt_stride, const void* a, const void* dt_bias, void* out, int64_t out_stride, int out_dtype, void* work,
+                         size_t work_bytes, void* stream);
+
+/* flags of sketchssm_integer_norm */
+#define SKETCHSSM_SIGMOID 0x1u         /* the gate goes through 1 / (1 + exp(-gate)); without it through gate / (1 + exp(-gate)) */
+
+/* Root-mean-square norm of rows, in groups of `group` elements with the same weights for every group, and the rows in 8-bit integers:
+ *     h = x;   with residual: h = x + residual, and residual_out = h (before rounding to io h goes on);
+ *     y = h / sqrt(mean(h^2) + eps) weight;   with gate: y times the gate's value
+ *     scale = max|y| / 127 over the row,  out8 = y 127 / max|y|, to nearest even (a row whose largest value is below 1e-30 is stored as zeros;
+ *     one with a value that is not finite as zeros or whole numbers with a scale that is not a number)
+ * and, if wanted, y to out (io).
+ *   rows >= 0; width at most 16384; group: a divisor of width that is a multiple of 8 (the width itself: a norm of whole rows)
+ *   x [rows][width] of x_dtype strided; weight [group] fp32; residual, residual_out [rows][width] io, dense, both or none, residual_out may be
+ *   residual; gate [rows][width] io strided, or NULL; residual and gate exclude one another; out [rows][width] io dense, or NULL;
+ *   out8 [rows][width] bytes; scale [rows] fp32. */
+int sketchssm_integer_norm(sketchssm_ctx* ctx, int rows, int width, int group, float eps, const void* x, int64_t x_stride, int x_dtype,
+                        const void* weight, const void* residual, void* residual_out, const void* gate, int64_t gate_stride, uint32_t flags,
+                        void* out, void* out8, void* scale, void* stream);
+
+/* Product of matrices of 8-bit integers with a scale for each row of either:
+ *     out[m][n] = a_scale[m] w_scale[n] sum_k a[m][k] w[n][k],
+ * the sum exact in 32-bit integers, then rounded to fp32 and scaled.
+ *   rows >= 0, cols >= 1 (each at most 2^30); inner >= 16, a multiple of 16, below 2^17; a [rows][inner], w [cols][inner] dense, values
+ *   -128..127; a_scale [rows], w_scale [cols] fp32 (4-byte aligned); out [rows][cols] of out_dtype, its stride at least cols, free of the
+ *   16-byte rule. */
+int sketchssm_integer_matmul(sketchssm_ctx* ctx, int rows, int cols, int inner, const void* a, const void* a_scale, const void* w,
+                          const void* w_scale, void* out, int64_t out_stride, int out_dtype, void* stream);
+
 /* Copy the status word back (synchronises `stream`).  Returns SKETCHSSM_OK if no kernel
  * recorded a fault, SKETCHSSM_DEVICE_TIMEOUT otherwise; `detail`, if not NULL, receives the
  * four status ints. */

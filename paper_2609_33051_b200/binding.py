@@ -23,6 +23,7 @@ TORCH_DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 NO_SKETCH = 0x1
 NO_APPEND = 0x1
 SILU = 0x1
+SIGMOID = 0x1
 
 EXPORTED = (
     "sketchssm_create", "sketchssm_destroy", "sketchssm_query_sizes", "sketchssm_bind",
@@ -32,6 +33,7 @@ EXPORTED = (
     "sketchssm_decode_step_static", "sketchssm_selftest_wait_timeout", "sketchssm_step_mixed",
     "sketchssm_causal_conv", "sketchssm_conv_step", "sketchssm_prompt_work_bytes", "sketchssm_prompt_scan",
     "sketchssm_rms_norm", "sketchssm_scaled_matmul",
+    "sketchssm_delta_step", "sketchssm_delta_work_bytes", "sketchssm_delta_scan", "sketchssm_integer_norm", "sketchssm_integer_matmul",
 )
 OP_DECODE, OP_FULL_READ, OP_UPDATE = 0, 1, 2
 
@@ -135,6 +137,13 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.sketchssm_rms_norm.argtypes = [vp, i32, i32, i32, ctypes.c_float, vp, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, i32,
                                        vp, vp, vp, vp]
     lib.sketchssm_scaled_matmul.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, i64, i32, vp]
+    f32 = ctypes.c_float
+    lib.sketchssm_delta_step.argtypes = [vp, i32, i32, f32, f32, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sketchssm_delta_work_bytes.argtypes = [vp, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sketchssm_delta_scan.argtypes = [vp, pb, i32, f32, f32, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, i32, vp,
+                                         ctypes.c_size_t, vp]
+    lib.sketchssm_integer_norm.argtypes = [vp, i32, i32, i32, f32, vp, i64, i32, vp, vp, vp, vp, i64, u32, vp, vp, vp, vp]
+    lib.sketchssm_integer_matmul.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, i64, i32, vp]
     lib.sketchssm_read_status.argtypes = [vp, ctypes.POINTER(ctypes.c_int32 * 4), vp]
     lib.sketchssm_last_launch_count.argtypes = [vp]
     lib.sketchssm_tune.argtypes = [vp, ctypes.c_char_p, i32]
@@ -239,6 +248,8 @@ class SketchSSM:
         lib = self.lib
         self._conv, self._step, self._scan = (head(f) for f in (lib.sketchssm_causal_conv, lib.sketchssm_conv_step, lib.sketchssm_prompt_scan))
         self._norm, self._matmul = head(lib.sketchssm_rms_norm), head(lib.sketchssm_scaled_matmul)
+        self._delta_step, self._delta_scan = (head(f) + (KIND[self.kind],) for f in (lib.sketchssm_delta_step, lib.sketchssm_delta_scan))
+        self._norm8, self._matmul8 = head(lib.sketchssm_integer_norm), head(lib.sketchssm_integer_matmul)
 
     def close(self):
         if self._ctx:
@@ -418,6 +429,63 @@ class SketchSSM:
         rc = (_CALLS or _calls()).scaled_matmul(*self._matmul, a, a_scale, w, w_scale, out, self._stream(stream))
         if rc:
             self._check("sketchssm_scaled_matmul", rc)
+        return out
+
+    # -- the delta rule's layer, and 8-bit integers ---------------------------------------------
+    def delta_step(self, x: torch.Tensor, b: torch.Tensor, dt: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
+                   state: torch.Tensor, a: torch.Tensor, dt_bias: Optional[torch.Tensor], token: dict, groups: int = 1, eps: float = 1e-6,
+                   q_scale: Optional[float] = None, stream=None) -> dict:
+        """sketchssm_delta_step (GDN, KDA): one token of every batch entry, x [B, H V + 2 G K], b [B, H] and dt [B, H] (GDN) or [B, H K] (KDA),
+        into the q, k, v, beta, decay of `token` (new_token_buffers), which the decode calls take.  dt_bias [H] or [H, K].
+        q_scale: None for 1 / sqrt(K)."""
+        rc = (_CALLS or _calls()).delta_step(*self._delta_step, x, b, dt, weight, bias, state, a, dt_bias, token["q"], token["k"], token["v"],
+                               token["beta"], token["decay"], groups, eps, self.K ** -0.5 if q_scale is None else q_scale, self._stream(stream))
+        if rc:
+            self._check("sketchssm_delta_step", rc)
+        return token
+
+    def new_delta_work(self, sequences: int, tokens: int) -> Optional[torch.Tensor]:
+        """Scratch of delta_scan for batches of at most this many sequences and tokens (None: none is needed)."""
+        n = ctypes.c_size_t()
+        self._check("sketchssm_delta_work_bytes", self.lib.sketchssm_delta_work_bytes(self._ctx, sequences, tokens, ctypes.byref(n)))
+        return torch.empty(n.value, dtype=torch.uint8, device=self.device) if n.value else None
+
+    def delta_scan(self, prompts: Prompts, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, b: torch.Tensor, dt: torch.Tensor,
+                   a: torch.Tensor, out: torch.Tensor, dt_bias: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   q_scale: Optional[float] = None, work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """sketchssm_delta_scan (GDN, KDA): the gated delta rule over packed prompts, q, k [T, G, K] (not normalised), v [T, H, V], b [T, H],
+        dt [T, H] (GDN) or [T, H K] (KDA) in io, a [H] f32, dt_bias [H] or [H, K] f32, into out [T, H, V] (f32 or bf16) and the
+        bound state.  q_scale: None for 1 / sqrt(K).  work: new_delta_work (allocated here if None)."""
+        if not prompts.on(self.device):
+            raise ValueError("prompts lie on the layer's device")
+        if work is None:
+            with on_stream(stream):
+                work = self.new_delta_work(prompts.sequences, prompts.tokens)
+        rc = (_CALLS or _calls()).delta_scan(*self._delta_scan, prompts.address, prompts.tokens, q, k, v, b, dt, a, out, dt_bias, work, eps,
+                               self.K ** -0.5 if q_scale is None else q_scale, self._stream(stream))
+        if rc:
+            self._check("sketchssm_delta_scan", rc)
+        return out
+
+    def integer_norm(self, x: torch.Tensor, weight: torch.Tensor, out8: torch.Tensor, scale: torch.Tensor, out: Optional[torch.Tensor] = None,
+                  residual: Optional[torch.Tensor] = None, residual_out: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                  act: str = "silu", eps: float = 1e-5, stream=None) -> torch.Tensor:
+        """sketchssm_integer_norm: the norm of x [T, D] (f32 or bf16) in groups of len(weight), after the residual's addition, or with the gate
+        (through `act`, "silu" or "sigmoid") behind it; into out8 [T, D] int8 with scale [T], and out (io) if wanted."""
+        if act not in ("silu", "sigmoid"):
+            raise ValueError("act is silu or sigmoid")
+        rc = (_CALLS or _calls()).integer_norm(*self._norm8, x, weight, out8, scale, out, residual, residual_out, gate, SIGMOID if act == "sigmoid" else 0,
+                              eps, self._stream(stream))
+        if rc:
+            self._check("sketchssm_integer_norm", rc)
+        return out8
+
+    def integer_matmul(self, a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, out: torch.Tensor,
+                    stream=None) -> torch.Tensor:
+        """sketchssm_integer_matmul: out [M, N] (f32 or bf16) = a [M, K] w [N, K]^T of 8-bit integers, with a_scale [M] and w_scale [N]."""
+        rc = (_CALLS or _calls()).integer_matmul(*self._matmul8, a, a_scale, w, w_scale, out, self._stream(stream))
+        if rc:
+            self._check("sketchssm_integer_matmul", rc)
         return out
 
     def selftest_wait_timeout(self, poll_limit: int = 2048, where: int = 99, stream=None):

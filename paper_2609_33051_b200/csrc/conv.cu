@@ -209,11 +209,11 @@ __device__ __forceinline__ void token_rows(const ConvStepParams& p, int b, int c
     in[W - 1] = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.x) + (long long)b * p.x_stride + c);
 }
 template <typename T, int W>
-__device__ __forceinline__ uint4 conv_token(const ConvStepParams& p, int b, int c, int C, const uint4 (&in)[W], const float (&w)[W][Vec16<T>::N],
-                                            const float (&bias)[Vec16<T>::N]) {
+__device__ __forceinline__ void conv_values(const ConvStepParams& p, int b, int c, int C, const uint4 (&in)[W], const float (&w)[W][Vec16<T>::N],
+                                            const float (&bias)[Vec16<T>::N], float (&y)[Vec16<T>::N]) {
     using V = Vec16<T>;
     constexpr int N = V::N;
-    float y[N], f[N];
+    float f[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = bias[e];
 #pragma unroll
@@ -225,7 +225,13 @@ __device__ __forceinline__ uint4 conv_token(const ConvStepParams& p, int b, int 
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) y[e] = silu<T>(y[e]);
-    return V::pack(y);
+}
+template <typename T, int W>
+__device__ __forceinline__ uint4 conv_token(const ConvStepParams& p, int b, int c, int C, const uint4 (&in)[W], const float (&w)[W][Vec16<T>::N],
+                                            const float (&bias)[Vec16<T>::N]) {
+    float y[Vec16<T>::N];
+    conv_values<T, W>(p, b, c, C, in, w, bias, y);
+    return Vec16<T>::pack(y);
 }
 
 template <typename T, int W>
@@ -281,6 +287,85 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) 
     }
 }
 
+// One token of a delta-rule layer.  Values as above.  A block's 32 pieces of keys or queries are whole rows of K (128 or 256 elements), each of
+// them some neighbouring lanes of one warp: the norm is a sum over those, of what the activation leaves in fp32, and what is stored is
+// rounded once.  The last blocks make the gates: beta, and the decay of a head or (KDA, 16 bytes a thread) of its channels.
+template <typename T, int W, bool KDA>
+__global__ void __launch_bounds__(128) delta_step_kernel(const DeltaStepParams d) {
+    constexpr int N = Vec16<T>::N;
+    const ConvStepParams& p = d.c;
+    __shared__ uint4 piece[kPieces];
+    grid_dep_wait();
+    grid_dep_launch_dependents();
+    const int tid = (int)threadIdx.x, hv = p.H * p.V, gk = p.G * p.K, C = hv + 2 * gk;
+    const int v_blocks = (hv / N + 127) / 128 * ((p.B + kEntries - 1) / kEntries), k_blocks = (2 * gk / N + kPieces - 1) / kPieces * p.B;
+    int i = (int)blockIdx.x;
+    if (i < k_blocks) {
+        const int b = i % p.B, first = hv + i / p.B * kPieces * N, n = min(kPieces, (C - first) / N), per = p.H / p.G, own = p.K / N;
+        if (tid < 32) {
+            float y[N], sq = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = 0.f;
+            if (tid < n) {
+                float w[W][N], bias[N];
+                uint4 in[W];
+                token_rows<T, W>(p, b, first + tid * N, C, in);
+                load_taps<W, N>(p.weight, p.bias, first + tid * N, w, bias);
+                conv_values<T, W>(p, b, first + tid * N, C, in, w, bias, y);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) sq = fmaf(y[e], y[e], sq);
+            for (int o = own / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            const float r = rsqrtf(sq + d.eps) * (first + tid * N < hv + gk ? 1.f : d.q_scale);
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] *= r;
+            piece[tid] = Vec16<T>::pack(y);
+        }
+        __syncthreads();
+        const int at = tid % kPieces, c = first - hv + at * N;
+        if (at >= n) return;
+        const bool key = c < gk;
+        const int e = key ? c : c - gk;
+        const uint4 r = piece[at];
+        T* dst = static_cast<T*>(key ? p.k : p.q) + ((size_t)b * p.H + (size_t)(e / p.K) * per) * p.K + e % p.K;
+        for (int h = tid / kPieces; h < per; h += 128 / kPieces) *reinterpret_cast<uint4*>(dst + (size_t)h * p.K) = r;
+        return;
+    }
+    i -= k_blocks;
+    if (i < v_blocks) {
+        const int groups = (p.B + kEntries - 1) / kEntries, b0 = i % groups * kEntries, c = (i / groups * 128 + tid) * N;
+        if (c >= hv) return;
+        float w[W][N], bias[N];
+        uint4 in[kEntries][W];
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+            if (b0 + k < p.B) token_rows<T, W>(p, b0 + k, c, C, in[k]);
+        load_taps<W, N>(p.weight, p.bias, c, w, bias);
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+            if (b0 + k < p.B) *reinterpret_cast<uint4*>(static_cast<T*>(p.v) + (size_t)(b0 + k) * hv + c) = conv_token<T, W>(p, b0 + k, c, C, in[k], w, bias);
+        return;
+    }
+    const long long j = (long long)(i - v_blocks) * 128 + tid;
+    if constexpr (KDA) {
+        const int per = p.K / N;                         // threads of a head
+        if (j >= (long long)p.B * p.H * per) return;
+        const int b = (int)(j / (p.H * per)), hk = (int)(j % (p.H * per)) * N, h = hk / p.K;
+        float f[N];
+        Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.dt) + (long long)b * p.dt_stride + hk), f);
+        const float a = p.a[h];
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = expf(a * softplus(f[e] + (p.dt_bias != nullptr ? p.dt_bias[hk + e] : 0.f)));
+        *reinterpret_cast<uint4*>(static_cast<T*>(d.decay) + (size_t)b * p.H * p.K + hk) = Vec16<T>::pack(f);
+        if (hk % p.K == 0) p.beta[(size_t)b * p.H + h] = 1.f / (1.f + expf(-(float)static_cast<const T*>(d.b)[(long long)b * d.b_stride + h]));
+    } else if (j < (long long)p.B * p.H) {
+        const int b = (int)(j / p.H), h = (int)(j % p.H);
+        const float x = (float)static_cast<const T*>(p.dt)[(long long)b * p.dt_stride + h] + (p.dt_bias != nullptr ? p.dt_bias[h] : 0.f);
+        p.beta[j] = 1.f / (1.f + expf(-(float)static_cast<const T*>(d.b)[(long long)b * d.b_stride + h]));
+        static_cast<float*>(d.decay)[j] = expf(p.a[h] * softplus(x));
+    }
+}
+
 template <typename T, int W>
 int conv_width(Ctx* ctx, const ConvParams& p, cudaStream_t stream) {
     const int bx = (p.C / 4 + 127) / 128;
@@ -301,7 +386,30 @@ int step_width(Ctx* ctx, const ConvStepParams& p, cudaStream_t stream) {
     return launch_layer(ctx, conv_step_kernel<T, W>, dim3((unsigned)(values + others + gates)), dim3(128), 0, stream, p);
 }
 
+template <typename T, int W, bool KDA>
+int delta_width(Ctx* ctx, const DeltaStepParams& d, cudaStream_t stream) {
+    constexpr int N = Vec16<T>::N;
+    const ConvStepParams& p = d.c;
+    const long long values = (long long)((p.H * p.V / N + 127) / 128) * ((p.B + kEntries - 1) / kEntries);
+    const long long others = (long long)((2 * p.G * p.K / N + kPieces - 1) / kPieces) * p.B, gates = ((long long)p.B * p.H * (KDA ? p.K / N : 1) + 127) / 128;
+    if (values + others + gates > 0x7fffffff) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    return launch_layer(ctx, delta_step_kernel<T, W, KDA>, dim3((unsigned)(values + others + gates)), dim3(128), 0, stream, d);
+}
+template <typename T>
+int delta_step_types(Ctx* ctx, const DeltaStepParams& p, cudaStream_t stream) {
+    const bool kda = ctx->cfg.kind == SKETCHSSM_KDA;
+    switch (p.c.W) {
+        case 2: return kda ? delta_width<T, 2, true>(ctx, p, stream) : delta_width<T, 2, false>(ctx, p, stream);
+        case 3: return kda ? delta_width<T, 3, true>(ctx, p, stream) : delta_width<T, 3, false>(ctx, p, stream);
+        default: return kda ? delta_width<T, 4, true>(ctx, p, stream) : delta_width<T, 4, false>(ctx, p, stream);
+    }
+}
+
 }  // namespace
+
+int launch_delta_step(Ctx* ctx, const DeltaStepParams& p, bool bf16, cudaStream_t stream) {
+    return bf16 ? delta_step_types<__nv_bfloat16>(ctx, p, stream) : delta_step_types<float>(ctx, p, stream);
+}
 
 int launch_causal_conv(Ctx* ctx, const ConvParams& p, bool bf16, cudaStream_t stream) {
     switch (p.W) {

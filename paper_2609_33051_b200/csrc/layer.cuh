@@ -55,6 +55,29 @@ struct ScanParams {
     int segments;          // tensor cores: parts that a sequence's tokens are split into
 };
 
+// A token of a delta-rule layer: the convolution as above; b and dt are the gates' arguments.
+struct DeltaStepParams {
+    ConvStepParams c;
+    const void* b;
+    void* decay;           // [B][H] fp32 (GDN) or [B][H][K] io (KDA)
+    long long b_stride;
+    float eps, q_scale;
+};
+
+struct DeltaParams {
+    PromptsDev pr;
+    const void *q, *k, *v, *b, *dt;
+    const float *a, *dt_bias;
+    void* out;
+    float* state;
+    unsigned char* work;
+    int* status;
+    long long q_stride, k_stride, v_stride, b_stride, dt_stride, out_stride;
+    float eps, q_scale;
+    int H, G, K, V, out_bf16;
+    int cols;              // CUDA cores: value columns per CTA
+};
+
 struct NormParams {
     const void* x;
     const float* weight;
@@ -68,6 +91,21 @@ struct NormParams {
     float* scale;
     long long x_stride, gate_stride, skip_stride;
     int rows, width, group, groups, skip_heads, x_bf16;
+    float eps;
+};
+
+// Norm with rows of 8-bit integers; `group` elements are taken together, with the same weights in every group.
+struct Norm8Params {
+    const void* x;
+    const float* weight;
+    const void* residual;
+    void* residual_out;
+    const void* gate;
+    void* out;
+    signed char* out8;
+    float* scale;
+    long long x_stride, gate_stride;
+    int rows, width, group, sigmoid;
     float eps;
 };
 
@@ -85,6 +123,11 @@ int launch_conv_step(Ctx* ctx, const ConvStepParams& p, bool bf16, cudaStream_t 
 int launch_prompt_scan(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
 int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t stream);    // tcgen05; UNSUPPORTED_SHAPE outside its domain
 int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens);     // parts that a sequence is split into
+int launch_delta_step(Ctx* ctx, const DeltaStepParams& p, bool bf16, cudaStream_t stream);
+int launch_delta_scan(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
+int launch_integer_norm(Ctx* ctx, const Norm8Params& p, bool bf16, bool x_bf16, cudaStream_t stream);
+int launch_integer_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
+int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);           // many rows; UNSUPPORTED_SHAPE where smaller tiles do
 int launch_rms_norm(Ctx* ctx, const NormParams& p, bool bf16, cudaStream_t stream);
 int launch_scaled_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
 int launch_scaled_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);         // many rows; UNSUPPORTED_SHAPE where a 128 x 128 tile an SM is enough

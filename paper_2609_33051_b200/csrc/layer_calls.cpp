@@ -109,6 +109,18 @@ int small(PyObject* o, const char* name) {
     return (int)v;
 }
 
+struct Work {
+    void* p;
+    size_t bytes;
+};
+// Scratch (None: none).
+Work scratch(PyObject* o, const Layer& l) {
+    if (o == Py_None) return {nullptr, 0};
+    const at::Tensor& w = tensor(o, "work");
+    if (!w.is_cuda() || w.get_device() != l.device || !w.is_contiguous()) throw Bad("work is a dense tensor on the layer's device");
+    return {w.data_ptr(), w.nbytes()};
+}
+
 // (function, context, device, B, H, K, V, io): the first eight arguments of every call
 constexpr int kHead = 8;
 Layer layer(PyObject* const* a) {
@@ -166,18 +178,11 @@ PyObject* prompt_scan(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const at::ScalarType od = f32_or_bf16(tensor(v[7], "out"), "out");
         const Rows q = rows(v[2], "q", l, l.io, {T, G, l.K}), k = rows(v[3], "k", l, l.io, {T, G, l.K}), x = rows(v[4], "v", l, l.io, {T, l.H, l.V}),
                    dt = rows(v[5], "dt", l, l.io, {T, l.H}), out = rows(v[7], "out", l, od, {T, l.H, l.V});
-        void* work = nullptr;
-        size_t bytes = 0;
-        if (v[10] != Py_None) {
-            const at::Tensor& w = tensor(v[10], "work");
-            if (!w.is_cuda() || w.get_device() != l.device || !w.is_contiguous()) throw Bad("work is a dense tensor on the layer's device");
-            work = w.data_ptr();
-            bytes = w.nbytes();
-        }
+        const Work work = scratch(v[10], l);
         return reinterpret_cast<decltype(&sketchssm_prompt_scan)>(address(fn))(
             l.ctx, static_cast<const sketchssm_prompts*>(address(v[0])), (int)G, q.p, q.stride, k.p, k.stride, x.p, x.stride, dt.p, dt.stride,
             dense(v[6], "a", l, kF32, {l.H}), dense(v[8], "dt_bias", l, kF32, {l.H}), dense(v[9], "skip", l, kF32, {l.H}), out.p, out.stride,
-            code(od), work, bytes, address(v[11]));
+            code(od), work.p, work.bytes, address(v[11]));
     });
 }
 
@@ -215,9 +220,86 @@ PyObject* scaled_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+bool kda(PyObject* o) { return number(o) == SKETCHSSM_KDA; }
+float real(PyObject* o, const char* name) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Bad(std::string(name) + " is no number");
+    }
+    return (float)x;
+}
+// The arguments of the decays of n rows: a number a head, or one for every channel of its keys (dense within a row).
+Rows decays(PyObject* o, const Layer& l, bool per_channel, int64_t n) {
+    if (!per_channel) return rows(o, "dt", l, l.io, {n, l.H});
+    const at::Tensor& t = tensor(o, "dt");
+    return t.dim() == 3 ? rows(o, "dt", l, l.io, {n, l.H, l.K}) : rows(o, "dt", l, l.io, {n, (int64_t)l.H * l.K});
+}
+void* biases(PyObject* o, const Layer& l, bool per_channel) {
+    return per_channel ? dense(o, "dt_bias", l, kF32, {l.H, l.K}) : dense(o, "dt_bias", l, kF32, {l.H});
+}
+
+// kind, x, b, dt, weight, bias, state, a, dt_bias, q, k, v, beta, decay, groups, eps, q_scale, stream
+PyObject* delta_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 18, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
+        const bool ch = kda(v[0]);
+        const int64_t G = small(v[14], "groups"), C = (int64_t)l.H * l.V + 2 * G * l.K, W = size_of(tensor(v[4], "weight"), 1, 2, "weight");
+        const Rows x = rows(v[1], "x", l, l.io, {l.B, C}), b = rows(v[2], "b", l, l.io, {l.B, l.H}), dt = decays(v[3], l, ch, l.B);
+        return reinterpret_cast<decltype(&sketchssm_delta_step)>(address(fn))(
+            l.ctx, (int)G, (int)W, real(v[15], "eps"), real(v[16], "q_scale"), dense(v[4], "weight", l, kF32, {C, W}), dense(v[5], "bias", l, kF32, {C}),
+            dense(v[6], "state", l, l.io, {l.B, W - 1, C}), x.p, x.stride, b.p, b.stride, dt.p, dt.stride, dense(v[7], "a", l, kF32, {l.H}),
+            biases(v[8], l, ch), dense(v[9], "q", l, l.io, {l.B, l.H, l.K}), dense(v[10], "k", l, l.io, {l.B, l.H, l.K}),
+            dense(v[11], "v", l, l.io, {l.B, l.H, l.V}), dense(v[12], "beta", l, kF32, {l.B, l.H}),
+            ch ? dense(v[13], "decay", l, l.io, {l.B, l.H, l.K}) : dense(v[13], "decay", l, kF32, {l.B, l.H}), address(v[17]));
+    });
+}
+
+// kind, prompts (address), T, q, k, v, b, dt, a, out, dt_bias, work, eps, q_scale, stream
+PyObject* delta_scan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 15, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
+        const bool ch = kda(v[0]);
+        const int64_t T = number(v[2]), G = size_of(tensor(v[3], "q"), 1, 3, "q");
+        const at::ScalarType od = f32_or_bf16(tensor(v[9], "out"), "out");
+        const Rows q = rows(v[3], "q", l, l.io, {T, G, l.K}), k = rows(v[4], "k", l, l.io, {T, G, l.K}), x = rows(v[5], "v", l, l.io, {T, l.H, l.V}),
+                   b = rows(v[6], "b", l, l.io, {T, l.H}), dt = decays(v[7], l, ch, T), out = rows(v[9], "out", l, od, {T, l.H, l.V});
+        const Work w = scratch(v[11], l);
+        return reinterpret_cast<decltype(&sketchssm_delta_scan)>(address(fn))(
+            l.ctx, static_cast<const sketchssm_prompts*>(address(v[1])), (int)G, real(v[12], "eps"), real(v[13], "q_scale"), q.p, q.stride, k.p, k.stride,
+            x.p, x.stride, b.p, b.stride, dt.p, dt.stride, dense(v[8], "a", l, kF32, {l.H}), biases(v[10], l, ch), out.p, out.stride, code(od), w.p,
+            w.bytes, address(v[14]));
+    });
+}
+
+// x, weight, out8, scale, out, residual, residual_out, gate, flags, eps, stream
+PyObject* integer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 11, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
+        const at::Tensor& xt = tensor(v[0], "x");
+        const int64_t T = size_of(xt, 0, 2, "x"), D = size_of(xt, 1, 2, "x"), group = size_of(tensor(v[1], "weight"), 0, 1, "weight");
+        const at::ScalarType xd = f32_or_bf16(xt, "x");
+        const Rows x = rows(v[0], "x", l, xd, {T, D}), none = {nullptr, 0}, gate = v[7] == Py_None ? none : rows(v[7], "gate", l, l.io, {T, D});
+        return reinterpret_cast<decltype(&sketchssm_integer_norm)>(address(fn))(
+            l.ctx, (int)T, (int)D, (int)group, real(v[9], "eps"), x.p, x.stride, code(xd), dense(v[1], "weight", l, kF32, {group}),
+            dense(v[5], "residual", l, l.io, {T, D}), dense(v[6], "residual_out", l, l.io, {T, D}), gate.p, gate.stride, (uint32_t)number(v[8]),
+            dense(v[4], "out", l, l.io, {T, D}), dense(v[2], "out8", l, at::kChar, {T, D}), dense(v[3], "scale", l, kF32, {T}), address(v[10]));
+    });
+}
+
+// a, a_scale, w, w_scale, out, stream
+PyObject* integer_matmul(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 6, [fn = n ? a[0] : nullptr](const Layer& l, PyObject* const* v) {
+        const int64_t M = size_of(tensor(v[0], "a"), 0, 2, "a"), K = size_of(tensor(v[0], "a"), 1, 2, "a"), N = size_of(tensor(v[2], "w"), 0, 2, "w");
+        const at::ScalarType od = f32_or_bf16(tensor(v[4], "out"), "out");
+        const Rows out = rows(v[4], "out", l, od, {M, N});
+        return reinterpret_cast<decltype(&sketchssm_integer_matmul)>(address(fn))(
+            l.ctx, (int)M, (int)N, (int)K, dense(v[0], "a", l, at::kChar, {M, K}), dense(v[1], "a_scale", l, kF32, {M}), dense(v[2], "w", l, at::kChar, {N, K}),
+            dense(v[3], "w_scale", l, kF32, {N}), out.p, out.stride, code(od), address(v[5]));
+    });
+}
+
 #define SKETCHSSM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {SKETCHSSM_METHOD(causal_conv), SKETCHSSM_METHOD(conv_step),    SKETCHSSM_METHOD(prompt_scan),
-                          SKETCHSSM_METHOD(rms_norm),    SKETCHSSM_METHOD(scaled_matmul), {nullptr, nullptr, 0, nullptr}};
+                          SKETCHSSM_METHOD(rms_norm),    SKETCHSSM_METHOD(scaled_matmul), SKETCHSSM_METHOD(delta_step), SKETCHSSM_METHOD(delta_scan),
+                          SKETCHSSM_METHOD(integer_norm),   SKETCHSSM_METHOD(integer_matmul), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_layer_calls", "Calls of the operators around the recurrence.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
