@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsketchssm.so")
 # the operators around the recurrence
 LAYER_UNITS = ("api_layer.cu", "conv.cu", "prompt_scan.cu", "prompt_scan_tc.cu", "rms_norm.cu", "scaled_matmul.cu", "scaled_matmul_pair.cu",
-               "delta_scan.cu", "integer_norm.cu", "integer_matmul.cu", "integer_matmul_pair.cu")
+               "delta_scan.cu", "delta_scan_tc.cu", "integer_norm.cu", "integer_matmul.cu", "integer_matmul_pair.cu")
 # (source, object suffix, extra defines); the decodes are compiled once per (recurrence kind, I/O type)
 UNITS = [("api.cu", "", []), ("update.cu", "", []), ("update_cols.cu", "", []), ("update_tc.cu", "", []),
          ("update_tc_ws.cu", "", []), ("update_tc_ws_gdn.cu", "", []), ("update_tc_ws_kda.cu", "", []), ("decode_static.cu", "", []), ("selftest.cu", "", []), ("coef_map.cu", "", []), ("coef_map_pivot.cu", "", []),

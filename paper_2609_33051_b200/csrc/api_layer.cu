@@ -235,7 +235,7 @@ int sketchssm_delta_step(sketchssm_ctx* ctx, int groups, int width, float eps, f
 
 int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes) {
     if (ctx == nullptr || bytes == nullptr || sequences < 0 || tokens < 0) return SKETCHSSM_INVALID_ARG;
-    *bytes = 0;
+    *bytes = delta_tc_work_bytes(ctx->cfg, sequences, tokens);
     return SKETCHSSM_OK;
 }
 

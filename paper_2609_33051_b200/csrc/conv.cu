@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(128) delta_step_kernel(const DeltaStepParams d
 #pragma unroll
             for (int e = 0; e < N; ++e) sq = fmaf(y[e], y[e], sq);
             for (int o = own / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-            const float r = rsqrtf(sq + d.eps) * (first + tid * N < hv + gk ? 1.f : d.q_scale);
+            const float r = inv_length(sq, d.eps) * (first + tid * N < hv + gk ? 1.f : d.q_scale);
 #pragma unroll
             for (int e = 0; e < N; ++e) y[e] *= r;
             piece[tid] = Vec16<T>::pack(y);

@@ -130,8 +130,8 @@ __global__ void __launch_bounds__(256) delta_scan_kernel(const DeltaParams p) {
             k2 = warp_sum(k2);
             q2 = warp_sum(q2);
             if (lane == 0) {
-                sg[t].y = rsqrtf(k2 + p.eps);
-                sg[t].w = p.q_scale * rsqrtf(q2 + p.eps);
+                sg[t].y = inv_length(k2, p.eps);
+                sg[t].w = p.q_scale * inv_length(q2, p.eps);
             }
         }
         if constexpr (KDA) {
@@ -248,6 +248,8 @@ int launch_cores(Ctx* ctx, const DeltaParams& p, long long units, cudaStream_t s
 }  // namespace
 
 int launch_delta_scan(Ctx* ctx, const DeltaParams& p0, bool bf16, cudaStream_t stream) {
+    const int rc = launch_delta_scan_tc(ctx, p0, bf16, stream);
+    if (rc != SKETCHSSM_UNSUPPORTED_SHAPE) return rc;
     DeltaParams p = p0;
     // As many columns of a head in a CTA (keys, queries and decays are then fetched once for them) as leave every SM four CTAs.
     const long long heads = (long long)p.pr.N * p.H;

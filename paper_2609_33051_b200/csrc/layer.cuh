@@ -125,6 +125,8 @@ int launch_prompt_scan_tc(Ctx* ctx, const ScanParams& p, bool bf16, cudaStream_t
 int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens);     // parts that a sequence is split into
 int launch_delta_step(Ctx* ctx, const DeltaStepParams& p, bool bf16, cudaStream_t stream);
 int launch_delta_scan(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
+int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream);    // tcgen05; UNSUPPORTED_SHAPE outside its domain
+size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens);
 int launch_integer_norm(Ctx* ctx, const Norm8Params& p, bool bf16, bool x_bf16, cudaStream_t stream);
 int launch_integer_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
 int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);           // many rows; UNSUPPORTED_SHAPE where smaller tiles do
@@ -205,6 +207,9 @@ __device__ __forceinline__ int starts_before(const PromptsDev& pr, int t) {
 }
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
+
+// One over a key's or query's length, from its square; a length that is not finite is not a number (as what it is taken of then is).
+__device__ __forceinline__ float inv_length(float sq, float eps) { return sq <= 3.4028235e38f ? rsqrtf(sq + eps) : __int_as_float(0x7fffffff); }
 
 // 16 bytes of io elements as floats and back.
 template <typename T>
