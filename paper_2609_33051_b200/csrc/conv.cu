@@ -287,75 +287,77 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) 
     }
 }
 
-// One token of a delta-rule layer.  Values as above.  A block's 32 pieces of keys or queries are whole rows of K (128 or 256 elements), each of
-// them some neighbouring lanes of one warp: the norm is a sum over those, of what the activation leaves in fp32, and what is stored is
-// rounded once.  The last blocks make the gates: beta, and the decay of a head or (KDA, 16 bytes a thread) of its channels.
+// One token of a delta-rule layer.  A warp takes 32 pieces of 16 bytes of channels for four batch entries, with the taps in registers: of values,
+// or of keys and queries, which are whole rows of K there (8, 16 or 32 neighbouring lanes): their norm is a sum over those, of what the
+// activation leaves in fp32, and the result, rounded once, goes to every head of the group.  The last blocks make the gates: beta, and the
+// decay of a head or (KDA, 16 bytes a thread) of its channels.
 template <typename T, int W, bool KDA>
 __global__ void __launch_bounds__(128) delta_step_kernel(const DeltaStepParams d) {
     constexpr int N = Vec16<T>::N;
     const ConvStepParams& p = d.c;
-    __shared__ uint4 piece[kPieces];
     grid_dep_wait();
     grid_dep_launch_dependents();
     const int tid = (int)threadIdx.x, hv = p.H * p.V, gk = p.G * p.K, C = hv + 2 * gk;
-    const int v_blocks = (hv / N + 127) / 128 * ((p.B + kEntries - 1) / kEntries), k_blocks = (2 * gk / N + kPieces - 1) / kPieces * p.B;
-    int i = (int)blockIdx.x;
-    if (i < k_blocks) {
-        const int b = i % p.B, first = hv + i / p.B * kPieces * N, n = min(kPieces, (C - first) / N), per = p.H / p.G, own = p.K / N;
-        if (tid < 32) {
+    const int sets = (p.B + kEntries - 1) / kEntries, v_warps = (hv / N + 31) / 32, warps = (v_warps + (2 * gk / N + 31) / 32) * sets;
+    const int blocks = (warps + 3) / 4;
+    if ((int)blockIdx.x < blocks) {
+        const int w0 = (int)blockIdx.x * 4 + (tid >> 5);
+        if (w0 >= warps) return;
+        const int b0 = w0 % sets * kEntries, unit = w0 / sets;
+        const bool value = unit < v_warps;
+        const int c = (value ? unit * 32 : hv / N + (unit - v_warps) * 32) * N + (tid & 31) * N;
+        const bool in = c < (value ? hv : C);
+        float w[W][N], bias[N];
+        uint4 rows[kEntries][W];
+        if (in) {
+#pragma unroll
+            for (int k = 0; k < kEntries; ++k)
+                if (b0 + k < p.B) token_rows<T, W>(p, b0 + k, c, C, rows[k]);
+            load_taps<W, N>(p.weight, p.bias, c, w, bias);
+        }
+        if (value) {
+            if (!in) return;
+#pragma unroll
+            for (int k = 0; k < kEntries; ++k)
+                if (b0 + k < p.B) *reinterpret_cast<uint4*>(static_cast<T*>(p.v) + (size_t)(b0 + k) * hv + c) = conv_token<T, W>(p, b0 + k, c, C, rows[k], w, bias);
+            return;
+        }
+        const bool key = c < hv + gk;
+        const int e = key ? c - hv : c - hv - gk, per = p.H / p.G;
+        const float scale = key ? 1.f : d.q_scale;
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k) {
+            if (b0 + k >= p.B) break;
             float y[N], sq = 0.f;
 #pragma unroll
-            for (int e = 0; e < N; ++e) y[e] = 0.f;
-            if (tid < n) {
-                float w[W][N], bias[N];
-                uint4 in[W];
-                token_rows<T, W>(p, b, first + tid * N, C, in);
-                load_taps<W, N>(p.weight, p.bias, first + tid * N, w, bias);
-                conv_values<T, W>(p, b, first + tid * N, C, in, w, bias, y);
+            for (int i = 0; i < N; ++i) y[i] = 0.f;
+            if (in) conv_values<T, W>(p, b0 + k, c, C, rows[k], w, bias, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sq = fmaf(y[i], y[i], sq);
+            for (int o = p.K / N / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+            const float r = inv_length(sq, d.eps) * scale;
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i] *= r;
+            if (in) {
+                T* dst = static_cast<T*>(key ? p.k : p.q) + ((size_t)(b0 + k) * p.H + (size_t)(e / p.K) * per) * p.K + e % p.K;
+                const uint4 u = Vec16<T>::pack(y);
+                for (int h = 0; h < per; ++h) *reinterpret_cast<uint4*>(dst + (size_t)h * p.K) = u;
             }
-#pragma unroll
-            for (int e = 0; e < N; ++e) sq = fmaf(y[e], y[e], sq);
-            for (int o = own / 2; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-            const float r = inv_length(sq, d.eps) * (first + tid * N < hv + gk ? 1.f : d.q_scale);
-#pragma unroll
-            for (int e = 0; e < N; ++e) y[e] *= r;
-            piece[tid] = Vec16<T>::pack(y);
         }
-        __syncthreads();
-        const int at = tid % kPieces, c = first - hv + at * N;
-        if (at >= n) return;
-        const bool key = c < gk;
-        const int e = key ? c : c - gk;
-        const uint4 r = piece[at];
-        T* dst = static_cast<T*>(key ? p.k : p.q) + ((size_t)b * p.H + (size_t)(e / p.K) * per) * p.K + e % p.K;
-        for (int h = tid / kPieces; h < per; h += 128 / kPieces) *reinterpret_cast<uint4*>(dst + (size_t)h * p.K) = r;
         return;
     }
-    i -= k_blocks;
-    if (i < v_blocks) {
-        const int groups = (p.B + kEntries - 1) / kEntries, b0 = i % groups * kEntries, c = (i / groups * 128 + tid) * N;
-        if (c >= hv) return;
-        float w[W][N], bias[N];
-        uint4 in[kEntries][W];
-#pragma unroll
-        for (int k = 0; k < kEntries; ++k)
-            if (b0 + k < p.B) token_rows<T, W>(p, b0 + k, c, C, in[k]);
-        load_taps<W, N>(p.weight, p.bias, c, w, bias);
-#pragma unroll
-        for (int k = 0; k < kEntries; ++k)
-            if (b0 + k < p.B) *reinterpret_cast<uint4*>(static_cast<T*>(p.v) + (size_t)(b0 + k) * hv + c) = conv_token<T, W>(p, b0 + k, c, C, in[k], w, bias);
-        return;
-    }
-    const long long j = (long long)(i - v_blocks) * 128 + tid;
+    const long long j = ((long long)blockIdx.x - blocks) * 128 + tid;
     if constexpr (KDA) {
         const int per = p.K / N;                         // threads of a head
         if (j >= (long long)p.B * p.H * per) return;
         const int b = (int)(j / (p.H * per)), hk = (int)(j % (p.H * per)) * N, h = hk / p.K;
-        float f[N];
+        float f[N], add[N];
         Vec16<T>::unpack(*reinterpret_cast<const uint4*>(static_cast<const T*>(p.dt) + (long long)b * p.dt_stride + hk), f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) add[e] = p.dt_bias != nullptr ? p.dt_bias[hk + e] : 0.f;
         const float a = p.a[h];
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = expf(a * softplus(f[e] + (p.dt_bias != nullptr ? p.dt_bias[hk + e] : 0.f)));
+        for (int e = 0; e < N; ++e) f[e] = expf(a * softplus(f[e] + add[e]));
         *reinterpret_cast<uint4*>(static_cast<T*>(d.decay) + (size_t)b * p.H * p.K + hk) = Vec16<T>::pack(f);
         if (hk % p.K == 0) p.beta[(size_t)b * p.H + h] = 1.f / (1.f + expf(-(float)static_cast<const T*>(d.b)[(long long)b * d.b_stride + h]));
     } else if (j < (long long)p.B * p.H) {
@@ -390,10 +392,10 @@ template <typename T, int W, bool KDA>
 int delta_width(Ctx* ctx, const DeltaStepParams& d, cudaStream_t stream) {
     constexpr int N = Vec16<T>::N;
     const ConvStepParams& p = d.c;
-    const long long values = (long long)((p.H * p.V / N + 127) / 128) * ((p.B + kEntries - 1) / kEntries);
-    const long long others = (long long)((2 * p.G * p.K / N + kPieces - 1) / kPieces) * p.B, gates = ((long long)p.B * p.H * (KDA ? p.K / N : 1) + 127) / 128;
-    if (values + others + gates > 0x7fffffff) return SKETCHSSM_UNSUPPORTED_SHAPE;
-    return launch_layer(ctx, delta_step_kernel<T, W, KDA>, dim3((unsigned)(values + others + gates)), dim3(128), 0, stream, d);
+    const long long warps = (long long)((p.H * p.V / N + 31) / 32 + (2 * p.G * p.K / N + 31) / 32) * ((p.B + kEntries - 1) / kEntries);
+    const long long blocks = (warps + 3) / 4 + ((long long)p.B * p.H * (KDA ? p.K / N : 1) + 127) / 128;
+    if (warps > 0x7fffffff || blocks > 0x7fffffff) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    return launch_layer(ctx, delta_step_kernel<T, W, KDA>, dim3((unsigned)blocks), dim3(128), 0, stream, d);
 }
 template <typename T>
 int delta_step_types(Ctx* ctx, const DeltaStepParams& p, cudaStream_t stream) {

@@ -2,22 +2,26 @@
 //
 // A sequence goes through in chunks of 64 tokens.  With c_t the sum of the chunk's log2 decays up to token t, unit keys k (a key as it is times
 // r_t) and S the state before the chunk, what the tokens add is U, the solution of a unit lower triangular system:
-//     (I + L) U = X,   L[t][s] = beta_t 2^(c_t - c_s) <k_t, k_s> for s < t,   X[t] = beta_t (v_t - 2^c_t S^T k_t)
+//     (I + L) U = diag(beta) X,   L[t][s] = beta_t 2^(c_t - c_s) <k_t, k_s> for s < t,   X[t] = v_t - 2^c_t S^T k_t
 //     Y[t] = 2^c_t S^T q_t + sum_{s <= t} P[t][s] U[s],   P[t][s] = 2^(c_t - c_s) <q_t, k_s>
 //     S <- 2^c_end S + sum_s 2^(c_end - c_s) k_s U[s]^T
-// T = (I + L)^-1 and P do not depend on the state: a first kernel makes them, all chunks at once, and leaves them in the scratch as
+// T = (I + L)^-1 diag(beta) and P do not depend on the state: a first kernel makes them, all chunks at once, and leaves them in the scratch as
 // matrix operands; a second one takes a sequence and head at a time through its chunks.
 //
 // There the state is kept transposed: 128 value columns are the lanes of tensor memory, so that everything a chunk reads of it is one
 // operand in tensor memory times a tile of shared memory (keys, queries, T, P), and a lane's thread scales, adds and splits without
-// another thread's help.  Per chunk: K S^T and, later, Q S^T;  X;  (T - I) X;  U and W = 2^(c_end - c) r U;  W K and U P;  S.
+// another thread's help.  Per chunk: K S^T and, later, Q S^T;  X;  (T - diag) X;  U and W = 2^(c_end - c) r U;  W K and U P;  S.
 //
-// Precision.  States are fp32, outputs sums of fp32 accuracy rounded once.  Keys and queries are exact bf16 operands.  S, X, T - I and W
-// go to the tensor cores in three parts of bf16 (24 bits; products of parts below 2^-24 are left out), so that the state's error stays that of
-// fp32 sums: with two parts of S, X and T it was 10 to 30 times larger.  What is for the outputs alone, S with the queries, P and
-// U, goes in two parts (2^-16 of a term), where an output's own rounding is 2^-8 of their sum.  Sums of log decays are made in 64 bits and
-// kept as a whole number and a rest of at most a half.
+// Precision.  States are fp32, outputs sums of fp32 accuracy rounded once.  What the tensor cores multiply are fp16 operands in two parts of 11
+// bits each (the product of the second parts is left out), summed in fp32.  fp16 has the bits but not the range, so everything is scaled by
+// powers of two, which round nothing: keys and queries by one each, to lengths between a half and one (then one part holds all of their bits
+// but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value and
+// state element in it: |U| is at most 65 of the former and 11.4 of the latter, |W| twice that, and is brought below 2^15.  T and P are below
+// one as they are.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
+// Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 #include "tma.cuh"
+
+#include <cuda_fp16.h>
 
 #include <utility>
 
@@ -29,14 +33,16 @@ using namespace tc;
 
 constexpr int kQ = 64;                                 // tokens of a chunk
 constexpr uint32_t kPart = 8192u;                      // 64 rows of 128 bytes
-constexpr uint32_t kTOff = 0, kPOff = 3 * kPart, kGOff = 5 * kPart;
-// gates of a chunk and head, 64 floats each: beta, beta 2^c r, 2^(c_end - c) r, q_scale 2^c / |q|, and 2^c_end
+// The scratch: for a chunk of a head two parts of T - diag, two of P and the gates; for one of a group the rows of K and Q, half of the channels at a time
+constexpr uint32_t kTOff = 0, kPOff = 2 * kPart, kGOff = 4 * kPart, kRows = 4 * kPart;
+// gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c / |q| (r and 1 / |q| of the scaled rows), and 2^c_end
 constexpr int kBeta = 0, kRead = 64, kPut = 128, kAsk = 192, kKeep = 256, kGates = 320;
-constexpr uint32_t kBlock = kGOff + kGates * 4u;       // bytes of the scratch for a chunk of a head
+constexpr uint32_t kBlock = kGOff + kGates * 4u;
 
 struct DeltaArgs {
     CUtensorMap tq, tk, tv;
     DeltaParams p;
+    unsigned char* rows;       // of the scratch, behind the heads' blocks
     int units;
 };
 
@@ -56,50 +62,39 @@ __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t (&r)[8]
                  "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+    __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+// Two floats as two parts of fp16 each: what the first leaves, rounded, is the second.  (The mixed multiply-add takes the halves as they are;
+// brought back to fp32 first, two conversions on the same pipe, they cost three times as much.)
+__device__ __forceinline__ void two_parts(uint64_t x, uint32_t& hi, uint32_t& lo) {
+    float a, b, c, d;
+    unpack2(x, a, b);
+    hi = half_pair(a, b);
+    asm("{\n\t.reg .b16 h, l, m;\n\tmov.b32 {l, h}, %2;\n\tmov.b16 m, 0xBC00;\n\t"
+        "fma.rn.f32.f16 %0, l, m, %3;\n\tfma.rn.f32.f16 %1, h, m, %4;\n\t}"
+        : "=f"(c), "=f"(d)
+        : "r"(hi), "f"(a), "f"(b));
+    lo = half_pair(c, d);
+}
 __device__ __forceinline__ void bulk_s2g(void* dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
-__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t*>(&h);
-}
-// Two floats as two parts of bfloat16 each: what the first leaves, rounded, is the second.
-__device__ __forceinline__ void two_parts(uint64_t x, uint32_t& hi, uint32_t& lo) {
-    float a, b;
-    unpack2(x, a, b);
-    hi = bf16x2(a, b);
-    unpack2(fma2(pack2(__uint_as_float(hi << 16), __uint_as_float(hi & 0xffff0000u)), pack2(-1.f, -1.f), x), a, b);
-    lo = bf16x2(a, b);
-}
-// Two floats as three parts each: the upper 16 bits of what is left, twice, and the rest rounded: 8 + 8 + 8 bits.
-__device__ __forceinline__ void three_parts(uint64_t x, uint32_t& p0, uint32_t& p1, uint32_t& p2) {
-    const uint64_t minus = pack2(-1.f, -1.f);
-    uint32_t lo = (uint32_t)x & 0xffff0000u, hi = (uint32_t)(x >> 32) & 0xffff0000u;
-    p0 = __byte_perm(lo, hi, 0x7632);
-    x = fma2(pack2(__uint_as_float(lo), __uint_as_float(hi)), minus, x);
-    lo = (uint32_t)x & 0xffff0000u;
-    hi = (uint32_t)(x >> 32) & 0xffff0000u;
-    p1 = __byte_perm(lo, hi, 0x7632);
-    x = fma2(pack2(__uint_as_float(lo), __uint_as_float(hi)), minus, x);
-    float a, b;
-    unpack2(x, a, b);
-    p2 = bf16x2(a, b);
-}
-
-constexpr uint32_t kTypes = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);      // bf16 x bf16 -> fp32, 128 rows
+constexpr uint32_t kTypes = (1u << 4) | ((128u >> 4) << 24);      // fp16 x fp16 -> fp32, 128 rows
 
 // ---- what does not depend on the state: T and P of every chunk ------------------------------------------------------------
 //
-// A CTA takes a chunk, a group and two of its heads.  One product gives the rows <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127);
+// A CTA takes a chunk, a group and two of its heads.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product gives the rows <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127);
 // threads 0..63 make -L of both heads from them, the others P.  T is found column by column: a thread holds a whole column in registers and
 // takes from the rows below what each of its elements puts there, so that nothing is waited for; two warps a head.
-// The columns from 32 on start at row 32: the heavy half changes schedulers with the CTA's number.
+// The columns from 32 on start at row 32: the heavy half changes schedulers with the CTA's number.  What is split and stored goes by rows
+// again, through shared memory.
 
 constexpr int kPrepThreads = 128;
-constexpr uint32_t kPrepL = 4 * kPart;                 // behind the tile of K and Q rows (whose place P takes): -L of two heads, [s][t] floats
-constexpr uint32_t kPrepNorm = kPrepL + 2u * kQ * kQ * 4u;        // 1 / |k|, 1 / |q|: [2][64]
+constexpr uint32_t kPrepNorm = 4 * kPart;              // behind the tile of K and Q rows (whose place -L of two heads takes, [s][t] floats): 1 / |k|, 1 / |q|: [2][64]
 constexpr uint32_t kPrepSum = kPrepNorm + 2u * kQ * 4u;           // of each head: whole, rest, beta: [2][3][64]
 constexpr uint32_t kPrepBar = kPrepSum + 6u * kQ * 4u;
 constexpr uint32_t kPrepSmem = kPrepBar + 32u + 1024u;
@@ -124,10 +119,10 @@ __device__ __forceinline__ void take(uint64_t (&T)[32], const float* l) {
 template <int FIRST, int... I>
 __device__ __forceinline__ void take_rows(uint64_t (&T)[32], const float* l, std::integer_sequence<int, I...>) { (take<FIRST + I>(T, l), ...); }
 
-__global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __grid_constant__ DeltaArgs g) {
+__global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __grid_constant__ DeltaArgs g) {
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    float* minus_l = reinterpret_cast<float*>(smem + kPrepL);
+    float* minus_l = reinterpret_cast<float*>(smem);
     float* norms = reinterpret_cast<float*>(smem + kPrepNorm);
     float* sums = reinterpret_cast<float*>(smem + kPrepSum);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kPrepBar);
@@ -207,23 +202,36 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             }
         }
         ok = mbar_wait_bounded(bar, 0);
-        // norms: a row of K or Q a thread
-        {
+        // norms: a row of K or Q a thread, which it then scales; rows behind the sequence are zeros
+        ok = __syncthreads_and(ok) != 0;
+        if (ok) {
             float sq = 0.f;
-            const unsigned char* row = smem + (tid & 64) * 128 + (tid & 63) * 128;
+            unsigned char* row = smem + tid * 128;
+            uint4 v[16];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int i = 0; i < 16; ++i) {
+                v[i] = *reinterpret_cast<const uint4*>(row + (i / 8) * 2 * kPart + (((i & 7) ^ (tid & 7)) * 16));
+                float f[8];
+                Vec16<__nv_bfloat16>::unpack(v[i], f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float f[8];
-                    Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(row + h * 2 * kPart + ((i ^ (tid & 7)) * 16)), f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sq = fmaf(f[e], f[e], sq);
-                }
+                for (int e = 0; e < 8; ++e) sq = fmaf(f[e], f[e], sq);
             }
-            norms[tid] = inv_length(sq, p.eps) * (tid < 64 ? 1.f : p.q_scale);
+            const float r = inv_length(sq, p.eps), scale = __uint_as_float(__float_as_uint(r) & 0x7f800000u);
+            norms[tid] = r / scale;
+            const bool in = (tid & 63) < valid;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float f[8];
+                Vec16<__nv_bfloat16>::unpack(v[i], f);
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = in ? half_pair(f[2 * e] * scale, f[2 * e + 1] * scale) : 0u;
+                *reinterpret_cast<uint4*>(row + (i / 8) * 2 * kPart + (((i & 7) ^ (tid & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            proxy_fence();
         }
         ok = __syncthreads_and(ok) != 0;
+        if (tid == 64 && ok && batch == 0) bulk_s2g(g.rows + ((size_t)chunk * p.G + group) * kRows, smem, kRows);
         if (warp == 0 && ok) {
             const uint64_t da = swizzled_desc(smem_u32(smem), 16u, 1024u);
 #pragma unroll
@@ -242,101 +250,128 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 const bool in = tid < valid;
                 const float e = exp2f(w) * exp2f(r), rest = exp2f(s[kQ - 1] - w) * exp2f(s[2 * kQ - 1] - r);
                 to[kBeta + tid] = s[2 * kQ + tid];
-                to[kRead + tid] = in ? s[2 * kQ + tid] * e * norms[tid] : 0.f;
+                to[kRead + tid] = in ? fmaf(s[2 * kQ + tid], 0.f, -e * norms[tid]) : 0.f;      // (not a number where beta is none: see the marks)
                 to[kPut + tid] = in ? rest * norms[tid] : 0.f;
                 to[kAsk + tid] = in ? e * norms[64 + tid] : 0.f;
                 if (tid == 63) to[kKeep] = e;
             }
         }
         ok = ok && mbar_wait_bounded(bar + 1, 0);
-        ok = __syncthreads_and(ok) != 0;                // (from here on the tile's place is P's)
+        if (tid == 64) tma_store_read();
+        ok = __syncthreads_and(ok) != 0;                // (from here on the tile's place is -L's)
         if (ok) {
             tc_fence_after();
             const int t = tid & 63;
             const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+            const uint64_t minus = pack2(-1.f, -1.f);
 #pragma unroll 1
             for (int j = 0; j < heads; ++j) {
-                const float *s = sums + j * 3 * kQ, w = s[t], r = s[kQ + t];
-                const bool in = t < valid;
+                const float* s = sums + j * 3 * kQ;
+                const uint64_t w = pack2(s[t], s[t]), r = pack2(s[kQ + t], s[kQ + t]);
+                // tokens e .. e + 15 of the row: the product times both norms (and `mine`) and the decay between, zero from `end` on
+                auto tokens = [&](int e0, uint64_t mine, int end, uint64_t (&x)[8]) {
+                    uint32_t d[16];
+                    tmem_ld16_async(tmem + lanes + e0, d);
+                    tmem_ld_wait();
+                    const ulonglong2 *w4 = reinterpret_cast<const ulonglong2*>(s + e0), *r4 = reinterpret_cast<const ulonglong2*>(s + kQ + e0),
+                                     *n4 = reinterpret_cast<const ulonglong2*>(norms + e0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const ulonglong2 we = w4[i], re = r4[i], ne = n4[i];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            float a, b, y0, y1;
+                            unpack2(add2(fma2(q ? we.y : we.x, minus, w), fma2(q ? re.y : re.x, minus, r)), a, b);
+                            const uint64_t f = mul2(mul2(mine, q ? ne.y : ne.x), pack2(__uint_as_float(d[4 * i + 2 * q]), __uint_as_float(d[4 * i + 2 * q + 1])));
+                            unpack2(mul2(f, pack2(ex2(a), ex2(b))), y0, y1);
+                            const int e = e0 + 4 * i + 2 * q;
+                            x[2 * i + q] = pack2(e < end ? y0 : 0.f, e + 1 < end ? y1 : 0.f);
+                        }
+                    }
+                };
+                const int last = 16 * ((warp & 1) * 2 + 2);                      // (a warp's rows end there)
                 if (tid < 64) {
                     const float mine = -s[2 * kQ + t] * norms[t];
                     float* to = minus_l + j * kQ * kQ + t;
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t d[16];
-                        tmem_ld16_async(tmem + lanes + c * 16, d);
-                        tmem_ld_wait();
+                    for (int e0 = 0; e0 < last; e0 += 16) {
+                        uint64_t x[8];
+                        tokens(e0, pack2(mine, mine), t < valid ? t : 0, x);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int e = c * 16 + i;
-                            const float x = mine * norms[e] * __uint_as_float(d[i]) * ex2((w - s[e]) + (r - s[kQ + e]));
-                            to[e * kQ] = in && e < t ? x : 0.f;
+                        for (int i = 0; i < 8; ++i) {
+                            float a, b;
+                            unpack2(x[i], a, b);
+                            to[(e0 + 2 * i) * kQ] = a;
+                            to[(e0 + 2 * i + 1) * kQ] = b;
                         }
                     }
                 } else {
                     const float mine = norms[64 + t];
-                    unsigned char* to = smem + j * 2 * kPart + t * 128;
+                    unsigned char* to = p.work + ((size_t)chunk * p.H + h0 + j) * kBlock + kPOff + t * 128;
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t d[16], hi[8], lo[8];
-                        tmem_ld16_async(tmem + lanes + c * 16, d);
-                        tmem_ld_wait();
+                    for (int e0 = 0; e0 < 64; e0 += 16) {
+                        uint32_t hi[8], lo[8];
 #pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            float x[2];
+                        for (int i = 0; i < 8; ++i) hi[i] = lo[i] = 0u;
+                        if (e0 < last) {
+                            uint64_t x[8];
+                            tokens(e0, pack2(mine, mine), t < valid ? t + 1 : 0, x);
 #pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                const int e = c * 16 + i + q;
-                                const float y = mine * norms[e] * __uint_as_float(d[i + q]) * ex2((w - s[e]) + (r - s[kQ + e]));
-                                x[q] = in && e <= t ? y : 0.f;
-                            }
-                            two_parts(pack2(x[0], x[1]), hi[i / 2], lo[i / 2]);
+                            for (int i = 0; i < 8; ++i) two_parts(x[i], hi[i], lo[i]);
                         }
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            unsigned char* at = to + (((c * 2 + q) ^ (t & 7)) * 16);
+                            unsigned char* at = to + (((e0 / 8 + q) ^ (t & 7)) * 16);
                             *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
                             *reinterpret_cast<uint4*>(at + kPart) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
                         }
                     }
-                    proxy_fence();
                 }
             }
             __syncthreads();
-            if (tid == 64)
-                for (int j = 0; j < heads; ++j) bulk_s2g(p.work + ((size_t)chunk * p.H + h0 + j) * kBlock + kPOff, smem + j * 2 * kPart, 2 * kPart);
             // column `col` of T: element t takes -L[t][s] T[s] from every s before it
             const int head = warp >> 1, col = (tid & 63) ^ ((blockIdx.x & 1) * 32);
             if (head < heads) {
                 uint64_t T[32];
 #pragma unroll
                 for (int i = 0; i < 32; ++i) T[i] = pack2(2 * i == col ? 1.f : 0.f, 2 * i + 1 == col ? 1.f : 0.f);
-                const float* l = minus_l + head * kQ * kQ;
+                float* l = minus_l + head * kQ * kQ;
                 if (col < 32) take_rows<0>(T, l, std::make_integer_sequence<int, 32>{});
                 take_rows<32>(T, l, std::make_integer_sequence<int, 31>{});
-                // T - I in three parts: rows t of 128 bytes, this thread's two of each
-                unsigned char* to = p.work + ((size_t)chunk * p.H + h0 + head) * kBlock + kTOff + (col % 8) * 2;
+                const float beta = sums[head * 3 * kQ + 2 * kQ + col];
+                const uint64_t beta2 = pack2(beta, beta);
+                asm volatile("bar.sync %0, 64;" ::"r"(head + 1) : "memory");    // (nobody reads L of this head any more)
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    float x[2];
-                    unpack2(T[i], x[0], x[1]);
+                    float a, b;
+                    unpack2(mul2(T[i], beta2), a, b);
+                    l[2 * i * kQ + col] = 2 * i > col ? a : 0.f;
+                    l[(2 * i + 1) * kQ + col] = 2 * i + 1 > col ? b : 0.f;
+                }
+                asm volatile("bar.sync %0, 64;" ::"r"(head + 1) : "memory");
+                // T - diag in two parts: eight elements of a row at a time (eight rows of 128 bytes are all banks, whichever piece of them)
+                unsigned char* to = p.work + ((size_t)chunk * p.H + h0 + head) * kBlock + kTOff;
+                const int piece = tid & 7;
+#pragma unroll 1
+                for (int row = (tid & 63) >> 3; row < kQ; row += 8) {
+                    uint32_t a[2][4];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const int t = 2 * i + q;
-                        float y = t > col ? x[q] : 0.f;
-                        unsigned short* at = reinterpret_cast<unsigned short*>(to + t * 128 + (((col / 8) ^ (t & 7)) * 16));
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t top = __float_as_uint(y) & 0xffff0000u;
-                            at[e * (kPart / 2)] = (unsigned short)(top >> 16);
-                            y -= __uint_as_float(top);
-                        }
-                        at[2 * (kPart / 2)] = __bfloat16_as_ushort(__float2bfloat16_rn(y));
+                    for (int i = 0; i < 4; ++i) a[0][i] = a[1][i] = 0u;
+                    if (piece * 8 < row) {
+                        const ulonglong2* from = reinterpret_cast<const ulonglong2*>(l + row * kQ + piece * 8);
+                        const ulonglong2 u = from[0], v = from[1];
+                        two_parts(u.x, a[0][0], a[1][0]);
+                        two_parts(u.y, a[0][1], a[1][1]);
+                        two_parts(v.x, a[0][2], a[1][2]);
+                        two_parts(v.y, a[0][3], a[1][3]);
                     }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<uint4*>(to + e * kPart + row * 128 + ((piece ^ (row & 7)) * 16)) = make_uint4(a[e][0], a[e][1], a[e][2], a[e][3]);
                 }
             }
-            if (tid == 64) tma_store_done();
         }
+        if (tid == 64) tma_store_done();
         if (!ok && tid == 0) record_fault(p.status, kFaultScanWait, 11);
     }
     tc_fence_before();
@@ -347,44 +382,53 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
 
 // ---- the chunks of a sequence, one after another ------------------------------------------------------------------------------
 //
-// Roles: warp 0 issues the copies, warp 1 the products; warps 4..11 hold the state, a lane of tensor memory and half of what is there to
-// split a thread (64 keys' channels of S, 32 tokens of X, U, W and Y).  They meet through mbarriers alone; every wait is bounded.
-// Operands go over in quarters (16 tokens, 32 channels), products follow them as they come; T and P are lower triangular, a quarter of
-// them meets the tokens from itself on only.
-// Tensor memory: three parts of S, whose place W K takes once Q S^T is there; three parts of X, then of W, and two of U; K S^T, then
-// (T - I) X; Y.
+// Roles: warp 0 issues the copies, warp 1 the products; warp 2 brings two tokens of every value column together and finds the columns' largest
+// values, warp 3 takes Y apart again and stores it; warps 4..11 hold the state, a lane of tensor memory and half of what is there to split
+// a thread (64 keys' channels of S, 32 tokens of X, U, W and Y).  They meet through mbarriers alone; every wait is bounded.
+// A chunk is a chain of four products and what stands between them: K S^T, X, (T - diag) X, W, W K, S.  Everything else is done while a product
+// of the chain runs: the last chunk's Y and the next one's V behind K S^T, U and the queries' part of Y behind W K.
+// T and P are lower triangular, 16 tokens of them meet the tokens from themselves on only.
+// Tensor memory: two parts of S, of X, then of W, and of U; K S^T, then (T - diag) X; Y; W K.
+//
+// What bounds it: the splitting.  Conversions, comparisons and two-element multiply-adds all issue every other cycle of a scheduler, and an
+// arrival at a barrier costs a warp 26 of its scheduler's cycles, a poll 16: few warps, and few barriers between them (sixteen warps with
+// a barrier for every quarter took half as long again).
 
-constexpr int kThreads = 384;
-constexpr uint32_t kKOff = 0, kQOff = 2 * kPart, kVOff = 4 * kPart, kWOff = 6 * kPart;
-constexpr uint32_t kStage = (kWOff + kBlock + 1023u) & ~1023u;
-constexpr uint32_t kBarOff = 2 * kStage;
-enum { bFull = 0, bEmpty = 2, bS = 4, bX = 8, bRead = 9, bXP = 10, bU = 14, bWP = 15, bProd = 19, bAsk = 20, bScaled = 21, bY = 22, bYFree = 23, kBars = 24 };
-constexpr uint32_t kMarkOff = kBarOff + kBars * 8u + 16u;        // [128]: see mark_of
-constexpr uint32_t kSmemTc = kMarkOff + 128u * 4u + 1024u;
+constexpr int kWarps = 8, kThreads = 32 * (4 + kWarps);
+constexpr uint32_t kWOff = kRows, kStage = (kWOff + kBlock + 1023u) & ~1023u;
+constexpr uint32_t kVOff = 2 * kStage;                 // two buffers: rows of 256 bytes, then pairs of rows, [32][128] pairs of bf16
+constexpr uint32_t kYOff = kVOff + 4 * kPart;          // the same
+constexpr uint32_t kBarOff = kYOff + 2 * kPart;
+enum { bFull = 0, bEmpty = 2, bRaw = 4, bFullV = 6, bEmptyV = 8, bS = 10, bXP = 12, bWP = 13, bUP = 14, bX = 15, bU = 16, bProd = 17, bAsk = 18, bY = 19, bOut = 20,
+       bOutFree = 21, bJoin = 22, kBars = 23 };
+constexpr uint32_t kMarkOff = kBarOff + (kBars + 1) * 8u + 16u;  // [128]: see mark_of
+constexpr uint32_t kLargeOff = kMarkOff + 128u * 4u;             // [4][128]: the largest values of chunk n at n & 3
+constexpr uint32_t kMostOff = kLargeOff + 512u * 4u;             // [2][2][128]: the largest elements of the state, by halves
+constexpr uint32_t kSmemTc = kMostOff + 512u * 4u + 1024u;
 
-// columns of tensor memory: parts of S (half h, part i: 96 h + 32 i), W K; parts of X and W, of U (part i, tokens s: 32 i + s / 2); K S^T and (T - I) X; Y
-constexpr uint32_t cS = 0, cW = 192, cU = 288, cX = 352, cY = 416;
+// columns of tensor memory: parts of S (part i, channel k: 64 i + k / 2); of X and W, of U (part i, token s: 32 i + s / 2); K S^T and (T - diag) X; Y; W K
+constexpr uint32_t cS = 0, cW = 128, cU = 192, cX = 256, cY = 320, cP = 384;
 
 // The products take every token's values into every token, and a zero weight times NaN or infinity is NaN: from a lane's first value
 // that is not finite on, zeros go to the products, and the lane's outputs and state become NaN afterwards.  A mark of chunk n holds that
 // token; the largest of several is the first token of the latest chunk, so that marks need no clearing.
 __device__ __forceinline__ uint32_t mark_of(int n, int token) { return ((uint32_t)n << 7) + (uint32_t)(kQ - token); }
 
+__device__ __forceinline__ bool finite16(uint32_t bf) { return (bf & 0x7f80u) != 0x7f80u; }
+
 __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid_constant__ DeltaArgs g) {
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kBarOff);
-    uint32_t* slot = reinterpret_cast<uint32_t*>(bar + kBars);
+    uint32_t* slot = reinterpret_cast<uint32_t*>(bar + kBars + 1);
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kMarkOff);
     const DeltaParams& p = g.p;
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 32) { prefetch_map(&g.tq); prefetch_map(&g.tk); prefetch_map(&g.tv); }
+    if (tid == 32) prefetch_map(&g.tv);
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
-            int n = 1;                                  // copies and commits of products arrive once
-            if (i == bEmpty || i == bEmpty + 1) n = 9;  // the products' commit and the eight warps
-            if ((i >= bS && i < bX) || (i >= bXP && i < bU) || (i >= bWP && i < bProd)) n = 4;      // the four warps of a quarter
-            if (i == bRead || i == bScaled || i == bYFree) n = 8;
+            int n = 1;                                  // copies, commits of products and single warps arrive once
+            if (i == bEmptyV || i == bEmptyV + 1 || (i >= bS && i < bX) || i == bOut || i == bJoin) n = kWarps;
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -413,14 +457,9 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     ok = n < 2 || mbar_wait_bounded(bar + bEmpty + b, (n / 2 - 1) & 1);
                     if (!ok) break;
                     unsigned char* to = smem + b * kStage;
-                    mbar_expect_tx(bar + bFull + b, 6 * kPart + kBlock);
-                    tma_load(to + kKOff, &g.tk, group * 128, t, bar + bFull + b);
-                    tma_load(to + kKOff + kPart, &g.tk, group * 128 + 64, t, bar + bFull + b);
+                    mbar_expect_tx(bar + bFull + b, kRows + kBlock);
+                    bulk_g2s(to, g.rows + ((size_t)chunk * p.G + group) * kRows, kRows, bar + bFull + b);
                     bulk_g2s(to + kWOff, p.work + ((size_t)chunk * p.H + head) * kBlock, kBlock, bar + bFull + b);
-                    tma_load(to + kVOff, &g.tv, head * 128, t, bar + bFull + b);
-                    tma_load(to + kVOff + kPart, &g.tv, head * 128 + 64, t, bar + bFull + b);
-                    tma_load(to + kQOff, &g.tq, group * 128, t, bar + bFull + b);
-                    tma_load(to + kQOff + kPart, &g.tq, group * 128 + 64, t, bar + bFull + b);
                 }
             }
             if (!ok) record_fault(p.status, kFaultScanWait, 12);
@@ -437,35 +476,26 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             const int2 rows = seq_rows(p.pr, seq);
             const bool fresh0 = seq_resume(p.pr, seq) < 0;
             for (int t = rows.x; t < rows.y && ok; t += kQ, ++n) {
-                const int b = n & 1, valid = min(kQ, rows.y - t);
+                const int b = n & 1;
                 const bool live = !(fresh0 && t == rows.x);                      // S is not zero
                 const uint32_t base = sbase + b * kStage;
-                const uint64_t dk = swizzled_desc(base + kKOff, 16u, 1024u), dq = swizzled_desc(base + kQOff, 16u, 1024u);
+                const uint64_t dk = swizzled_desc(base, 16u, 1024u), dq = swizzled_desc(base + kPart, 16u, 1024u);
                 const uint64_t dt = swizzled_desc(base + kWOff + kTOff, 16u, 1024u), dp = swizzled_desc(base + kWOff + kPOff, 16u, 1024u);
-                const uint64_t dkt = swizzled_desc(base + kKOff, kPart, 1024u);
+                const uint64_t dkt = swizzled_desc(base, 2 * kPart, 1024u);
                 ok = warp_wait(bar + bFull + b, (n / 2) & 1);
                 if (!ok) break;
-                if (valid < kQ) {                        // rows of the next sequence are no part of this one
-                    for (int r = valid + lane / 8; r < kQ; r += 4) {
-                        unsigned char* k = smem + b * kStage + kKOff + r * 128 + lane % 8 * 16;
-                        *reinterpret_cast<uint4*>(k) = *reinterpret_cast<uint4*>(k + kPart) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    proxy_fence();
-                    __syncwarp();
-                }
-                if (live) {                              // K S^T: 32 channels at a time, three parts
+                if (live) {                              // K S^T: first the first 32 channels of both halves
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int q = i / 2 + i % 2 * 2;                         // quarters 0, 2, 1, 3
-                        ok = ok && warp_wait(bar + bS + q, m & 1);
+                    for (int i = 0; i < 2; ++i) {
+                        ok = ok && warp_wait(bar + bS + i, m & 1);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
-                        for (int e = 0; e < 6; ++e) {                            // (two steps of 16 channels, three parts)
-                            const int step = e & 1, part = e >> 1;
+                        for (int e = 0; e < 8; ++e) {                            // (two halves, two steps of 16 channels, two parts)
+                            const int half = e >> 2, step = (e >> 1) & 1, part = e & 1;
                             if (elect())
-                                mma_ts(tmem + cX, tmem + cS + (q / 2) * 96 + part * 32 + (q & 1) * 16 + step * 8,
-                                       dk + (uint32_t)(q / 2) * (kPart >> 4) + (uint32_t)((q & 1) * 2 + step) * 2u, kN64, i > 0 || e > 0);
+                                mma_ts(tmem + cX, tmem + cS + part * 64 + half * 32 + i * 16 + step * 8,
+                                       dk + (uint32_t)half * (2 * kPart >> 4) + (uint32_t)(i * 2 + step) * 2u, kN64, i > 0 || e > 0);
                         }
                         __syncwarp();
                     }
@@ -473,61 +503,45 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     if (elect()) tc_commit(bar + bX);
                     __syncwarp();
                 }
-                // (T - I) X, 16 tokens at a time
-                ok = warp_wait(bar + bRead, n & 1);
+                ok = warp_wait(bar + bXP, n & 1);
+                if (!ok) break;
+                tc_fence_after();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int q = i / 2 + i % 2 * 2;
-                    ok = ok && warp_wait(bar + bXP + q, n & 1);
-                    if (!ok) break;
-                    tc_fence_after();
+                for (int q = 0; q < 4; ++q) {            // (T - diag) X, 16 tokens at a time
                     const uint32_t desc = kTypes | ((uint32_t)((64 - 16 * q) >> 3) << 17);
                     const uint64_t rows_q = dt + (uint32_t)q * (2048u >> 4) + (uint32_t)q * 2u;
 #pragma unroll
-                    for (int e = 0; e < 6; ++e) {                                // parts (T, X): 00 01 10 11 02 20
-                        const int tp = e == 2 || e == 3 ? 1 : e == 5 ? 2 : 0, xp = e == 1 || e == 3 ? 1 : e == 4 ? 2 : 0;
-                        if (elect()) mma_ts(tmem + cX + 16 * q, tmem + cW + xp * 32 + q * 8, rows_q + (uint32_t)tp * (kPart >> 4), desc, i > 0 || e > 0);
-                    }
-                    __syncwarp();
+                    for (int e = 0; e < 3; ++e)                                  // parts (T, X): 00 01 10
+                        if (elect())
+                            mma_ts(tmem + cX + 16 * q, tmem + cW + (e == 1) * 32 + q * 8, rows_q + (uint32_t)(e == 2) * (kPart >> 4), desc, q > 0 || e > 0);
                 }
-                if (!ok) break;
                 if (elect()) tc_commit(bar + bU);
                 __syncwarp();
-                ok = n < 1 || warp_wait(bar + bYFree, (n - 1) & 1);
+                ok = n < 1 || warp_wait(bar + bOut, (n - 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                if (live) {                              // Q S^T in two parts
+                if (live) {                              // Q S^T
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int part = i >> 3, k = i & 7;
                         if (elect())
-                            mma_ts(tmem + cY, tmem + cS + (k / 4) * 96 + part * 32 + (k & 3) * 8, dq + (uint32_t)(k / 4) * (kPart >> 4) + (uint32_t)(k & 3) * 2u,
-                                   kN64, i > 0);
+                            mma_ts(tmem + cY, tmem + cS + part * 64 + k * 8, dq + (uint32_t)(k / 4) * (2 * kPart >> 4) + (uint32_t)(k & 3) * 2u, kN64, i > 0);
                     }
                     if (elect()) tc_commit(bar + bAsk);
                     __syncwarp();
-                    ok = warp_wait(bar + bAsk, m & 1);   // (W K takes the place of S)
+                    ++m;
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {            // W K, 16 tokens at a time
-                    const int q = i / 2 + i % 2 * 2;
-                    ok = ok && warp_wait(bar + bWP + q, n & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (elect()) mma_ts(tmem + cS, tmem + cW + e * 32 + q * 8, dkt + (uint32_t)q * 128u, kProdDesc, i > 0 || e > 0);
-                    __syncwarp();
-                }
+                ok = warp_wait(bar + bWP, n & 1);
                 if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)              // W K
+                    if (elect()) mma_ts(tmem + cP, tmem + cW + (e & 1) * 32 + (e >> 1) * 8, dkt + (uint32_t)(e >> 1) * 128u, kProdDesc, e > 0);
                 if (elect()) tc_commit(bar + bProd);
                 __syncwarp();
-                if (live) {
-                    ok = warp_wait(bar + bScaled, m & 1);
-                    ++m;
-                    if (!ok) break;
-                    tc_fence_after();
-                }
+                ok = warp_wait(bar + bUP, n & 1);
+                if (!ok) break;
+                tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {            // U P
                     const uint32_t desc = kTypes | ((uint32_t)((64 - 16 * q) >> 3) << 17);
@@ -537,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         if (elect())
                             mma_ts(tmem + cY + 16 * q, tmem + cU + (e == 1) * 32 + q * 8, rows_q + (uint32_t)(e == 2) * (kPart >> 4), desc, live || q > 0 || e > 0);
                 }
-                if (elect()) {
+                if (elect()) {                           // (what the other warps read of the stage they have read: U is made of it)
                     tc_commit(bar + bY);
                     tc_commit(bar + bEmpty + b);
                 }
@@ -546,52 +560,209 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 13);
         __syncwarp();
-    } else if (warp < 4) {
+    } else if (warp == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // V, copied a chunk ahead: four columns a lane; two rows at a time become one of pairs, in their place
+        int next_u = (int)blockIdx.x, next_n = 0;
+        int2 next = next_u < g.units ? seq_rows(p.pr, next_u / p.H) : make_int2(0, 0);
+        auto copy = [&]() {                              // the next copy, if there is one
+            while (next_u < g.units && next.x >= next.y) {
+                next_u += (int)gridDim.x;
+                if (next_u < g.units) next = seq_rows(p.pr, next_u / p.H);
+            }
+            if (next_u >= g.units) return;
+            const int b = next_n & 1;
+            ok = ok && (next_n < 2 || warp_wait(bar + bEmptyV + b, (next_n / 2 - 1) & 1));
+            if (!ok) return;
+            if (lane == 0) {
+                mbar_expect_tx(bar + bRaw + b, 2 * kPart);
+                tma_load(smem + kVOff + b * 2 * kPart, &g.tv, next_u % p.H * 128, next.x, bar + bRaw + b);
+            }
+            __syncwarp();
+            ++next_n;
+            next.x += kQ;
+        };
+        copy();
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
+            const int2 rows = seq_rows(p.pr, u / p.H);
+            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
+                const int b = n & 1, valid = min(kQ, rows.y - t);
+                copy();
+                ok = ok && warp_wait(bar + bRaw + b, (n / 2) & 1);
+                if (!ok) break;
+                unsigned char* v = smem + kVOff + b * 2 * kPart;
+                uint32_t top[4] = {0u, 0u, 0u, 0u};
+#pragma unroll 1
+                for (int r = 0; r < 32; r += 4) {
+                    uint2 a[4], c[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        a[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + lane * 8);
+                        c[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + 256 + lane * 8);
+                    }
+                    if (2 * r + 8 > valid) {             // rows of the next sequence are no part of this one
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (2 * (r + i) >= valid) a[i] = make_uint2(0u, 0u);
+                            if (2 * (r + i) + 1 >= valid) c[i] = make_uint2(0u, 0u);
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 w = make_uint4(__byte_perm(a[i].x, c[i].x, 0x5410), __byte_perm(a[i].x, c[i].x, 0x7632), __byte_perm(a[i].y, c[i].y, 0x5410),
+                                                   __byte_perm(a[i].y, c[i].y, 0x7632));
+                        *reinterpret_cast<uint4*>(v + (r + i) * 512 + lane * 16) = w;
+                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[0]) : "r"(w.x & 0x7fff7fffu));
+                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[1]) : "r"(w.y & 0x7fff7fffu));
+                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[2]) : "r"(w.z & 0x7fff7fffu));
+                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[3]) : "r"(w.w & 0x7fff7fffu));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!finite16(top[i]) || !finite16(top[i] >> 16)) {          // (tokens before it keep their accuracy: of those that are finite)
+                        top[i] = 0u;
+                        __threadfence_block();
+#pragma unroll 1
+                        for (int r = 0; r < 32; ++r) {
+                            const uint32_t w = *reinterpret_cast<const volatile uint32_t*>(v + r * 512 + lane * 16 + i * 4) & 0x7fff7fffu;
+                            asm("max.bf16x2 %0, %0, %1;" : "+r"(top[i]) : "r"((finite16(w) ? w & 0xffffu : 0u) | (finite16(w >> 16) ? w & 0xffff0000u : 0u)));
+                        }
+                    }
+                }
+                float4 large;
+                large.x = fmaxf(__uint_as_float(top[0] << 16), __uint_as_float(top[0] & 0xffff0000u));
+                large.y = fmaxf(__uint_as_float(top[1] << 16), __uint_as_float(top[1] & 0xffff0000u));
+                large.z = fmaxf(__uint_as_float(top[2] << 16), __uint_as_float(top[2] & 0xffff0000u));
+                large.w = fmaxf(__uint_as_float(top[3] << 16), __uint_as_float(top[3] & 0xffff0000u));
+                *reinterpret_cast<float4*>(smem + kLargeOff + (n & 3) * 512 + lane * 16) = large;
+                proxy_fence();                           // (the next copy writes where this warp has)
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(bar + bFullV + b);
+            }
+        }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 16);
+        // (as above)
+        for (int i = next_n < 2 ? 0 : next_n - 2; i < next_n; ++i) mbar_wait_bounded(bar + (ok ? bEmptyV : bRaw) + (i & 1), (i / 2) & 1, ok ? 1u << 22 : 1u << 16);
+        __syncwarp();
+    } else if (warp == 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // Y: four columns a lane, two rows at a time
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
+            const int head = u % p.H, seq = u / p.H;
+            const int2 rows = seq_rows(p.pr, seq);
+            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
+                const int valid = min(kQ, rows.y - t);
+                ok = warp_wait(bar + bOut, n & 1);
+                if (!ok) break;
+                unsigned char* to = static_cast<unsigned char*>(p.out) + ((long long)t * p.out_stride + (long long)head * 128 + lane * 4) * 2;
+                const long long step = p.out_stride * 2;
+#pragma unroll 4
+                for (int r = 0; r < 32; ++r) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(smem + kYOff + r * 512 + lane * 16);
+                    if (2 * r < valid) *reinterpret_cast<uint2*>(to) = make_uint2(__byte_perm(w.x, w.y, 0x5410), __byte_perm(w.z, w.w, 0x5410));
+                    to += step;
+                    if (2 * r + 1 < valid) *reinterpret_cast<uint2*>(to) = make_uint2(__byte_perm(w.x, w.y, 0x7632), __byte_perm(w.z, w.w, 0x7632));
+                    to += step;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(bar + bOutFree);
+            }
+        }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 15);
+        __syncwarp();
     } else {
         // (384 threads start with 168 registers: 128 x 56 + 256 x 224 of 64512)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int quad = warp & 3, half = (warp - 4) >> 2, col = quad * 32 + lane;       // value column; half of the channels and tokens
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        uint64_t S[32];                                 // channels 64 half ..
+        const float* large = reinterpret_cast<const float*>(smem + kLargeOff) + col;
+        float* most = reinterpret_cast<float*>(smem + kMostOff) + col;
+        uint64_t S[32];                                 // channels 64 half .., times `up`
+        uint32_t f[16];                                 // the next chunk's values of this half, two tokens each
+        float up = 1.f, down = 1.f;                     // the lane's scale and its inverse
+        float length = 0.f;                             // bounds the length of the lane's state before the chunk
+        int units = 0;                                  // with tokens, so far
         auto arrive = [&](int i) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_one(bar + i);
         };
-        // S as an operand: 16 columns of a part for 32 channels
-        auto give_state = [&]() {
+        auto fetch = [&](int c) {
+            const int b = c & 1;
+            ok = warp_wait(bar + bFullV + b, (c / 2) & 1);
+            if (!ok) return;
+            const uint32_t* v = reinterpret_cast<const uint32_t*>(smem + kVOff + b * 2 * kPart) + half * 16 * 128 + col;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t a[3][8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) three_parts(S[q * 16 + c * 8 + i], a[0][i], a[1][i], a[2][i]);
-#pragma unroll
-                    for (int e = 0; e < 3; ++e) tmem_st8u(lanes + cS + half * 96 + e * 32 + q * 16 + c * 8, a[e]);
-                }
-                tmem_st_wait();
-                arrive(bS + half * 2 + q);
-            }
+            for (int i = 0; i < 16; ++i) f[i] = v[i * 128];
+            __syncwarp();
+            if (lane == 0) mbar_arrive_one(bar + bEmptyV + b);
         };
-        // Y of a chunk, behind the next one's X: where it goes, how many of this half's tokens there are, and from which on they are not finite
-        __nv_bfloat16* y_to = nullptr;
-        int y_tokens = 0, y_bad = 0, y_n = 0;
+        // The largest element of this half of the state, for the other half too.
+        auto state_most = [&](int c) {
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float a, d;
+                unpack2(S[i], a, d);
+                top = fmaxf(top, fmaxf(fabsf(a), fabsf(d)));
+            }
+            most[((c & 1) * 2 + half) * 128] = top * down;
+        };
+        auto length_of = [&](int c) {
+            const volatile float* from = most + (c & 1) * 256;
+            return 11.4f * fmaxf(from[0], from[128]);
+        };
+        // The scale for chunk c: where what bounds its values, times the scale, would be beyond 2^14 or below 2^9 (then the second parts would
+        // lose bits), a new one.  Returns the new scale over the old one.
+        auto rescale = [&](int c) {
+            const float all = 65.f * reinterpret_cast<const volatile float*>(large)[(c & 3) * 128] + length, now = all * up;
+            if (now <= 16384.f && (now >= 512.f || all == 0.f)) return 1.f;
+            const int e = max(-100, (int)((__float_as_uint(all) & 0x7f800000u) >> 23) - 127);     // (below 2^(e + 1); below 2^13 then)
+            const float old = down;
+            up = __uint_as_float((uint32_t)(127 + 12 - e) << 23);
+            down = __uint_as_float((uint32_t)(127 - 12 + e) << 23);
+            return up * old;
+        };
+        // Channels 32 i .. of this half of S as an operand.
+        auto give = [&](int i) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t a[2][8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) two_parts(S[i * 16 + c * 8 + j], a[0][j], a[1][j]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cS + e * 64 + half * 32 + i * 16 + c * 8, a[e]);
+            }
+            tmem_st_wait();
+            arrive(bS + i);
+        };
+        // Y of chunk y_n, times y_scale; from token y_bad of this half on it is not finite
+        int y_bad = 0, y_n = -1;
+        float y_scale = 0.f;
         auto write_y = [&]() {
-            ok = warp_wait(bar + bY, y_n & 1);
+            ok = warp_wait(bar + bY, y_n & 1) && (y_n < 1 || warp_wait(bar + bOutFree, (y_n - 1) & 1));
             if (!ok) return;
             tc_fence_after();
             uint32_t d[32];
             tmem_ld32_async(lanes + cY + half * 32, d);
             tmem_ld_wait();
-            arrive(bYFree);
-            __nv_bfloat16* to = y_to;
+            if (y_bad < 32) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                if (i < y_tokens) *to = __float2bfloat16_rn(i >= y_bad ? __int_as_float(0x7fffffff) : __uint_as_float(d[i]));
-                to += p.out_stride;
+                for (int i = 0; i < 32; ++i)
+                    if (i >= y_bad) d[i] = 0x7fffffffu;
             }
+            uint32_t* to = reinterpret_cast<uint32_t*>(smem + kYOff) + half * 16 * 128 + col;
+            const uint64_t scale2 = pack2(y_scale, y_scale);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float a, c;
+                unpack2(mul2(scale2, pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]))), a, c);
+                const __nv_bfloat162 h = __floats2bfloat162_rn(a, c);
+                to[i * 128] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            arrive(bOut);
         };
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const int head = u % p.H, seq = u / p.H;
@@ -602,148 +773,164 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 const float* from = p.state + (size_t)src * p.H * 128 * 128 + at;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) S[i] = pack2(from[2 * i * 128], from[(2 * i + 1) * 128]);
-                if (rows.x < rows.y) give_state();
             } else {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) S[i] = 0ull;
             }
+            up = down = 1.f;
+            if (rows.x < rows.y) {
+                fetch(n);
+                if (!ok) break;
+                state_most(n);
+                arrive(bJoin);
+                ok = warp_wait(bar + bJoin, units & 1);
+                ++units;
+                if (!ok) break;
+                length = length_of(n);
+                const float r = rescale(n);
+                const uint64_t r2 = pack2(r, r);
+                if (src >= 0) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) S[i] = mul2(r2, S[i]);
+                    give(0);
+                    give(1);
+                }
+            }
             for (int t = rows.x; t < rows.y; t += kQ, ++n) {
-                const int b = n & 1, valid = min(kQ, rows.y - t);
-                const bool live = src >= 0 || t > rows.x;
-                const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff);
+                const int b = n & 1, left = rows.y - t - half * 32;              // tokens of the sequence from this half on
+                const bool live = src >= 0 || t > rows.x, more = t + kQ < rows.y;
+                const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff) + half * 32;
+                if (y_n >= 0) {
+                    write_y();
+                    if (!ok) break;
+                }
                 ok = warp_wait(bar + bFull + b, (n / 2) & 1);
                 if (!ok) break;
-                // X of this half's tokens
+                // X of this half's tokens: the values, scaled (times powers of two in bf16), less what the state has for their keys
                 uint64_t X[16];
                 {
-                    const unsigned char* v = smem + b * kStage + kVOff + (col >> 6) * kPart + half * 32 * 128 + (col & 7) * 2;
-                    const int cv = (col & 63) >> 3;
-                    const ulonglong2* be = reinterpret_cast<const ulonglong2*>(gate + kBeta + half * 32);
+                    const uint32_t up16 = __float_as_uint(up) >> 16;
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        float f[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int s = 2 * i + e;
-                            const uint32_t w = *reinterpret_cast<const unsigned short*>(v + s * 128 + ((cv ^ (s & 7)) * 16));
-                            f[e] = half * 32 + s < valid ? __uint_as_float(w << 16) : 0.f;
-                        }
-                        const ulonglong2 bb = be[i / 2];
-                        X[i] = mul2(bb.x, pack2(f[0], f[1]));
-                        X[i + 1] = mul2(bb.y, pack2(f[2], f[3]));
+                    for (int i = 0; i < 16; ++i) {
+                        float a, c;
+                        asm("{\n\t.reg .b16 l, h, s, x;\n\tmov.b32 {l, h}, %2;\n\tmov.b32 {s, x}, %3;\n\t"
+                            "fma.rn.f32.bf16 %0, l, s, 0f00000000;\n\tfma.rn.f32.bf16 %1, h, s, 0f00000000;\n\t}"
+                            : "=f"(a), "=f"(c)
+                            : "r"(f[i]), "r"(up16));
+                        X[i] = pack2(a, c);
                     }
                 }
+                // What bounds the next chunk's state: from the state itself every eighth chunk (the halves meet behind the next product), else
+                // from the length before and what the tokens add to it.
+                const bool look = (n & 7) == 7;
+                if (more) {
+                    if (look) state_most(n);
+                    fetch(n + 1);
+                    if (!ok) break;
+                }
+                uint32_t d[32];
                 if (live) {
                     ok = warp_wait(bar + bX, m & 1);
                     if (!ok) break;
                     tc_fence_after();
-                }
-                uint32_t d[32];
-                if (live) {
                     tmem_ld32_async(lanes + cX + half * 32, d);
                     tmem_ld_wait();
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) d[i] = 0u;
                 }
-                arrive(bRead);
-                uint64_t odd = 0ull;
                 {
-                    const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead + half * 32);
-                    const uint64_t minus = pack2(-1.f, -1.f);
-                    const int left = valid - half * 32;
+                    const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead);
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const ulonglong2 r = rd[i / 2];
-                        // (rows behind the sequence: their scales are zeros, but what the products left of them may be anything)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (2 * i + e >= left) d[2 * i + e] = 0u;
-                        X[i] = fma2(mul2(r.x, minus), pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1])), X[i]);
-                        X[i + 1] = fma2(mul2(r.y, minus), pack2(__uint_as_float(d[2 * i + 2]), __uint_as_float(d[2 * i + 3])), X[i + 1]);
-                        odd = fma2(X[i], 0ull, odd);
-                        odd = fma2(X[i + 1], 0ull, odd);
+                    for (int i = 0; i < 8; ++i) {
+                        const ulonglong2 r = rd[i];
+                        if (live) {
+                            X[2 * i] = fma2(r.x, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]);
+                            X[2 * i + 1] = fma2(r.y, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]);
+                        } else {                         // (a key that is not finite counts, whatever it is taken of)
+                            X[2 * i] = fma2(r.x, 0ull, X[2 * i]);
+                            X[2 * i + 1] = fma2(r.y, 0ull, X[2 * i + 1]);
+                        }
                     }
                 }
                 {
-                    float o0, o1;
-                    unpack2(odd, o0, o1);
-                    if (!(o0 + o1 == 0.f)) {
-                        int first = kQ;
+                    uint32_t a[2][16], odd = 0u;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        two_parts(X[i], a[0][i], a[1][i]);
+                        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(a[0][i] & 0x7fff7fffu));
+                    }
+                    if ((odd & 0x7c00u) == 0x7c00u || (odd & 0x7c000000u) == 0x7c000000u) {
+                        int first = 32;
 #pragma unroll
                         for (int i = 15; i >= 0; --i) {
-                            float a, c;
-                            unpack2(X[i], a, c);
-                            if (!(fabsf(c) <= 3.4028235e38f)) first = half * 32 + 2 * i + 1;
-                            if (!(fabsf(a) <= 3.4028235e38f)) first = half * 32 + 2 * i;
+                            if ((a[0][i] & 0x7c000000u) == 0x7c000000u) first = 2 * i + 1;
+                            if ((a[0][i] & 0x7c00u) == 0x7c00u) first = 2 * i;
                         }
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            float a, c;
-                            unpack2(X[i], a, c);
-                            X[i] = pack2(half * 32 + 2 * i >= first ? 0.f : a, half * 32 + 2 * i + 1 >= first ? 0.f : c);
+                            const uint32_t keep = (2 * i < first ? 0xffffu : 0u) | (2 * i + 1 < first ? 0xffff0000u : 0u);
+                            a[0][i] &= keep;
+                            a[1][i] &= keep;
                         }
-                        atomicMax(marks + col, mark_of(n + 1, first));
+                        if (first < left) atomicMax(marks + col, mark_of(n + 1, half * 32 + first));
                     }
-                }
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    uint32_t a[3][8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) three_parts(X[q * 8 + i], a[0][i], a[1][i], a[2][i]);
-#pragma unroll
-                    for (int e = 0; e < 3; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t lo[8] = {a[e][0], a[e][1], a[e][2], a[e][3], a[e][4], a[e][5], a[e][6], a[e][7]};
+                        const uint32_t hi[8] = {a[e][8], a[e][9], a[e][10], a[e][11], a[e][12], a[e][13], a[e][14], a[e][15]};
+                        tmem_st8u(lanes + cW + e * 32 + half * 16, lo);
+                        tmem_st8u(lanes + cW + e * 32 + half * 16 + 8, hi);
+                    }
                     tmem_st_wait();
-                    arrive(bXP + half * 2 + q);
-                }
-                if (y_to != nullptr) {
-                    write_y();
-                    if (!ok) break;
+                    arrive(bXP);
                 }
                 // U and W
                 ok = warp_wait(bar + bU, n & 1);
                 if (!ok) break;
                 tc_fence_after();
                 tmem_ld32_async(lanes + cX + half * 32, d);
-                tmem_ld_wait();
                 const uint32_t mark = reinterpret_cast<const volatile uint32_t*>(marks)[col];
                 const bool bad = (mark >> 7) == (uint32_t)n + 1u;
-                const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : kQ;
-                if (bad) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float a, c;
-                        unpack2(X[i], a, c);
-                        if (2 * i >= first) { a = 0.f; d[2 * i] = 0u; }
-                        if (2 * i + 1 >= first) { c = 0.f; d[2 * i + 1] = 0u; }
-                        X[i] = pack2(a, c);
-                    }
-                }
+                const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : 32;
+                const float keep = gate[kKeep - half * 32];
+                tmem_ld_wait();
                 {
-                    const ulonglong2* put = reinterpret_cast<const ulonglong2*>(gate + kPut + half * 32);
+                    const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const ulonglong2 be = beta[i];
+                        X[2 * i] = fma2(be.x, X[2 * i], pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])));
+                        X[2 * i + 1] = fma2(be.y, X[2 * i + 1], pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])));
+                    }
+                    if (first < 32) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float b0, b1;
+                            unpack2(X[i], b0, b1);
+                            X[i] = pack2(2 * i >= first ? 0.f : b0, 2 * i + 1 >= first ? 0.f : b1);
+                        }
+                    }
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        uint32_t a[3][8], w[2][8];
+                        uint32_t a[2][8];
 #pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            const int j = q * 8 + i;
-                            const ulonglong2 f = put[j / 2];
-                            const uint64_t u0 = add2(X[j], pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
-                            const uint64_t u1 = add2(X[j + 1], pack2(__uint_as_float(d[2 * j + 2]), __uint_as_float(d[2 * j + 3])));
-                            three_parts(mul2(f.x, u0), a[0][i], a[1][i], a[2][i]);
-                            three_parts(mul2(f.y, u1), a[0][i + 1], a[1][i + 1], a[2][i + 1]);
-                            two_parts(u0, w[0][i], w[1][i]);
-                            two_parts(u1, w[0][i + 1], w[1][i + 1]);
+                        for (int i = 0; i < 4; ++i) {
+                            const ulonglong2 w = put[q * 4 + i];
+                            two_parts(mul2(w.x, X[q * 8 + 2 * i]), a[0][2 * i], a[1][2 * i]);
+                            two_parts(mul2(w.y, X[q * 8 + 2 * i + 1]), a[0][2 * i + 1], a[1][2 * i + 1]);
                         }
 #pragma unroll
-                        for (int e = 0; e < 3; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
+                        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
+                    }
+                    tmem_st_wait();
+                    arrive(bWP);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, w[e]);
-                        tmem_st_wait();
-                        arrive(bWP + half * 2 + q);
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t a[2][8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) two_parts(X[q * 8 + i], a[0][i], a[1][i]);
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, a[e]);
                     }
                 }
-                const float keep = gate[kKeep];
                 if (live) {                              // Q S^T is there: its tokens' factors
                     ok = warp_wait(bar + bAsk, m & 1);
                     ++m;
@@ -751,48 +938,58 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     tc_fence_after();
                     tmem_ld32_async(lanes + cY + half * 32, d);
                     tmem_ld_wait();
-                    const float4* ask = reinterpret_cast<const float4*>(gate + kAsk + half * 32);
+                    const ulonglong2* ask = reinterpret_cast<const ulonglong2*>(gate + kAsk);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float4 f = ask[2 * i], h = ask[2 * i + 1];
-                        const float w[8] = {f.x, f.y, f.z, f.w, h.x, h.y, h.z, h.w};
                         uint32_t r[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) r[e] = __float_as_uint(w[e] * __uint_as_float(d[8 * i + e]));
+                        for (int e = 0; e < 2; ++e) {
+                            const ulonglong2 w = ask[2 * i + e];
+                            const uint64_t y0 = mul2(w.x, pack2(__uint_as_float(d[8 * i + 4 * e]), __uint_as_float(d[8 * i + 4 * e + 1])));
+                            const uint64_t y1 = mul2(w.y, pack2(__uint_as_float(d[8 * i + 4 * e + 2]), __uint_as_float(d[8 * i + 4 * e + 3])));
+                            r[4 * e] = (uint32_t)y0;
+                            r[4 * e + 1] = (uint32_t)(y0 >> 32);
+                            r[4 * e + 2] = (uint32_t)y1;
+                            r[4 * e + 3] = (uint32_t)(y1 >> 32);
+                        }
                         tmem_st8u(lanes + cY + half * 32 + 8 * i, r);
                     }
-                    tmem_st_wait();
-                    arrive(bScaled);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive_one(bar + bEmpty + b);
-                y_to = static_cast<__nv_bfloat16*>(p.out) + (long long)(t + half * 32) * p.out_stride + (long long)head * 128 + col;
-                y_tokens = valid - half * 32;
+                tmem_st_wait();
+                arrive(bUP);
                 y_bad = first;
                 y_n = n;
-                // S
+                y_scale = p.q_scale * down;
+                float r = down;
+                if (more) {
+                    length = (look ? length_of(n) : length) + 64.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
+                    r = rescale(n + 1);
+                }
+                const uint64_t r2 = pack2(r, r), keep2 = pack2(keep * r, keep * r);
+                const bool same = __all_sync(0xffffffffu, r == 1.f);
+                // S, times the next chunk's scale (behind the last chunk as it is)
                 ok = warp_wait(bar + bProd, n & 1);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t keep2 = pack2(keep, keep);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    tmem_ld32_async(lanes + cS + half * 64 + c * 32, d);
+                for (int i = 0; i < 2; ++i) {
+                    tmem_ld32_async(lanes + cP + half * 64 + i * 32, d);
                     tmem_ld_wait();
+                    if (same) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        S[c * 16 + i] = fma2(keep2, S[c * 16 + i], pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1])));
-                }
-                if (bad) {
-                    const float nan = __int_as_float(0x7fffffff);
+                        for (int j = 0; j < 16; ++j) S[i * 16 + j] = fma2(keep2, S[i * 16 + j], pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) S[i] = pack2(nan, nan);
+                        for (int j = 0; j < 16; ++j)
+                            S[i * 16 + j] = fma2(r2, pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])), mul2(keep2, S[i * 16 + j]));
+                    }
+                    if (bad) {
+                        const float nan = __int_as_float(0x7fffffff);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) S[i * 16 + j] = pack2(nan, nan);
+                    }
+                    if (more) give(i);
                 }
-                // (both halves of W K have been read: the parts take their place)
-                tc_fence_before();
-                asm volatile("bar.sync %0, 64;" ::"r"(quad + 1) : "memory");
-                tc_fence_after();
-                if (t + kQ < rows.y) give_state();
             }
             if (!ok) break;
             if (dst >= 0) {
@@ -806,7 +1003,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
             }
         }
-        if (ok && y_to != nullptr) write_y();
+        if (ok && y_n >= 0) write_y();
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 14);
     }
     tc_fence_before();
@@ -817,9 +1014,20 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
 
 }  // namespace
 
+// bf16 rows in tiles of 64 x 128 elements, as they are.
+static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t stride) {
+    const auto encode = tensor_map_encoder();
+    if (encode == nullptr) return false;
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {stride};
+    const cuuint32_t box[2] = {128, kQ}, steps[2] = {1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens) {
     if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens == 0) return 0;
-    return (size_t)(tokens / kQ + sequences) * c.heads * kBlock;
+    // (the groups are not known here: every head may be one)
+    return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows);
 }
 
 int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream) {
@@ -830,9 +1038,10 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     const long long preps = chunks * p.G * ((p.H / p.G + 1) / 2);
     if (units > (1 << 30) || preps > 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
     g.units = (int)units;
+    g.rows = p.work + (size_t)chunks * p.H * kBlock;
     if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
         !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ) ||
-        !make_map(&g.tv, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.v, (uint64_t)p.H * 128, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2, kQ)) {
+        !make_rows_map(&g.tv, p.v, (uint64_t)p.H * 128, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2)) {
         ctx->last_cuda_error = cudaErrorInvalidValue;
         return SKETCHSSM_CUDA_ERROR;
     }
