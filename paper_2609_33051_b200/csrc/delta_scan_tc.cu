@@ -384,9 +384,9 @@ __global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __gri
 //
 // Roles: warp 0 issues the copies, warp 1 the products; warp 2 brings two tokens of every value column together and finds the columns' largest
 // values, warp 3 takes Y apart again and stores it; warps 4..11 hold the state, a lane of tensor memory and half of what is there to split
-// a thread (64 keys' channels of S, 32 tokens of X, U, W and Y).  They meet through mbarriers alone; every wait is bounded.
+// a thread (64 keys' channels of S, 32 tokens of X, U and W); warps 12..15 scale Y, a lane a thread.  They meet through mbarriers alone; every wait is bounded.
 // A chunk is a chain of four products and what stands between them: K S^T, X, (T - diag) X, W, W K, S.  Everything else is done while a product
-// of the chain runs: the last chunk's Y and the next one's V behind K S^T, U and the queries' part of Y behind W K.
+// of the chain runs or by other warps: the next chunk's V behind K S^T, U behind W K.
 // T and P are lower triangular, 16 tokens of them meet the tokens from themselves on only.
 // Tensor memory: two parts of S, of X, then of W, and of U; K S^T, then (T - diag) X; Y; W K.
 //
@@ -394,17 +394,18 @@ __global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __gri
 // arrival at a barrier costs a warp 26 of its scheduler's cycles, a poll 16: few warps, and few barriers between them (sixteen warps with
 // a barrier for every quarter took half as long again).
 
-constexpr int kWarps = 8, kThreads = 32 * (4 + kWarps);
+constexpr int kWarps = 8, kThreads = 32 * (8 + kWarps);
 constexpr uint32_t kWOff = kRows, kStage = (kWOff + kBlock + 1023u) & ~1023u;
 constexpr uint32_t kVOff = 2 * kStage;                 // two buffers: rows of 256 bytes, then pairs of rows, [32][128] pairs of bf16
 constexpr uint32_t kYOff = kVOff + 4 * kPart;          // the same
 constexpr uint32_t kBarOff = kYOff + 2 * kPart;
 enum { bFull = 0, bEmpty = 2, bRaw = 4, bFullV = 6, bEmptyV = 8, bS = 10, bXP = 12, bWP = 13, bUP = 14, bX = 15, bU = 16, bProd = 17, bAsk = 18, bY = 19, bOut = 20,
-       bOutFree = 21, bJoin = 22, kBars = 23 };
-constexpr uint32_t kMarkOff = kBarOff + (kBars + 1) * 8u + 16u;  // [128]: see mark_of
+       bOutFree = 21, bJoin = 22, bScaled = 23, kBars = 24 };
+constexpr uint32_t kMarkOff = kBarOff + kBars * 8u + 16u;  // [128]: see mark_of
 constexpr uint32_t kLargeOff = kMarkOff + 128u * 4u;             // [4][128]: the largest values of chunk n at n & 3
 constexpr uint32_t kMostOff = kLargeOff + 512u * 4u;             // [2][2][128]: the largest elements of the state, by halves
-constexpr uint32_t kSmemTc = kMostOff + 512u * 4u + 1024u;
+constexpr uint32_t kAsideOff = kMostOff + 512u * 4u;              // [2][2][128]: for Y of chunk n at n & 1, its factor and the first token that is not finite
+constexpr uint32_t kSmemTc = kAsideOff + 512u * 4u + 1024u;
 
 // columns of tensor memory: parts of S (part i, channel k: 64 i + k / 2); of X and W, of U (part i, token s: 32 i + s / 2); K S^T and (T - diag) X; Y; W K
 constexpr uint32_t cS = 0, cW = 128, cU = 192, cX = 256, cY = 320, cP = 384;
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kBarOff);
-    uint32_t* slot = reinterpret_cast<uint32_t*>(bar + kBars + 1);
+    uint32_t* slot = reinterpret_cast<uint32_t*>(bar + kBars);
     uint32_t* marks = reinterpret_cast<uint32_t*>(smem + kMarkOff);
     const DeltaParams& p = g.p;
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -428,7 +429,8 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     if (tid == 0) {
         for (int i = 0; i < kBars; ++i) {
             int n = 1;                                  // copies, commits of products and single warps arrive once
-            if (i == bEmptyV || i == bEmptyV + 1 || (i >= bS && i < bX) || i == bOut || i == bJoin) n = kWarps;
+            if (i == bEmptyV || i == bEmptyV + 1 || (i >= bS && i < bX) || i == bJoin) n = kWarps;
+            if (i == bOut || i == bScaled) n = 4;
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -529,7 +531,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     }
                     if (elect()) tc_commit(bar + bAsk);
                     __syncwarp();
-                    ++m;
                 }
                 ok = warp_wait(bar + bWP, n & 1);
                 if (!ok) break;
@@ -539,8 +540,9 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     if (elect()) mma_ts(tmem + cP, tmem + cW + (e & 1) * 32 + (e >> 1) * 8, dkt + (uint32_t)(e >> 1) * 128u, kProdDesc, e > 0);
                 if (elect()) tc_commit(bar + bProd);
                 __syncwarp();
-                ok = warp_wait(bar + bUP, n & 1);
+                ok = warp_wait(bar + bUP, n & 1) && (!live || warp_wait(bar + bScaled, m & 1));
                 if (!ok) break;
+                if (live) ++m;
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {            // U P
@@ -551,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         if (elect())
                             mma_ts(tmem + cY + 16 * q, tmem + cU + (e == 1) * 32 + q * 8, rows_q + (uint32_t)(e == 2) * (kPart >> 4), desc, live || q > 0 || e > 0);
                 }
-                if (elect()) {                           // (what the other warps read of the stage they have read: U is made of it)
+                if (elect()) {                           // (what the other warps read of the stage they have read: U and Y's factors)
                     tc_commit(bar + bY);
                     tc_commit(bar + bEmpty + b);
                 }
@@ -672,9 +674,86 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 15);
         __syncwarp();
+    } else if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        // Y of a value column: Q S^T times its tokens' factors, and what U P has added to it
+        const int col = (warp & 3) * 32 + lane;
+        const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + cY;
+        const float* aside = reinterpret_cast<const float*>(smem + kAsideOff) + col;
+        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
+            const int seq = u / p.H;
+            const int2 rows = seq_rows(p.pr, seq);
+            const int src = seq_resume(p.pr, seq);
+            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
+                if (src >= 0 || t > rows.x) {
+                    const float* gate = reinterpret_cast<const float*>(smem + (n & 1) * kStage + kWOff + kGOff) + kAsk;
+                    ok = warp_wait(bar + bFull + (n & 1), (n / 2) & 1) && warp_wait(bar + bAsk, m & 1);
+                    if (!ok) break;
+                    ++m;
+                    tc_fence_after();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t d[32];
+                        tmem_ld32_async(at + h * 32, d);
+                        tmem_ld_wait();
+                        const ulonglong2* ask = reinterpret_cast<const ulonglong2*>(gate + h * 32);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t r[8];
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const ulonglong2 w = ask[2 * i + e];
+                                const uint64_t y0 = mul2(w.x, pack2(__uint_as_float(d[8 * i + 4 * e]), __uint_as_float(d[8 * i + 4 * e + 1])));
+                                const uint64_t y1 = mul2(w.y, pack2(__uint_as_float(d[8 * i + 4 * e + 2]), __uint_as_float(d[8 * i + 4 * e + 3])));
+                                r[4 * e] = (uint32_t)y0;
+                                r[4 * e + 1] = (uint32_t)(y0 >> 32);
+                                r[4 * e + 2] = (uint32_t)y1;
+                                r[4 * e + 3] = (uint32_t)(y1 >> 32);
+                            }
+                            tmem_st8u(at + h * 32 + 8 * i, r);
+                        }
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_one(bar + bScaled);
+                }
+                ok = warp_wait(bar + bUP, n & 1);
+                if (!ok) break;
+                const float scale = reinterpret_cast<const volatile float*>(aside)[(n & 1) * 256];
+                const int first = __float_as_int(reinterpret_cast<const volatile float*>(aside)[(n & 1) * 256 + 128]);
+                ok = warp_wait(bar + bY, n & 1) && (n < 1 || warp_wait(bar + bOutFree, (n - 1) & 1));
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t scale2 = pack2(scale, scale);
+                uint32_t* to = reinterpret_cast<uint32_t*>(smem + kYOff) + col;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t d[32];
+                    tmem_ld32_async(at + h * 32, d);
+                    tmem_ld_wait();
+                    if (first < kQ) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (h * 32 + i >= first) d[i] = 0x7fffffffu;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float a, c;
+                        unpack2(mul2(scale2, pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]))), a, c);
+                        const __nv_bfloat162 y = __floats2bfloat162_rn(a, c);
+                        to[(h * 16 + i) * 128] = *reinterpret_cast<const uint32_t*>(&y);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_one(bar + bOut);
+            }
+        }
+        if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 17);
     } else {
-        // (384 threads start with 168 registers: 128 x 56 + 256 x 224 of 64512)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        // (512 threads start with 128 registers: 128 x 56 + 256 x 176 + 128 x 96 of 65536)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
         const int quad = warp & 3, half = (warp - 4) >> 2, col = quad * 32 + lane;       // value column; half of the channels and tokens
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const float* large = reinterpret_cast<const float*>(smem + kLargeOff) + col;
@@ -738,32 +817,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             tmem_st_wait();
             arrive(bS + i);
         };
-        // Y of chunk y_n, times y_scale; from token y_bad of this half on it is not finite
-        int y_bad = 0, y_n = -1;
-        float y_scale = 0.f;
-        auto write_y = [&]() {
-            ok = warp_wait(bar + bY, y_n & 1) && (y_n < 1 || warp_wait(bar + bOutFree, (y_n - 1) & 1));
-            if (!ok) return;
-            tc_fence_after();
-            uint32_t d[32];
-            tmem_ld32_async(lanes + cY + half * 32, d);
-            tmem_ld_wait();
-            if (y_bad < 32) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i >= y_bad) d[i] = 0x7fffffffu;
-            }
-            uint32_t* to = reinterpret_cast<uint32_t*>(smem + kYOff) + half * 16 * 128 + col;
-            const uint64_t scale2 = pack2(y_scale, y_scale);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                float a, c;
-                unpack2(mul2(scale2, pack2(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]))), a, c);
-                const __nv_bfloat162 h = __floats2bfloat162_rn(a, c);
-                to[i * 128] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            arrive(bOut);
-        };
         for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
             const int head = u % p.H, seq = u / p.H;
             const int2 rows = seq_rows(p.pr, seq);
@@ -800,10 +853,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 const int b = n & 1, left = rows.y - t - half * 32;              // tokens of the sequence from this half on
                 const bool live = src >= 0 || t > rows.x, more = t + kQ < rows.y;
                 const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff) + half * 32;
-                if (y_n >= 0) {
-                    write_y();
-                    if (!ok) break;
-                }
                 ok = warp_wait(bar + bFull + b, (n / 2) & 1);
                 if (!ok) break;
                 // X of this half's tokens: the values, scaled (times powers of two in bf16), less what the state has for their keys
@@ -829,55 +878,53 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     if (!ok) break;
                 }
                 uint32_t d[32];
+                const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead);
                 if (live) {
                     ok = warp_wait(bar + bX, m & 1);
                     if (!ok) break;
+                    ++m;
                     tc_fence_after();
                     tmem_ld32_async(lanes + cX + half * 32, d);
                     tmem_ld_wait();
-                }
-                {
-                    const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead);
+                } else {                                 // (a key that is not finite counts, whatever it is taken of)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const ulonglong2 r = rd[i];
-                        if (live) {
-                            X[2 * i] = fma2(r.x, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]);
-                            X[2 * i + 1] = fma2(r.y, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]);
-                        } else {                         // (a key that is not finite counts, whatever it is taken of)
-                            X[2 * i] = fma2(r.x, 0ull, X[2 * i]);
-                            X[2 * i + 1] = fma2(r.y, 0ull, X[2 * i + 1]);
-                        }
-                    }
+                    for (int i = 0; i < 32; ++i) d[i] = 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const ulonglong2 r = rd[i];
+                    X[2 * i] = fma2(r.x, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]);
+                    X[2 * i + 1] = fma2(r.y, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]);
                 }
                 {
-                    uint32_t a[2][16], odd = 0u;
+                    uint32_t a[4][8], odd = 0u;          // first parts of 16 tokens, of 16 more; second parts
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        two_parts(X[i], a[0][i], a[1][i]);
-                        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(a[0][i] & 0x7fff7fffu));
+                        two_parts(X[i], a[i / 8][i % 8], a[2 + i / 8][i % 8]);
+                        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(a[i / 8][i % 8] & 0x7fff7fffu));
                     }
-                    if ((odd & 0x7c00u) == 0x7c00u || (odd & 0x7c000000u) == 0x7c000000u) {
+                    auto store = [&]() {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) tmem_st8u(lanes + cW + (e >> 1) * 32 + half * 16 + (e & 1) * 8, a[e]);
+                    };
+                    const bool wild = (odd & 0x7c00u) == 0x7c00u || (odd & 0x7c000000u) == 0x7c000000u;
+                    if (!__any_sync(0xffffffffu, wild)) {
+                        store();
+                    } else {
                         int first = 32;
 #pragma unroll
                         for (int i = 15; i >= 0; --i) {
-                            if ((a[0][i] & 0x7c000000u) == 0x7c000000u) first = 2 * i + 1;
-                            if ((a[0][i] & 0x7c00u) == 0x7c00u) first = 2 * i;
+                            if ((a[i / 8][i % 8] & 0x7c000000u) == 0x7c000000u) first = 2 * i + 1;
+                            if ((a[i / 8][i % 8] & 0x7c00u) == 0x7c00u) first = 2 * i;
                         }
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const uint32_t keep = (2 * i < first ? 0xffffu : 0u) | (2 * i + 1 < first ? 0xffff0000u : 0u);
-                            a[0][i] &= keep;
-                            a[1][i] &= keep;
+                            a[i / 8][i % 8] &= keep;
+                            a[2 + i / 8][i % 8] &= keep;
                         }
-                        if (first < left) atomicMax(marks + col, mark_of(n + 1, half * 32 + first));
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const uint32_t lo[8] = {a[e][0], a[e][1], a[e][2], a[e][3], a[e][4], a[e][5], a[e][6], a[e][7]};
-                        const uint32_t hi[8] = {a[e][8], a[e][9], a[e][10], a[e][11], a[e][12], a[e][13], a[e][14], a[e][15]};
-                        tmem_st8u(lanes + cW + e * 32 + half * 16, lo);
-                        tmem_st8u(lanes + cW + e * 32 + half * 16 + 8, hi);
+                        if (first < 32 && first < left) atomicMax(marks + col, mark_of(n + 1, half * 32 + first));
+                        store();
                     }
                     tmem_st_wait();
                     arrive(bXP);
@@ -890,7 +937,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 const uint32_t mark = reinterpret_cast<const volatile uint32_t*>(marks)[col];
                 const bool bad = (mark >> 7) == (uint32_t)n + 1u;
                 const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : 32;
-                const float keep = gate[kKeep - half * 32];
+                const float keep = bad ? __int_as_float(0x7fffffff) : gate[kKeep - half * 32];       // (NaN: all of the lane's state)
                 tmem_ld_wait();
                 {
                     const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
@@ -900,66 +947,49 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         X[2 * i] = fma2(be.x, X[2 * i], pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])));
                         X[2 * i + 1] = fma2(be.y, X[2 * i + 1], pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])));
                     }
-                    if (first < 32) {
+                    auto store = [&]() {
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t a[2][8];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const ulonglong2 w = put[q * 4 + i];
+                                two_parts(mul2(w.x, X[q * 8 + 2 * i]), a[0][2 * i], a[1][2 * i]);
+                                two_parts(mul2(w.y, X[q * 8 + 2 * i + 1]), a[0][2 * i + 1], a[1][2 * i + 1]);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
+                        }
+                        tmem_st_wait();
+                        arrive(bWP);
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t a[2][8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) two_parts(X[q * 8 + i], a[0][i], a[1][i]);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, a[e]);
+                        }
+                    };
+                    if (!__any_sync(0xffffffffu, first < 32)) {
+                        store();
+                    } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             float b0, b1;
                             unpack2(X[i], b0, b1);
                             X[i] = pack2(2 * i >= first ? 0.f : b0, 2 * i + 1 >= first ? 0.f : b1);
                         }
-                    }
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        uint32_t a[2][8];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const ulonglong2 w = put[q * 4 + i];
-                            two_parts(mul2(w.x, X[q * 8 + 2 * i]), a[0][2 * i], a[1][2 * i]);
-                            two_parts(mul2(w.y, X[q * 8 + 2 * i + 1]), a[0][2 * i + 1], a[1][2 * i + 1]);
-                        }
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
-                    }
-                    tmem_st_wait();
-                    arrive(bWP);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        uint32_t a[2][8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) two_parts(X[q * 8 + i], a[0][i], a[1][i]);
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, a[e]);
+                        store();
                     }
                 }
-                if (live) {                              // Q S^T is there: its tokens' factors
-                    ok = warp_wait(bar + bAsk, m & 1);
-                    ++m;
-                    if (!ok) break;
-                    tc_fence_after();
-                    tmem_ld32_async(lanes + cY + half * 32, d);
-                    tmem_ld_wait();
-                    const ulonglong2* ask = reinterpret_cast<const ulonglong2*>(gate + kAsk);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t r[8];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const ulonglong2 w = ask[2 * i + e];
-                            const uint64_t y0 = mul2(w.x, pack2(__uint_as_float(d[8 * i + 4 * e]), __uint_as_float(d[8 * i + 4 * e + 1])));
-                            const uint64_t y1 = mul2(w.y, pack2(__uint_as_float(d[8 * i + 4 * e + 2]), __uint_as_float(d[8 * i + 4 * e + 3])));
-                            r[4 * e] = (uint32_t)y0;
-                            r[4 * e + 1] = (uint32_t)(y0 >> 32);
-                            r[4 * e + 2] = (uint32_t)y1;
-                            r[4 * e + 3] = (uint32_t)(y1 >> 32);
-                        }
-                        tmem_st8u(lanes + cY + half * 32 + 8 * i, r);
-                    }
+                if (half == 0) {
+                    float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (n & 1) * 256 + col;
+                    aside[0] = p.q_scale * down;
+                    aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
                 }
                 tmem_st_wait();
                 arrive(bUP);
-                y_bad = first;
-                y_n = n;
-                y_scale = p.q_scale * down;
                 float r = down;
                 if (more) {
                     length = (look ? length_of(n) : length) + 64.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
@@ -983,11 +1013,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         for (int j = 0; j < 16; ++j)
                             S[i * 16 + j] = fma2(r2, pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])), mul2(keep2, S[i * 16 + j]));
                     }
-                    if (bad) {
-                        const float nan = __int_as_float(0x7fffffff);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) S[i * 16 + j] = pack2(nan, nan);
-                    }
                     if (more) give(i);
                 }
             }
@@ -1003,7 +1028,6 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
             }
         }
-        if (ok && y_n >= 0) write_y();
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 14);
     }
     tc_fence_before();
