@@ -87,42 +87,75 @@ constexpr uint32_t kTypes = (1u << 4) | ((128u >> 4) << 24);      // fp16 x fp16
 
 // ---- what does not depend on the state: T and P of every chunk ------------------------------------------------------------
 //
-// A CTA takes a chunk, a group and two of its heads.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product gives the rows <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127);
-// threads 0..63 make -L of both heads from them, the others P.  T is found column by column: a thread holds a whole column in registers and
-// takes from the rows below what each of its elements puts there, so that nothing is waited for; two warps a head.
-// The columns from 32 on start at row 32: the heavy half changes schedulers with the CTA's number.  What is split and stored goes by rows
-// again, through shared memory.
+// A CTA takes a chunk, a group and two of its heads.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product
+// gives <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127).  Of four warps a head, two make P from the latter and store it, two make -L and from
+// it T, in blocks of sixteen by sixteen: D_b, the inverses of the diagonal ones, column by column, a column a thread, all four at once; then
+//     T[b][c] = D_b sum_{c <= e < b} -L[b][e] T[e][c],   T[b][b] = D_b diag(beta),
+// transposed, so that what one product leaves in registers is the next one's first operand (mma.sync, in two parts as above: operands of this
+// size are in registers before a tcgen05 product could be set up).  (All of it column by column is as many multiply-adds on CUDA
+// cores, but their second operands, broadcast from shared memory at 128 bytes a cycle, were most of 160 us for 16384 tokens of 32 heads.)
 
-constexpr int kPrepThreads = 128;
-constexpr uint32_t kPrepNorm = 4 * kPart;              // behind the tile of K and Q rows (whose place -L of two heads takes, [s][t] floats): 1 / |k|, 1 / |q|: [2][64]
-constexpr uint32_t kPrepSum = kPrepNorm + 2u * kQ * 4u;           // of each head: whole, rest, beta: [2][3][64]
+constexpr int kPrepThreads = 256;
+// behind the tile of K and Q rows, whose place -L of both heads takes (two parts, rows t), then T: the diagonal blocks of -L, [4][s][t] floats
+// a head; their inverses, [4][2 parts][t][s]; 1 / |k|, 1 / |q|, and 1 / |k| or zero: [3][64]; halves of their squares; whole, rest, beta: [2][3][64]
+constexpr uint32_t kPrepDiag = 4 * kPart, kPrepInv = kPrepDiag + 2u * 4096u;
+constexpr uint32_t kPrepNorm = kPrepInv + 2u * 4096u, kPrepHalf = kPrepNorm + 3u * kQ * 4u, kPrepSum = kPrepHalf + 4u * kQ * 4u;
 constexpr uint32_t kPrepBar = kPrepSum + 6u * kQ * 4u;
 constexpr uint32_t kPrepSmem = kPrepBar + 32u + 1024u;
 
-// What element S of a column puts into the rows below: l holds -L, [s][t].
+// Element S of sixteen neighbouring ones of a column puts -L[t][s] of itself into those behind it: l holds their block of -L, [s][t].
 template <int S>
-__device__ __forceinline__ void take(uint64_t (&T)[32], const float* l) {
+__device__ __forceinline__ void take_near(uint64_t (&T)[8], const float* l) {
     float a, b;
     unpack2(T[S / 2], a, b);
     const float ts = S % 2 ? b : a;
     const uint64_t ts2 = pack2(ts, ts);
-    if constexpr (S % 2 == 0) T[S / 2] = pack2(a, fmaf(l[S * kQ + S + 1], ts, b));
+    if constexpr (S % 2 == 0) T[S / 2] = pack2(a, fmaf(l[S * 16 + S + 1], ts, b));
     constexpr int first = S / 2 + 1;                    // the first pair behind S
-    if constexpr (first % 2 == 1 && first < 32) T[first] = fma2(*reinterpret_cast<const uint64_t*>(l + S * kQ + 2 * first), ts2, T[first]);
+    if constexpr (first % 2 == 1) T[first] = fma2(*reinterpret_cast<const uint64_t*>(l + S * 16 + 2 * first), ts2, T[first]);
 #pragma unroll
-    for (int i = (first + 1) / 2; i < 16; ++i) {
-        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(l + S * kQ + 4 * i);
+    for (int i = (first + 1) / 2; i < 4; ++i) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(l + S * 16 + 4 * i);
         T[2 * i] = fma2(v.x, ts2, T[2 * i]);
         T[2 * i + 1] = fma2(v.y, ts2, T[2 * i + 1]);
     }
 }
-template <int FIRST, int... I>
-__device__ __forceinline__ void take_rows(uint64_t (&T)[32], const float* l, std::integer_sequence<int, I...>) { (take<FIRST + I>(T, l), ...); }
+template <int... I>
+__device__ __forceinline__ void take_fifteen(uint64_t (&T)[8], const float* l, std::integer_sequence<int, I...>) { (take_near<I>(T, l), ...); }
 
-__global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __grid_constant__ DeltaArgs g) {
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void stmatrix4_trans(uint32_t at, const uint32_t (&r)[4]) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void mma_block(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// c (16 x 16, two tiles of 8 columns) += a b^T: a in two parts, of b two parts of sixteen rows of sixteen.
+__device__ __forceinline__ void mma_sixteen(float (&c)[2][4], const uint32_t (&hi)[4], const uint32_t (&lo)[4], uint32_t b_hi, uint32_t b_lo) {
+    uint32_t bh[4], bl[4];                              // (first eight rows: both halves of their columns; the other eight)
+    ldmatrix4(bh, b_hi);
+    ldmatrix4(bl, b_lo);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        mma_block(c[i], hi, bh[2 * i], bh[2 * i + 1]);
+        mma_block(c[i], hi, bl[2 * i], bl[2 * i + 1]);
+        mma_block(c[i], lo, bh[2 * i], bh[2 * i + 1]);
+    }
+}
+// What a product leaves as the first operand of the next.
+__device__ __forceinline__ void as_operand(const float (&c)[2][4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) two_parts(pack2(c[i >> 1][(i & 1) * 2], c[i >> 1][(i & 1) * 2 + 1]), hi[i], lo[i]);
+}
+// Byte of element (row, column) of a part: rows of 128 bytes in the 128-byte swizzle.
+__device__ __forceinline__ uint32_t at_swizzled(int row, int col) { return (uint32_t)(row * 128 + (((col >> 3) ^ (row & 7)) * 16) + (col & 7) * 2); }
+
+__global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __grid_constant__ DeltaArgs g) {
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    float* minus_l = reinterpret_cast<float*>(smem);
     float* norms = reinterpret_cast<float*>(smem + kPrepNorm);
     float* sums = reinterpret_cast<float*>(smem + kPrepSum);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kPrepBar);
@@ -167,24 +200,35 @@ __global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __gri
             }
         }
         const int h0 = group * per + batch * 2, heads = min(2, per - batch * 2);
+        const int mine = warp >> 2, role = warp & 3;     // this warp's head of the two; what it does for it
         // gates, while the rows are under way: a warp a head, two neighbouring tokens a lane
-        if (warp < heads) {
-            const int h = h0 + warp;
-            float* s = sums + warp * 3 * kQ;
+        if (role == 0 && mine < heads) {
+            const int h = h0 + mine;
+            float* s = sums + mine * 3 * kQ;
             const float a2 = p.a[h] * 1.4426950408889634f, bias = p.dt_bias != nullptr ? p.dt_bias[h] : 0.f;
+            float x[2] = {0.f, 0.f}, y[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane * 2 + i < valid) {
+                    const long long r = t0 + lane * 2 + i;
+                    x[i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.b)[r * p.b_stride + h]);
+                    y[i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.dt)[r * p.dt_stride + h]);
+                }
             double c[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int t = lane * 2 + i;
-                float l = 0.f, beta = 0.f;
-                if (t < valid) {
-                    const long long r = t0 + t;
-                    beta = 1.f / (1.f + expf(-__bfloat162float(static_cast<const __nv_bfloat16*>(p.b)[r * p.b_stride + h])));
-                    l = a2 * softplus(__bfloat162float(static_cast<const __nv_bfloat16*>(p.dt)[r * p.dt_stride + h]) + bias);
-                    if (l < -160.f) l = -160.f;         // (2^-160 is zero in fp32; the bound keeps the sums finite; NaN passes it)
+                const bool in = lane * 2 + i < valid;
+                float l = a2 * softplus(y[i] + bias);
+                if (l < -160.f) l = -160.f;             // (2^-160 is zero in fp32; the bound keeps the sums finite)
+                // What is not finite counts in beta, by which its token is known: sums, L and T stay finite, as products of sixteen rows
+                // would carry it to the tokens before.
+                float beta = 1.f / (1.f + expf(-x[i]));
+                if (!(l <= 3.4028235e38f)) {
+                    l = 0.f;
+                    beta = __int_as_float(0x7fffffff);
                 }
-                s[2 * kQ + t] = beta;
-                c[i] = i > 0 ? c[0] + (double)l : (double)l;
+                s[2 * kQ + lane * 2 + i] = in ? beta : 0.f;
+                c[i] = (i > 0 ? c[0] : 0.0) + (double)(in ? l : 0.f);
             }
             double before = c[1];
 #pragma unroll
@@ -202,31 +246,42 @@ __global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __gri
             }
         }
         ok = mbar_wait_bounded(bar, 0);
-        // norms: a row of K or Q a thread, which it then scales; rows behind the sequence are zeros
         ok = __syncthreads_and(ok) != 0;
+        // norms: half a row of K or Q a thread, which it then scales; rows behind the sequence are zeros
         if (ok) {
-            float sq = 0.f;
-            unsigned char* row = smem + tid * 128;
-            uint4 v[16];
+            const int r = tid & 127;
+            unsigned char* row = smem + (tid >> 7) * 2 * kPart + r * 128;
+            float* halves = reinterpret_cast<float*>(smem + kPrepHalf);
+            uint64_t sq[4] = {0ull, 0ull, 0ull, 0ull};
+            uint4 v[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] = *reinterpret_cast<const uint4*>(row + (i / 8) * 2 * kPart + (((i & 7) ^ (tid & 7)) * 16));
+            for (int i = 0; i < 8; ++i) {
+                v[i] = *reinterpret_cast<const uint4*>(row + ((i ^ (r & 7)) * 16));
                 float f[8];
                 Vec16<__nv_bfloat16>::unpack(v[i], f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq = fmaf(f[e], f[e], sq);
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t x = pack2(f[2 * e], f[2 * e + 1]);
+                    sq[e] = fma2(x, x, sq[e]);
+                }
             }
-            const float r = inv_length(sq, p.eps), scale = __uint_as_float(__float_as_uint(r) & 0x7f800000u);
-            norms[tid] = r / scale;
-            const bool in = (tid & 63) < valid;
+            float even, odd;
+            unpack2(add2(add2(sq[0], sq[1]), add2(sq[2], sq[3])), even, odd);
+            halves[tid] = even + odd;
+            __syncthreads();
+            const float inv = inv_length(halves[r] + halves[r + 128], p.eps), scale = __uint_as_float(__float_as_uint(inv) & 0x7f800000u);
+            const bool fine = inv == inv;                // (a row that is not finite: zeros, and a factor that is not a number)
+            if (tid < 128) norms[r] = fine ? inv / scale : inv;
+            if (tid < 64) norms[128 + r] = fine ? inv / scale : 0.f;
+            const bool in = (r & 63) < valid && fine;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 float f[8];
                 Vec16<__nv_bfloat16>::unpack(v[i], f);
                 uint32_t h[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[e] = in ? half_pair(f[2 * e] * scale, f[2 * e + 1] * scale) : 0u;
-                *reinterpret_cast<uint4*>(row + (i / 8) * 2 * kPart + (((i & 7) ^ (tid & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(row + ((i ^ (r & 7)) * 16)) = make_uint4(h[0], h[1], h[2], h[3]);
             }
             proxy_fence();
         }
@@ -243,131 +298,201 @@ __global__ void __launch_bounds__(kPrepThreads, 4) delta_prep_kernel(const __gri
             __syncwarp();
         }
         // what the second kernel reads of the gates
-        if (ok && tid < 64) {
-            for (int j = 0; j < heads; ++j) {
-                const float *s = sums + j * 3 * kQ, w = s[tid], r = s[kQ + tid];
-                float* to = reinterpret_cast<float*>(p.work + ((size_t)chunk * p.H + h0 + j) * kBlock + kGOff);
-                const bool in = tid < valid;
-                const float e = exp2f(w) * exp2f(r), rest = exp2f(s[kQ - 1] - w) * exp2f(s[2 * kQ - 1] - r);
-                to[kBeta + tid] = s[2 * kQ + tid];
-                to[kRead + tid] = in ? fmaf(s[2 * kQ + tid], 0.f, -e * norms[tid]) : 0.f;      // (not a number where beta is none: see the marks)
-                to[kPut + tid] = in ? rest * norms[tid] : 0.f;
-                to[kAsk + tid] = in ? e * norms[64 + tid] : 0.f;
-                if (tid == 63) to[kKeep] = e;
-            }
+        if (ok && role >= 2 && mine < heads) {
+            const int t = tid & 63;
+            const float *s = sums + mine * 3 * kQ, w = s[t], r = s[kQ + t];
+            float* to = reinterpret_cast<float*>(p.work + ((size_t)chunk * p.H + h0 + mine) * kBlock + kGOff);
+            const bool in = t < valid;
+            const float e = exp2f(w) * exp2f(r), rest = exp2f(s[kQ - 1] - w) * exp2f(s[2 * kQ - 1] - r);
+            to[kBeta + t] = s[2 * kQ + t];
+            to[kRead + t] = in ? fmaf(s[2 * kQ + t], 0.f, -e * norms[t]) : 0.f;      // (not a number where beta is none: see the marks)
+            to[kPut + t] = in ? rest * norms[t] : 0.f;
+            to[kAsk + t] = in ? e * norms[64 + t] : 0.f;
+            if (t == 63) to[kKeep] = e;
         }
         ok = ok && mbar_wait_bounded(bar + 1, 0);
         if (tid == 64) tma_store_read();
         ok = __syncthreads_and(ok) != 0;                // (from here on the tile's place is -L's)
-        if (ok) {
+        if (ok && mine < heads) {
             tc_fence_after();
             const int t = tid & 63;
-            const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+            const uint32_t lanes = (uint32_t)(role * 32) << 16;
             const uint64_t minus = pack2(-1.f, -1.f);
-#pragma unroll 1
-            for (int j = 0; j < heads; ++j) {
-                const float* s = sums + j * 3 * kQ;
-                const uint64_t w = pack2(s[t], s[t]), r = pack2(s[kQ + t], s[kQ + t]);
-                // tokens e .. e + 15 of the row: the product times both norms (and `mine`) and the decay between, zero from `end` on
-                auto tokens = [&](int e0, uint64_t mine, int end, uint64_t (&x)[8]) {
-                    uint32_t d[16];
-                    tmem_ld16_async(tmem + lanes + e0, d);
-                    tmem_ld_wait();
-                    const ulonglong2 *w4 = reinterpret_cast<const ulonglong2*>(s + e0), *r4 = reinterpret_cast<const ulonglong2*>(s + kQ + e0),
-                                     *n4 = reinterpret_cast<const ulonglong2*>(norms + e0);
+            const float* s = sums + mine * 3 * kQ;
+            const uint64_t w = pack2(s[t], s[t]), r = pack2(s[kQ + t], s[kQ + t]);
+            // tokens e0 .. e0 + 15 of the row: the product times both norms (and `factor`) and the decay between.  (Rows behind the sequence are
+            // zeros as K's and Q's are.)
+            auto tokens = [&](int e0, uint64_t factor, uint64_t (&x)[8]) {
+                uint32_t d[16];
+                tmem_ld16_async(tmem + lanes + e0, d);
+                tmem_ld_wait();
+                const ulonglong2 *w4 = reinterpret_cast<const ulonglong2*>(s + e0), *r4 = reinterpret_cast<const ulonglong2*>(s + kQ + e0),
+                                 *n4 = reinterpret_cast<const ulonglong2*>(norms + 128 + e0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const ulonglong2 we = w4[i], re = r4[i], ne = n4[i];
+                for (int i = 0; i < 4; ++i) {
+                    const ulonglong2 we = w4[i], re = r4[i], ne = n4[i];
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            float a, b, y0, y1;
-                            unpack2(add2(fma2(q ? we.y : we.x, minus, w), fma2(q ? re.y : re.x, minus, r)), a, b);
-                            const uint64_t f = mul2(mul2(mine, q ? ne.y : ne.x), pack2(__uint_as_float(d[4 * i + 2 * q]), __uint_as_float(d[4 * i + 2 * q + 1])));
-                            unpack2(mul2(f, pack2(ex2(a), ex2(b))), y0, y1);
-                            const int e = e0 + 4 * i + 2 * q;
-                            x[2 * i + q] = pack2(e < end ? y0 : 0.f, e + 1 < end ? y1 : 0.f);
-                        }
+                    for (int q = 0; q < 2; ++q) {
+                        float a, b;
+                        unpack2(add2(fma2(q ? we.y : we.x, minus, w), fma2(q ? re.y : re.x, minus, r)), a, b);
+                        const uint64_t f = mul2(mul2(factor, q ? ne.y : ne.x), pack2(__uint_as_float(d[4 * i + 2 * q]), __uint_as_float(d[4 * i + 2 * q + 1])));
+                        x[2 * i + q] = mul2(f, pack2(ex2(a), ex2(b)));
                     }
-                };
-                const int last = 16 * ((warp & 1) * 2 + 2);                      // (a warp's rows end there)
-                if (tid < 64) {
-                    const float mine = -s[2 * kQ + t] * norms[t];
-                    float* to = minus_l + j * kQ * kQ + t;
+                }
+            };
+            // sixteen tokens of row t in two parts
+            auto put = [&](unsigned char* to, int e0, const uint64_t (&x)[8]) {
+                uint32_t hi[8], lo[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) two_parts(x[i], hi[i], lo[i]);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    unsigned char* at = to + t * 128 + (((e0 / 8 + q) ^ (t & 7)) * 16);
+                    *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
+                    *reinterpret_cast<uint4*>(at + kPart) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
+                }
+            };
+            unsigned char* block = p.work + ((size_t)chunk * p.H + h0 + mine) * kBlock;
+            if (role >= 2) {
+                const uint64_t factor = pack2(norms[64 + t], norms[64 + t]);
+                const int last = 32 * (role & 1) + 32;   // (a warp's rows end there)
 #pragma unroll 1
-                    for (int e0 = 0; e0 < last; e0 += 16) {
-                        uint64_t x[8];
-                        tokens(e0, pack2(mine, mine), t < valid ? t : 0, x);
+                for (int e0 = 0; e0 < 64; e0 += 16) {
+                    uint64_t x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = 0ull;
+                    if (e0 < last) tokens(e0, factor, x);
+                    if (e0 + 16 > last - 32) {           // (the diagonal is in these rows)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             float a, b;
                             unpack2(x[i], a, b);
-                            to[(e0 + 2 * i) * kQ] = a;
-                            to[(e0 + 2 * i + 1) * kQ] = b;
+                            x[i] = pack2(e0 + 2 * i <= t ? a : 0.f, e0 + 2 * i + 1 <= t ? b : 0.f);
                         }
                     }
+                    put(block + kPOff, e0, x);
+                }
+            } else {
+                unsigned char* L = smem + mine * 2 * kPart;
+                float* diag = reinterpret_cast<float*>(smem + kPrepDiag + mine * 4096);
+                {
+                    const float beta = s[2 * kQ + t], f = beta == beta ? -beta * norms[128 + t] : 0.f;
+#pragma unroll 1
+                    for (int e0 = 0; e0 < 32 * role + 32; e0 += 16) {
+                        uint64_t x[8];
+                        tokens(e0, pack2(f, f), x);      // (what it leaves on and above the diagonal nobody reads)
+                        put(L, e0, x);
+                        if (e0 == (t & 48)) {
+                            float* to = diag + e0 * 16 + (t & 15);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                float a, b;
+                                unpack2(x[i], a, b);
+                                to[2 * i * 16] = a;
+                                to[(2 * i + 1) * 16] = b;
+                            }
+                        }
+                    }
+                }
+                __syncwarp();
+                // the inverses: this warp's two blocks, a column a lane
+                {
+                    const int blk = t >> 4, c = t & 15;
+                    uint64_t x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = pack2(2 * i == c ? 1.f : 0.f, 2 * i + 1 == c ? 1.f : 0.f);
+                    take_fifteen(x, diag + blk * 256, std::make_integer_sequence<int, 15>{});
+                    unsigned short* to = reinterpret_cast<unsigned short*>(smem + kPrepInv + mine * 4096 + blk * 1024) + c;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t hi, lo;
+                        two_parts(x[i], hi, lo);
+                        to[2 * i * 16] = (unsigned short)hi;
+                        to[(2 * i + 1) * 16] = (unsigned short)(hi >> 16);
+                        to[2 * i * 16 + 256] = (unsigned short)lo;
+                        to[(2 * i + 1) * 16 + 256] = (unsigned short)(lo >> 16);
+                    }
+                }
+                asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");    // L and the inverses are there
+                // T diag(beta): block columns 0 and 3 by one warp, 1 and 2 by the other.  Of block column c the blocks c .. 3.
+                const uint32_t l_at = smem_u32(L), inv_at = smem_u32(smem + kPrepInv + mine * 4096) + (uint32_t)((lane & 7) + (lane >> 4) * 8) * 32u + (uint32_t)((lane >> 3) & 1) * 16u;
+                uint32_t th[5][4], tl[5][4];             // blocks: of the first block column, up to four; of the second one or two
+                auto column = [&](auto first, auto at0) {
+                    constexpr int C = decltype(first)::value, A = decltype(at0)::value;
+#pragma unroll
+                    for (int b = C; b < 4; ++b) {
+                        float c[2][4], d[2][4];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) c[i >> 2][i & 3] = d[i >> 2][i & 3] = 0.f;
+                        if (b == C) {
+                            // (a product's lane has row lane / 4, and eight more, and columns 2 (lane % 4) and one more of either tile)
+                            const int m = lane >> 2, k = (lane & 3) * 2;
+                            float b0 = s[2 * kQ + C * 16 + m], b1 = s[2 * kQ + C * 16 + m + 8];
+                            b0 = b0 == b0 ? b0 : 0.f;
+                            b1 = b1 == b1 ? b1 : 0.f;
+                            c[0][0] = m == k ? b0 : 0.f;
+                            c[0][1] = m == k + 1 ? b0 : 0.f;
+                            c[1][2] = m == k ? b1 : 0.f;
+                            c[1][3] = m == k + 1 ? b1 : 0.f;
+                        } else {
+#pragma unroll
+                            for (int e = C; e < b; ++e) {
+                                const uint32_t at = l_at + at_swizzled(b * 16 + (lane & 7) + (lane >> 4) * 8, e * 16 + ((lane >> 3) & 1) * 8);
+                                mma_sixteen(c, th[A + e - C], tl[A + e - C], at, at + kPart);
+                            }
+                        }
+                        uint32_t ch[4], cl[4];
+                        as_operand(c, ch, cl);
+                        mma_sixteen(d, ch, cl, inv_at + b * 1024, inv_at + b * 1024 + 512);
+                        as_operand(d, th[A + b - C], tl[A + b - C]);
+                    }
+                };
+                auto store = [&](auto first, auto at0) {
+                    constexpr int C = decltype(first)::value, A = decltype(at0)::value;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        // (tiles of the operand: rows 0..7 and 8..15 of columns 0..7, then of 8..15; stored transposed: T's rows are its columns)
+                        const uint32_t at = l_at + at_swizzled(b * 16 + (lane & 7) + (lane >> 4) * 8, C * 16 + ((lane >> 3) & 1) * 8);
+                        const uint32_t none[4] = {0u, 0u, 0u, 0u};
+                        if (b < C) {
+                            stmatrix4_trans(at, none);
+                            stmatrix4_trans(at + kPart, none);
+                        } else {
+                            stmatrix4_trans(at, th[b < C ? 0 : A + b - C]);
+                            stmatrix4_trans(at + kPart, tl[b < C ? 0 : A + b - C]);
+                        }
+                    }
+                };
+                using I0 = std::integral_constant<int, 0>;
+                using I1 = std::integral_constant<int, 1>;
+                using I2 = std::integral_constant<int, 2>;
+                using I3 = std::integral_constant<int, 3>;
+                using I4 = std::integral_constant<int, 4>;
+                if (role == 0) {
+                    column(I0{}, I0{});
+                    column(I3{}, I4{});
                 } else {
-                    const float mine = norms[64 + t];
-                    unsigned char* to = p.work + ((size_t)chunk * p.H + h0 + j) * kBlock + kPOff + t * 128;
-#pragma unroll 1
-                    for (int e0 = 0; e0 < 64; e0 += 16) {
-                        uint32_t hi[8], lo[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) hi[i] = lo[i] = 0u;
-                        if (e0 < last) {
-                            uint64_t x[8];
-                            tokens(e0, pack2(mine, mine), t < valid ? t + 1 : 0, x);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) two_parts(x[i], hi[i], lo[i]);
-                        }
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            unsigned char* at = to + (((e0 / 8 + q) ^ (t & 7)) * 16);
-                            *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
-                            *reinterpret_cast<uint4*>(at + kPart) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
-                        }
-                    }
+                    column(I1{}, I0{});
+                    column(I2{}, I3{});
                 }
-            }
-            __syncthreads();
-            // column `col` of T: element t takes -L[t][s] T[s] from every s before it
-            const int head = warp >> 1, col = (tid & 63) ^ ((blockIdx.x & 1) * 32);
-            if (head < heads) {
-                uint64_t T[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) T[i] = pack2(2 * i == col ? 1.f : 0.f, 2 * i + 1 == col ? 1.f : 0.f);
-                float* l = minus_l + head * kQ * kQ;
-                if (col < 32) take_rows<0>(T, l, std::make_integer_sequence<int, 32>{});
-                take_rows<32>(T, l, std::make_integer_sequence<int, 31>{});
-                const float beta = sums[head * 3 * kQ + 2 * kQ + col];
-                const uint64_t beta2 = pack2(beta, beta);
-                asm volatile("bar.sync %0, 64;" ::"r"(head + 1) : "memory");    // (nobody reads L of this head any more)
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float a, b;
-                    unpack2(mul2(T[i], beta2), a, b);
-                    l[2 * i * kQ + col] = 2 * i > col ? a : 0.f;
-                    l[(2 * i + 1) * kQ + col] = 2 * i + 1 > col ? b : 0.f;
+                asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");    // (nobody reads L any more)
+                if (role == 0) {
+                    store(I0{}, I0{});
+                    store(I3{}, I4{});
+                } else {
+                    store(I1{}, I0{});
+                    store(I2{}, I3{});
                 }
-                asm volatile("bar.sync %0, 64;" ::"r"(head + 1) : "memory");
-                // T - diag in two parts: eight elements of a row at a time (eight rows of 128 bytes are all banks, whichever piece of them)
-                unsigned char* to = p.work + ((size_t)chunk * p.H + h0 + head) * kBlock + kTOff;
-                const int piece = tid & 7;
-#pragma unroll 1
-                for (int row = (tid & 63) >> 3; row < kQ; row += 8) {
-                    uint32_t a[2][4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a[0][i] = a[1][i] = 0u;
-                    if (piece * 8 < row) {
-                        const ulonglong2* from = reinterpret_cast<const ulonglong2*>(l + row * kQ + piece * 8);
-                        const ulonglong2 u = from[0], v = from[1];
-                        two_parts(u.x, a[0][0], a[1][0]);
-                        two_parts(u.y, a[0][1], a[1][1]);
-                        two_parts(v.x, a[0][2], a[1][2]);
-                        two_parts(v.y, a[0][3], a[1][3]);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<uint4*>(to + e * kPart + row * 128 + ((piece ^ (row & 7)) * 16)) = make_uint4(a[e][0], a[e][1], a[e][2], a[e][3]);
+                asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");
+                {                                        // the diagonal's part of U is added in fp32
+                    unsigned short* to = reinterpret_cast<unsigned short*>(L + at_swizzled(t, t));
+                    to[0] = to[kPart / 2] = 0;
+                }
+                proxy_fence();
+                asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");
+                if (t == 0) {
+                    bulk_s2g(block + kTOff, L, 2 * kPart);
+                    tma_store_done();
                 }
             }
         }
