@@ -42,12 +42,64 @@ constexpr uint32_t kBlock = kGOff + kGates * 4u;
 struct DeltaArgs {
     CUtensorMap tq, tk, tv;
     DeltaParams p;
-    unsigned char* rows;       // of the scratch, behind the heads' blocks
-    int units;
+    // of the scratch, behind the heads' blocks: rows of K and Q; sequences by their lengths; states between segments
+    unsigned char* rows;
+    int* order;
+    float* states;
+    int units, preps;
+    int segments, pass;        // parts that a sequence is split into; 0: whole ones, 1, 2: see decode_unit
 };
+
+// What a CTA of the second kernel takes at a time: a sequence and head, or a segment of one.
+struct Unit {
+    int t0, t1;                // rows
+    int seq, head, chunk;      // chunk: of the first row, in the scratch
+    int seg, kind;             // kWhole and kFirst begin with the stored state, kLater with the segment's, kAlone with zeros, kMap with the unit matrix
+    bool outputs;
+};
+enum { kWhole, kFirst, kLater, kAlone, kMap };
 
 // The first chunk of sequence i in the scratch: chunks of sequences that follow one another never meet, whatever their lengths are.
 __device__ __forceinline__ int chunk_base(int row0, int i) { return row0 / kQ + i; }
+
+// Unit number `it` of this CTA.  Whole sequences go out in the order of their lengths, the longest first, to and fro over the CTAs.
+// Few sequences and heads leave most of the card idle for as long as the longest takes.  Then a sequence is split into n segments.  What
+// a segment makes of a state is linear: S <- M S + N.  The first pass takes the first segment with its outputs, and of each that others follow N
+// (from a state of zeros) and M (from the unit matrix, without values), side by side; a small kernel goes through them, and the second pass takes
+// all others from the states that they begin with.
+__device__ __forceinline__ bool decode_unit(const DeltaArgs& g, int it, Unit& x) {
+    const DeltaParams& p = g.p;
+    const int G = (int)gridDim.x, i = (int)blockIdx.x, k = it * G + ((it & 1) ? G - 1 - i : i);
+    if (k >= g.units) return false;
+    int part = 0, u = k;
+    x.kind = kWhole;
+    x.seg = 0;
+    if (g.pass != 0) {
+        const int parts = g.pass == 1 ? 2 * g.segments - 3 : g.segments - 1;
+        part = k % parts;
+        u = k / parts;
+        x.kind = g.pass == 2 ? kLater : part == 0 ? kFirst : (part & 1) ? kAlone : kMap;
+        x.seg = g.pass == 2 ? part + 1 : (part + 1) / 2;
+    }
+    x.head = u % p.H;
+    x.seq = u / p.H;
+    if (g.order != nullptr) x.seq = min(max(g.order[x.seq], 0), p.pr.N - 1);
+    x.outputs = x.kind <= kLater;
+    const int2 rows = seq_rows(p.pr, x.seq);
+    const int chunks = (rows.y - rows.x + kQ - 1) / kQ, per = g.pass == 0 ? chunks : (chunks + g.segments - 1) / g.segments;
+    x.t0 = min(rows.y, rows.x + x.seg * per * kQ);
+    x.t1 = min(rows.y, x.t0 + per * kQ);
+    x.chunk = chunk_base(rows.x, x.seq) + x.seg * per;
+    return true;
+}
+// The stored state before the unit, and whether it is one (not zeros).
+__device__ __forceinline__ bool has_state(const DeltaArgs& g, const Unit& x) {
+    return x.kind >= kLater ? x.kind != kAlone : seq_resume(g.p.pr, x.seq) >= 0;
+}
+// State i of a sequence and head in the scratch: before segments 1 .. n - 1; then N and M of segments 1 .. n - 2.
+__device__ __forceinline__ float* scratch_state(const DeltaArgs& g, int seq, int head, int i) {
+    return g.states + (((size_t)seq * g.p.H + head) * (3 * g.segments - 5) + i) * 128 * 128;
+}
 
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) { tc_mma_bf16(d, a, b, idesc, acc ? 1u : 0u); }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
@@ -164,6 +216,22 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
     const int tid = (int)threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int per = p.H / p.G, batches = (per + 1) / 2;
     int u = (int)blockIdx.x;
+    if (u == g.preps) {                                  // (one CTA more: every sequence's place by its number of chunks)
+        grid_dep_wait();
+        grid_dep_launch_dependents();
+        for (int i = tid; i < p.pr.N; i += kPrepThreads) {
+            const int2 rows = seq_rows(p.pr, i);
+            const int mine = (rows.y - rows.x + kQ - 1) / kQ;
+            int place = 0;
+            for (int j = 0; j < p.pr.N; ++j) {
+                const int2 r = seq_rows(p.pr, j);
+                const int other = (r.y - r.x + kQ - 1) / kQ;
+                place += other > mine || (other == mine && j < i);
+            }
+            g.order[place] = i;
+        }
+        return;
+    }
     const int batch = u % batches;
     u /= batches;
     const int group = u % p.G, chunk = u / p.G;
@@ -575,11 +643,11 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     if (warp == 0) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (lane == 0) {
-            for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-                const int head = u % p.H, seq = u / p.H, group = head / (p.H / p.G);
-                const int2 rows = seq_rows(p.pr, seq);
-                int chunk = chunk_base(rows.x, seq);
-                for (int t = rows.x; t < rows.y; t += kQ, ++chunk, ++n) {
+            Unit x;
+            for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+                const int head = x.head, group = head / (p.H / p.G);
+                int chunk = x.chunk;
+                for (int t = x.t0; t < x.t1; t += kQ, ++chunk, ++n) {
                     const int b = n & 1;
                     ok = n < 2 || mbar_wait_bounded(bar + bEmpty + b, (n / 2 - 1) & 1);
                     if (!ok) break;
@@ -598,13 +666,13 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     } else if (warp == 1) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         constexpr uint32_t kN64 = kTypes | ((64u >> 3) << 17), kProdDesc = kTypes | (1u << 16) | ((128u >> 3) << 17);
-        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-            const int seq = u / p.H;
-            const int2 rows = seq_rows(p.pr, seq);
-            const bool fresh0 = seq_resume(p.pr, seq) < 0;
-            for (int t = rows.x; t < rows.y && ok; t += kQ, ++n) {
+        Unit x;
+        int o = 0, om = 0;                              // chunks with outputs; those of them with a state before them
+        for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+            const bool stored = has_state(g, x);
+            for (int t = x.t0; t < x.t1 && ok; t += kQ, ++n) {
                 const int b = n & 1;
-                const bool live = !(fresh0 && t == rows.x);                      // S is not zero
+                const bool live = stored || t > x.t0;                            // S is not zero
                 const uint32_t base = sbase + b * kStage;
                 const uint64_t dk = swizzled_desc(base, 16u, 1024u), dq = swizzled_desc(base + kPart, 16u, 1024u);
                 const uint64_t dt = swizzled_desc(base + kWOff + kTOff, 16u, 1024u), dp = swizzled_desc(base + kWOff + kPOff, 16u, 1024u);
@@ -629,6 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     if (!ok) break;
                     if (elect()) tc_commit(bar + bX);
                     __syncwarp();
+                    ++m;
                 }
                 ok = warp_wait(bar + bXP, n & 1);
                 if (!ok) break;
@@ -644,10 +713,12 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
                 if (elect()) tc_commit(bar + bU);
                 __syncwarp();
-                ok = n < 1 || warp_wait(bar + bOut, (n - 1) & 1);
-                if (!ok) break;
-                tc_fence_after();
-                if (live) {                              // Q S^T
+                if (x.outputs) {
+                    ok = o < 1 || warp_wait(bar + bOut, (o - 1) & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (live && x.outputs) {                 // Q S^T
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int part = i >> 3, k = i & 7;
@@ -665,9 +736,15 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     if (elect()) mma_ts(tmem + cP, tmem + cW + (e & 1) * 32 + (e >> 1) * 8, dkt + (uint32_t)(e >> 1) * 128u, kProdDesc, e > 0);
                 if (elect()) tc_commit(bar + bProd);
                 __syncwarp();
-                ok = warp_wait(bar + bUP, n & 1) && (!live || warp_wait(bar + bScaled, m & 1));
+                if (!x.outputs) {                        // (what the other warps read of the stage they have read: W is made of it)
+                    if (elect()) tc_commit(bar + bEmpty + b);
+                    __syncwarp();
+                    continue;
+                }
+                ok = warp_wait(bar + bUP, o & 1) && (!live || warp_wait(bar + bScaled, om & 1));
                 if (!ok) break;
-                if (live) ++m;
+                ++o;
+                if (live) ++om;
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {            // U P
@@ -690,30 +767,31 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     } else if (warp == 2) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // V, copied a chunk ahead: four columns a lane; two rows at a time become one of pairs, in their place
-        int next_u = (int)blockIdx.x, next_n = 0;
-        int2 next = next_u < g.units ? seq_rows(p.pr, next_u / p.H) : make_int2(0, 0);
+        Unit next, x;
+        int next_it = 0, next_n = 0, next_t = 0;
+        bool there = decode_unit(g, 0, next);
+        if (there) next_t = next.t0;
         auto copy = [&]() {                              // the next copy, if there is one
-            while (next_u < g.units && next.x >= next.y) {
-                next_u += (int)gridDim.x;
-                if (next_u < g.units) next = seq_rows(p.pr, next_u / p.H);
+            while (there && next_t >= next.t1) {
+                there = decode_unit(g, ++next_it, next);
+                if (there) next_t = next.t0;
             }
-            if (next_u >= g.units) return;
+            if (!there) return;
             const int b = next_n & 1;
             ok = ok && (next_n < 2 || warp_wait(bar + bEmptyV + b, (next_n / 2 - 1) & 1));
             if (!ok) return;
             if (lane == 0) {
                 mbar_expect_tx(bar + bRaw + b, 2 * kPart);
-                tma_load(smem + kVOff + b * 2 * kPart, &g.tv, next_u % p.H * 128, next.x, bar + bRaw + b);
+                tma_load(smem + kVOff + b * 2 * kPart, &g.tv, next.head * 128, next_t, bar + bRaw + b);
             }
             __syncwarp();
             ++next_n;
-            next.x += kQ;
+            next_t += kQ;
         };
         copy();
-        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-            const int2 rows = seq_rows(p.pr, u / p.H);
-            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
-                const int b = n & 1, valid = min(kQ, rows.y - t);
+        for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+            for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                const int b = n & 1, valid = x.kind == kMap ? 0 : min(kQ, x.t1 - t);     // (M is made without values)
                 copy();
                 ok = ok && warp_wait(bar + bRaw + b, (n / 2) & 1);
                 if (!ok) break;
@@ -776,11 +854,12 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     } else if (warp == 3) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // Y: four columns a lane, two rows at a time
-        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-            const int head = u % p.H, seq = u / p.H;
-            const int2 rows = seq_rows(p.pr, seq);
-            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
-                const int valid = min(kQ, rows.y - t);
+        Unit x;
+        for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+            if (!x.outputs) continue;
+            const int head = x.head;
+            for (int t = x.t0; t < x.t1; t += kQ, ++n) {
+                const int valid = min(kQ, x.t1 - t);
                 ok = warp_wait(bar + bOut, n & 1);
                 if (!ok) break;
                 unsigned char* to = static_cast<unsigned char*>(p.out) + ((long long)t * p.out_stride + (long long)head * 128 + lane * 4) * 2;
@@ -805,12 +884,16 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         const int col = (warp & 3) * 32 + lane;
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + cY;
         const float* aside = reinterpret_cast<const float*>(smem + kAsideOff) + col;
-        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-            const int seq = u / p.H;
-            const int2 rows = seq_rows(p.pr, seq);
-            const int src = seq_resume(p.pr, seq);
-            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
-                if (src >= 0 || t > rows.x) {
+        Unit x;
+        int o = 0;                                      // chunks with outputs
+        for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+            if (!x.outputs) {
+                n += (x.t1 - x.t0 + kQ - 1) / kQ;
+                continue;
+            }
+            const bool stored = has_state(g, x);
+            for (int t = x.t0; t < x.t1; t += kQ, ++n, ++o) {
+                if (stored || t > x.t0) {
                     const float* gate = reinterpret_cast<const float*>(smem + (n & 1) * kStage + kWOff + kGOff) + kAsk;
                     ok = warp_wait(bar + bFull + (n & 1), (n / 2) & 1) && warp_wait(bar + bAsk, m & 1);
                     if (!ok) break;
@@ -843,11 +926,11 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bScaled);
                 }
-                ok = warp_wait(bar + bUP, n & 1);
+                ok = warp_wait(bar + bUP, o & 1);
                 if (!ok) break;
-                const float scale = reinterpret_cast<const volatile float*>(aside)[(n & 1) * 256];
-                const int first = __float_as_int(reinterpret_cast<const volatile float*>(aside)[(n & 1) * 256 + 128]);
-                ok = warp_wait(bar + bY, n & 1) && (n < 1 || warp_wait(bar + bOutFree, (n - 1) & 1));
+                const float scale = reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256];
+                const int first = __float_as_int(reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256 + 128]);
+                ok = warp_wait(bar + bY, o & 1) && (o < 1 || warp_wait(bar + bOutFree, (o - 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t scale2 = pack2(scale, scale);
@@ -942,18 +1025,21 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             tmem_st_wait();
             arrive(bS + i);
         };
-        for (int u = (int)blockIdx.x; u < g.units && ok; u += (int)gridDim.x) {
-            const int head = u % p.H, seq = u / p.H;
-            const int2 rows = seq_rows(p.pr, seq);
-            const int src = seq_resume(p.pr, seq), dst = seq_slot(p.pr, seq);
-            const size_t at = (size_t)head * 128 * 128 + (size_t)half * 64 * 128 + col;
-            if (src >= 0) {
-                const float* from = p.state + (size_t)src * p.H * 128 * 128 + at;
+        Unit x;
+        int o = 0;                                      // chunks with outputs
+        for (int it = 0; ok && decode_unit(g, it, x); ++it) {
+            const int2 rows = make_int2(x.t0, x.t1);
+            const bool stored = has_state(g, x);
+            const size_t at = (size_t)half * 64 * 128 + col;
+            if (stored && x.kind != kMap) {
+                const float* from = (x.kind == kLater ? scratch_state(g, x.seq, x.head, x.seg - 1)
+                                                      : p.state + ((size_t)seq_resume(p.pr, x.seq) * p.H + x.head) * 128 * 128) + at;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) S[i] = pack2(from[2 * i * 128], from[(2 * i + 1) * 128]);
             } else {
+                const int one = x.kind == kMap ? col - half * 64 : -1;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) S[i] = 0ull;
+                for (int i = 0; i < 32; ++i) S[i] = pack2(2 * i == one ? 1.f : 0.f, 2 * i + 1 == one ? 1.f : 0.f);
             }
             up = down = 1.f;
             if (rows.x < rows.y) {
@@ -967,7 +1053,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 length = length_of(n);
                 const float r = rescale(n);
                 const uint64_t r2 = pack2(r, r);
-                if (src >= 0) {
+                if (stored) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) S[i] = mul2(r2, S[i]);
                     give(0);
@@ -976,7 +1062,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             }
             for (int t = rows.x; t < rows.y; t += kQ, ++n) {
                 const int b = n & 1, left = rows.y - t - half * 32;              // tokens of the sequence from this half on
-                const bool live = src >= 0 || t > rows.x, more = t + kQ < rows.y;
+                const bool live = stored || t > rows.x, more = t + kQ < rows.y;
                 const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff) + half * 32;
                 ok = warp_wait(bar + bFull + b, (n / 2) & 1);
                 if (!ok) break;
@@ -1087,6 +1173,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         }
                         tmem_st_wait();
                         arrive(bWP);
+                        if (!x.outputs) return;
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             uint32_t a[2][8];
@@ -1108,13 +1195,16 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         store();
                     }
                 }
-                if (half == 0) {
-                    float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (n & 1) * 256 + col;
-                    aside[0] = p.q_scale * down;
-                    aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
+                if (x.outputs) {
+                    if (half == 0) {
+                        float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (o & 1) * 256 + col;
+                        aside[0] = p.q_scale * down;
+                        aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
+                    }
+                    tmem_st_wait();
+                    arrive(bUP);
+                    ++o;
                 }
-                tmem_st_wait();
-                arrive(bUP);
                 float r = down;
                 if (more) {
                     length = (look ? length_of(n) : length) + 64.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
@@ -1142,8 +1232,12 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
             }
             if (!ok) break;
-            if (dst >= 0) {
-                float* to = p.state + (size_t)dst * p.H * 128 * 128 + at;
+            const int dst = x.kind == kWhole || (x.kind == kLater && x.seg == g.segments - 1) ? seq_slot(p.pr, x.seq) : -1;
+            float* to = dst >= 0 ? p.state + ((size_t)dst * p.H + x.head) * 128 * 128
+                        : x.kind == kFirst ? scratch_state(g, x.seq, x.head, 0)
+                        : x.kind >= kAlone ? scratch_state(g, x.seq, x.head, g.segments - 1 + 2 * (x.seg - 1) + (x.kind == kMap)) : nullptr;
+            if (to != nullptr) {
+                to += at;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     float a, c;
@@ -1161,6 +1255,49 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     if (warp == 1) tmem_free<512>(tmem);
 }
 
+// The states that segments 2 .. n - 1 begin with: one after the other M S + N.  A CTA takes 16 value columns of a sequence and head; a thread
+// two rows of four columns.
+constexpr int kJoinThreads = 256;
+constexpr uint32_t kJoinSmem = (128u * 132u + 128u * 16u) * 4u;
+__global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaArgs g) {
+    extern __shared__ float mat[];                       // M [128][132], S [128][16]
+    float* sx = mat + 128 * 132;
+    grid_dep_wait();
+    grid_dep_launch_dependents();
+    const int tid = (int)threadIdx.x, n = g.segments, c0 = (int)blockIdx.x % 8 * 16, head = (int)blockIdx.x / 8 % g.p.H, seq = (int)blockIdx.x / 8 / g.p.H;
+    for (int i = tid; i < 512; i += kJoinThreads)
+        *reinterpret_cast<float4*>(sx + i * 4) = *reinterpret_cast<const float4*>(scratch_state(g, seq, head, 0) + i / 4 * 128 + c0 + i % 4 * 4);
+    const int k = tid / 4, c = tid % 4 * 4;              // rows k and k + 64
+    for (int s = 1; s < n - 1; ++s) {
+        const float* N = scratch_state(g, seq, head, n - 1 + 2 * (s - 1));
+        const float4* M = reinterpret_cast<const float4*>(scratch_state(g, seq, head, n - 1 + 2 * (s - 1) + 1));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int e = i * kJoinThreads + tid;
+            *reinterpret_cast<float4*>(mat + e / 32 * 132 + e % 32 * 4) = M[e];
+        }
+        float4 a = *reinterpret_cast<const float4*>(N + k * 128 + c0 + c), b = *reinterpret_cast<const float4*>(N + (k + 64) * 128 + c0 + c);
+        __syncthreads();
+#pragma unroll 4
+        for (int j = 0; j < 128; j += 4) {
+            const float4 ma = *reinterpret_cast<const float4*>(mat + k * 132 + j), mb = *reinterpret_cast<const float4*>(mat + (k + 64) * 132 + j);
+            const float fa[4] = {ma.x, ma.y, ma.z, ma.w}, fb[4] = {mb.x, mb.y, mb.z, mb.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float4 x = *reinterpret_cast<const float4*>(sx + (j + e) * 16 + c);
+                a.x = fmaf(fa[e], x.x, a.x); a.y = fmaf(fa[e], x.y, a.y); a.z = fmaf(fa[e], x.z, a.z); a.w = fmaf(fa[e], x.w, a.w);
+                b.x = fmaf(fb[e], x.x, b.x); b.y = fmaf(fb[e], x.y, b.y); b.z = fmaf(fb[e], x.z, b.z); b.w = fmaf(fb[e], x.w, b.w);
+            }
+        }
+        __syncthreads();
+        *reinterpret_cast<float4*>(sx + k * 16 + c) = a;
+        *reinterpret_cast<float4*>(sx + (k + 64) * 16 + c) = b;
+        float* to = scratch_state(g, seq, head, s);
+        *reinterpret_cast<float4*>(to + k * 128 + c0 + c) = a;
+        *reinterpret_cast<float4*>(to + (k + 64) * 128 + c0 + c) = b;
+    }
+}
+
 }  // namespace
 
 // bf16 rows in tiles of 64 x 128 elements, as they are.
@@ -1173,10 +1310,21 @@ static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uin
                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Segments of a sequence: three or more, as many as give each SM one of the first pass's 2 n - 3 units, of 1024 tokens at least on the average.
+static int delta_segments(long long sequences, long long heads, long long tokens) {
+    const long long units = sequences * heads;
+    if (units > 49) return 1;
+    long long n = (148 / units + 3) / 2;
+    if (n > tokens / (sequences * 1024)) n = tokens / (sequences * 1024);
+    return n < 3 ? 1 : n > 16 ? 16 : (int)n;
+}
+
 size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens) {
     if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens == 0) return 0;
-    // (the groups are not known here: every head may be one)
-    return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows);
+    // (The groups are not known here: every head may be one.  Fewer sequences than asked for may be split into more segments: of all of them
+    // together at most 148 (3 n - 5) / (2 n - 3) states.)
+    const size_t states = c.heads <= 49 && tokens >= 3 * 1024 ? 222 : 0;
+    return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows) + ((size_t)sequences * 4 + 15) / 16 * 16 + states * 128 * 128 * 4;
 }
 
 int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream) {
@@ -1185,9 +1333,15 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     g.p = p;
     const long long units = (long long)p.pr.N * p.H, chunks = (long long)p.pr.T / kQ + p.pr.N;
     const long long preps = chunks * p.G * ((p.H / p.G + 1) / 2);
-    if (units > (1 << 30) || preps > 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
-    g.units = (int)units;
+    if (units > (1 << 30) || preps >= 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    g.segments = delta_segments(p.pr.N, p.H, p.pr.T);
+    g.preps = (int)preps;
     g.rows = p.work + (size_t)chunks * p.H * kBlock;
+    unsigned char* behind = g.rows + (size_t)chunks * p.H * kRows;
+    // (A rank among N sequences takes N comparisons: beyond some thousands the order is left as it is.)
+    const bool sort = g.segments == 1 && p.pr.N > 1 && p.pr.N <= 4096;
+    g.order = sort ? reinterpret_cast<int*>(behind) : nullptr;
+    g.states = reinterpret_cast<float*>(behind + ((size_t)p.pr.N * 4 + 15) / 16 * 16);
     if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
         !make_map(&g.tk, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.k, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.k_stride * 2, kQ) ||
         !make_rows_map(&g.tv, p.v, (uint64_t)p.H * 128, (uint64_t)p.pr.T, (uint64_t)p.v_stride * 2)) {
@@ -1196,11 +1350,19 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     }
     cudaError_t e = unlock_smem(ctx, delta_prep_kernel);
     if (e == cudaSuccess) e = unlock_smem(ctx, delta_scan_tc_kernel);
+    if (e == cudaSuccess && g.segments > 1) e = unlock_smem(ctx, delta_join_kernel);
     if (e != cudaSuccess) { ctx->last_cuda_error = e; return SKETCHSSM_CUDA_ERROR; }
-    const int rc = launch_layer<DeltaArgs>(ctx, delta_prep_kernel, dim3((unsigned)preps), dim3(kPrepThreads), kPrepSmem, stream, g);
-    if (rc != SKETCHSSM_OK) return rc;
-    const unsigned grid = (unsigned)(units < sm_count(ctx) ? units : sm_count(ctx));
-    return launch_layer<DeltaArgs>(ctx, delta_scan_tc_kernel, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
+    int rc = launch_layer<DeltaArgs>(ctx, delta_prep_kernel, dim3((unsigned)(preps + sort)), dim3(kPrepThreads), kPrepSmem, stream, g);
+    auto scan = [&](int pass, long long parts) {
+        g.pass = pass;
+        g.units = (int)(units * parts);
+        const unsigned grid = (unsigned)(g.units < sm_count(ctx) ? g.units : sm_count(ctx));
+        return launch_layer<DeltaArgs>(ctx, delta_scan_tc_kernel, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
+    };
+    if (rc == SKETCHSSM_OK && g.segments == 1) return scan(0, 1);
+    if (rc == SKETCHSSM_OK) rc = scan(1, 2 * g.segments - 3);
+    if (rc == SKETCHSSM_OK) rc = launch_layer<DeltaArgs>(ctx, delta_join_kernel, dim3((unsigned)(units * 8)), dim3(kJoinThreads), kJoinSmem, stream, g);
+    return rc == SKETCHSSM_OK ? scan(2, g.segments - 1) : rc;
 }
 
 }  // namespace sketchssm

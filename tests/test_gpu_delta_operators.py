@@ -50,6 +50,10 @@ SCAN = [
     ("kda", [200], 2, 1, 128, 64, "f32", "f32", None, None, 0, 0),
     ("gdn", [40] * 60, 16, 4, 128, 128, "f32", "f32", [-1] * 55 + [0, 1, 2, 3, 4], [i % 3 + 5 if i % 4 else -1 for i in range(60)], 0, 0),
     ("kda", [20, 41] * 40, 8, 8, 64, 64, "f32", "f32", [-1] * 75 + [0, 1, 2, 3, 4], None, 0, 0),
+    # sequences split into segments: one from a stored state into the same entry, ragged ones with an empty and a short one, many segments
+    ("gdn", [3300], 2, 1, 128, 128, "bf16", "bf16", [4], [4], 0, 3),
+    ("gdn", [5000, 0, 90, 7500], 3, 3, 128, 128, "bf16", "bf16", [0, 1, 2, 3], [-1, 6, 2, 3], 2, 0),
+    ("gdn", [9100], 1, 1, 128, 128, "bf16", "bf16", None, None, 0, 0),
     ("gdn", [70, 128, 63] * 20, 8, 4, 128, 128, "bf16", "bf16", [-1] * 55 + [0, 1, 2, 3, 4], [i % 3 + 5 if i % 4 else -1 for i in range(60)], 0, 0),
 ]
 
