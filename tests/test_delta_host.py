@@ -56,6 +56,13 @@ def test_scan_scratch_refusals(lib):
                 assert scan(lib, ctx, pr=prompts(sequences=3, tokens=tokens), **bad) == INVALID
 
 
+@pytest.mark.parametrize("kind", [GDN, KDA])
+def test_no_sequences_need_no_scratch(lib, kind):
+    ctx, n = context(lib, kind=kind, dv=128), ctypes.c_size_t(7)
+    assert lib.sketchssm_delta_work_bytes(ctx, 0, 100, ctypes.byref(n)) == OK and n.value == 0
+    assert scan(lib, ctx, pr=prompts(sequences=0, tokens=100), work=None, wb=0) == OK
+
+
 def step(lib, ctx, G=2, W=4, eps=1e-6, qs=0.1, weight=P, bias=P, state=P, x=P, xs=1536, b=P, bs=8, dt=P, ds=1024, a=P, dt_bias=P, q=P, k=P, v=P, beta=P,
          decay=P):
     return lib.sketchssm_delta_step(ctx, G, W, eps, qs, weight, bias, state, x, xs, b, bs, dt, ds, a, dt_bias, q, k, v, beta, decay, None)
