@@ -236,7 +236,7 @@ int sketchssm_delta_step(sketchssm_ctx* ctx, int groups, int width, float eps, f
 int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes) {
     if (ctx == nullptr || bytes == nullptr || sequences < 0 || tokens < 0) return SKETCHSSM_INVALID_ARG;
     const sketchssm_config& c = ctx->cfg;
-    *bytes = c.kind == SKETCHSSM_KDA ? (size_t)tokens * c.heads * c.dk * 4 : delta_tc_work_bytes(c, sequences, tokens);
+    *bytes = c.kind == SKETCHSSM_KDA ? (sequences > 0 ? (size_t)tokens * c.heads * c.dk * 4 : 0) : delta_tc_work_bytes(c, sequences, tokens);
     return SKETCHSSM_OK;
 }
 
