@@ -10,6 +10,10 @@
 //
 // Roles: one thread issues the copies (TMA, 128-byte swizzle), one warp the products (an elected lane of the converged warp), the
 // others take the sums out.
+//
+// What bounds it (weights from memory, replayed from a graph): 64 x 12352 x 2048 takes 9.8 us, of which the weights' 25 MB are 3.9 at 6.46 TB/s;
+// the rest is the start, the first copies' way and the end of 97 CTAs with one tile each, the fullest use of 148 SMs that tiles of 128 weights
+// allow.  777 x 2049 x 4096, 119 tiles, 13.8 us: 125 MB of operands from L2 at 9 TB/s, near what it gives.
 #include "tma.cuh"
 
 namespace sketchssm {
@@ -262,14 +266,17 @@ int launch_integer_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) 
         const int rc = launch_integer_matmul_pair(ctx, p, stream);
         if (rc != SKETCHSSM_UNSUPPORTED_SHAPE) return rc;
     }
-    // The narrowest tile that holds the tokens.
+    // The narrowest tile that holds the tokens (1 x 12352 x 2048: 8.1 us; 64: 9.8; 128: 10.8).
     const int bn = p.M <= 16 ? 16 : p.M <= 32 ? 32 : p.M <= 64 ? 64 : 128;
     const long long tiles = nt * ((p.M + bn - 1) / bn);
-    // Few tiles: the inner axis split over a cluster, while that leaves a CTA two blocks and every SM one CTA.
+    // Few tiles: the inner axis split over a cluster, while that leaves a CTA two blocks and every SM one CTA.  (Clusters of eight CTAs that have an SM
+    // to themselves find no place for more than about half of the SMs at a time: 128 x 2048 x 4096 in 8.9 us with clusters of four, 15.0 with
+    // eight; but 100 x 1024 x 8192, 8 tiles, 10.7 and 9.0.  Not split: 13.5 us for the first; 64 x 2048 x 4096 12.3, split 7.9.)
     int ks = 1;
-    while (ks < 8 && tiles * ks * 2 <= (long long)sms && p.KB >= ks * 4) ks *= 2;
+    while (ks < 8 && tiles * ks * 2 <= (long long)(bn == 128 && ks == 4 ? sms / 2 : sms) && p.KB >= ks * 4) ks *= 2;
     if (bn == 16) return launch_tiles<16, 4, 6, 2>(ctx, p, ks, stream);
     if (bn == 32) return launch_tiles<32, 4, 5, 2>(ctx, p, ks, stream);
+    // (64 x 12352 x 2048, not split: 9.8 us with eight stages, 10.6 with four and two CTAs an SM; 64 x 2048 x 4096, by eight: 11.6 and 7.9.)
     if (bn == 64) return ks <= 2 ? launch_tiles<64, 4, 8, 1>(ctx, p, ks, stream) : launch_tiles<64, 4, 4, 2>(ctx, p, ks, stream);
     return launch_tiles<128, 8, 6, 1>(ctx, p, ks, stream);
 }

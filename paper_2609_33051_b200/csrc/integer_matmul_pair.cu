@@ -7,6 +7,11 @@
 // Roles per CTA: one thread issues the copies of its half (they report to the leader's barrier), one warp of the leader the products;
 // sixteen warps take a tile's sums out (32 lanes, 64 columns each), times both scales, and store them through shared memory (TMA), or
 // directly where a row or the row stride is no multiple of 16 bytes.
+//
+// What bounds it: the operands' way from L2.  16384 x 12352 x 2048 to bf16 takes 293 us (L2 flushed before each call; 298 one after another):
+// 2.83 Pop/s, and 3136 tiles of 1 MB of operands are 11 TB/s, about what L2 gives.  The output's 405 MB are 63 us of memory.  With four
+// stages 320 us; five are what 227 KB hold beside the stores' staging.  Bands of 8 or 16 tiles of tokens, walked down a band first so that fewer
+// operand tiles are in use at a time: 301 and 294, no gain.
 #include "tma.cuh"
 
 namespace sketchssm {
@@ -15,7 +20,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kStages = 4, kEpiWarps = 16, kThreads = 32 * (4 + kEpiWarps);
+constexpr int kStages = 5, kEpiWarps = 16, kThreads = 32 * (4 + kEpiWarps);
 constexpr uint32_t kHalf = 128u * 128u, kStageBytes = 2u * kHalf;
 constexpr uint32_t kOut = kStages * kStageBytes;
 constexpr uint32_t kBars = kOut + kEpiWarps * 4096u;
@@ -220,7 +225,9 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
 int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
     const long long nt = (p.N + 255) / 256, tiles = nt * ((p.M + 255) / 256);
     const int pairs = sm_count(ctx) / 2;
-    // From where the other kernel's 128 x 128 tiles are more than the SMs, so that some of them would take two.
+    // From where the other kernel's 128 x 128 tiles are more than the SMs, so that some of them would take two.  (256 x 9472 x 2048, 148 such tiles:
+    // 11.0 us there, 11.9 here; 256 x 9600, 150 of them, 15.3 and 11.8; 777 x 2049 x 4096, 119, 14.7 and 19.6; 4096 x 2048 x 4096, 512, 45.4
+    // and 28.2.)
     const long long small = (long long)((p.N + 127) / 128) * ((p.M + 127) / 128);
     if (small <= sm_count(ctx) || tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
     PairArgs g;
