@@ -9,11 +9,17 @@
 //     u_a = beta_a (v_a - S^T E_a k_a - sum_{s < a} <k_a, D_sa k_s> u_s),   out_a = S^T E_a q_a + sum_{s <= a} <q_a, D_sa k_s> u_s,
 //     S <- E_3 S + sum_s D_s3 k_s u_s^T,
 // so that S is read with four keys and four queries at once and moved on once, and the sums over the lanes, which everything waits for, are
-// made once in four tokens (token by token, four ragged prompts in a row took 3.5 times as long where there are few heads).
+// made once in four tokens.
 //
 // A CTA takes `cols` value columns of one head of one sequence, the longest sequences first.  LK neighbouring lanes share four columns: eight, so
-// that a thread holds sixteen rows (K = 128: four runs of four) of them, or sixteen where there are few heads.  Tokens come through shared memory, a stage of them while the one
-// before is worked on; what four tokens have to do with one another is worked out by a warp, its lanes over the channels.
+// that a thread holds sixteen rows (K = 128: four runs of four) of them, or sixteen where there are few heads.  Tokens come through shared memory,
+// a stage of them while the one before is worked on; what four tokens have to do with one another is worked out by a warp, its lanes over the
+// channels.
+//
+// What bounds it: multiplications.  4096 KDA tokens in 8 prompts of 32 heads, 64 columns a CTA, take 560 us (token by token 1400); three products with
+// 16384 elements of a state a token are 6.4 G, 180 us at the card's rate.  Per four tokens a thread has 416 instructions for two such
+// products each, two cycles long, and 175 others in the same pipe; the longest prompt's CTAs end last.  1500 fp32 tokens in 7
+// prompts of 24 heads of 80 columns, 16 columns a CTA: 203 us (token by token 306), bound by the longest prompt's chain of sums over lanes.
 #include "pairs.cuh"
 
 namespace sketchssm {
@@ -216,7 +222,8 @@ __device__ __forceinline__ int by_length(const PromptsDev& pr, int place) {
 }
 
 template <typename T, int K, bool KDA, int LK>
-__global__ void __launch_bounds__(LK * 32) delta_scan_kernel(const DeltaParams p) {
+// (All the registers that it asks for, 170 to 190: with 168, three CTAs an SM, KDA's 560 us become 718.)
+__global__ void __maxnreg__(255) delta_scan_kernel(const DeltaParams p) {
     constexpr int RUNS = K / (4 * LK), RP = 2 * RUNS, STEPS = LK == 8 ? 3 : 4;     // runs of four rows and pairs of rows of a thread; halvings of its lanes
     constexpr int TOK = kTok<KDA>, GR = TOK / 4;
     extern __shared__ __align__(16) unsigned char sm[];
@@ -506,8 +513,9 @@ int launch_lanes(Ctx* ctx, const DeltaParams& p, long long units, cudaStream_t s
 template <typename T, int K, bool KDA>
 int launch_cores(Ctx* ctx, const DeltaParams& p0, cudaStream_t stream) {
     DeltaParams p = p0;
-    // All columns of a head in a CTA, or half of them (what four tokens have to do with one another is then worked out once for them), where that
-    // leaves every SM a CTA; below that sixteen columns and sixteen lanes for four of them.
+    // 64 or 80 columns of a head in a CTA (what four tokens have to do with one another is then worked out once for them) where that leaves every SM
+    // two; below that sixteen columns and sixteen lanes for four of them.  Measured: 8 KDA prompts of 32 heads, 64 columns and 8 lanes 560 us, 64
+    // and 16 lanes 647, 16 and 8 lanes more than twice as long as 64; 7 prompts of 24 heads, 80 columns, sixteen at a time: 8 lanes 283 us, 16 lanes 223.
     const long long heads = (long long)p.pr.N * p.H;
     p.cols = 16;
     for (int c : {64, 80})
