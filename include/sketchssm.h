@@ -392,7 +392,13 @@ int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int toke
  * not touched: a sketchssm_state_update without a token builds them before the first decode step.
  *   q, k : [T][G][K] io strided, a group for H / G heads;  v : [T][H][V] io strided;  b : [T][H] io (stride free of the 16-byte rule);
  *   dt : [T][H] io (stride free of it; GDN) or [T][H][K] io strided (KDA);  a [H] fp32, <= 0;  dt_bias [H] or [H][K] fp32, or NULL;
- *   eps > 0;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked here, the call says it. */
+ *   eps > 0;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked here, the call says it.
+ * GDN with bf16 io and out, dk = dv = 128 and more than 32 tokens goes through the tensor cores in chunks of 64, everything else over CUDA cores.  Either way
+ * states are fp32, sums of fp32 accuracy (operands of 22 bits), and an output is rounded once.  Results do not depend on the order in which
+ * parts of the GPU run; they do, in their last bits, on the number of sequences and heads (how the tokens are split).
+ * A token that is not finite (a key or query whose squared length is not, counts as such): from it on its sequence and head's outputs and state
+ * are not finite, all of them or those columns and rows that it reaches; no other sequence's, no other head's, no earlier token's.
+ * The scratch is 4 K bytes a token and head (KDA), 50 to 75 KB for 64 tokens of a head and 14 MB at most (GDN on the tensor cores), else none. */
 int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, float eps, float q_scale, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* b, int64_t b_stride, const void* dt,
                          int64_t dt_stride, const void* a, const void* dt_bias, void* out, int64_t out_stride, int out_dtype, void* work,
@@ -405,7 +411,7 @@ int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, i
  *     h = x;   with residual: h = x + residual, and residual_out = h (before rounding to io h goes on);
  *     y = h / sqrt(mean(h^2) + eps) weight;   with gate: y times the gate's value
  *     scale = max|y| / 127 over the row,  out8 = y 127 / max|y|, to nearest even (a row whose largest value is below 1e-30 is stored as zeros;
- *     one with a value that is not finite as zeros or whole numbers with a scale that is not a number)
+ *     one with a value that is not finite as zeros with a scale that is not a number)
  * and, if wanted, y to out (io).
  *   rows >= 0; width at most 16384; group: a divisor of width that is a multiple of 8 (the width itself: a norm of whole rows)
  *   x [rows][width] of x_dtype strided; weight [group] fp32; residual, residual_out [rows][width] io, dense, both or none, residual_out may be

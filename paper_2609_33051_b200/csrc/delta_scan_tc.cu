@@ -219,17 +219,32 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
     if (u == g.preps) {                                  // (one CTA more: every sequence's place by its number of chunks)
         grid_dep_wait();
         grid_dep_launch_dependents();
-        for (int i = tid; i < p.pr.N; i += kPrepThreads) {
+        // (sorted by counting: a length's exponent and first three bits are its class; which of a class comes first is left open, and changes nothing
+        // but the time)
+        int* count = reinterpret_cast<int*>(smem);
+        auto place = [&](int i) {
             const int2 rows = seq_rows(p.pr, i);
-            const int mine = (rows.y - rows.x + kQ - 1) / kQ;
-            int place = 0;
-            for (int j = 0; j < p.pr.N; ++j) {
-                const int2 r = seq_rows(p.pr, j);
-                const int other = (r.y - r.x + kQ - 1) / kQ;
-                place += other > mine || (other == mine && j < i);
-            }
-            g.order[place] = i;
+            const int chunks = (rows.y - rows.x + kQ - 1) / kQ;
+            return kPrepThreads - 1 - (chunks > 0 ? min((int)(__float_as_uint((float)chunks) >> 20) - (127 << 3) + 1, kPrepThreads - 1) : 0);
+        };
+        count[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < p.pr.N; i += kPrepThreads) atomicAdd(count + place(i), 1);
+        __syncthreads();
+        const int mine = count[tid];
+        int before = mine;                               // of the classes up to this one
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, before, o);
+            if (lane >= o) before += up;
         }
+        int* totals = count + kPrepThreads;
+        if (lane == 31) totals[warp] = before;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) before += totals[w];
+        count[tid] = before - mine;
+        __syncthreads();
+        for (int i = tid; i < p.pr.N; i += kPrepThreads) g.order[min(atomicAdd(count + place(i), 1), p.pr.N - 1)] = i;
         return;
     }
     const int batch = u % batches;
@@ -248,9 +263,14 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
     grid_dep_launch_dependents();
     const uint32_t tmem = *slot;
     // the sequence of this chunk: the last one whose first chunk is not behind it
-    int n = 0;
-    for (int j = lane; j - lane < p.pr.N; j += 32)
-        n += __popc(__ballot_sync(0xffffffffu, j < p.pr.N && chunk_base(seq_start(p.pr, min(j, p.pr.N - 1)), j) <= chunk));
+    auto not_behind = [&](int j, int end) { return __popc(__ballot_sync(0xffffffffu, j < end && chunk_base(seq_start(p.pr, min(j, p.pr.N - 1)), j) <= chunk)); };
+    int n = 0, end = p.pr.N;                             // (n of them are not behind it, those from `end` on are)
+    while (end - n > 32) {
+        const int step = (end - n + 31) / 32, c = not_behind(n + (lane + 1) * step - 1, end);
+        n += c * step;
+        end = min(end, n + step);
+    }
+    n += not_behind(n + lane, end);
     bool ok = n > 0;
     int t0 = 0, valid = 0;
     if (ok) {
@@ -1319,8 +1339,13 @@ static int delta_segments(long long sequences, long long heads, long long tokens
     return n < 3 ? 1 : n > 16 ? 16 : (int)n;
 }
 
+// Tokens of a batch up to which the CUDA cores are faster whatever the sequences are: 1 token of 4 heads in 6.7 us, 18.5 here; 16 sequences of 2
+// tokens, 32 heads, 27.6 and 47.3; one of 32 tokens, 32 heads, 13.4 and 18.9; but one of 64 22.5 and 18.4.  (More sequences of a few tokens would be faster
+// there too, 256 of 4, 4 heads, 45 and 81, but one long one among them would not, and the lengths are not known here.)
+constexpr long long kFewTokens = 32;
+
 size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens) {
-    if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens == 0) return 0;
+    if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens <= kFewTokens) return 0;
     // (The groups are not known here: every head may be one.  Fewer sequences than asked for may be split into more segments: of all of them
     // together at most 148 (3 n - 5) / (2 n - 3) states.)
     const size_t states = c.heads <= 49 && tokens >= 3 * 1024 ? 222 : 0;
@@ -1328,7 +1353,7 @@ size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long 
 }
 
 int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream) {
-    if (!bf16 || !p.out_bf16 || p.K != 128 || p.V != 128 || p.pr.T == 0 || ctx->cfg.kind != SKETCHSSM_GDN) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    if (!bf16 || !p.out_bf16 || p.K != 128 || p.V != 128 || p.pr.T <= kFewTokens || ctx->cfg.kind != SKETCHSSM_GDN) return SKETCHSSM_UNSUPPORTED_SHAPE;
     DeltaArgs g;
     g.p = p;
     const long long units = (long long)p.pr.N * p.H, chunks = (long long)p.pr.T / kQ + p.pr.N;
@@ -1338,8 +1363,7 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     g.preps = (int)preps;
     g.rows = p.work + (size_t)chunks * p.H * kBlock;
     unsigned char* behind = g.rows + (size_t)chunks * p.H * kRows;
-    // (A rank among N sequences takes N comparisons: beyond some thousands the order is left as it is.)
-    const bool sort = g.segments == 1 && p.pr.N > 1 && p.pr.N <= 4096;
+    const bool sort = g.segments == 1 && p.pr.N > 1;
     g.order = sort ? reinterpret_cast<int*>(behind) : nullptr;
     g.states = reinterpret_cast<float*>(behind + ((size_t)p.pr.N * 4 + 15) / 16 * 16);
     if (!make_map(&g.tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.q, (uint64_t)p.G * 128, (uint64_t)p.pr.T, (uint64_t)p.q_stride * 2, kQ) ||
