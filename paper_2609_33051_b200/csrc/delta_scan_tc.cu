@@ -47,7 +47,7 @@ struct DeltaArgs {
     int* order;
     float* states;
     int units, preps;
-    int segments, pass;        // parts that a sequence is split into; 0: whole ones, 1, 2: see decode_unit
+    int segments, turns, pass; // parts that a sequence is split into; units of the first pass a CTA; 0: whole ones, 1, 2: see decode_unit
 };
 
 // What a CTA of the second kernel takes at a time: a sequence and head, or a segment of one.
@@ -65,31 +65,54 @@ __device__ __forceinline__ int chunk_base(int row0, int i) { return row0 / kQ + 
 // Unit number `it` of this CTA.  Whole sequences go out in the order of their lengths, the longest first, to and fro over the CTAs.
 // Few sequences and heads leave most of the card idle for as long as the longest takes.  Then a sequence is split into n segments.  What
 // a segment makes of a state is linear: S <- M S + N.  The first pass takes the first segment with its outputs, and of each that others follow N
-// (from a state of zeros) and M (from the unit matrix, without values), side by side; a small kernel goes through them, and the second pass takes
-// all others from the states that they begin with.
+// (from a state of zeros) and M (from the unit matrix, without values); a small kernel goes through them, and the second pass takes
+// all others from the states that they begin with.  In the first pass a CTA takes a first segment, or `turns` of the other units, and the first
+// segment is that many times as long.
 __device__ __forceinline__ bool decode_unit(const DeltaArgs& g, int it, Unit& x) {
     const DeltaParams& p = g.p;
-    const int G = (int)gridDim.x, i = (int)blockIdx.x, k = it * G + ((it & 1) ? G - 1 - i : i);
-    if (k >= g.units) return false;
-    int part = 0, u = k;
+    const int G = (int)gridDim.x, i = (int)blockIdx.x;
+    int u;
     x.kind = kWhole;
     x.seg = 0;
-    if (g.pass != 0) {
-        const int parts = g.pass == 1 ? 2 * g.segments - 3 : g.segments - 1;
-        part = k % parts;
-        u = k / parts;
-        x.kind = g.pass == 2 ? kLater : part == 0 ? kFirst : (part & 1) ? kAlone : kMap;
-        x.seg = g.pass == 2 ? part + 1 : (part + 1) / 2;
+    if (g.pass == 1) {
+        const int pairs = p.pr.N * p.H;
+        if (i < pairs) {
+            if (it > 0) return false;
+            x.kind = kFirst;
+            u = i;
+        } else {
+            const int k = (i - pairs) * g.turns + it;
+            if (it >= g.turns || k >= g.units) return false;
+            x.kind = (k & 1) ? kMap : kAlone;
+            x.seg = k / 2 / pairs + 1;
+            u = k / 2 % pairs;
+        }
+    } else {
+        const int k = it * G + ((it & 1) ? G - 1 - i : i);
+        if (k >= g.units) return false;
+        u = k;
+        if (g.pass == 2) {
+            x.kind = kLater;
+            x.seg = k % (g.segments - 1) + 1;
+            u = k / (g.segments - 1);
+        }
     }
     x.head = u % p.H;
     x.seq = u / p.H;
     if (g.order != nullptr) x.seq = min(max(g.order[x.seq], 0), p.pr.N - 1);
     x.outputs = x.kind <= kLater;
     const int2 rows = seq_rows(p.pr, x.seq);
-    const int chunks = (rows.y - rows.x + kQ - 1) / kQ, per = g.pass == 0 ? chunks : (chunks + g.segments - 1) / g.segments;
-    x.t0 = min(rows.y, rows.x + x.seg * per * kQ);
-    x.t1 = min(rows.y, x.t0 + per * kQ);
-    x.chunk = chunk_base(rows.x, x.seq) + x.seg * per;
+    const int chunks = (rows.y - rows.x + kQ - 1) / kQ;
+    if (g.pass == 0) {
+        x.t0 = rows.x;
+        x.t1 = rows.y;
+        x.chunk = chunk_base(rows.x, x.seq);
+    } else {
+        const int all = g.turns + g.segments - 1, per = (chunks + all - 1) / all, first = x.seg == 0 ? 0 : (g.turns + x.seg - 1) * per;
+        x.t0 = (int)min((long long)rows.y, rows.x + (long long)first * kQ);
+        x.t1 = (int)min((long long)rows.y, x.t0 + (long long)(x.seg == 0 ? g.turns * per : per) * kQ);
+        x.chunk = chunk_base(rows.x, x.seq) + first;
+    }
     return true;
 }
 // The stored state before the unit, and whether it is one (not zeros).
@@ -1275,46 +1298,65 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     if (warp == 1) tmem_free<512>(tmem);
 }
 
-// The states that segments 2 .. n - 1 begin with: one after the other M S + N.  A CTA takes 16 value columns of a sequence and head; a thread
-// two rows of four columns.
+// The states that segments 2 .. n - 1 begin with: one after the other M S + N.  A CTA takes 32 value columns of a sequence and head; a thread
+// four rows of four columns.  The next M comes while one is multiplied.
 constexpr int kJoinThreads = 256;
-constexpr uint32_t kJoinSmem = (128u * 132u + 128u * 16u) * 4u;
+constexpr uint32_t kJoinMat = 128u * 132u;
+constexpr uint32_t kJoinSmem = (2u * kJoinMat + 128u * 32u) * 4u;
 __global__ void __launch_bounds__(kJoinThreads) delta_join_kernel(const DeltaArgs g) {
-    extern __shared__ float mat[];                       // M [128][132], S [128][16]
-    float* sx = mat + 128 * 132;
+    extern __shared__ __align__(16) float mat[];         // two times M [128][132], S [128][32]
+    float* sx = mat + 2 * kJoinMat;
     grid_dep_wait();
     grid_dep_launch_dependents();
-    const int tid = (int)threadIdx.x, n = g.segments, c0 = (int)blockIdx.x % 8 * 16, head = (int)blockIdx.x / 8 % g.p.H, seq = (int)blockIdx.x / 8 / g.p.H;
-    for (int i = tid; i < 512; i += kJoinThreads)
-        *reinterpret_cast<float4*>(sx + i * 4) = *reinterpret_cast<const float4*>(scratch_state(g, seq, head, 0) + i / 4 * 128 + c0 + i % 4 * 4);
-    const int k = tid / 4, c = tid % 4 * 4;              // rows k and k + 64
-    for (int s = 1; s < n - 1; ++s) {
-        const float* N = scratch_state(g, seq, head, n - 1 + 2 * (s - 1));
-        const float4* M = reinterpret_cast<const float4*>(scratch_state(g, seq, head, n - 1 + 2 * (s - 1) + 1));
+    const int tid = (int)threadIdx.x, n = g.segments, c0 = (int)blockIdx.x % 4 * 32, head = (int)blockIdx.x / 4 % g.p.H, seq = (int)blockIdx.x / 4 / g.p.H;
+    auto copy = [&](int s) {
+        const float* M = scratch_state(g, seq, head, n - 1 + 2 * (s - 1) + 1);
+        float* to = mat + (s & 1) * kJoinMat;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int e = i * kJoinThreads + tid;
-            *reinterpret_cast<float4*>(mat + e / 32 * 132 + e % 32 * 4) = M[e];
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + e / 32 * 132 + e % 32 * 4)), "l"(M + e * 4) : "memory");
         }
-        float4 a = *reinterpret_cast<const float4*>(N + k * 128 + c0 + c), b = *reinterpret_cast<const float4*>(N + (k + 64) * 128 + c0 + c);
-        __syncthreads();
-#pragma unroll 4
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    copy(1);
+    for (int i = tid; i < 1024; i += kJoinThreads)
+        *reinterpret_cast<float4*>(sx + i * 4) = *reinterpret_cast<const float4*>(scratch_state(g, seq, head, 0) + i / 8 * 128 + c0 + i % 8 * 4);
+    const int k = tid / 8, c = tid % 8 * 4;              // rows k, k + 32, ..
+    for (int s = 1; s < n - 1; ++s) {
+        const float* N = scratch_state(g, seq, head, n - 1 + 2 * (s - 1)) + k * 128 + c0 + c;
+        float4 y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = *reinterpret_cast<const float4*>(N + q * 32 * 128);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();                                 // M and S are there, and nobody reads the other M any more
+        if (s + 1 < n - 1) copy(s + 1);
+        const float* M = mat + (s & 1) * kJoinMat + k * 132;
+#pragma unroll 2
         for (int j = 0; j < 128; j += 4) {
-            const float4 ma = *reinterpret_cast<const float4*>(mat + k * 132 + j), mb = *reinterpret_cast<const float4*>(mat + (k + 64) * 132 + j);
-            const float fa[4] = {ma.x, ma.y, ma.z, ma.w}, fb[4] = {mb.x, mb.y, mb.z, mb.w};
+            float m[4][4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 v = *reinterpret_cast<const float4*>(M + q * 32 * 132 + j);
+                m[q][0] = v.x; m[q][1] = v.y; m[q][2] = v.z; m[q][3] = v.w;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float4 x = *reinterpret_cast<const float4*>(sx + (j + e) * 16 + c);
-                a.x = fmaf(fa[e], x.x, a.x); a.y = fmaf(fa[e], x.y, a.y); a.z = fmaf(fa[e], x.z, a.z); a.w = fmaf(fa[e], x.w, a.w);
-                b.x = fmaf(fb[e], x.x, b.x); b.y = fmaf(fb[e], x.y, b.y); b.z = fmaf(fb[e], x.z, b.z); b.w = fmaf(fb[e], x.w, b.w);
+                const float4 x = *reinterpret_cast<const float4*>(sx + (j + e) * 32 + c);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    y[q].x = fmaf(m[q][e], x.x, y[q].x); y[q].y = fmaf(m[q][e], x.y, y[q].y);
+                    y[q].z = fmaf(m[q][e], x.z, y[q].z); y[q].w = fmaf(m[q][e], x.w, y[q].w);
+                }
             }
         }
-        __syncthreads();
-        *reinterpret_cast<float4*>(sx + k * 16 + c) = a;
-        *reinterpret_cast<float4*>(sx + (k + 64) * 16 + c) = b;
-        float* to = scratch_state(g, seq, head, s);
-        *reinterpret_cast<float4*>(to + k * 128 + c0 + c) = a;
-        *reinterpret_cast<float4*>(to + (k + 64) * 128 + c0 + c) = b;
+        __syncthreads();                                 // nobody reads S any more
+        float* to = scratch_state(g, seq, head, s) + k * 128 + c0 + c;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            *reinterpret_cast<float4*>(sx + (k + q * 32) * 32 + c) = y[q];
+            *reinterpret_cast<float4*>(to + q * 32 * 128) = y[q];
+        }
     }
 }
 
@@ -1330,13 +1372,27 @@ static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uin
                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Segments of a sequence: three or more, as many as give each SM one of the first pass's 2 n - 3 units, of 1024 tokens at least on the average.
-static int delta_segments(long long sequences, long long heads, long long tokens) {
-    const long long units = sequences * heads;
-    if (units > 49) return 1;
-    long long n = (148 / units + 3) / 2;
-    if (n > tokens / (sequences * 1024)) n = tokens / (sequences * 1024);
-    return n < 3 ? 1 : n > 16 ? 16 : (int)n;
+// Segments of a sequence (1: none) and units of the first pass a CTA, for the least time, estimated for sequences of the average length: turns + 1
+// times a segment's chunks at 3 us each, and what the small kernel and the units' starts take, some 30 us and 8 a segment.  Each pass has an
+// SM for each of its CTAs: in the first one of every first segment and one for `turns` of the 2 (n - 2) others, in the second n - 1.
+// One prompt of 16384 tokens: 32 heads 921 us whole, 692 with n = 3 and one turn.
+struct Split {
+    int segments, turns;
+};
+static Split delta_split(long long sequences, long long heads, long long tokens) {
+    const long long pairs = sequences * heads, chunks = (tokens / sequences + kQ - 1) / kQ;
+    Split best = {1, 1};
+    long long least = 3 * chunks;
+    for (int turns = 1; turns <= 4; ++turns)
+        for (int n = 3; n <= 16; ++n) {
+            if ((n - 1) * pairs > 148 || pairs + (2 * (n - 2) * pairs + turns - 1) / turns > 148) break;
+            const long long per = (chunks + turns + n - 2) / (turns + n - 1), time = 3 * (turns + 1) * per + 30 + 8 * (n - 2);
+            if (time < least) {
+                least = time;
+                best = {n, turns};
+            }
+        }
+    return best;
 }
 
 // Tokens of a batch up to which the CUDA cores are faster whatever the sequences are: 1 token of 4 heads in 6.7 us, 18.5 here; 16 sequences of 2
@@ -1347,8 +1403,8 @@ constexpr long long kFewTokens = 32;
 size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens) {
     if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens <= kFewTokens) return 0;
     // (The groups are not known here: every head may be one.  Fewer sequences than asked for may be split into more segments: of all of them
-    // together at most 148 (3 n - 5) / (2 n - 3) states.)
-    const size_t states = c.heads <= 49 && tokens >= 3 * 1024 ? 222 : 0;
+    // together 3 n - 5 states, less than three times 148.  Sequences below 15 chunks are not split.)
+    const size_t states = c.heads <= 74 && 3 * tokens > 64 * 38 ? 444 : 0;
     return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows) + ((size_t)sequences * 4 + 15) / 16 * 16 + states * 128 * 128 * 4;
 }
 
@@ -1359,7 +1415,9 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     const long long units = (long long)p.pr.N * p.H, chunks = (long long)p.pr.T / kQ + p.pr.N;
     const long long preps = chunks * p.G * ((p.H / p.G + 1) / 2);
     if (units > (1 << 30) || preps >= 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
-    g.segments = delta_segments(p.pr.N, p.H, p.pr.T);
+    const Split split = delta_split(p.pr.N, p.H, p.pr.T);
+    g.segments = split.segments;
+    g.turns = split.turns;
     g.preps = (int)preps;
     g.rows = p.work + (size_t)chunks * p.H * kBlock;
     unsigned char* behind = g.rows + (size_t)chunks * p.H * kRows;
@@ -1380,12 +1438,13 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     auto scan = [&](int pass, long long parts) {
         g.pass = pass;
         g.units = (int)(units * parts);
-        const unsigned grid = (unsigned)(g.units < sm_count(ctx) ? g.units : sm_count(ctx));
+        const long long ctas = pass == 1 ? units + (g.units + g.turns - 1) / g.turns : g.units;
+        const unsigned grid = (unsigned)(pass == 1 || ctas < sm_count(ctx) ? ctas : sm_count(ctx));
         return launch_layer<DeltaArgs>(ctx, delta_scan_tc_kernel, dim3(grid), dim3(kThreads), kSmemTc, stream, g);
     };
     if (rc == SKETCHSSM_OK && g.segments == 1) return scan(0, 1);
-    if (rc == SKETCHSSM_OK) rc = scan(1, 2 * g.segments - 3);
-    if (rc == SKETCHSSM_OK) rc = launch_layer<DeltaArgs>(ctx, delta_join_kernel, dim3((unsigned)(units * 8)), dim3(kJoinThreads), kJoinSmem, stream, g);
+    if (rc == SKETCHSSM_OK) rc = scan(1, 2 * (g.segments - 2));
+    if (rc == SKETCHSSM_OK) rc = launch_layer<DeltaArgs>(ctx, delta_join_kernel, dim3((unsigned)(units * 4)), dim3(kJoinThreads), kJoinSmem, stream, g);
     return rc == SKETCHSSM_OK ? scan(2, g.segments - 1) : rc;
 }
 
