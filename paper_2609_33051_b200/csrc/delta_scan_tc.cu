@@ -289,8 +289,8 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
     auto not_behind = [&](int j, int end) { return __popc(__ballot_sync(0xffffffffu, j < end && chunk_base(seq_start(p.pr, min(j, p.pr.N - 1)), j) <= chunk)); };
     int n = 0, end = p.pr.N;                             // (n of them are not behind it, those from `end` on are)
     while (end - n > 32) {
-        const int step = (end - n + 31) / 32, c = not_behind(n + (lane + 1) * step - 1, end);
-        n += c * step;
+        const int step = (end - n + 31) / 32, m = not_behind(n + (lane + 1) * step - 1, end);
+        n += m * step;
         end = min(end, n + step);
     }
     n += not_behind(n + lane, end);
@@ -312,12 +312,12 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
         }
         const int h0 = group * per + batch * 2, heads = min(2, per - batch * 2);
         const int mine = warp >> 2, role = warp & 3;     // this warp's head of the two; what it does for it
-        // gates, while the rows are under way: a warp a head, two neighbouring tokens a lane
+        // the gates' arguments: a warp a head, two neighbouring tokens a lane (asked for here, and used behind the norms)
+        float x[2] = {0.f, 0.f}, y[2] = {0.f, 0.f}, a2 = 0.f, bias = 0.f;
         if (role == 0 && mine < heads) {
             const int h = h0 + mine;
-            float* s = sums + mine * 3 * kQ;
-            const float a2 = p.a[h] * 1.4426950408889634f, bias = p.dt_bias != nullptr ? p.dt_bias[h] : 0.f;
-            float x[2] = {0.f, 0.f}, y[2] = {0.f, 0.f};
+            a2 = p.a[h] * 1.4426950408889634f;
+            bias = p.dt_bias != nullptr ? p.dt_bias[h] : 0.f;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (lane * 2 + i < valid) {
@@ -325,36 +325,6 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     x[i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.b)[r * p.b_stride + h]);
                     y[i] = __bfloat162float(static_cast<const __nv_bfloat16*>(p.dt)[r * p.dt_stride + h]);
                 }
-            double c[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bool in = lane * 2 + i < valid;
-                float l = a2 * softplus(y[i] + bias);
-                if (l < -160.f) l = -160.f;             // (2^-160 is zero in fp32; the bound keeps the sums finite)
-                // What is not finite counts in beta, by which its token is known: sums, L and T stay finite, as products of sixteen rows
-                // would carry it to the tokens before.
-                float beta = 1.f / (1.f + expf(-x[i]));
-                if (!(l <= 3.4028235e38f)) {
-                    l = 0.f;
-                    beta = __int_as_float(0x7fffffff);
-                }
-                s[2 * kQ + lane * 2 + i] = in ? beta : 0.f;
-                c[i] = (i > 0 ? c[0] : 0.0) + (double)(in ? l : 0.f);
-            }
-            double before = c[1];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double up = __shfl_up_sync(0xffffffffu, before, o);
-                if (lane >= o) before += up;
-            }
-            before = __shfl_up_sync(0xffffffffu, before, 1);
-            if (lane == 0) before = 0.0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const double x = c[i] + before, w = rint(x);
-                s[lane * 2 + i] = (float)w;
-                s[kQ + lane * 2 + i] = (float)(x - w);
-            }
         }
         ok = mbar_wait_bounded(bar, 0);
         ok = __syncthreads_and(ok) != 0;
@@ -398,7 +368,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
         }
         ok = __syncthreads_and(ok) != 0;
         if (tid == 64 && ok && batch == 0) bulk_s2g(g.rows + ((size_t)chunk * p.G + group) * kRows, smem, kRows);
-        if (warp == 0 && ok) {
+        if (warp == 1 && ok) {
             const uint64_t da = swizzled_desc(smem_u32(smem), 16u, 1024u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -408,6 +378,43 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             if (elect()) tc_commit(bar + 1);
             __syncwarp();
         }
+        // gates, while the product is made
+        if (ok && role == 0 && mine < heads) {
+            float* s = sums + mine * 3 * kQ;
+            double c[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool in = lane * 2 + i < valid;
+                float l = a2 * softplus(y[i] + bias);
+                if (l < -160.f) l = -160.f;             // (2^-160 is zero in fp32; the bound keeps the sums finite)
+                // What is not finite counts in beta, by which its token is known: sums, L and T stay finite, as products of sixteen rows
+                // would carry it to the tokens before.
+                float beta = 1.f / (1.f + expf(-x[i]));
+                if (!(l <= 3.4028235e38f)) {
+                    l = 0.f;
+                    beta = __int_as_float(0x7fffffff);
+                }
+                s[2 * kQ + lane * 2 + i] = in ? beta : 0.f;
+                c[i] = (i > 0 ? c[0] : 0.0) + (double)(in ? l : 0.f);
+            }
+            double before = c[1];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double up = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before += up;
+            }
+            before = __shfl_up_sync(0xffffffffu, before, 1);
+            if (lane == 0) before = 0.0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const double x = c[i] + before, w = rint(x);
+                s[lane * 2 + i] = (float)w;
+                s[kQ + lane * 2 + i] = (float)(x - w);
+            }
+        }
+        ok = ok && mbar_wait_bounded(bar + 1, 0);
+        if (tid == 64) tma_store_read();
+        ok = __syncthreads_and(ok) != 0;                // (from here on the tile's place is -L's)
         // what the second kernel reads of the gates
         if (ok && role >= 2 && mine < heads) {
             const int t = tid & 63;
@@ -421,9 +428,6 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             to[kAsk + t] = in ? e * norms[64 + t] : 0.f;
             if (t == 63) to[kKeep] = e;
         }
-        ok = ok && mbar_wait_bounded(bar + 1, 0);
-        if (tid == 64) tma_store_read();
-        ok = __syncthreads_and(ok) != 0;                // (from here on the tile's place is -L's)
         if (ok && mine < heads) {
             tc_fence_after();
             const int t = tid & 63;
@@ -463,6 +467,22 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     *reinterpret_cast<uint4*>(at + kPart) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
                 }
             };
+            // the same to memory, where a sector is written at once: two pieces of sixteen bytes, in the order that the swizzle gives them
+            auto put_out = [&](unsigned char* to, int e0, const uint64_t (&x)[8]) {
+                uint32_t h[2][8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) two_parts(x[i], h[0][i], h[1][i]);
+                unsigned char* at = to + t * 128 + (((e0 / 8) ^ (t & 6)) * 16);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t a[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) a[i] = (t & 1) ? h[e][i ^ 4] : h[e][i];
+                    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at + e * kPart), "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]),
+                                 "r"(a[4]), "r"(a[5]), "r"(a[6]), "r"(a[7])
+                                 : "memory");
+                }
+            };
             unsigned char* block = p.work + ((size_t)chunk * p.H + h0 + mine) * kBlock;
             if (role >= 2) {
                 const uint64_t factor = pack2(norms[64 + t], norms[64 + t]);
@@ -481,7 +501,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                             x[i] = pack2(e0 + 2 * i <= t ? a : 0.f, e0 + 2 * i + 1 <= t ? b : 0.f);
                         }
                     }
-                    put(block + kPOff, e0, x);
+                    put_out(block + kPOff, e0, x);
                 }
             } else {
                 unsigned char* L = smem + mine * 2 * kPart;
@@ -1405,13 +1425,14 @@ size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long 
     // (The groups are not known here: every head may be one.  Fewer sequences than asked for may be split into more segments: of all of them
     // together 3 n - 5 states, less than three times 148.  Sequences below 15 chunks are not split.)
     const size_t states = c.heads <= 74 && 3 * tokens > 64 * 38 ? 444 : 0;
-    return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows) + ((size_t)sequences * 4 + 15) / 16 * 16 + states * 128 * 128 * 4;
+    return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows) + ((size_t)sequences * 4 + 15) / 16 * 16 + states * 128 * 128 * 4 + 16;
 }
 
 int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream) {
     if (!bf16 || !p.out_bf16 || p.K != 128 || p.V != 128 || p.pr.T <= kFewTokens || ctx->cfg.kind != SKETCHSSM_GDN) return SKETCHSSM_UNSUPPORTED_SHAPE;
     DeltaArgs g;
     g.p = p;
+    g.p.work += -reinterpret_cast<uintptr_t>(p.work) & 31u;     // (whole sectors are written there; the scratch begins on 16 bytes)
     const long long units = (long long)p.pr.N * p.H, chunks = (long long)p.pr.T / kQ + p.pr.N;
     const long long preps = chunks * p.G * ((p.H / p.G + 1) / 2);
     if (units > (1 << 30) || preps >= 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
@@ -1419,7 +1440,7 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     g.segments = split.segments;
     g.turns = split.turns;
     g.preps = (int)preps;
-    g.rows = p.work + (size_t)chunks * p.H * kBlock;
+    g.rows = g.p.work + (size_t)chunks * p.H * kBlock;
     unsigned char* behind = g.rows + (size_t)chunks * p.H * kRows;
     const bool sort = g.segments == 1 && p.pr.N > 1;
     g.order = sort ? reinterpret_cast<int*>(behind) : nullptr;
