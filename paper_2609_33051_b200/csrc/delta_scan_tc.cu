@@ -710,6 +710,11 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             for (int it = 0; ok && decode_unit(g, it, x); ++it) {
                 const int head = x.head, group = head / (p.H / p.G);
                 int chunk = x.chunk;
+                if (has_state(g, x) && x.kind != kMap) {         // (two chunks ahead of the warps that read it)
+                    const float* from = x.kind == kLater ? scratch_state(g, x.seq, x.head, x.seg - 1)
+                                                         : p.state + ((size_t)seq_resume(p.pr, x.seq) * p.H + x.head) * 128 * 128;
+                    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"(128 * 128 * 4) : "memory");
+                }
                 for (int t = x.t0; t < x.t1; t += kQ, ++chunk, ++n) {
                     const int b = n & 1;
                     ok = n < 2 || mbar_wait_bounded(bar + bEmpty + b, (n / 2 - 1) & 1);
