@@ -291,6 +291,8 @@ __global__ void __launch_bounds__(128) conv_step_kernel(const ConvStepParams p) 
 // or of keys and queries, which are whole rows of K there (8, 16 or 32 neighbouring lanes): their norm is a sum over those, of what the
 // activation leaves in fp32, and the result, rounded once, goes to every head of the group.  The last blocks make the gates: beta, and the
 // decay of a head or (KDA, 16 bytes a thread) of its channels.
+// What bounds it: memory, behind two rounds of latency.  512 KDA entries of 32 heads take 22 to 26 us for 109 MB (17 at 6.46 TB/s); with eight bytes of
+// channels a thread and an entry at a time it took 60.
 template <typename T, int W, bool KDA>
 __global__ void __launch_bounds__(128) delta_step_kernel(const DeltaStepParams d) {
     constexpr int N = Vec16<T>::N;

@@ -19,6 +19,11 @@
 // state element in it: |U| is at most 65 of the former and 11.4 of the latter, |W| twice that, and is brought below 2^15.  T and P are below
 // one as they are.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
+//
+// What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.1 us of which the products are less than a
+// third; a sequence's chunks follow one another.  16384 tokens of 32 heads: one prompt 580 us (130 the first kernel; 280, 21 and 156 the passes
+// over five segments, see decode_unit; 921 whole), 48 ragged prompts 449.  The first kernel: waiting, for loads and for its own warps, and
+// memory, of which it reads and writes 0.5 GB (4 TB/s).  100 tokens: 24 us, half of it the first kernel.
 #include "tma.cuh"
 
 #include <cuda_fp16.h>
@@ -162,7 +167,8 @@ constexpr uint32_t kTypes = (1u << 4) | ((128u >> 4) << 24);      // fp16 x fp16
 
 // ---- what does not depend on the state: T and P of every chunk ------------------------------------------------------------
 //
-// A CTA takes a chunk, a group and two of its heads.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product
+// A CTA takes a chunk, a group and two of its heads.  The gates' arguments, 64 rows far apart, are what it waits for longest: they are used behind the
+// norms only.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product
 // gives <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127).  Of four warps a head, two make P from the latter and store it, two make -L and from
 // it T, in blocks of sixteen by sixteen: D_b, the inverses of the diagonal ones, column by column, a column a thread, all four at once; then
 //     T[b][c] = D_b sum_{c <= e < b} -L[b][e] T[e][c],   T[b][b] = D_b diag(beta),
@@ -1400,7 +1406,8 @@ static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uin
 // Segments of a sequence (1: none) and units of the first pass a CTA, for the least time, estimated for sequences of the average length: turns + 1
 // times a segment's chunks at 3 us each, and what the small kernel and the units' starts take, some 30 us and 8 a segment.  Each pass has an
 // SM for each of its CTAs: in the first one of every first segment and one for `turns` of the 2 (n - 2) others, in the second n - 1.
-// One prompt of 16384 tokens: 32 heads 921 us whole, 692 with n = 3 and one turn.
+// One prompt, a key head for each head, whole and split: 16384 tokens of 4 heads 791 and 235 us, of 32 952 and 646, of 64 1157 and 1050; 2048 of 16
+// heads 120 and 99.  16384 of 32 heads, a key head for two: 921, 692 with n = 3 and one turn, 580 with n = 5 and two.
 struct Split {
     int segments, turns;
 };
