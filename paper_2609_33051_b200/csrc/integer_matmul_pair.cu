@@ -1,11 +1,11 @@
-// The product of integer_matmul.cu for many rows: tiles of 256 tokens x 256 weights on pairs of SMs (tcgen05, cta_group::2).
+// The product of integer_matmul.cu for many rows: tiles of 256 tokens x BN weights, 256 or 128, on pairs of SMs (tcgen05, cta_group::2).
 //
 // A pair shares both operands, half of each in either SM: a block of 128 of the inner axis is 32 KB of copies for an SM.  The tokens are the
-// accumulator's lanes, the weights its columns.  The inner axis runs into one accumulator of 256 columns; there are two, so that a tile is
+// accumulator's lanes, the weights its columns.  The inner axis runs into one accumulator of BN columns; there are two, so that a tile is
 // scaled and stored while the next one is multiplied.
 //
 // Roles per CTA: one thread issues the copies of its half (they report to the leader's barrier), one warp of the leader the products;
-// sixteen warps take a tile's sums out (32 lanes, 64 columns each), times both scales, and store them through shared memory (TMA), or
+// BN / 16 warps take a tile's sums out (32 lanes, 64 columns each), times both scales, and store them through shared memory (TMA), or
 // directly where a row or the row stride is no multiple of 16 bytes.
 //
 // What bounds it: the operands' way from L2.  16384 x 12352 x 2048 to bf16 takes 293 us (L2 flushed before each call; 298 one after another):
@@ -20,11 +20,13 @@ namespace {
 
 using namespace tc;
 
-constexpr int kStages = 5, kEpiWarps = 16, kThreads = 32 * (4 + kEpiWarps);
-constexpr uint32_t kHalf = 128u * 128u, kStageBytes = 2u * kHalf;
-constexpr uint32_t kOut = kStages * kStageBytes;
-constexpr uint32_t kBars = kOut + kEpiWarps * 4096u;
-constexpr uint32_t kSmem = kBars + (2 * kStages + 4) * 8u + 16u + 1024u;
+constexpr uint32_t kHalf = 128u * 128u;                // of the tokens
+template <int BN, int NS>
+struct PairShape {
+    static constexpr int kEpiWarps = BN / 16, kThreads = 32 * (4 + kEpiWarps);
+    static constexpr uint32_t kStageBytes = kHalf + (uint32_t)BN / 2u * 128u;
+    static constexpr uint32_t kOut = NS * kStageBytes, kBars = kOut + kEpiWarps * 4096u, kSmem = kBars + (2 * NS + 4) * 8u + 16u + 1024u;
+};
 
 struct PairArgs {
     CUtensorMap ta, tw, to;
@@ -47,7 +49,11 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
                  : "memory");
 }
 
-__global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const __grid_constant__ PairArgs g) {
+template <int BN, int kStages>
+__global__ void __launch_bounds__(PairShape<BN, kStages>::kThreads, 1) integer_matmul_pair_kernel(const __grid_constant__ PairArgs g) {
+    using L = PairShape<BN, kStages>;
+    constexpr int kEpiWarps = L::kEpiWarps, kColumns = 2 * BN;         // two accumulators
+    constexpr uint32_t kStageBytes = L::kStageBytes, kOut = L::kOut, kBars = L::kBars;
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     uint64_t* full = reinterpret_cast<uint64_t*>(smem + kBars);        // the leader's: both halves are there
@@ -63,7 +69,7 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
         mbar_fence_init();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(slot)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "n"(kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -79,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
             int it = 0;
             bool ok = true;
             for (int tile = first; tile < g.tiles && ok; tile += step) {
-                const int m = tile / g.n_tiles * 256 + rank * 128, n = tile % g.n_tiles * 256 + rank * 128;
+                const int m = tile / g.n_tiles * 256 + rank * 128, n = tile % g.n_tiles * BN + rank * (BN / 2);
                 for (int kb = 0; kb < p.KB; ++kb, ++it) {
                     const int s = it % kStages;
                     if (it >= kStages && !mbar_wait_bounded(empty + s, (it / kStages - 1) & 1)) {
@@ -104,7 +110,7 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
         __syncwarp();
     } else if (warp == 1) {
         if (rank == 0) {
-            constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((256u >> 3) << 17) | ((256u >> 4) << 24);      // s8 x s8 -> s32
+            constexpr uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((256u >> 4) << 24);      // s8 x s8 -> s32
             int it = 0, n = 0;
             bool ok = true;
             for (int tile = first; tile < g.tiles && ok; tile += step, ++n) {
@@ -123,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
                             asm volatile(
                                 "{\n\t.reg .pred p;\n\t"
                                 "setp.ne.b32 p, %4, 0;\n\t"
-                                "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * 256)),
+                                "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + (uint32_t)(as * BN)),
                                 "l"(da + 2u * j), "l"(dw + 2u * j), "r"(idesc), "r"((uint32_t)(j | kb))
                                 : "memory");
                     if (elect()) {
@@ -144,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
         int it = 0;
         for (int tile = first; tile < g.tiles; tile += step, ++it) {
             const int as = it & 1;
-            const int m0 = tile / g.n_tiles * 256 + rank * 128 + quad * 32, n0 = tile % g.n_tiles * 256 + part * 64;
+            const int m0 = tile / g.n_tiles * 256 + rank * 128 + quad * 32, n0 = tile % g.n_tiles * BN + part * 64;
             const float s = m0 + lane < p.M ? p.a_scale[m0 + lane] : 0.f;
             const float w0 = n0 + lane < p.N ? p.w_scale[n0 + lane] : 0.f, w1 = n0 + 32 + lane < p.N ? p.w_scale[n0 + 32 + lane] : 0.f;
             bool ok = mbar_wait_bounded(acc_full + as, (it / 2) & 1);
@@ -155,8 +161,8 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
             }
             tc_fence_after();
             uint32_t d[2][32];
-            tmem_ld32_async(at0 + (uint32_t)(as * 256), d[0]);
-            tmem_ld32_async(at0 + (uint32_t)(as * 256 + 32), d[1]);
+            tmem_ld32_async(at0 + (uint32_t)(as * BN), d[0]);
+            tmem_ld32_async(at0 + (uint32_t)(as * BN + 32), d[1]);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
@@ -217,19 +223,15 @@ __global__ void __launch_bounds__(kThreads, 1) integer_matmul_pair_kernel(const 
     __syncthreads();
     cluster_sync();                                    // nobody reaches into a CTA that has ended
     tc_fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kColumns));
 }
 
-}  // namespace
-
-int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
-    const long long nt = (p.N + 255) / 256, tiles = nt * ((p.M + 255) / 256);
+template <int BN, int NS>
+int launch_pairs(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
+    using L = PairShape<BN, NS>;
+    const long long nt = (p.N + BN - 1) / BN, tiles = nt * ((p.M + 255) / 256);
     const int pairs = sm_count(ctx) / 2;
-    // From where the other kernel's 128 x 128 tiles are more than the SMs, so that some of them would take two.  (256 x 9472 x 2048, 148 such tiles:
-    // 11.0 us there, 11.9 here; 256 x 9600, 150 of them, 15.3 and 11.8; 777 x 2049 x 4096, 119, 14.7 and 19.6; 4096 x 2048 x 4096, 512, 45.4
-    // and 28.2.)
-    const long long small = (long long)((p.N + 127) / 128) * ((p.M + 127) / 128);
-    if (small <= sm_count(ctx) || tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
+    if (tiles > (1 << 27)) return SKETCHSSM_UNSUPPORTED_SHAPE;
     PairArgs g;
     g.p = p;
     g.n_tiles = (int)nt;
@@ -237,16 +239,35 @@ int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t str
     const int size = p.out_bf16 ? 2 : 4;
     g.tma_out = (p.out_stride * size) % 16 == 0 && (p.N * (long long)size) % 16 == 0;     // (a store ends on 16 bytes of a row)
     if (!make_map(&g.ta, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.a, (uint64_t)p.K, (uint64_t)p.M, (uint64_t)p.K, 128) ||
-        !make_map(&g.tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, (uint64_t)p.K, (uint64_t)p.N, (uint64_t)p.K, 128) ||
+        !make_map(&g.tw, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.w, (uint64_t)p.K, (uint64_t)p.N, (uint64_t)p.K, BN / 2) ||
         (g.tma_out && !make_map(&g.to, p.out_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, size, p.out, (uint64_t)p.N,
                                 (uint64_t)p.M, (uint64_t)p.out_stride * size, 32))) {
         ctx->last_cuda_error = cudaErrorInvalidValue;
         return SKETCHSSM_CUDA_ERROR;
     }
-    const cudaError_t e = unlock_smem(ctx, integer_matmul_pair_kernel);
+    const auto kern = integer_matmul_pair_kernel<BN, NS>;
+    const cudaError_t e = unlock_smem(ctx, kern);
     if (e != cudaSuccess) { ctx->last_cuda_error = e; return SKETCHSSM_CUDA_ERROR; }
     const int grid = 2 * (int)(tiles < pairs ? tiles : pairs);
-    return launch_layer<PairArgs>(ctx, integer_matmul_pair_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, stream, g, 2);
+    return launch_layer<PairArgs>(ctx, kern, dim3((unsigned)grid), dim3(L::kThreads), L::kSmem, stream, g, 2);
+}
+
+}  // namespace
+
+int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream) {
+    // From where the other kernel's 128 x 128 tiles are more than the SMs, so that some of them would take two.  (256 x 9472 x 2048, 148 such tiles:
+    // 11.0 us there, 11.9 here; 256 x 9600, 150 of them, 15.3 and 11.8; 777 x 2049 x 4096, 119, 14.7 and 19.6; 4096 x 2048 x 4096, 512, 45.4
+    // and 28.2.)
+    const long long small = (long long)((p.N + 127) / 128) * ((p.M + 127) / 128);
+    if (small > sm_count(ctx)) return launch_pairs<256, 5>(ctx, p, stream);
+    // Down to half as many, pairs with tiles of 256 x 128, one each, bring a quarter fewer operands than two tiles there, but their stores are slower
+    // where rows are no whole 16 bytes.  (300 x 4096 x 2048: 10.1 us there, 9.3 here; 640 x 2048 x 4096 14.6 and 13.7; 256 x 9472 x 2048 11.6
+    // and 11.0; 777 x 2049 x 4096 14.9 and 16.7.  Fewer tiles are split there.)
+    const int size = p.out_bf16 ? 2 : 4;
+    const long long wide = (long long)((p.N + 127) / 128) * ((p.M + 255) / 256);
+    if (2 * small > sm_count(ctx) && 2 * wide <= sm_count(ctx) && (p.out_stride * size) % 16 == 0 && (p.N * (long long)size) % 16 == 0)
+        return launch_pairs<128, 7>(ctx, p, stream);
+    return SKETCHSSM_UNSUPPORTED_SHAPE;
 }
 
 }  // namespace sketchssm
