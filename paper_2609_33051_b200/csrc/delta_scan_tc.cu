@@ -494,11 +494,9 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 const uint64_t factor = pack2(norms[64 + t], norms[64 + t]);
                 const int last = 32 * (role & 1) + 32;   // (a warp's rows end there)
 #pragma unroll 1
-                for (int e0 = 0; e0 < 64; e0 += 16) {
+                for (int e0 = 0; e0 < last; e0 += 16) {  // (blocks above the diagonal are not read)
                     uint64_t x[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = 0ull;
-                    if (e0 < last) tokens(e0, factor, x);
+                    tokens(e0, factor, x);
                     if (e0 + 16 > last - 32) {           // (the diagonal is in these rows)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -507,7 +505,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                             x[i] = pack2(e0 + 2 * i <= t ? a : 0.f, e0 + 2 * i + 1 <= t ? b : 0.f);
                         }
                     }
-                    put_out(block + kPOff, e0, x);
+                    if (e0 <= t) put_out(block + kPOff, e0, x);
                 }
             } else {
                 unsigned char* L = smem + mine * 2 * kPart;
@@ -587,17 +585,11 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 auto store = [&](auto first, auto at0) {
                     constexpr int C = decltype(first)::value, A = decltype(at0)::value;
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
+                    for (int b = C; b < 4; ++b) {        // (blocks above the diagonal are not read)
                         // (tiles of the operand: rows 0..7 and 8..15 of columns 0..7, then of 8..15; stored transposed: T's rows are its columns)
                         const uint32_t at = l_at + at_swizzled(b * 16 + (lane & 7) + (lane >> 4) * 8, C * 16 + ((lane >> 3) & 1) * 8);
-                        const uint32_t none[4] = {0u, 0u, 0u, 0u};
-                        if (b < C) {
-                            stmatrix4_trans(at, none);
-                            stmatrix4_trans(at + kPart, none);
-                        } else {
-                            stmatrix4_trans(at, th[b < C ? 0 : A + b - C]);
-                            stmatrix4_trans(at + kPart, tl[b < C ? 0 : A + b - C]);
-                        }
+                        stmatrix4_trans(at, th[A + b - C]);
+                        stmatrix4_trans(at + kPart, tl[A + b - C]);
                     }
                 };
                 using I0 = std::integral_constant<int, 0>;

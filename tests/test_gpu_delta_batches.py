@@ -83,3 +83,20 @@ def test_a_graph_that_brings_its_own_scratch():
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
         assert torch.equal(m.state[[0, 1, 2, 4]], state[[0, 1, 2, 4]])
     m.check_status()
+
+
+@pytest.mark.parametrize("kind,lengths", [("gdn", [100, 0, 321]), ("gdn", [3500]), ("kda", [70, 33])])
+def test_what_the_scratch_holds_before_changes_nothing(kind, lengths):
+    """Scratch of zeros, of bytes that are no numbers in any type, and at an address of the smallest alignment: the same to the bit."""
+    x = {n: t.to(DEV) for n, t in scan_inputs(kind, lengths, 4, 2, 128, 128, "bf16", 4).items()}
+    pr, m = batch_of(lengths, None, None)[1], layer(4, 4, kind=kind)
+    need = m.new_delta_work(len(lengths), sum(lengths)).numel()
+    got = []
+    for fill, at in ((0, 0), (255, 0), (255, 16)):
+        work = torch.full((need + 64,), fill, dtype=torch.uint8, device=DEV)
+        out = torch.empty_like(x["v"])
+        run_scan(m, pr, x, out, work=work[at:at + need])
+        got.append((out, m.state.clone()))
+        assert (work[:at] == fill).all() and (work[at + need:] == fill).all()
+    for out, state in got[1:]:
+        assert torch.equal(out, got[0][0]) and torch.equal(state, got[0][1])
