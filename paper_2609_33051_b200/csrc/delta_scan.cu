@@ -515,14 +515,14 @@ int launch_lanes(Ctx* ctx, const DeltaParams& p, long long units, cudaStream_t s
 template <typename T, int K, bool KDA>
 int launch_cores(Ctx* ctx, const DeltaParams& p0, cudaStream_t stream) {
     DeltaParams p = p0;
-    // 64 or 80 columns of a head in a CTA (what four tokens have to do with one another is then worked out once for them) where that leaves every SM
-    // two; below that sixteen columns and sixteen lanes for four of them.  Measured: 8 KDA prompts of 32 heads, 64 columns and 8 lanes 560 us, 64
-    // and 16 lanes 647, 16 and 8 lanes more than twice as long as 64; 7 prompts of 24 heads, 80 columns, sixteen at a time: 8 lanes 283 us, 16 lanes 223.
+    // Many heads: 64 or 80 columns of one in a CTA (what four tokens have to do with one another is then worked out once for them), eight lanes for
+    // four of them.  Where that leaves SMs with a CTA alone or none, the chain of a token counts: 32 columns, or 16 of 80, and sixteen lanes.
+    // Measured, with 64 or 80 columns and with 32 or 16: KDA, 1136 tokens, one prompt of 32 heads 589 us and 433, two 608 and 453, four 622 and
+    // 896 (16 columns: 1249); 8 prompts of 512 558 and 741.  fp32 GDN, 500 tokens, one prompt of 32 heads 152 and 121, four 262 and 350; 8
+    // prompts of 300, 16 heads of V = 64 95 and 110; V = 80, 24 heads, 3 prompts of 500 238 and 201, 7 of 300 289 and 231, 16 of 200 both 297.
     const long long heads = (long long)p.pr.N * p.H;
-    p.cols = 16;
-    for (int c : {64, 80})
-        if (p.V % c == 0 && heads * (p.V / c) >= 2ll * sm_count(ctx)) p.cols = c;
-    const bool many = p.cols > 16;
+    const bool many = p.V == 80 ? heads >= 2ll * sm_count(ctx) : heads * (p.V / 32) > (KDA ? 2ll : 1ll) * sm_count(ctx);
+    p.cols = p.V == 80 ? (many ? 80 : 16) : many ? 64 : 32;
     const long long units = heads * (p.V / p.cols);
     if (units > 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
     if constexpr (KDA) {
