@@ -21,8 +21,8 @@
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
 // What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.1 us of which the products are less than a
-// third; a sequence's chunks follow one another.  16384 tokens of 32 heads: one prompt 580 us (130 the first kernel; 280, 21 and 156 the passes
-// over five segments, see decode_unit; 921 whole), 48 ragged prompts 449.  The first kernel: waiting, for loads and for its own warps, and
+// third; a sequence's chunks follow one another.  16384 tokens of 32 heads: one prompt 579 us (125 the first kernel; 280, 21 and 156 the passes
+// over five segments, see decode_unit; 921 whole), 48 ragged prompts 446.  The first kernel: waiting, for loads and for its own warps, and
 // memory, of which it reads and writes 0.5 GB (4 TB/s).  100 tokens: 24 us, half of it the first kernel.
 #include "tma.cuh"
 
