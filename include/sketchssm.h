@@ -413,7 +413,7 @@ int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, i
  *     y = h / sqrt(mean(h^2) + eps) weight;   with gate: y times the gate's value
  *     scale = max|y| / 127 over the row,  out8 = y 127 / max|y|, to nearest even (a row whose largest value is below 1e-30 is stored as zeros;
  *     one with a value that is not finite as zeros with a scale that is not a number)
- * and, if wanted, y to out (io).
+ * and, if wanted, y to out (io).  Squares are summed in fp32: values up to 10^17.
  *   rows >= 0; width at most 16384; group: a divisor of width that is a multiple of 8 (the width itself: a norm of whole rows)
  *   x [rows][width] of x_dtype strided; weight [group] fp32; residual, residual_out [rows][width] io, dense, both or none, residual_out may be
  *   residual; gate [rows][width] io strided, or NULL; residual and gate exclude one another; out [rows][width] io dense, or NULL;
