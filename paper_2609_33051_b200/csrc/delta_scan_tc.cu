@@ -653,9 +653,11 @@ constexpr uint32_t kWOff = kRows, kStage = (kWOff + kBlock + 1023u) & ~1023u;
 constexpr uint32_t kVOff = 2 * kStage;                 // two buffers: rows of 256 bytes, then pairs of rows, [32][128] pairs of bf16
 constexpr uint32_t kYOff = kVOff + 4 * kPart;          // the same
 constexpr uint32_t kBarOff = kYOff + 2 * kPart;
-enum { bFull = 0, bEmpty = 2, bRaw = 4, bFullV = 6, bEmptyV = 8, bS = 10, bXP = 12, bWP = 13, bUP = 14, bX = 15, bU = 16, bProd = 17, bAsk = 18, bY = 19, bOut = 20,
-       bOutFree = 21, bJoin = 22, bScaled = 23, kBars = 24 };
-constexpr uint32_t kMarkOff = kBarOff + kBars * 8u + 16u;  // [128]: see mark_of
+// (bUP has two that take turns: nothing but its arrivals holds the state's warps back until the Y warps have seen them, and those could be a
+// chunk ahead of a late one, which then would not see that phase end.  Two chunks ahead they are never: U of the next chunk but one waits for Y.)
+enum { bFull = 0, bEmpty = 2, bRaw = 4, bFullV = 6, bEmptyV = 8, bS = 10, bXP = 12, bWP = 13, bUP = 14, bX = 16, bU = 17, bProd = 18, bAsk = 19, bY = 20, bOut = 21,
+       bOutFree = 22, bJoin = 23, bScaled = 24, kBars = 25 };
+constexpr uint32_t kMarkOff = (kBarOff + kBars * 8u + 4u + 15u) & ~15u;  // [128]: see mark_of
 constexpr uint32_t kLargeOff = kMarkOff + 128u * 4u;             // [4][128]: the largest values of chunk n at n & 3
 constexpr uint32_t kMostOff = kLargeOff + 512u * 4u;             // [2][2][128]: the largest elements of the state, by halves
 constexpr uint32_t kAsideOff = kMostOff + 512u * 4u;              // [2][2][128]: for Y of chunk n at n & 1, its factor and the first token that is not finite
@@ -807,7 +809,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     __syncwarp();
                     continue;
                 }
-                ok = warp_wait(bar + bUP, o & 1) && (!live || warp_wait(bar + bScaled, om & 1));
+                ok = warp_wait(bar + bUP + (o & 1), (o >> 1) & 1) && (!live || warp_wait(bar + bScaled, om & 1));
                 if (!ok) break;
                 ++o;
                 if (live) ++om;
@@ -992,7 +994,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     __syncwarp();
                     if (lane == 0) mbar_arrive_one(bar + bScaled);
                 }
-                ok = warp_wait(bar + bUP, o & 1);
+                ok = warp_wait(bar + bUP + (o & 1), (o >> 1) & 1);
                 if (!ok) break;
                 const float scale = reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256];
                 const int first = __float_as_int(reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256 + 128]);
@@ -1268,7 +1270,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
                     }
                     tmem_st_wait();
-                    arrive(bUP);
+                    arrive(bUP + (o & 1));
                     ++o;
                 }
                 float r = down;
