@@ -15,8 +15,9 @@
 // Precision.  States are fp32, outputs sums of fp32 accuracy rounded once.  What the tensor cores multiply are fp16 operands in two parts of 11
 // bits each (the product of the second parts is left out), summed in fp32.  fp16 has the bits but not the range, so everything is scaled by
 // powers of two, which round nothing: keys and queries by one each, to lengths between a half and one (then one part holds all of their bits
-// but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value and
-// state element in it: |U| is at most 65 of the former and 11.4 of the latter, |W| twice that, and is brought below 2^15.  T and P are below
+// but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value v in it and the length
+// of the state before it.  A token leaves the state's length |S|^2 at most d^2 |S|^2 + v^2 (a convex mean along its key), a chunk leaves it at
+// most 2^c_end |S| + 8 v; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are below
 // one as they are.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
@@ -1069,11 +1070,11 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             const volatile float* from = most + (c & 1) * 256;
             return 11.4f * fmaxf(from[0], from[128]);
         };
-        // The scale for chunk c: where what bounds its values, times the scale, would be beyond 2^14 or below 2^9 (then the second parts would
+        // The scale for chunk c: where what bounds its values, times the scale, would be beyond 2^14 or below 2^11 (the second parts would
         // lose bits), a new one.  Returns the new scale over the old one.
         auto rescale = [&](int c) {
-            const float all = 65.f * reinterpret_cast<const volatile float*>(large)[(c & 3) * 128] + length, now = all * up;
-            if (now <= 16384.f && (now >= 512.f || all == 0.f)) return 1.f;
+            const float all = 9.f * reinterpret_cast<const volatile float*>(large)[(c & 3) * 128] + length, now = all * up;
+            if (now <= 16384.f && (now >= 2048.f || all == 0.f)) return 1.f;
             const int e = max(-100, (int)((__float_as_uint(all) & 0x7f800000u) >> 23) - 127);     // (below 2^(e + 1); below 2^13 then)
             const float old = down;
             up = __uint_as_float((uint32_t)(127 + 12 - e) << 23);
@@ -1148,8 +1149,8 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         X[i] = pack2(a, c);
                     }
                 }
-                // What bounds the next chunk's state: from the state itself every eighth chunk (the halves meet behind the next product), else
-                // from the length before and what the tokens add to it.
+                // What bounds the next chunk's state: this one's, from the state itself every eighth chunk (the halves meet behind the next
+                // product), less what decays of it, and what the tokens add to it.
                 const bool look = (n & 7) == 7;
                 if (more) {
                     if (look) state_most(n);
@@ -1216,7 +1217,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 const uint32_t mark = reinterpret_cast<const volatile uint32_t*>(marks)[col];
                 const bool bad = (mark >> 7) == (uint32_t)n + 1u;
                 const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : 32;
-                const float keep = bad ? __int_as_float(0x7fffffff) : gate[kKeep - half * 32];       // (NaN: all of the lane's state)
+                const float end = gate[kKeep - half * 32], keep = bad ? __int_as_float(0x7fffffff) : end;       // (NaN: all of the lane's state)
                 tmem_ld_wait();
                 {
                     const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
@@ -1275,7 +1276,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
                 float r = down;
                 if (more) {
-                    length = (look ? length_of(n) : length) + 64.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
+                    length = end * (look ? length_of(n) : length) + 8.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
                     r = rescale(n + 1);
                 }
                 const uint64_t r2 = pack2(r, r), keep2 = pack2(keep * r, keep * r);

@@ -1,0 +1,25 @@
+"""The delta rule's scan over numbers of very different size: step sizes, values and states that a chunk's common scale has to hold.  Tolerances are
+delta_ref's bound of fp32 arithmetic, and, where the error as a whole is looked at, what the other tests of the operator allow it."""
+import pytest
+import torch
+
+from tests.test_gpu_delta_operators import batch_of, check_scan, layer, scan_inputs
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(lengths, H=2, **kw):
+    return scan_inputs("gdn", lengths, H, 1, 128, 128, "bf16", 8, **kw)
+
+
+@pytest.mark.parametrize("size", [1e6, 1e8])
+@pytest.mark.parametrize("od", ["bf16", "f32"])
+def test_a_large_state_that_decays_over_chunks(size, od):
+    """A stored state far above the values, of which a chunk leaves a five-hundredth or so: the tokens hundreds of places behind it have their own size's
+    accuracy."""
+    x = inputs([1000], seed=12)
+    x["state"] = x["state"] * size
+    x["a"], x["bias"] = torch.full((2,), -1.0), torch.full((2,), -2.3)
+    x["dt"] = x["dt"] * 0.1
+    starts, pr = batch_of([1000], None, [1])
+    check_scan(layer(8, 2), x, starts, pr, None, [1], od)
