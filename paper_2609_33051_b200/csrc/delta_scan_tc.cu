@@ -2,15 +2,15 @@
 //
 // A sequence goes through in chunks of 64 tokens.  With c_t the sum of the chunk's log2 decays up to token t, unit keys k (a key as it is times
 // r_t) and S the state before the chunk, what the tokens add is U, the solution of a unit lower triangular system:
-//     (I + L) U = diag(beta) X,   L[t][s] = beta_t 2^(c_t - c_s) <k_t, k_s> for s < t,   X[t] = v_t - 2^c_t S^T k_t
+//     U = diag(beta) T X,   T = (I + L)^-1,   L[t][s] = 2^(c_t - c_s) <k_t, k_s> beta_s for s < t,   X[t] = v_t - 2^c_t S^T k_t
 //     Y[t] = 2^c_t S^T q_t + sum_{s <= t} P[t][s] U[s],   P[t][s] = 2^(c_t - c_s) <q_t, k_s>
 //     S <- 2^c_end S + sum_s 2^(c_end - c_s) k_s U[s]^T
-// T = (I + L)^-1 diag(beta) and P do not depend on the state: a first kernel makes them, all chunks at once, and leaves them in the scratch as
+// T and P do not depend on the state: a first kernel makes them, all chunks at once, and leaves them in the scratch as
 // matrix operands; a second one takes a sequence and head at a time through its chunks.
 //
 // There the state is kept transposed: 128 value columns are the lanes of tensor memory, so that everything a chunk reads of it is one
 // operand in tensor memory times a tile of shared memory (keys, queries, T, P), and a lane's thread scales, adds and splits without
-// another thread's help.  Per chunk: K S^T and, later, Q S^T;  X;  (T - diag) X;  U and W = 2^(c_end - c) r U;  W K and U P;  S.
+// another thread's help.  Per chunk: K S^T and, later, Q S^T;  X;  (T - I) X;  U and W = 2^(c_end - c) r U;  W K and U P;  S.
 //
 // Precision.  States are fp32, outputs sums of fp32 accuracy rounded once.  What the tensor cores multiply are fp16 operands in two parts of 11
 // bits each (the product of the second parts is left out), summed in fp32.  fp16 has the bits but not the range, so everything is scaled by
@@ -18,7 +18,8 @@
 // but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value v in it and the length
 // of the state before it.  A token leaves the state's length |S|^2 at most d^2 |S|^2 + v^2 (a convex mean along its key), a chunk leaves it at
 // most 2^c_end |S| + 8 v; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are below
-// one as they are.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
+// one as they are, T because the rows' step sizes are left to U: a part ends at 2^-24, and rows of small ones would lose their bits (with
+// b = -7 everywhere states were 4e-5 off).  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
 // What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.1 us of which the products are less than a
@@ -39,7 +40,7 @@ using namespace tc;
 
 constexpr int kQ = 64;                                 // tokens of a chunk
 constexpr uint32_t kPart = 8192u;                      // 64 rows of 128 bytes
-// The scratch: for a chunk of a head two parts of T - diag, two of P and the gates; for one of a group the rows of K and Q, half of the channels at a time
+// The scratch: for a chunk of a head two parts of T - I, two of P and the gates; for one of a group the rows of K and Q, half of the channels at a time
 constexpr uint32_t kTOff = 0, kPOff = 2 * kPart, kGOff = 4 * kPart, kRows = 4 * kPart;
 // gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c / |q| (r and 1 / |q| of the scaled rows), and 2^c_end
 constexpr int kBeta = 0, kRead = 64, kPut = 128, kAsk = 192, kKeep = 256, kGates = 320;
@@ -172,17 +173,17 @@ constexpr uint32_t kTypes = (1u << 4) | ((128u >> 4) << 24);      // fp16 x fp16
 // norms only.  The rows of K and Q are scaled to fp16 in place (and kept for the second kernel).  One product
 // gives <k_t, k_s> (lanes 0..63) and <q_t, k_s> (64..127).  Of four warps a head, two make P from the latter and store it, two make -L and from
 // it T, in blocks of sixteen by sixteen: D_b, the inverses of the diagonal ones, column by column, a column a thread, all four at once; then
-//     T[b][c] = D_b sum_{c <= e < b} -L[b][e] T[e][c],   T[b][b] = D_b diag(beta),
+//     T[b][c] = D_b sum_{c <= e < b} -L[b][e] T[e][c],   T[b][b] = D_b,
 // transposed, so that what one product leaves in registers is the next one's first operand (mma.sync, in two parts as above: operands of this
 // size are in registers before a tcgen05 product could be set up).  (All of it column by column is as many multiply-adds on CUDA
 // cores, but their second operands, broadcast from shared memory at 128 bytes a cycle, were most of 160 us for 16384 tokens of 32 heads.)
 
 constexpr int kPrepThreads = 256;
 // behind the tile of K and Q rows, whose place -L of both heads takes (two parts, rows t), then T: the diagonal blocks of -L, [4][s][t] floats
-// a head; their inverses, [4][2 parts][t][s]; 1 / |k|, 1 / |q|, and 1 / |k| or zero: [3][64]; halves of their squares; whole, rest, beta: [2][3][64]
+// a head; their inverses, [4][2 parts][t][s]; 1 / |k|, 1 / |q|, and 1 / |k| or zero: [3][64]; halves of their squares; whole, rest, beta: [2][3][64]; beta / |k|: [2][64]
 constexpr uint32_t kPrepDiag = 4 * kPart, kPrepInv = kPrepDiag + 2u * 4096u;
 constexpr uint32_t kPrepNorm = kPrepInv + 2u * 4096u, kPrepHalf = kPrepNorm + 3u * kQ * 4u, kPrepSum = kPrepHalf + 4u * kQ * 4u;
-constexpr uint32_t kPrepBar = kPrepSum + 6u * kQ * 4u;
+constexpr uint32_t kPrepPut = kPrepSum + 6u * kQ * 4u, kPrepBar = kPrepPut + 2u * kQ * 4u;
 constexpr uint32_t kPrepSmem = kPrepBar + 32u + 1024u;
 
 // Element S of sixteen neighbouring ones of a column puts -L[t][s] of itself into those behind it: l holds their block of -L, [s][t].
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
     extern __shared__ unsigned char raw[];
     unsigned char* smem = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
     float* norms = reinterpret_cast<float*>(smem + kPrepNorm);
-    float* sums = reinterpret_cast<float*>(smem + kPrepSum);
+    float *sums = reinterpret_cast<float*>(smem + kPrepSum), *puts = reinterpret_cast<float*>(smem + kPrepPut);
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + kPrepBar);
     uint32_t* slot = reinterpret_cast<uint32_t*>(bar + 2);
     const DeltaParams& p = g.p;
@@ -387,7 +388,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
         }
         // gates, while the product is made
         if (ok && role == 0 && mine < heads) {
-            float* s = sums + mine * 3 * kQ;
+            float *s = sums + mine * 3 * kQ, *put = puts + mine * kQ;
             double c[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -402,6 +403,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     beta = __int_as_float(0x7fffffff);
                 }
                 s[2 * kQ + lane * 2 + i] = in ? beta : 0.f;
+                put[lane * 2 + i] = in && beta == beta ? beta * norms[128 + lane * 2 + i] : 0.f;
                 c[i] = (i > 0 ? c[0] : 0.0) + (double)(in ? l : 0.f);
             }
             double before = c[1];
@@ -442,14 +444,14 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             const uint64_t minus = pack2(-1.f, -1.f);
             const float* s = sums + mine * 3 * kQ;
             const uint64_t w = pack2(s[t], s[t]), r = pack2(s[kQ + t], s[kQ + t]);
-            // tokens e0 .. e0 + 15 of the row: the product times both norms (and `factor`) and the decay between.  (Rows behind the sequence are
-            // zeros as K's and Q's are.)
-            auto tokens = [&](int e0, uint64_t factor, uint64_t (&x)[8]) {
+            // tokens e0 .. e0 + 15 of the row: the product times the row's factor, the columns' and the decay between.  (Rows behind the sequence
+            // are zeros as K's and Q's are.)
+            auto tokens = [&](int e0, uint64_t factor, const float* columns, uint64_t (&x)[8]) {
                 uint32_t d[16];
                 tmem_ld16_async(tmem + lanes + e0, d);
                 tmem_ld_wait();
                 const ulonglong2 *w4 = reinterpret_cast<const ulonglong2*>(s + e0), *r4 = reinterpret_cast<const ulonglong2*>(s + kQ + e0),
-                                 *n4 = reinterpret_cast<const ulonglong2*>(norms + 128 + e0);
+                                 *n4 = reinterpret_cast<const ulonglong2*>(columns + e0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const ulonglong2 we = w4[i], re = r4[i], ne = n4[i];
@@ -497,7 +499,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
 #pragma unroll 1
                 for (int e0 = 0; e0 < last; e0 += 16) {  // (blocks above the diagonal are not read)
                     uint64_t x[8];
-                    tokens(e0, factor, x);
+                    tokens(e0, factor, norms + 128, x);
                     if (e0 + 16 > last - 32) {           // (the diagonal is in these rows)
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -512,11 +514,11 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 unsigned char* L = smem + mine * 2 * kPart;
                 float* diag = reinterpret_cast<float*>(smem + kPrepDiag + mine * 4096);
                 {
-                    const float beta = s[2 * kQ + t], f = beta == beta ? -beta * norms[128 + t] : 0.f;
+                    const float f = -norms[128 + t];
 #pragma unroll 1
                     for (int e0 = 0; e0 < 32 * role + 32; e0 += 16) {
                         uint64_t x[8];
-                        tokens(e0, pack2(f, f), x);      // (what it leaves on and above the diagonal nobody reads)
+                        tokens(e0, pack2(f, f), puts + mine * kQ, x);      // (what it leaves on and above the diagonal nobody reads)
                         put(L, e0, x);
                         if (e0 == (t & 48)) {
                             float* to = diag + e0 * 16 + (t & 15);
@@ -550,7 +552,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     }
                 }
                 asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");    // L and the inverses are there
-                // T diag(beta): block columns 0 and 3 by one warp, 1 and 2 by the other.  Of block column c the blocks c .. 3.
+                // T: block columns 0 and 3 by one warp, 1 and 2 by the other.  Of block column c the blocks c .. 3.
                 const uint32_t l_at = smem_u32(L), inv_at = smem_u32(smem + kPrepInv + mine * 4096) + (uint32_t)((lane & 7) + (lane >> 4) * 8) * 32u + (uint32_t)((lane >> 3) & 1) * 16u;
                 uint32_t th[5][4], tl[5][4];             // blocks: of the first block column, up to four; of the second one or two
                 auto column = [&](auto first, auto at0) {
@@ -563,13 +565,8 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                         if (b == C) {
                             // (a product's lane has row lane / 4, and eight more, and columns 2 (lane % 4) and one more of either tile)
                             const int m = lane >> 2, k = (lane & 3) * 2;
-                            float b0 = s[2 * kQ + C * 16 + m], b1 = s[2 * kQ + C * 16 + m + 8];
-                            b0 = b0 == b0 ? b0 : 0.f;
-                            b1 = b1 == b1 ? b1 : 0.f;
-                            c[0][0] = m == k ? b0 : 0.f;
-                            c[0][1] = m == k + 1 ? b0 : 0.f;
-                            c[1][2] = m == k ? b1 : 0.f;
-                            c[1][3] = m == k + 1 ? b1 : 0.f;
+                            c[0][0] = c[1][2] = m == k ? 1.f : 0.f;
+                            c[0][1] = c[1][3] = m == k + 1 ? 1.f : 0.f;
                         } else {
 #pragma unroll
                             for (int e = C; e < b; ++e) {
@@ -614,7 +611,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     store(I2{}, I3{});
                 }
                 asm volatile("bar.sync %0, 64;" ::"r"(mine + 1) : "memory");
-                {                                        // the diagonal's part of U is added in fp32
+                {                                        // the diagonal's part of T X is added in fp32
                     unsigned short* to = reinterpret_cast<unsigned short*>(L + at_swizzled(t, t));
                     to[0] = to[kPart / 2] = 0;
                 }
@@ -640,10 +637,10 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
 // Roles: warp 0 issues the copies, warp 1 the products; warp 2 brings two tokens of every value column together and finds the columns' largest
 // values, warp 3 takes Y apart again and stores it; warps 4..11 hold the state, a lane of tensor memory and half of what is there to split
 // a thread (64 keys' channels of S, 32 tokens of X, U and W); warps 12..15 scale Y, a lane a thread.  They meet through mbarriers alone; every wait is bounded.
-// A chunk is a chain of four products and what stands between them: K S^T, X, (T - diag) X, W, W K, S.  Everything else is done while a product
+// A chunk is a chain of four products and what stands between them: K S^T, X, (T - I) X, W, W K, S.  Everything else is done while a product
 // of the chain runs or by other warps: the next chunk's V behind K S^T, U behind W K.
 // T and P are lower triangular, 16 tokens of them meet the tokens from themselves on only.
-// Tensor memory: two parts of S, of X, then of W, and of U; K S^T, then (T - diag) X; Y; W K.
+// Tensor memory: two parts of S, of X, then of W, and of U; K S^T, then (T - I) X; Y; W K.
 //
 // What bounds it: the splitting.  Conversions, comparisons and two-element multiply-adds all issue every other cycle of a scheduler, and an
 // arrival at a barrier costs a warp 26 of its scheduler's cycles, a poll 16: few warps, and few barriers between them (sixteen warps with
@@ -664,7 +661,7 @@ constexpr uint32_t kMostOff = kLargeOff + 512u * 4u;             // [2][2][128]:
 constexpr uint32_t kAsideOff = kMostOff + 512u * 4u;              // [2][2][128]: for Y of chunk n at n & 1, its factor and the first token that is not finite
 constexpr uint32_t kSmemTc = kAsideOff + 512u * 4u + 1024u;
 
-// columns of tensor memory: parts of S (part i, channel k: 64 i + k / 2); of X and W, of U (part i, token s: 32 i + s / 2); K S^T and (T - diag) X; Y; W K
+// columns of tensor memory: parts of S (part i, channel k: 64 i + k / 2); of X and W, of U (part i, token s: 32 i + s / 2); K S^T and (T - I) X; Y; W K
 constexpr uint32_t cS = 0, cW = 128, cU = 192, cX = 256, cY = 320, cP = 384;
 
 // The products take every token's values into every token, and a zero weight times NaN or infinity is NaN: from a lane's first value
@@ -772,7 +769,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {            // (T - diag) X, 16 tokens at a time
+                for (int q = 0; q < 4; ++q) {            // (T - I) X, 16 tokens at a time
                     const uint32_t desc = kTypes | ((uint32_t)((64 - 16 * q) >> 3) << 17);
                     const uint64_t rows_q = dt + (uint32_t)q * (2048u >> 4) + (uint32_t)q * 2u;
 #pragma unroll
@@ -1224,8 +1221,8 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const ulonglong2 be = beta[i];
-                        X[2 * i] = fma2(be.x, X[2 * i], pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])));
-                        X[2 * i + 1] = fma2(be.y, X[2 * i + 1], pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])));
+                        X[2 * i] = mul2(be.x, add2(X[2 * i], pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1]))));
+                        X[2 * i + 1] = mul2(be.y, add2(X[2 * i + 1], pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3]))));
                     }
                     auto store = [&]() {
 #pragma unroll

@@ -3,7 +3,8 @@ delta_ref's bound of fp32 arithmetic, and, where the error as a whole is looked 
 import pytest
 import torch
 
-from tests.test_gpu_delta_operators import batch_of, check_scan, layer, scan_inputs
+from tests import delta_ref as dref
+from tests.test_gpu_delta_operators import DEV, NAMES, batch_of, check_scan, layer, run_scan, scan_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,19 @@ def test_a_large_state_that_decays_over_chunks(size, od):
     x["dt"] = x["dt"] * 0.1
     starts, pr = batch_of([1000], None, [1])
     check_scan(layer(8, 2), x, starts, pr, None, [1], od)
+
+
+@pytest.mark.parametrize("b", [-5.0, -7.0])
+def test_small_step_sizes_keep_their_bits(b):
+    """Outputs and states are as small as the step sizes, and still right to the accuracy of their own size: the bounds of
+    test_scan_keeps_fp32s_accuracy, for decays of a length that does not grow with the prompt."""
+    x = inputs([300], seed=11)
+    x["b"] = (x["b"].float() * 0.25 + b).to(torch.bfloat16)
+    x["a"] = torch.tensor([-4.0, -0.5])
+    starts, pr = batch_of([300])
+    m = layer(8, 2)
+    want, _, new, _ = dref.scan(starts, None, None, *(x[n] for n in NAMES), x["bias"], x["state"], 8)
+    out = torch.empty(300, 2, 128, dtype=torch.bfloat16, device=DEV)
+    run_scan(m, pr, x, out)
+    assert (m.state[:1].cpu().double() - new[:1]).norm() <= 1e-6 * new[:1].norm()
+    assert (out.cpu().double() - want).norm() <= 2.0e-3 * want.norm()
