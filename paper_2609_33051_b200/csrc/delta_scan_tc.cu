@@ -17,9 +17,10 @@
 // powers of two, which round nothing: keys and queries by one each, to lengths between a half and one (then one part holds all of their bits
 // but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value v in it and the length
 // of the state before it.  A token leaves the state's length |S|^2 at most d^2 |S|^2 + v^2 (a convex mean along its key), a chunk leaves it at
-// most 2^c_end |S| + 8 v; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are below
-// one as they are, T because the rows' step sizes are left to U: a part ends at 2^-24, and rows of small ones would lose their bits (with
-// b = -7 everywhere states were 4e-5 off).  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
+// most 2^c_end |S| + 8 v; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are at most
+// one as they are, T because the rows' step sizes are left to U (a part ends at 2^-24, and rows of small ones would lose their bits: with
+// b = -7 everywhere states were 4e-5 off), and are made kTile times as large, so that what has decayed to 2^-25 of a large value ends there, and not
+// that of one.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
 // What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.1 us of which the products are less than a
@@ -40,9 +41,10 @@ using namespace tc;
 
 constexpr int kQ = 64;                                 // tokens of a chunk
 constexpr uint32_t kPart = 8192u;                      // 64 rows of 128 bytes
+constexpr float kTile = 16384.f;                       // factor of T and P
 // The scratch: for a chunk of a head two parts of T - I, two of P and the gates; for one of a group the rows of K and Q, half of the channels at a time
 constexpr uint32_t kTOff = 0, kPOff = 2 * kPart, kGOff = 4 * kPart, kRows = 4 * kPart;
-// gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c / |q| (r and 1 / |q| of the scaled rows), and 2^c_end
+// gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c kTile / |q| (r and 1 / |q| of the scaled rows), and 2^c_end
 constexpr int kBeta = 0, kRead = 64, kPut = 128, kAsk = 192, kKeep = 256, kGates = 320;
 constexpr uint32_t kBlock = kGOff + kGates * 4u;
 
@@ -228,10 +230,12 @@ __device__ __forceinline__ void mma_sixteen(float (&c)[2][4], const uint32_t (&h
         mma_block(c[i], lo, bh[2 * i], bh[2 * i + 1]);
     }
 }
-// What a product leaves as the first operand of the next.
+// What a product leaves as the first operand of the next: both of its operands are kTile times what they stand for, and so is this one.  (It is at most
+// one: what a key reads of the state that a value of one has left.)
 __device__ __forceinline__ void as_operand(const float (&c)[2][4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+    const uint64_t back = pack2(1.f / kTile, 1.f / kTile);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) two_parts(pack2(c[i >> 1][(i & 1) * 2], c[i >> 1][(i & 1) * 2 + 1]), hi[i], lo[i]);
+    for (int i = 0; i < 4; ++i) two_parts(mul2(pack2(c[i >> 1][(i & 1) * 2], c[i >> 1][(i & 1) * 2 + 1]), back), hi[i], lo[i]);
 }
 // Byte of element (row, column) of a part: rows of 128 bytes in the 128-byte swizzle.
 __device__ __forceinline__ uint32_t at_swizzled(int row, int col) { return (uint32_t)(row * 128 + (((col >> 3) ^ (row & 7)) * 16) + (col & 7) * 2); }
@@ -434,7 +438,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             to[kBeta + t] = s[2 * kQ + t];
             to[kRead + t] = in ? fmaf(s[2 * kQ + t], 0.f, -e * norms[t]) : 0.f;      // (not a number where beta is none: see the marks)
             to[kPut + t] = in ? rest * norms[t] : 0.f;
-            to[kAsk + t] = in ? e * norms[64 + t] : 0.f;
+            to[kAsk + t] = in ? e * kTile * norms[64 + t] : 0.f;
             if (t == 63) to[kKeep] = e;
         }
         if (ok && mine < heads) {
@@ -464,11 +468,11 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                     }
                 }
             };
-            // sixteen tokens of row t in two parts
+            // sixteen tokens of row t, times kTile, in two parts
             auto put = [&](unsigned char* to, int e0, const uint64_t (&x)[8]) {
                 uint32_t hi[8], lo[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) two_parts(x[i], hi[i], lo[i]);
+                for (int i = 0; i < 8; ++i) two_parts(mul2(x[i], pack2(kTile, kTile)), hi[i], lo[i]);
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
                     unsigned char* at = to + t * 128 + (((e0 / 8 + q) ^ (t & 7)) * 16);
@@ -494,7 +498,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             };
             unsigned char* block = p.work + ((size_t)chunk * p.H + h0 + mine) * kBlock;
             if (role >= 2) {
-                const uint64_t factor = pack2(norms[64 + t], norms[64 + t]);
+                const uint64_t factor = pack2(kTile * norms[64 + t], kTile * norms[64 + t]);
                 const int last = 32 * (role & 1) + 32;   // (a warp's rows end there)
 #pragma unroll 1
                 for (int e0 = 0; e0 < last; e0 += 16) {  // (blocks above the diagonal are not read)
@@ -544,7 +548,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         uint32_t hi, lo;
-                        two_parts(x[i], hi, lo);
+                        two_parts(mul2(x[i], pack2(kTile, kTile)), hi, lo);
                         to[2 * i * 16] = (unsigned short)hi;
                         to[(2 * i + 1) * 16] = (unsigned short)(hi >> 16);
                         to[2 * i * 16 + 256] = (unsigned short)lo;
@@ -565,8 +569,8 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                         if (b == C) {
                             // (a product's lane has row lane / 4, and eight more, and columns 2 (lane % 4) and one more of either tile)
                             const int m = lane >> 2, k = (lane & 3) * 2;
-                            c[0][0] = c[1][2] = m == k ? 1.f : 0.f;
-                            c[0][1] = c[1][3] = m == k + 1 ? 1.f : 0.f;
+                            c[0][0] = c[1][2] = m == k ? kTile * kTile : 0.f;
+                            c[0][1] = c[1][3] = m == k + 1 ? kTile * kTile : 0.f;
                         } else {
 #pragma unroll
                             for (int e = C; e < b; ++e) {
@@ -1218,11 +1222,12 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 tmem_ld_wait();
                 {
                     const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
+                    const uint64_t back = pack2(1.f / kTile, 1.f / kTile);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const ulonglong2 be = beta[i];
-                        X[2 * i] = mul2(be.x, add2(X[2 * i], pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1]))));
-                        X[2 * i + 1] = mul2(be.y, add2(X[2 * i + 1], pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3]))));
+                        X[2 * i] = mul2(be.x, fma2(back, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]));
+                        X[2 * i + 1] = mul2(be.y, fma2(back, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]));
                     }
                     auto store = [&]() {
 #pragma unroll
@@ -1264,7 +1269,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 if (x.outputs) {
                     if (half == 0) {
                         float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (o & 1) * 256 + col;
-                        aside[0] = p.q_scale * down;
+                        aside[0] = p.q_scale * down * (1.f / kTile);
                         aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
                     }
                     tmem_st_wait();

@@ -40,3 +40,15 @@ def test_small_step_sizes_keep_their_bits(b):
     run_scan(m, pr, x, out)
     assert (m.state[:1].cpu().double() - new[:1]).norm() <= 1e-6 * new[:1].norm()
     assert (out.cpu().double() - want).norm() <= 2.0e-3 * want.norm()
+
+
+@pytest.mark.parametrize("od", ["bf16", "f32"])
+def test_what_has_decayed_of_larger_values_leaves_no_trace(od):
+    """Values some hundred times as large at a chunk's start, of which a token leaves two thirds: the tokens that meet nothing of them are right to their
+    own size."""
+    x = inputs([300], seed=20)
+    x["v"][64:67] *= 256
+    x["v"][130, :, ::3] *= 512
+    x["a"], x["bias"], x["dt"] = torch.full((2,), -1.0), torch.full((2,), -0.7), x["dt"] * 0.1
+    starts, pr = batch_of([300], None, [1])
+    check_scan(layer(8, 2), x, starts, pr, None, [1], od)
