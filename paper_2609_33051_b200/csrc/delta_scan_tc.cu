@@ -44,9 +44,22 @@ constexpr uint32_t kPart = 8192u;                      // 64 rows of 128 bytes
 constexpr float kTile = 16384.f;                       // factor of T and P
 // The scratch: for a chunk of a head two parts of T - I, two of P and the gates; for one of a group the rows of K and Q, half of the channels at a time
 constexpr uint32_t kTOff = 0, kPOff = 2 * kPart, kGOff = 4 * kPart, kRows = 4 * kPart;
-// gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c kTile / |q| (r and 1 / |q| of the scaled rows), and 2^c_end
-constexpr int kBeta = 0, kRead = 64, kPut = 128, kAsk = 192, kKeep = 256, kGates = 320;
-constexpr uint32_t kBlock = kGOff + kGates * 4u;
+// gates, 64 floats each: beta, -2^c r, 2^(c_end - c) r, 2^c kTile / |q| (r and 1 / |q| of the scaled rows), and 2^c_end and whether no beta is below kLeastBeta
+constexpr int kBeta = 0, kRead = 64, kPut = 128, kAsk = 192, kKeep = 256, kPlain = 257, kGates = 320;
+// behind them, and not copied with them: a token's decay, r and 1 / |q|, for chunks taken token by token
+constexpr int kDecay = kGates, kKey = kGates + 64, kQuery = kGates + 128, kFloats = kGates + 192;
+constexpr uint32_t kCopied = kGOff + kGates * 4u, kBlock = kGOff + kFloats * 4u;
+
+// Numbers of very different size.  A column's scale is its chunk's largest; an operand is 2^-25 off at that scale where it is small, so a token keeps the
+// accuracy of its own column's numbers only while those, scaled, stay above some floor: the larger one of its value and the one before it (whose
+// weight the state has), or what earlier ones and the state were, less what has decayed since; and no value counts that beta keeps out.  Where they
+// do not (a value or a state 2^14 times as large as the others that a chunk meets, beta below 2^-12 throughout) the columns of a pair of warps go through
+// the chunk token by token, in fp32, and the products meet zeros: 50 to 100 us instead of 3.  It is looked at where a pair of tokens 2 i and 2 i + 1 is
+// below the floor (of normal numbers one in a million columns and chunks; the look takes 12 us, most of it for instructions that nobody has run
+// lately), or the state that a unit begins with, or a beta below kLeastBeta.  (Small tokens that stand beside a large one of their own pair, each of
+// them, are not seen: a small one behind another then has some bits less.)
+// (The floor: 2^-25 is 2^-20 of it; a token meets such errors in what it reads of the state, in X, U and W.)
+constexpr float kFloor = 1.f / 32.f, kLeastBeta = 1.f / 4096.f;
 
 struct DeltaArgs {
     CUtensorMap tq, tk, tv;
@@ -393,6 +406,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
         // gates, while the product is made
         if (ok && role == 0 && mine < heads) {
             float *s = sums + mine * 3 * kQ, *put = puts + mine * kQ;
+            bool plain = true;
             double c[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -408,6 +422,7 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 }
                 s[2 * kQ + lane * 2 + i] = in ? beta : 0.f;
                 put[lane * 2 + i] = in && beta == beta ? beta * norms[128 + lane * 2 + i] : 0.f;
+                plain = plain && (!in || beta >= kLeastBeta);
                 c[i] = (i > 0 ? c[0] : 0.0) + (double)(in ? l : 0.f);
             }
             double before = c[1];
@@ -424,6 +439,8 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
                 s[lane * 2 + i] = (float)w;
                 s[kQ + lane * 2 + i] = (float)(x - w);
             }
+            plain = __all_sync(0xffffffffu, plain);
+            if (lane == 0) reinterpret_cast<float*>(p.work + ((size_t)chunk * p.H + h0 + mine) * kBlock + kGOff)[kPlain] = plain ? 1.f : 0.f;
         }
         ok = ok && mbar_wait_bounded(bar + 1, 0);
         if (tid == 64) tma_store_read();
@@ -440,6 +457,9 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
             to[kPut + t] = in ? rest * norms[t] : 0.f;
             to[kAsk + t] = in ? e * kTile * norms[64 + t] : 0.f;
             if (t == 63) to[kKeep] = e;
+            to[kDecay + t] = exp2f((t > 0 ? w - s[t - 1] : w) + (t > 0 ? r - s[kQ + t - 1] : r));
+            to[kKey + t] = in ? norms[t] : 0.f;
+            to[kQuery + t] = in ? norms[64 + t] : 0.f;
         }
         if (ok && mine < heads) {
             tc_fence_after();
@@ -651,19 +671,22 @@ __global__ void __launch_bounds__(kPrepThreads, 3) delta_prep_kernel(const __gri
 // a barrier for every quarter took half as long again).
 
 constexpr int kWarps = 8, kThreads = 32 * (8 + kWarps);
-constexpr uint32_t kWOff = kRows, kStage = (kWOff + kBlock + 1023u) & ~1023u;
+constexpr uint32_t kWOff = kRows, kStage = (kWOff + kCopied + 1023u) & ~1023u;
 constexpr uint32_t kVOff = 2 * kStage;                 // two buffers: rows of 256 bytes, then pairs of rows, [32][128] pairs of bf16
 constexpr uint32_t kYOff = kVOff + 4 * kPart;          // the same
 constexpr uint32_t kBarOff = kYOff + 2 * kPart;
 // (bUP has two that take turns: nothing but its arrivals holds the state's warps back until the Y warps have seen them, and those could be a
-// chunk ahead of a late one, which then would not see that phase end.  Two chunks ahead they are never: U of the next chunk but one waits for Y.)
+// chunk ahead of a late one, which then would not see that phase end.  Two chunks ahead they are never: U of the next chunk but one waits for Y.
+// bOutFree has two as well: the state's warps, which ask for it now and then, may come when it is two phases back.)
 enum { bFull = 0, bEmpty = 2, bRaw = 4, bFullV = 6, bEmptyV = 8, bS = 10, bXP = 12, bWP = 13, bUP = 14, bX = 16, bU = 17, bProd = 18, bAsk = 19, bY = 20, bOut = 21,
-       bOutFree = 22, bJoin = 23, bScaled = 24, kBars = 25 };
+       bOutFree = 22, bJoin = 24, bScaled = 25, bPair = 26, kBars = 30 };
 constexpr uint32_t kMarkOff = (kBarOff + kBars * 8u + 4u + 15u) & ~15u;  // [128]: see mark_of
-constexpr uint32_t kLargeOff = kMarkOff + 128u * 4u;             // [4][128]: the largest values of chunk n at n & 3
-constexpr uint32_t kMostOff = kLargeOff + 512u * 4u;             // [2][2][128]: the largest elements of the state, by halves
+constexpr uint32_t kLargeOff = kMarkOff + 128u * 4u;             // [4][128][2]: the largest values of chunk n at n & 3, and the least of its pairs' larger ones
+constexpr uint32_t kMostOff = kLargeOff + 1024u * 4u;             // [2][2][128]: the largest elements of the state, by halves
 constexpr uint32_t kAsideOff = kMostOff + 512u * 4u;              // [2][2][128]: for Y of chunk n at n & 1, its factor and the first token that is not finite
-constexpr uint32_t kSmemTc = kAsideOff + 512u * 4u + 1024u;
+constexpr uint32_t kPairOff = kAsideOff + 512u * 4u;              // [2][2][2][128]: what the halves of a column read by a key and a query
+constexpr uint32_t kRowsOff = kPairOff + 1024u * 4u;              // [4][2][256]: for every pair of warps a token's key and query, of two tokens in turn
+constexpr uint32_t kSmemTc = kRowsOff + 2048u * 4u + 1024u;
 
 // columns of tensor memory: parts of S (part i, channel k: 64 i + k / 2); of X and W, of U (part i, token s: 32 i + s / 2); K S^T and (T - I) X; Y; W K
 constexpr uint32_t cS = 0, cW = 128, cU = 192, cX = 256, cY = 320, cP = 384;
@@ -672,6 +695,198 @@ constexpr uint32_t cS = 0, cW = 128, cU = 192, cX = 256, cY = 320, cP = 384;
 // that is not finite on, zeros go to the products, and the lane's outputs and state become NaN afterwards.  A mark of chunk n holds that
 // token; the largest of several is the first token of the latest chunk, so that marks need no clearing.
 __device__ __forceinline__ uint32_t mark_of(int n, int token) { return ((uint32_t)n << 7) + (uint32_t)(kQ - token); }
+
+// To the outputs' warps in the place of a column's first token that is not finite (kQ: none): its outputs are there already.
+constexpr int kOutputsThere = -1;
+
+// The scale for what is bounded by `all`: where that, times the scale, would be beyond 2^14 or below 2^11 (the second parts would lose bits), a new one.
+// Returns the new scale over the old one.
+__device__ __forceinline__ float new_scale(float all, float& up, float& down) {
+    const float now = all * up;
+    if (now <= 16384.f && (now >= 2048.f || all == 0.f)) return 1.f;
+    const int e = max(-100, (int)((__float_as_uint(all) & 0x7f800000u) >> 23) - 127);     // (below 2^(e + 1); below 2^13 then)
+    const float old = down;
+    up = __uint_as_float((uint32_t)(127 + 12 - e) << 23);
+    down = __uint_as_float((uint32_t)(127 - 12 + e) << 23);
+    return up * old;
+}
+__device__ __forceinline__ void arrive_warp(uint64_t* bar, int lane) {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_one(bar);
+}
+// Channels 32 i .. of a half of S as an operand, in the lanes at `lanes`.
+__device__ __forceinline__ void give_state(const uint64_t (&S)[32], int i, uint32_t lanes, uint64_t* bar, int lane) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        uint32_t a[2][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) two_parts(S[i * 16 + c * 8 + j], a[0][j], a[1][j]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cS + e * 64 + i * 16 + c * 8, a[e]);
+    }
+    tmem_st_wait();
+    arrive_warp(bar, lane);
+}
+constexpr float kLength = 11.4f;                        // bounds the length of 128 elements of at most one
+
+// A chunk for the 32 columns of two warps, half of the channels each: whether its numbers are too far apart for one scale, and then the chunk, token by
+// token.  The values are where the outputs will stand.
+struct Alone {
+    uint64_t S[32];            // times 1 / down
+    unsigned char *smem, *stage;
+    uint64_t *bar, *pair;      // pair: where the two meet
+    const float* rest;         // the chunk's gates in the scratch
+    const volatile float *most, *next;         // the largest elements of the state's halves, 128 apart; the next chunk's largest value
+    float up, down, length, q_scale;
+    uint32_t lanes;            // of tensor memory, and this half's columns there
+    int n, m, o, col, half, valid, met;
+    bool zero, outputs, live, more, ok;
+};
+__device__ __noinline__ bool token_by_token(Alone& g) {
+    const int lane = (int)threadIdx.x & 31, half = g.half, valid = g.valid;
+    const bool outputs = g.outputs;
+    const float up = g.up, q_scale = g.q_scale;
+    unsigned char* const stage = g.stage;
+    uint64_t* const pair = g.pair;
+    int met = g.met;
+    auto meet = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive_one(pair);
+        const bool ok = warp_wait(pair, met & 1);
+        ++met;
+        if (!ok) g.ok = false;
+        return ok;
+    };
+    const float* beta = reinterpret_cast<const float*>(stage + kWOff + kGOff) + kBeta;
+    volatile unsigned short* value = reinterpret_cast<volatile unsigned short*>(g.smem + kYOff + g.col * 4);     // of token t: at(t)
+    auto at = [](int t) { return (t >> 1) * 256 + (t & 1); };
+    // (a lane has two tokens' decays, keys' and queries' factors)
+    const float d0 = __ldcg(g.rest + kDecay + lane), d1 = __ldcg(g.rest + kDecay + 32 + lane), k0 = __ldcg(g.rest + kKey + lane),
+                k1 = __ldcg(g.rest + kKey + 32 + lane), q0 = __ldcg(g.rest + kQuery + lane), q1 = __ldcg(g.rest + kQuery + 32 + lane);
+    auto of = [](float low, float high, int i) { return __shfl_sync(0xffffffffu, i < 32 ? low : high, i & 31); };
+    if (!meet()) return false;
+    {
+        float a = 0.f, last = fmaxf(g.most[0], g.most[128]);
+        g.met = met;
+        if (__all_sync(0xffffffffu, last * beta[kKeep - kBeta] * up >= kFloor)) return false;      // (the state alone is large enough, up to the last token)
+        bool nothing = g.zero, over = false, alone = false;      // neither a state nor a value so far; nothing behind it is finite
+#pragma unroll 1
+        for (int i = 0; i < valid; ++i) {
+            const float size = __uint_as_float((uint32_t)(value[at(i)] & 0x7fff) << 16), counts = beta[i] >= kLeastBeta ? size : 0.f;
+            a = fmaxf(fmaxf(counts, last), of(d0, d1, i) * a);
+            last = counts;
+            over = over || !(size <= 3.4028235e38f);
+            if (over || (nothing && size == 0.f)) continue;
+            if (!(a * up >= kFloor)) alone = true;
+            nothing = false;
+        }
+        if (!__any_sync(0xffffffffu, alone)) return false;
+    }
+    uint64_t S[32];                                     // channels 64 half ..
+    const uint64_t down2 = pack2(g.down, g.down);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) S[i] = mul2(down2, g.S[i]);
+    // Keys and queries as floats, a token's at a time, by its half of the channels: two a lane.  [key, query][64]
+    float* const row = reinterpret_cast<float*>(g.smem + kRowsOff) + (g.col >> 5) * 512 + half * 128;
+    auto spread = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const __half2 w = *reinterpret_cast<const __half2*>(stage + half * (2 * kPart) + i * kPart + t * 128 + (((lane >> 2) ^ (t & 7)) * 16) + (lane & 3) * 4);
+            *reinterpret_cast<float2*>(row + (t & 1) * 256 + i * 64 + lane * 2) = __half22float2(w);
+        }
+        __syncwarp();
+    };
+    // the state times one of them
+    auto read_by = [&](const float* x) {
+        uint64_t sum[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(x + 4 * i);
+            sum[i % 2 * 2] = fma2(S[2 * i], w.x, sum[i % 2 * 2]);
+            sum[i % 2 * 2 + 1] = fma2(S[2 * i + 1], w.y, sum[i % 2 * 2 + 1]);
+        }
+        float lo, hi;
+        unpack2(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), lo, hi);
+        return lo + hi;
+    };
+    volatile float* both = reinterpret_cast<volatile float*>(g.smem + kPairOff) + g.col;
+    float asked = 0.f;                                  // by the query of the token before
+#pragma unroll 1
+    for (int i = 0; i <= valid; ++i) {
+        volatile float* to = both + (i & 1) * 512;
+        const float* x = row + (i & 1) * 256;
+        if (i < valid) spread(i);
+        to[half * 256] = i < valid ? read_by(x) : 0.f;
+        to[half * 256 + 128] = asked;
+        if (!meet()) return false;
+        const float query = of(q0, q1, i > 0 ? i - 1 : 0);
+        if (half == 0 && i > 0 && outputs) value[at(i - 1)] = __bfloat16_as_ushort(__float2bfloat16_rn(q_scale * query * (to[128] + to[256 + 128])));
+        if (i == valid) break;
+        const float d = of(d0, d1, i), r = of(k0, k1, i);
+        const float u = beta[i] * fmaf(-(d * r), to[0] + to[256], __uint_as_float((uint32_t)value[at(i)] << 16));
+        const uint64_t d2 = pack2(d, d), u2 = pack2(u * r, u * r);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(x + 4 * j);
+            S[2 * j] = fma2(u2, w.x, mul2(d2, S[2 * j]));
+            S[2 * j + 1] = fma2(u2, w.y, mul2(d2, S[2 * j + 1]));
+        }
+        asked = outputs ? read_by(x + 64) : 0.f;
+    }
+    // The state is the one behind the chunk; zeros go to the products, for the other columns' sake.
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        float a, b;
+        unpack2(S[i], a, b);
+        most = fmaxf(most, fmaxf(fabsf(a), fabsf(b)));
+    }
+    both[half * 256 + (valid & 1 ? 0 : 512)] = most;    // (the other one than the last token's)
+    if (!meet()) return false;
+    most = fmaxf(both[valid & 1 ? 0 : 512], both[256 + (valid & 1 ? 0 : 512)]);
+    g.met = met;
+    auto wait = [&](int i, int k) { return g.ok = warp_wait(g.bar + i, k & 1); };
+    if (g.live && !wait(bX, g.m)) return false;
+    tc_fence_after();
+    const uint32_t none[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) tmem_st8u(g.lanes + cW + (e >> 1) * 32 + half * 16 + (e & 1) * 8, none);
+    tmem_st_wait();
+    arrive_warp(g.bar + bXP, lane);
+    if (!wait(bU, g.n)) return false;
+    tc_fence_after();
+    arrive_warp(g.bar + bWP, lane);
+    if (outputs) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tmem_st8u(g.lanes + cU + (e >> 1) * 32 + half * 16 + (e & 1) * 8, none);
+        if (half == 0) {
+            volatile float* aside = reinterpret_cast<volatile float*>(g.smem + kAsideOff) + (g.o & 1) * 256 + g.col;
+            aside[0] = 0.f;
+            aside[128] = __int_as_float(kOutputsThere);
+        }
+        tmem_st_wait();
+        arrive_warp(g.bar + bUP + (g.o & 1), lane);
+    }
+    g.up = g.down = 1.f;
+    if (g.more) {
+        if (!wait(bFullV + ((g.n + 1) & 1), (g.n + 1) >> 1)) return false;
+        g.length = kLength * most;
+        const float r = new_scale(9.f * *g.next + g.length, g.up, g.down);
+        const uint64_t r2 = pack2(r, r);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) S[i] = mul2(r2, S[i]);
+    }
+    if (!wait(bProd, g.n)) return false;
+    tc_fence_after();
+    if (g.more) {
+        give_state(S, 0, g.lanes + half * 32, g.bar + bS, lane);
+        give_state(S, 1, g.lanes + half * 32, g.bar + bS + 1, lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g.S[i] = S[i];
+    return true;
+}
 
 __device__ __forceinline__ bool finite16(uint32_t bf) { return (bf & 0x7f80u) != 0x7f80u; }
 
@@ -689,6 +904,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             int n = 1;                                  // copies, commits of products and single warps arrive once
             if (i == bEmptyV || i == bEmptyV + 1 || (i >= bS && i < bX) || i == bJoin) n = kWarps;
             if (i == bOut || i == bScaled) n = 4;
+            if (i >= bPair) n = 2;
             mbar_init(bar + i, n);
         }
         mbar_fence_init();
@@ -706,7 +922,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     int n = 0, m = 0;                                   // chunks so far, over all units of the CTA; those with a state before them
 
     if (warp == 0) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (lane == 0) {
             Unit x;
             for (int it = 0; ok && decode_unit(g, it, x); ++it) {
@@ -722,9 +938,9 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     ok = n < 2 || mbar_wait_bounded(bar + bEmpty + b, (n / 2 - 1) & 1);
                     if (!ok) break;
                     unsigned char* to = smem + b * kStage;
-                    mbar_expect_tx(bar + bFull + b, kRows + kBlock);
+                    mbar_expect_tx(bar + bFull + b, kRows + kCopied);
                     bulk_g2s(to, g.rows + ((size_t)chunk * p.G + group) * kRows, kRows, bar + bFull + b);
-                    bulk_g2s(to + kWOff, p.work + ((size_t)chunk * p.H + head) * kBlock, kBlock, bar + bFull + b);
+                    bulk_g2s(to + kWOff, p.work + ((size_t)chunk * p.H + head) * kBlock, kCopied, bar + bFull + b);
                 }
             }
             if (!ok) record_fault(p.status, kFaultScanWait, 12);
@@ -734,7 +950,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         __syncwarp();
     } else if (warp == 1) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         constexpr uint32_t kN64 = kTypes | ((64u >> 3) << 17), kProdDesc = kTypes | (1u << 16) | ((128u >> 3) << 17);
         Unit x;
         int o = 0, om = 0;                              // chunks with outputs; those of them with a state before them
@@ -835,7 +1051,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 13);
         __syncwarp();
     } else if (warp == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         // V, copied a chunk ahead: four columns a lane; two rows at a time become one of pairs, in their place
         Unit next, x;
         int next_it = 0, next_n = 0, next_t = 0;
@@ -866,7 +1082,9 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 ok = ok && warp_wait(bar + bRaw + b, (n / 2) & 1);
                 if (!ok) break;
                 unsigned char* v = smem + kVOff + b * 2 * kPart;
-                uint32_t top[4] = {0u, 0u, 0u, 0u};
+                // The largest size, and the least of the larger ones of two neighbouring tokens, two columns at a time.  (As whole numbers: sizes in bf16
+                // are in their order, with what is not finite above all.)
+                uint32_t top[2] = {0u, 0u}, least[2] = {0x7f7f7f7fu, 0x7f7f7f7fu};
 #pragma unroll 1
                 for (int r = 0; r < 32; r += 4) {
                     uint2 a[4], c[4];
@@ -875,12 +1093,34 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         a[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + lane * 8);
                         c[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + 256 + lane * 8);
                     }
-                    if (2 * r + 8 > valid) {             // rows of the next sequence are no part of this one
+                    auto sizes = [&](int j, auto whole) {
+                        uint32_t first = 0u;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t y = (j ? a[i].y : a[i].x) & 0x7fff7fffu, z = (j ? c[i].y : c[i].x) & 0x7fff7fffu, both = __vmaxu2(y, z);
+                            if constexpr (decltype(whole)::value) {
+                                if (i % 2) {
+                                    top[j] = __vimax3_u16x2(top[j], first, both);
+                                    least[j] = __vimin3_u16x2(least[j], first, both);
+                                }
+                                first = both;
+                            } else {
+                                top[j] = __vmaxu2(top[j], both);
+                                if (2 * (r + i) < valid) least[j] = __vminu2(least[j], 2 * (r + i) + 1 < valid ? both : y);
+                            }
+                        }
+                    };
+                    if (2 * r + 8 <= valid) {
+                        sizes(0, std::true_type{});
+                        sizes(1, std::true_type{});
+                    } else {                             // rows of the next sequence are no part of this one
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             if (2 * (r + i) >= valid) a[i] = make_uint2(0u, 0u);
                             if (2 * (r + i) + 1 >= valid) c[i] = make_uint2(0u, 0u);
                         }
+                        sizes(0, std::false_type{});
+                        sizes(1, std::false_type{});
                     }
                     __syncwarp();
 #pragma unroll
@@ -888,30 +1128,26 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         const uint4 w = make_uint4(__byte_perm(a[i].x, c[i].x, 0x5410), __byte_perm(a[i].x, c[i].x, 0x7632), __byte_perm(a[i].y, c[i].y, 0x5410),
                                                    __byte_perm(a[i].y, c[i].y, 0x7632));
                         *reinterpret_cast<uint4*>(v + (r + i) * 512 + lane * 16) = w;
-                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[0]) : "r"(w.x & 0x7fff7fffu));
-                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[1]) : "r"(w.y & 0x7fff7fffu));
-                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[2]) : "r"(w.z & 0x7fff7fffu));
-                        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(top[3]) : "r"(w.w & 0x7fff7fffu));
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (!finite16(top[i]) || !finite16(top[i] >> 16)) {          // (tokens before it keep their accuracy: of those that are finite)
-                        top[i] = 0u;
+                    if (!finite16(top[i / 2] >> (i % 2 * 16))) {                 // (tokens before it keep their accuracy: of those that are finite)
+                        uint32_t most = 0u;
                         __threadfence_block();
 #pragma unroll 1
                         for (int r = 0; r < 32; ++r) {
                             const uint32_t w = *reinterpret_cast<const volatile uint32_t*>(v + r * 512 + lane * 16 + i * 4) & 0x7fff7fffu;
-                            asm("max.bf16x2 %0, %0, %1;" : "+r"(top[i]) : "r"((finite16(w) ? w & 0xffffu : 0u) | (finite16(w >> 16) ? w & 0xffff0000u : 0u)));
+                            most = __vmaxu2(most, (finite16(w) ? w & 0xffffu : 0u) | (finite16(w >> 16) ? w & 0xffff0000u : 0u));
                         }
+                        most = max(most & 0xffffu, most >> 16);
+                        top[i / 2] = i % 2 ? __byte_perm(top[i / 2], most, 0x5410) : __byte_perm(most, top[i / 2], 0x7610);
                     }
                 }
-                float4 large;
-                large.x = fmaxf(__uint_as_float(top[0] << 16), __uint_as_float(top[0] & 0xffff0000u));
-                large.y = fmaxf(__uint_as_float(top[1] << 16), __uint_as_float(top[1] & 0xffff0000u));
-                large.z = fmaxf(__uint_as_float(top[2] << 16), __uint_as_float(top[2] & 0xffff0000u));
-                large.w = fmaxf(__uint_as_float(top[3] << 16), __uint_as_float(top[3] & 0xffff0000u));
-                *reinterpret_cast<float4*>(smem + kLargeOff + (n & 3) * 512 + lane * 16) = large;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    *reinterpret_cast<float4*>(smem + kLargeOff + (n & 3) * 1024 + lane * 32 + i * 16) =
+                        make_float4(__uint_as_float(top[i] << 16), __uint_as_float(least[i] << 16), __uint_as_float(top[i] & 0xffff0000u), __uint_as_float(least[i] & 0xffff0000u));
                 proxy_fence();                           // (the next copy writes where this warp has)
                 __syncwarp();
                 if (lane == 0) mbar_arrive_one(bar + bFullV + b);
@@ -922,7 +1158,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         for (int i = next_n < 2 ? 0 : next_n - 2; i < next_n; ++i) mbar_wait_bounded(bar + (ok ? bEmptyV : bRaw) + (i & 1), (i / 2) & 1, ok ? 1u << 22 : 1u << 16);
         __syncwarp();
     } else if (warp == 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         // Y: four columns a lane, two rows at a time
         Unit x;
         for (int it = 0; ok && decode_unit(g, it, x); ++it) {
@@ -943,13 +1179,13 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     to += step;
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive_one(bar + bOutFree);
+                if (lane == 0) mbar_arrive_one(bar + bOutFree + (n & 1));
             }
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 15);
         __syncwarp();
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         // Y of a value column: Q S^T times its tokens' factors, and what U P has added to it
         const int col = (warp & 3) * 32 + lane;
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + cY;
@@ -1000,7 +1236,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 if (!ok) break;
                 const float scale = reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256];
                 const int first = __float_as_int(reinterpret_cast<const volatile float*>(aside)[(o & 1) * 256 + 128]);
-                ok = warp_wait(bar + bY, o & 1) && (o < 1 || warp_wait(bar + bOutFree, (o - 1) & 1));
+                ok = warp_wait(bar + bY, o & 1) && (o < 1 || warp_wait(bar + bOutFree + ((o - 1) & 1), ((o - 1) >> 1) & 1));
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t scale2 = pack2(scale, scale);
@@ -1011,6 +1247,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     tmem_ld32_async(at + h * 32, d);
                     tmem_ld_wait();
                     if (first < kQ) {
+                        if (first == kOutputsThere) continue;                    // (the same for the whole warp)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (h * 32 + i >= first) d[i] = 0x7fffffffu;
@@ -1030,29 +1267,29 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 17);
     } else {
-        // (512 threads start with 128 registers: 128 x 56 + 256 x 176 + 128 x 96 of 65536)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+        // (512 threads start with 128 registers: 128 x 48 + 256 x 192 + 128 x 80 are all 65536)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int quad = warp & 3, half = (warp - 4) >> 2, col = quad * 32 + lane;       // value column; half of the channels and tokens
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        const float* large = reinterpret_cast<const float*>(smem + kLargeOff) + col;
+        const float2* large = reinterpret_cast<const float2*>(smem + kLargeOff) + col;
         float* most = reinterpret_cast<float*>(smem + kMostOff) + col;
         uint64_t S[32];                                 // channels 64 half .., times `up`
         uint32_t f[16];                                 // the next chunk's values of this half, two tokens each
         float up = 1.f, down = 1.f;                     // the lane's scale and its inverse
         float length = 0.f;                             // bounds the length of the lane's state before the chunk
+        bool zero = false;                              // a lane without a state before the unit
+        bool doubt = false;                             // the least of the chunk's numbers may be too small for its scale
+        int met = 0;                                    // meetings of a column's halves
         int units = 0;                                  // with tokens, so far
-        auto arrive = [&](int i) {
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_one(bar + i);
-        };
-        auto fetch = [&](int c) {
+        auto arrive = [&](int i) { arrive_warp(bar + i, lane); };
+        auto fetch = [&](int c, uint32_t* begin = nullptr) {     // begin: for the chunk's first two values
             const int b = c & 1;
             ok = warp_wait(bar + bFullV + b, (c / 2) & 1);
             if (!ok) return;
             const uint32_t* v = reinterpret_cast<const uint32_t*>(smem + kVOff + b * 2 * kPart) + half * 16 * 128 + col;
 #pragma unroll
             for (int i = 0; i < 16; ++i) f[i] = v[i * 128];
+            if (begin != nullptr) *begin = v[half * -16 * 128];
             __syncwarp();
             if (lane == 0) mbar_arrive_one(bar + bEmptyV + b);
         };
@@ -1067,34 +1304,18 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             }
             most[((c & 1) * 2 + half) * 128] = top * down;
         };
-        auto length_of = [&](int c) {
+        auto most_of = [&](int c) {
             const volatile float* from = most + (c & 1) * 256;
-            return 11.4f * fmaxf(from[0], from[128]);
+            return fmaxf(from[0], from[128]);
         };
-        // The scale for chunk c: where what bounds its values, times the scale, would be beyond 2^14 or below 2^11 (the second parts would
-        // lose bits), a new one.  Returns the new scale over the old one.
         auto rescale = [&](int c) {
-            const float all = 9.f * reinterpret_cast<const volatile float*>(large)[(c & 3) * 128] + length, now = all * up;
-            if (now <= 16384.f && (now >= 2048.f || all == 0.f)) return 1.f;
-            const int e = max(-100, (int)((__float_as_uint(all) & 0x7f800000u) >> 23) - 127);     // (below 2^(e + 1); below 2^13 then)
-            const float old = down;
-            up = __uint_as_float((uint32_t)(127 + 12 - e) << 23);
-            down = __uint_as_float((uint32_t)(127 - 12 + e) << 23);
-            return up * old;
+            const float2 sizes = large[(c & 3) * 128];
+            const float all = 9.f * sizes.x + length;
+            const float r = new_scale(all, up, down);
+            doubt = !(sizes.y * up >= kFloor) && all != 0.f;
+            return r;
         };
-        // Channels 32 i .. of this half of S as an operand.
-        auto give = [&](int i) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t a[2][8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) two_parts(S[i * 16 + c * 8 + j], a[0][j], a[1][j]);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cS + e * 64 + half * 32 + i * 16 + c * 8, a[e]);
-            }
-            tmem_st_wait();
-            arrive(bS + i);
-        };
+        auto give = [&](int i) { give_state(S, i, lanes + half * 32, bar + bS + i, lane); };
         Unit x;
         int o = 0;                                      // chunks with outputs
         for (int it = 0; ok && decode_unit(g, it, x); ++it) {
@@ -1113,15 +1334,19 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
             }
             up = down = 1.f;
             if (rows.x < rows.y) {
-                fetch(n);
+                uint32_t begin = 0u;
+                fetch(n, &begin);
                 if (!ok) break;
                 state_most(n);
                 arrive(bJoin);
                 ok = warp_wait(bar + bJoin, units & 1);
                 ++units;
                 if (!ok) break;
-                length = length_of(n);
-                const float r = rescale(n);
+                length = kLength * most_of(n);
+                zero = length == 0.f;
+                const float r = rescale(n), first = __uint_as_float(begin << 16 & 0x7fff0000u);
+                // (Without a state the first token, if it is small by itself, keeps some bits less than the others.)
+                doubt = doubt || (zero ? first > 0.f && !(first * up >= kFloor / 128.f) : !(most_of(n) * up >= kFloor));
                 const uint64_t r2 = pack2(r, r);
                 if (stored) {
 #pragma unroll
@@ -1130,176 +1355,242 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     give(1);
                 }
             }
-            for (int t = rows.x; t < rows.y; t += kQ, ++n) {
-                const int b = n & 1, left = rows.y - t - half * 32;              // tokens of the sequence from this half on
-                const bool live = stored || t > rows.x, more = t + kQ < rows.y;
-                const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff) + half * 32;
-                ok = warp_wait(bar + bFull + b, (n / 2) & 1);
-                if (!ok) break;
-                // X of this half's tokens: the values, scaled (times powers of two in bf16), less what the state has for their keys
-                uint64_t X[16];
-                {
-                    const uint32_t up16 = __float_as_uint(up) >> 16;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float a, c;
-                        asm("{\n\t.reg .b16 l, h, s, x;\n\tmov.b32 {l, h}, %2;\n\tmov.b32 {s, x}, %3;\n\t"
-                            "fma.rn.f32.bf16 %0, l, s, 0f00000000;\n\tfma.rn.f32.bf16 %1, h, s, 0f00000000;\n\t}"
-                            : "=f"(a), "=f"(c)
-                            : "r"(f[i]), "r"(up16));
-                        X[i] = pack2(a, c);
-                    }
-                }
-                // What bounds the next chunk's state: this one's, from the state itself every eighth chunk (the halves meet behind the next
-                // product), less what decays of it, and what the tokens add to it.
-                const bool look = (n & 7) == 7;
-                if (more) {
-                    if (look) state_most(n);
-                    fetch(n + 1);
+            int t = rows.x;
+            bool checked = x.kind == kMap;               // (a map has no values, and what it is off by decays as it does)
+            while (ok && t < rows.y) {
+                for (; t < rows.y; t += kQ, ++n) {
+                    const int b = n & 1, left = rows.y - t - half * 32;              // tokens of the sequence from this half on
+                    const bool live = stored || t > rows.x, more = t + kQ < rows.y;
+                    const float* gate = reinterpret_cast<const float*>(smem + b * kStage + kWOff + kGOff) + half * 32;
+                    ok = warp_wait(bar + bFull + b, (n / 2) & 1);
                     if (!ok) break;
-                }
-                uint32_t d[32];
-                const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead);
-                if (live) {
-                    ok = warp_wait(bar + bX, m & 1);
-                    if (!ok) break;
-                    ++m;
-                    tc_fence_after();
-                    tmem_ld32_async(lanes + cX + half * 32, d);
-                    tmem_ld_wait();
-                } else {                                 // (a key that is not finite counts, whatever it is taken of)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) d[i] = 0u;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const ulonglong2 r = rd[i];
-                    X[2 * i] = fma2(r.x, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]);
-                    X[2 * i + 1] = fma2(r.y, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]);
-                }
-                {
-                    uint32_t a[4][8], odd = 0u;          // first parts of 16 tokens, of 16 more; second parts
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        two_parts(X[i], a[i / 8][i % 8], a[2 + i / 8][i % 8]);
-                        asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(a[i / 8][i % 8] & 0x7fff7fffu));
-                    }
-                    auto store = [&]() {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) tmem_st8u(lanes + cW + (e >> 1) * 32 + half * 16 + (e & 1) * 8, a[e]);
-                    };
-                    const bool wild = (odd & 0x7c00u) == 0x7c00u || (odd & 0x7c000000u) == 0x7c000000u;
-                    if (!__any_sync(0xffffffffu, wild)) {
-                        store();
-                    } else {
-                        int first = 32;
-#pragma unroll
-                        for (int i = 15; i >= 0; --i) {
-                            if ((a[i / 8][i % 8] & 0x7c000000u) == 0x7c000000u) first = 2 * i + 1;
-                            if ((a[i / 8][i % 8] & 0x7c00u) == 0x7c00u) first = 2 * i;
-                        }
+                    const bool plain = gate[kPlain - half * 32] != 0.f;
+                    if (__any_sync(0xffffffffu, doubt || !plain) && !checked) break;
+                    checked = x.kind == kMap;
+                    // X of this half's tokens: the values, scaled (times powers of two in bf16), less what the state has for their keys
+                    uint64_t X[16];
+                    {
+                        const uint32_t up16 = __float_as_uint(up) >> 16;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const uint32_t keep = (2 * i < first ? 0xffffu : 0u) | (2 * i + 1 < first ? 0xffff0000u : 0u);
-                            a[i / 8][i % 8] &= keep;
-                            a[2 + i / 8][i % 8] &= keep;
+                            float a, c;
+                            asm("{\n\t.reg .b16 l, h, s, x;\n\tmov.b32 {l, h}, %2;\n\tmov.b32 {s, x}, %3;\n\t"
+                                "fma.rn.f32.bf16 %0, l, s, 0f00000000;\n\tfma.rn.f32.bf16 %1, h, s, 0f00000000;\n\t}"
+                                : "=f"(a), "=f"(c)
+                                : "r"(f[i]), "r"(up16));
+                            X[i] = pack2(a, c);
                         }
-                        if (first < 32 && first < left) atomicMax(marks + col, mark_of(n + 1, half * 32 + first));
-                        store();
                     }
-                    tmem_st_wait();
-                    arrive(bXP);
-                }
-                // U and W
-                ok = warp_wait(bar + bU, n & 1);
-                if (!ok) break;
-                tc_fence_after();
-                tmem_ld32_async(lanes + cX + half * 32, d);
-                const uint32_t mark = reinterpret_cast<const volatile uint32_t*>(marks)[col];
-                const bool bad = (mark >> 7) == (uint32_t)n + 1u;
-                const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : 32;
-                const float end = gate[kKeep - half * 32], keep = bad ? __int_as_float(0x7fffffff) : end;       // (NaN: all of the lane's state)
-                tmem_ld_wait();
-                {
-                    const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
-                    const uint64_t back = pack2(1.f / kTile, 1.f / kTile);
+                    // What bounds the next chunk's state: this one's, from the state itself every eighth chunk (the halves meet behind the next
+                    // product), less what decays of it, and what the tokens add to it.
+                    const bool look = (n & 7) == 7;
+                    if (more) {
+                        if (look) state_most(n);
+                        fetch(n + 1);
+                        if (!ok) break;
+                    }
+                    uint32_t d[32];
+                    const ulonglong2* rd = reinterpret_cast<const ulonglong2*>(gate + kRead);
+                    if (live) {
+                        ok = warp_wait(bar + bX, m & 1);
+                        if (!ok) break;
+                        ++m;
+                        tc_fence_after();
+                        tmem_ld32_async(lanes + cX + half * 32, d);
+                        tmem_ld_wait();
+                    } else {                                 // (a key that is not finite counts, whatever it is taken of)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) d[i] = 0u;
+                    }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        const ulonglong2 be = beta[i];
-                        X[2 * i] = mul2(be.x, fma2(back, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]));
-                        X[2 * i + 1] = mul2(be.y, fma2(back, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]));
+                        const ulonglong2 r = rd[i];
+                        X[2 * i] = fma2(r.x, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]);
+                        X[2 * i + 1] = fma2(r.y, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]);
                     }
-                    auto store = [&]() {
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t a[2][8];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const ulonglong2 w = put[q * 4 + i];
-                                two_parts(mul2(w.x, X[q * 8 + 2 * i]), a[0][2 * i], a[1][2 * i]);
-                                two_parts(mul2(w.y, X[q * 8 + 2 * i + 1]), a[0][2 * i + 1], a[1][2 * i + 1]);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
-                        }
-                        tmem_st_wait();
-                        arrive(bWP);
-                        if (!x.outputs) return;
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t a[2][8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) two_parts(X[q * 8 + i], a[0][i], a[1][i]);
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, a[e]);
-                        }
-                    };
-                    if (!__any_sync(0xffffffffu, first < 32)) {
-                        store();
-                    } else {
+                    {
+                        uint32_t a[4][8], odd = 0u;          // first parts of 16 tokens, of 16 more; second parts
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            float b0, b1;
-                            unpack2(X[i], b0, b1);
-                            X[i] = pack2(2 * i >= first ? 0.f : b0, 2 * i + 1 >= first ? 0.f : b1);
+                            two_parts(X[i], a[i / 8][i % 8], a[2 + i / 8][i % 8]);
+                            asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(odd) : "r"(a[i / 8][i % 8] & 0x7fff7fffu));
                         }
-                        store();
-                    }
-                }
-                if (x.outputs) {
-                    if (half == 0) {
-                        float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (o & 1) * 256 + col;
-                        aside[0] = p.q_scale * down * (1.f / kTile);
-                        aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
-                    }
-                    tmem_st_wait();
-                    arrive(bUP + (o & 1));
-                    ++o;
-                }
-                float r = down;
-                if (more) {
-                    length = end * (look ? length_of(n) : length) + 8.f * reinterpret_cast<const volatile float*>(large)[(n & 3) * 128];
-                    r = rescale(n + 1);
-                }
-                const uint64_t r2 = pack2(r, r), keep2 = pack2(keep * r, keep * r);
-                const bool same = __all_sync(0xffffffffu, r == 1.f);
-                // S, times the next chunk's scale (behind the last chunk as it is)
-                ok = warp_wait(bar + bProd, n & 1);
-                if (!ok) break;
-                tc_fence_after();
+                        auto store = [&]() {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    tmem_ld32_async(lanes + cP + half * 64 + i * 32, d);
+                            for (int e = 0; e < 4; ++e) tmem_st8u(lanes + cW + (e >> 1) * 32 + half * 16 + (e & 1) * 8, a[e]);
+                        };
+                        const bool wild = (odd & 0x7c00u) == 0x7c00u || (odd & 0x7c000000u) == 0x7c000000u;
+                        if (!__any_sync(0xffffffffu, wild)) {
+                            store();
+                        } else {
+                            int first = 32;
+#pragma unroll
+                            for (int i = 15; i >= 0; --i) {
+                                if ((a[i / 8][i % 8] & 0x7c000000u) == 0x7c000000u) first = 2 * i + 1;
+                                if ((a[i / 8][i % 8] & 0x7c00u) == 0x7c00u) first = 2 * i;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const uint32_t keep = (2 * i < first ? 0xffffu : 0u) | (2 * i + 1 < first ? 0xffff0000u : 0u);
+                                a[i / 8][i % 8] &= keep;
+                                a[2 + i / 8][i % 8] &= keep;
+                            }
+                            if (first < 32 && first < left) atomicMax(marks + col, mark_of(n + 1, half * 32 + first));
+                            store();
+                        }
+                        tmem_st_wait();
+                        arrive(bXP);
+                    }
+                    // U and W
+                    ok = warp_wait(bar + bU, n & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    tmem_ld32_async(lanes + cX + half * 32, d);
+                    const uint32_t mark = reinterpret_cast<const volatile uint32_t*>(marks)[col];
+                    const bool bad = (mark >> 7) == (uint32_t)n + 1u;
+                    const int first = bad ? kQ - (int)(mark & 127u) - half * 32 : 32;
+                    const float end = gate[kKeep - half * 32], keep = bad ? __int_as_float(0x7fffffff) : end;       // (NaN: all of the lane's state)
                     tmem_ld_wait();
-                    if (same) {
+                    {
+                        const ulonglong2 *put = reinterpret_cast<const ulonglong2*>(gate + kPut), *beta = reinterpret_cast<const ulonglong2*>(gate + kBeta);
+                        const uint64_t back = pack2(1.f / kTile, 1.f / kTile);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) S[i * 16 + j] = fma2(keep2, S[i * 16 + j], pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
-                    } else {
+                        for (int i = 0; i < 8; ++i) {
+                            const ulonglong2 be = beta[i];
+                            X[2 * i] = mul2(be.x, fma2(back, pack2(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1])), X[2 * i]));
+                            X[2 * i + 1] = mul2(be.y, fma2(back, pack2(__uint_as_float(d[4 * i + 2]), __uint_as_float(d[4 * i + 3])), X[2 * i + 1]));
+                        }
+                        auto store = [&]() {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            S[i * 16 + j] = fma2(r2, pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])), mul2(keep2, S[i * 16 + j]));
+                            for (int q = 0; q < 2; ++q) {
+                                uint32_t a[2][8];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const ulonglong2 w = put[q * 4 + i];
+                                    two_parts(mul2(w.x, X[q * 8 + 2 * i]), a[0][2 * i], a[1][2 * i]);
+                                    two_parts(mul2(w.y, X[q * 8 + 2 * i + 1]), a[0][2 * i + 1], a[1][2 * i + 1]);
+                                }
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cW + e * 32 + half * 16 + q * 8, a[e]);
+                            }
+                            tmem_st_wait();
+                            arrive(bWP);
+                            if (!x.outputs) return;
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                uint32_t a[2][8];
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) two_parts(X[q * 8 + i], a[0][i], a[1][i]);
+#pragma unroll
+                                for (int e = 0; e < 2; ++e) tmem_st8u(lanes + cU + e * 32 + half * 16 + q * 8, a[e]);
+                            }
+                        };
+                        if (!__any_sync(0xffffffffu, first < 32)) {
+                            store();
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                float b0, b1;
+                                unpack2(X[i], b0, b1);
+                                X[i] = pack2(2 * i >= first ? 0.f : b0, 2 * i + 1 >= first ? 0.f : b1);
+                            }
+                            store();
+                        }
                     }
-                    if (more) give(i);
+                    if (x.outputs) {
+                        if (half == 0) {
+                            float* aside = reinterpret_cast<float*>(smem + kAsideOff) + (o & 1) * 256 + col;
+                            aside[0] = p.q_scale * down * (1.f / kTile);
+                            aside[128] = __int_as_float(bad ? kQ - (int)(mark & 127u) : kQ);
+                        }
+                        tmem_st_wait();
+                        arrive(bUP + (o & 1));
+                        ++o;
+                    }
+                    float r = down;
+                    if (more) {
+                        const float big = large[(n & 3) * 128].x;
+                        length = end * (look ? kLength * most_of(n) : length) + 8.f * big;
+                        r = rescale(n + 1);
+                    }
+                    const uint64_t r2 = pack2(r, r), keep2 = pack2(keep * r, keep * r);
+                    const bool same = __all_sync(0xffffffffu, r == 1.f);
+                    // S, times the next chunk's scale (behind the last chunk as it is)
+                    ok = warp_wait(bar + bProd, n & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        tmem_ld32_async(lanes + cP + half * 64 + i * 32, d);
+                        tmem_ld_wait();
+                        if (same) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) S[i * 16 + j] = fma2(keep2, S[i * 16 + j], pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                S[i * 16 + j] = fma2(r2, pack2(__uint_as_float(d[2 * j]), __uint_as_float(d[2 * j + 1])), mul2(keep2, S[i * 16 + j]));
+                        }
+                        if (more) give(i);
+                    }
+                }
+                if (!ok || t >= rows.y) break;
+                // A chunk whose numbers may be too far apart.
+                if (x.outputs && o > 0) ok = warp_wait(bar + bOutFree + ((o - 1) & 1), ((o - 1) >> 1) & 1);
+                if (!ok) break;
+                Alone c;
+                uint32_t* v = reinterpret_cast<uint32_t*>(smem + kYOff) + half * 16 * 128 + col;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i * 128] = f[i];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) c.S[i] = S[i];
+                state_most(n);
+                c.smem = smem;
+                c.stage = smem + (n & 1) * kStage;
+                c.bar = bar;
+                c.pair = bar + bPair + quad;
+                c.rest = reinterpret_cast<const float*>(p.work + ((size_t)(x.chunk + (t - rows.x) / kQ) * p.H + x.head) * kBlock + kGOff);
+                c.most = most + (n & 1) * 256;
+                c.next = &large[((n + 1) & 3) * 128].x;
+                c.up = up;
+                c.down = down;
+                c.length = length;
+                c.q_scale = p.q_scale;
+                c.lanes = lanes;
+                c.n = n;
+                c.m = m;
+                c.o = o;
+                c.col = col;
+                c.half = half;
+                c.valid = min(kQ, rows.y - t);
+                c.met = met;
+                c.zero = t == rows.x && zero;
+                c.outputs = x.outputs;
+                c.live = stored || t > rows.x;
+                c.more = t + kQ < rows.y;
+                c.ok = true;
+                const bool alone = token_by_token(c);
+                met = c.met;
+                ok = c.ok;
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) S[i] = c.S[i];
+                if (alone) {
+                    up = c.up;
+                    down = c.down;
+                    length = c.length;
+                    if (c.live) ++m;
+                    if (x.outputs) ++o;
+                    t += kQ;
+                    ++n;
+                    if (t >= rows.y) break;
+                    fetch(n);
+                    const float2 sizes = large[(n & 3) * 128];
+                    doubt = !(sizes.y * up >= kFloor) && (sizes.x > 0.f || length > 0.f);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) f[i] = v[i * 128];
+                    checked = true;
                 }
             }
             if (!ok) break;

@@ -5,17 +5,18 @@ whatever warp is late, and wherever, the others must not get two phases ahead of
 turn, the others go on as far as they can, and then the stopped one's next wait is looked at."""
 import pytest
 
-NEED = {"empty_v": 8, "s": 8, "xp": 8, "wp": 8, "up": 8, "join": 8, "out": 4, "scaled": 4}      # arrivals that end a phase; others: one
+NEED = {"empty_v": 8, "s": 8, "xp": 8, "wp": 8, "up": 8, "join": 8, "pair": 8, "out": 4, "scaled": 4}      # arrivals that end a phase; others: one
 
 
 def roles(units):
-    """[(name, [(wait or arrive, barrier, phase)])] of a CTA's units: (outputs, stored state, chunks)."""
-    chunks = [(outputs, stored or i > 0, i == 0, i == n - 1) for outputs, stored, n in units for i in range(n)]
+    """[(name, [(wait or arrive, barrier, phase)])] of a CTA's units: (outputs, stored state, chunks, those that are looked at, and then taken token by
+    token)."""
+    chunks = [(outputs, stored or i > 0, i == 0, i == n - 1, i in looked, i in alone) for outputs, stored, n, looked, alone in units for i in range(n)]
     two = lambda bar, n: (f"{bar}{n & 1}", n >> 1)  # noqa: E731
     copies, products, values, store = [], [], [], []
     y, state = [], []
-    o = om = m = u = 0
-    for n, (outputs, live, first, last) in enumerate(chunks):
+    o = om = m = u = met = 0
+    for n, (outputs, live, first, last, looked, alone) in enumerate(chunks):
         wait, arrive = lambda to: lambda bar, k: to.append(("wait", bar, k)), lambda to: lambda bar: to.append(("arrive", bar, None))
         # the copies
         if n >= 2:
@@ -54,16 +55,26 @@ def roles(units):
             if live:
                 a("s0"), a("s1")
         w(*two("full", n))
-        if not last:
+        if looked or alone:
+            if outputs and o:
+                w(*two("out_free", o - 1))
+            for _ in range(4 if alone else 1):
+                a("pair"), w("pair", met)
+                met += 1
+        if not last and not alone:
             w(*two("full_v", n + 1)), a(two("empty_v", n + 1)[0])
         if live:
             w("x", m)
         a("xp"), w("u", n), a("wp")
         if outputs:
             a(two("up", o)[0])
+        if not last and alone:
+            w(*two("full_v", n + 1))
         w("prod", n)
         if not last:
             a("s0"), a("s1")
+        if not last and alone:
+            w(*two("full_v", n + 1)), a(two("empty_v", n + 1)[0])
         # the outputs
         if outputs:
             w, a = wait(y), arrive(y)
@@ -71,9 +82,9 @@ def roles(units):
                 w(*two("full", n)), w("ask", om), a("scaled")
             w(*two("up", o)), w("y", o)
             if o:
-                w("out_free", o - 1)
+                w(*two("out_free", o - 1))
             a("out")
-            wait(store)("out", o), arrive(store)("out_free")
+            wait(store)("out", o), arrive(store)(two("out_free", o)[0])
             o += 1
             om += live
         m += live
@@ -109,7 +120,9 @@ class Play:
 
 
 # whole sequences from zeros and from stored states, of one chunk and more; the first pass over segments, without outputs
-UNITS = [[(True, False, 1)], [(True, True, 5)], [(True, False, 4), (True, True, 1), (True, False, 1), (True, True, 3)], [(False, False, 4), (False, True, 3)]]
+UNITS = [[(True, False, 1, (), ())], [(True, False, 2, (), (0,))], [(True, True, 5, (2, 3), (0, 1, 4))],
+         [(True, False, 4, (), (2,)), (True, True, 1, (), (0,)), (True, False, 1, (0,), ()), (True, True, 3, (1,), ())],
+         [(False, False, 4, (2,), (1, 3)), (False, True, 3, (0,), ())]]
 
 
 @pytest.mark.parametrize("units", UNITS)
