@@ -381,8 +381,8 @@ int sketchssm_delta_step(sketchssm_ctx* ctx, int groups, int width, float eps, f
                          const void* x, int64_t x_stride, const void* b, int64_t b_stride, const void* dt, int64_t dt_stride, const void* a,
                          const void* dt_bias, void* q, void* k, void* v, void* beta, void* decay, void* stream);
 
-/* Bytes of `work` that sketchssm_delta_scan needs for batches of at most this many sequences and tokens (may be 0).
- * Host-only.  The scratch is transient; calls that overlap on the GPU need separate ones. */
+/* Bytes of `work` that sketchssm_delta_scan needs for batches of at most this many sequences and tokens (may be 0), into bf16 and for any number of
+ * groups.  Host-only.  The scratch is transient; calls that overlap on the GPU need separate ones. */
 int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int tokens, size_t* bytes);
 
 /* Gated delta rule over packed prompts (GDN, KDA): per sequence and head, token by token, with k, q, beta and the decay D (a number, or a
@@ -400,8 +400,8 @@ int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int toke
  * parts of the GPU run; they do, in their last bits, on the number of sequences and heads (how the tokens are split).
  * A token that is not finite (a key or query whose squared length is not, counts as such): from it on its sequence and head's outputs and state
  * are not finite, all of them or those columns and rows that it reaches; no other sequence's, no other head's, no earlier token's.
- * The scratch is 4 K bytes a token and head (KDA), about 67 KB for 64 tokens of a head and up to 29 MB (GDN on the tensor cores), else none; a long
- * prompt can be taken in pieces, each going on from the state that the one before it leaves. */
+ * The scratch is 4 K bytes a token and head (KDA), about 67 KB for 64 tokens of a head and up to 29 MB (GDN on the tensor cores), else none: with fp32
+ * out a GDN call takes any work_bytes.  A long prompt can be taken in pieces, each going on from the state that the one before it leaves. */
 int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, float eps, float q_scale, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const void* b, int64_t b_stride, const void* dt,
                          int64_t dt_stride, const void* a, const void* dt_bias, void* out, int64_t out_stride, int out_dtype, void* work,

@@ -455,10 +455,10 @@ class SketchSSM:
                    q_scale: Optional[float] = None, work: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """sketchssm_delta_scan (GDN, KDA): the gated delta rule over packed prompts, q, k [T, G, K] (not normalised), v [T, H, V], b [T, H],
         dt [T, H] (GDN) or [T, H K] (KDA) in io, a [H] f32, dt_bias [H] or [H, K] f32, into out [T, H, V] (f32 or bf16) and the
-        bound state.  q_scale: None for 1 / sqrt(K).  work: new_delta_work (allocated here if None)."""
+        bound state.  q_scale: None for 1 / sqrt(K).  work: new_delta_work (allocated here if None and needed)."""
         if not prompts.on(self.device):
             raise ValueError("prompts lie on the layer's device")
-        if work is None:
+        if work is None and not (self.kind == "gdn" and out.dtype == torch.float32):      # (needs none)
             with on_stream(stream):
                 work = self.new_delta_work(prompts.sequences, prompts.tokens)
         rc = (_CALLS or _calls()).delta_scan(*self._delta_scan, prompts.address, prompts.tokens, q, k, v, b, dt, a, out, dt_bias, work, eps,

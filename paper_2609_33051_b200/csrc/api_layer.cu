@@ -264,7 +264,8 @@ int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, i
         !stride_ok(out_stride, hv, out_dtype == SKETCHSSM_BF16 ? 2 : 4) || b_stride < c.heads || !decay_ok(ctx, dt, dt_stride))
         return SKETCHSSM_INVALID_ARG;
     size_t need = 0;
-    rc = sketchssm_delta_work_bytes(ctx, p.pr.N, p.pr.T, &need);
+    // (GDN into fp32 goes over CUDA cores, which need none)
+    if (c.kind == SKETCHSSM_KDA || out_dtype == SKETCHSSM_BF16) rc = sketchssm_delta_work_bytes(ctx, p.pr.N, p.pr.T, &need);
     if (rc != SKETCHSSM_OK) return rc;
     if (work_bytes < need || (need > 0 && !good(work))) return SKETCHSSM_INVALID_ARG;
     if (p.pr.N == 0) return SKETCHSSM_OK;

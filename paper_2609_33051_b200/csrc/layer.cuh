@@ -126,7 +126,7 @@ int prompt_scan_tc_segments(Ctx* ctx, int groups, int sequences, int tokens);   
 int launch_delta_step(Ctx* ctx, const DeltaStepParams& p, bool bf16, cudaStream_t stream);
 int launch_delta_scan(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream);       // CUDA cores, every configuration
 int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t stream);    // tcgen05; UNSUPPORTED_SHAPE outside its domain
-size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens);
+size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens);                               // 0 outside its domain
 int launch_integer_norm(Ctx* ctx, const Norm8Params& p, bool bf16, bool x_bf16, cudaStream_t stream);
 int launch_integer_matmul(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);
 int launch_integer_matmul_pair(Ctx* ctx, const MatmulParams& p, cudaStream_t stream);           // many rows; UNSUPPORTED_SHAPE where smaller tiles do

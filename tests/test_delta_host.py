@@ -57,6 +57,18 @@ def test_scan_scratch_refusals(lib):
 
 
 @pytest.mark.parametrize("kind", [GDN, KDA])
+def test_scan_into_fp32_needs_scratch_for_kda_alone(lib, kind):
+    """GDN goes over CUDA cores then, whatever the number of tokens, and the tensor cores' scratch is not asked for: such a call gets as far as its device
+    (one that no machine has)."""
+    ctx, n = context(lib, kind=kind, dv=128, device=1000), ctypes.c_size_t(0)
+    assert lib.sketchssm_delta_work_bytes(ctx, 3, 1000, ctypes.byref(n)) == OK and n.value > 0
+    for none in (dict(work=None, wb=0), dict(work=Q), dict(wb=n.value - 1)):
+        got = scan(lib, ctx, pr=prompts(sequences=3, tokens=1000), od=0, **none)
+        assert (got == INVALID) == (kind == KDA), none
+    assert scan(lib, ctx, pr=prompts(sequences=0, tokens=1000), od=0, work=None, wb=0) == OK
+
+
+@pytest.mark.parametrize("kind", [GDN, KDA])
 def test_no_sequences_need_no_scratch(lib, kind):
     ctx, n = context(lib, kind=kind, dv=128), ctypes.c_size_t(7)
     assert lib.sketchssm_delta_work_bytes(ctx, 0, 100, ctypes.byref(n)) == OK and n.value == 0
