@@ -1699,13 +1699,13 @@ static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uin
 struct Split {
     int segments, turns;
 };
-static Split delta_split(long long sequences, long long heads, long long tokens) {
+static Split delta_split(long long sequences, long long heads, long long tokens, int sms) {
     const long long pairs = sequences * heads, chunks = (tokens / sequences + kQ - 1) / kQ;
     Split best = {1, 1};
     long long least = 3 * chunks;
     for (int turns = 1; turns <= 4; ++turns)
         for (int n = 3; n <= 16; ++n) {
-            if ((n - 1) * pairs > 148 || pairs + (2 * (n - 2) * pairs + turns - 1) / turns > 148) break;
+            if ((n - 1) * pairs > sms || pairs + (2 * (n - 2) * pairs + turns - 1) / turns > sms) break;
             const long long per = (chunks + turns + n - 2) / (turns + n - 1), time = 3 * (turns + 1) * per + 30 + 8 * (n - 2);
             if (time < least) {
                 least = time;
@@ -1720,11 +1720,14 @@ static Split delta_split(long long sequences, long long heads, long long tokens)
 // there too, 256 of 4, 4 heads, 45 and 81, but one long one among them would not, and the lengths are not known here.)
 constexpr long long kFewTokens = 32;
 
+// (The scratch's size is asked for without a device: it holds for so many SMs, and no more of them are counted on.)
+constexpr int kMostSms = 148;
+
 size_t delta_tc_work_bytes(const sketchssm_config& c, long long sequences, long long tokens) {
     if (c.kind != SKETCHSSM_GDN || c.io_dtype != SKETCHSSM_BF16 || c.dk != 128 || c.dv != 128 || sequences == 0 || tokens <= kFewTokens) return 0;
     // (The groups are not known here: every head may be one.  Fewer sequences than asked for may be split into more segments: of all of them
-    // together 3 n - 5 states, less than three times 148.  Sequences below 15 chunks are not split.)
-    const size_t states = c.heads <= 74 && 3 * tokens > 64 * 38 ? 444 : 0;
+    // together 3 n - 5 states, less than three times the SMs.  Sequences below 15 chunks are not split.)
+    const size_t states = c.heads <= kMostSms / 2 && 3 * tokens > 64 * 38 ? 3 * kMostSms : 0;
     return (size_t)(tokens / kQ + sequences) * c.heads * (kBlock + kRows) + ((size_t)sequences * 4 + 15) / 16 * 16 + states * 128 * 128 * 4 + 16;
 }
 
@@ -1736,7 +1739,7 @@ int launch_delta_scan_tc(Ctx* ctx, const DeltaParams& p, bool bf16, cudaStream_t
     const long long units = (long long)p.pr.N * p.H, chunks = (long long)p.pr.T / kQ + p.pr.N;
     const long long preps = chunks * p.G * ((p.H / p.G + 1) / 2);
     if (units > (1 << 30) || preps >= 0x7fffffffll) return SKETCHSSM_UNSUPPORTED_SHAPE;
-    const Split split = delta_split(p.pr.N, p.H, p.pr.T);
+    const Split split = delta_split(p.pr.N, p.H, p.pr.T, sm_count(ctx) < kMostSms ? sm_count(ctx) : kMostSms);
     g.segments = split.segments;
     g.turns = split.turns;
     g.preps = (int)preps;
