@@ -232,7 +232,7 @@ int norm_types(Ctx* ctx, const Norm8Params& p, cudaStream_t stream) {
     while (nv < 4 && (vecs + nv - 1) / nv > 512) nv *= 2;
     const int tx = ((vecs + nv - 1) / nv + 31) / 32 * 32;
     const int rows_per_cta = tx == 32 ? 4 : 1;
-    const dim3 block((unsigned)tx, (unsigned)rows_per_cta), grid((unsigned)((p.rows + rows_per_cta - 1) / rows_per_cta));
+    const dim3 block((unsigned)tx, (unsigned)rows_per_cta), grid((unsigned)(((long long)p.rows + rows_per_cta - 1) / rows_per_cta));
     if (nv == 4) return norm_mode<T, X, 4>(ctx, p, grid, block, stream);
     if (nv == 2) return norm_mode<T, X, 2>(ctx, p, grid, block, stream);
     return norm_mode<T, X, 1>(ctx, p, grid, block, stream);
