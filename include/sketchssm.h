@@ -399,7 +399,8 @@ int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int toke
  * below 2^-12) 32 columns of these tokens are taken one by one in fp32, which takes 50 to 100 us for them.  Results do not depend on the order in which
  * parts of the GPU run; they do, in their last bits, on the number of sequences and heads (how the tokens are split).
  * A token that is not finite (a key or query whose squared length is not, counts as such): from it on its sequence and head's outputs and state
- * are not finite, all of them or those columns and rows that it reaches; no other sequence's, no other head's, no earlier token's.
+ * are not finite, all of them or those columns and rows that it reaches (a query reaches its own token alone); no other sequence's, no other head's, no
+ * earlier token's.  Gates of infinite b and dt are finite: step sizes and decays of zero and one.
  * The scratch is 4 K bytes a token and head (KDA), about 67 KB for 64 tokens of a head and up to 29 MB (GDN on the tensor cores), else none: with fp32
  * out a GDN call takes any work_bytes.  A long prompt can be taken in pieces, each going on from the state that the one before it leaves. */
 int sketchssm_delta_scan(sketchssm_ctx* ctx, const sketchssm_prompts* prompts, int groups, float eps, float q_scale, const void* q, int64_t q_stride,

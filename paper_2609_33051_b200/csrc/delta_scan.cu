@@ -321,7 +321,7 @@ __global__ void __maxnreg__(255) delta_scan_kernel(const DeltaParams p) {
         for (int i4 = 0; i4 < n4 / 4; ++i4) {
             const int t4 = i4 * 4;
             const float* w = near + i4 * kNear;
-            // four rows 4 r + 32 j of a token's key, of its query, and of what its u is put with
+            // four rows 4 r + 4 LK j .. of a token's key, of its query, and of what its u is put with
             auto key = [&](int u, int j, uint64_t& x, uint64_t& y) {
                 if constexpr (KDA) four(kp + (t4 + u) * K + j * 4 * LK + 4 * r, x, y);
                 else four(sk + (t4 + u) * K + j * 4 * LK + 4 * r, x, y);

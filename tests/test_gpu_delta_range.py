@@ -166,3 +166,16 @@ def test_large_values_twice_are_the_same_to_the_bit():
         run_scan(m, pr, x, out)
         outs.append((out.view(torch.int16), m.state.clone().view(torch.int32)))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("kind,od", [("gdn", "bf16"), ("gdn", "f32"), ("kda", "bf16")])
+def test_infinite_gates_are_what_the_formulas_give(kind, od):
+    """Step sizes of nothing and of one, decays of nothing and of one, from arguments that are infinite: nothing that is not finite comes of them."""
+    x = scan_inputs(kind, [200, 20], 2, 1, 128, 128, "bf16", 8, seed=21)
+    inf = float("inf")
+    for t, h, value in ((3, 0, inf), (70, 1, -inf), (71, 1, inf), (130, 0, -inf), (210, 1, -inf)):
+        x["b"][t, h] = value
+    for t, h, value in ((5, 0, -inf), (66, 1, inf), (100, 0, inf), (140, 1, -inf), (205, 0, inf)):
+        x["dt"][t, h] = value
+    starts, pr = batch_of([200, 20], None, [1, 5])
+    check_scan(layer(8, 2, kind=kind), x, starts, pr, None, [1, 5], od)
