@@ -1093,34 +1093,26 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                         a[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + lane * 8);
                         c[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + 256 + lane * 8);
                     }
-                    auto sizes = [&](int j, auto whole) {
-                        uint32_t first = 0u;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t y = (j ? a[i].y : a[i].x) & 0x7fff7fffu, z = (j ? c[i].y : c[i].x) & 0x7fff7fffu, both = __vmaxu2(y, z);
-                            if constexpr (decltype(whole)::value) {
-                                if (i % 2) {
-                                    top[j] = __vimax3_u16x2(top[j], first, both);
-                                    least[j] = __vimin3_u16x2(least[j], first, both);
-                                }
-                                first = both;
-                            } else {
-                                top[j] = __vmaxu2(top[j], both);
-                                if (2 * (r + i) < valid) least[j] = __vminu2(least[j], 2 * (r + i) + 1 < valid ? both : y);
-                            }
-                        }
-                    };
-                    if (2 * r + 8 <= valid) {
-                        sizes(0, std::true_type{});
-                        sizes(1, std::true_type{});
-                    } else {                             // rows of the next sequence are no part of this one
+                    if (2 * r + 8 > valid) {             // rows of the next sequence are no part of this one
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             if (2 * (r + i) >= valid) a[i] = make_uint2(0u, 0u);
                             if (2 * (r + i) + 1 >= valid) c[i] = make_uint2(0u, 0u);
                         }
-                        sizes(0, std::false_type{});
-                        sizes(1, std::false_type{});
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t larger[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) larger[i] = __vmaxu2((j ? a[i].y : a[i].x) & 0x7fff7fffu, (j ? c[i].y : c[i].x) & 0x7fff7fffu);
+                        top[j] = __vimax3_u16x2(__vimax3_u16x2(top[j], larger[0], larger[1]), larger[2], larger[3]);
+                        if (2 * r + 8 <= valid) {
+                            least[j] = __vimin3_u16x2(__vimin3_u16x2(least[j], larger[0], larger[1]), larger[2], larger[3]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (2 * (r + i) < valid) least[j] = __vminu2(least[j], larger[i]);
+                        }
                     }
                     __syncwarp();
 #pragma unroll
