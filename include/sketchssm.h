@@ -395,7 +395,7 @@ int sketchssm_delta_work_bytes(const sketchssm_ctx* ctx, int sequences, int toke
  *   eps > 0;  out : [T][H][V] out_dtype, strided: config.out_dtype is not asked here, the call says it.
  * GDN with bf16 io and out, dk = dv = 128 and more than 32 tokens goes through the tensor cores in chunks of 64, everything else over CUDA cores.  Either way
  * states are fp32, sums of fp32 accuracy (operands of 22 bits), and an output is rounded once.  The operands of 64 tokens and a column share a
- * scale; where their numbers are too far apart for it (a value or a stored state some 2^14 times as large as others that count beside it, step sizes
+ * scale; where their numbers are too far apart for it (a value or a stored state some 2^16 times as large as others that count beside it, step sizes
  * below 2^-12) 32 columns of these tokens are taken one by one in fp32, which takes 50 to 100 us for them.  Results do not depend on the order in which
  * parts of the GPU run; they do, in their last bits, on the number of sequences and heads (how the tokens are split).
  * A token that is not finite (a key or query whose squared length is not, counts as such): from it on its sequence and head's outputs and state

@@ -53,13 +53,14 @@ constexpr uint32_t kCopied = kGOff + kGates * 4u, kBlock = kGOff + kFloats * 4u;
 // Numbers of very different size.  A column's scale is its chunk's largest; an operand is 2^-25 off at that scale where it is small, so a token keeps the
 // accuracy of its own column's numbers only while those, scaled, stay above some floor: the larger one of its value and the one before it (whose
 // weight the state has), or what earlier ones and the state were, less what has decayed since; and no value counts that beta keeps out.  Where they
-// do not (a value or a state 2^14 times as large as the others that a chunk meets, beta below 2^-12 throughout) the columns of a pair of warps go through
+// do not (a value or a state 2^16 times as large as the others that a chunk meets, beta below 2^-12 throughout) the columns of a pair of warps go through
 // the chunk token by token, in fp32, and the products meet zeros: 50 to 100 us instead of 3.  It is looked at where a pair of tokens 2 i and 2 i + 1 is
-// below the floor (of normal numbers one in a million columns and chunks; the look takes 12 us, most of it for instructions that nobody has run
-// lately), or the state that a unit begins with, or a beta below kLeastBeta.  (Small tokens that stand beside a large one of their own pair, each of
-// them, are not seen: a small one behind another then has some bits less.)
-// (The floor: 2^-25 is 2^-20 of it; a token meets such errors in what it reads of the state, in X, U and W.)
-constexpr float kFloor = 1.f / 32.f, kLeastBeta = 1.f / 4096.f;
+// below the floor (of normal numbers one in ten million columns and chunks), or the state that a unit begins with, or a beta below kLeastBeta; a look
+// takes 2 us, and 12 where nobody has run its instructions lately.  (Small tokens that stand beside a large one of their own pair, each of them, are
+// not seen: a small one behind another then has some bits less.)
+// (The floor: 2^-25 is 2^-18 of it, and what shows of it in outputs and states, measured where there was no floor, a twentieth of that: the tests' bound
+// is 2^-18.7.  With a floor of 1 / 32 there were looks in one of four calls of 16384 tokens.)
+constexpr float kFloor = 1.f / 128.f, kLeastBeta = 1.f / 4096.f;
 
 struct DeltaArgs {
     CUtensorMap tq, tk, tv;
@@ -1110,8 +1111,8 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                             least[j] = __vimin3_u16x2(__vimin3_u16x2(least[j], larger[0], larger[1]), larger[2], larger[3]);
                         } else {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (2 * (r + i) < valid) least[j] = __vminu2(least[j], larger[i]);
+                            for (int i = 0; i < 4; ++i)      // (the last one of an odd number is no pair, unless it is all there is)
+                                if (2 * (r + i) + 1 < valid || (r + i == 0 && valid == 1)) least[j] = __vminu2(least[j], larger[i]);
                         }
                     }
                     __syncwarp();
