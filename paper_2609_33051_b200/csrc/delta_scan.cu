@@ -16,10 +16,12 @@
 // a stage of them while the one before is worked on; what four tokens have to do with one another is worked out by a warp, its lanes over the
 // channels.
 //
-// What bounds it: multiplications.  4096 KDA tokens in 8 prompts of 32 heads, 64 columns a CTA, take 560 us (token by token 1400); three products with
+// What bounds it: multiplications.  4096 KDA tokens in 8 prompts of 512, 32 heads, 64 columns a CTA, take 566 us (in ragged ones 574 to 970: 0.55 us for
+// each token of the longest; token by token 1400); three products with
 // 16384 elements of a state a token are 6.4 G, 180 us at the card's rate.  Per four tokens a thread has 416 instructions for two such
 // products each, two cycles long, and 175 others in the same pipe; the longest prompt's CTAs end last.  1500 fp32 tokens in 7
-// prompts of 24 heads of 80 columns, 16 columns a CTA: 203 us (token by token 306), bound by the longest prompt's chain of sums over lanes.
+// prompts of 24 heads of 80 columns, 16 columns a CTA: 181 to 222 us by their lengths (token by token 306), bound by the longest prompt's chain of
+// sums over lanes.
 #include "pairs.cuh"
 
 namespace sketchssm {
@@ -224,7 +226,7 @@ __device__ __forceinline__ int by_length(const PromptsDev& pr, int place) {
 }
 
 template <typename T, int K, bool KDA, int LK>
-// (All the registers that it asks for, 170 to 190: with 168, three CTAs an SM, KDA's 560 us become 718.)
+// (All the registers that it asks for, 170 to 190: with 168, three CTAs an SM, KDA's 566 us become 718.)
 __global__ void __maxnreg__(255) delta_scan_kernel(const DeltaParams p) {
     constexpr int RUNS = K / (4 * LK), RP = 2 * RUNS, STEPS = LK == 8 ? 3 : 4;     // runs of four rows and pairs of rows of a thread; halvings of its lanes
     constexpr int TOK = kTok<KDA>, GR = TOK / 4;

@@ -23,10 +23,10 @@
 // that of one.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
-// What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.1 us of which the products are less than a
-// third; a sequence's chunks follow one another.  16384 tokens of 32 heads: one prompt 579 us (125 the first kernel; 280, 21 and 156 the passes
-// over five segments, see decode_unit; 921 whole), 48 ragged prompts 446.  The first kernel: waiting, for loads and for its own warps, and
-// memory, of which it reads and writes 0.5 GB (4 TB/s).  100 tokens: 24 us, half of it the first kernel.
+// What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.0 to 3.3 us of which the products are less
+// than a third; a sequence's chunks follow one another.  16384 tokens of 32 heads (SM clock 1965 MHz): one prompt 600 us (125 the first kernel; 286, 21
+// and 167 the passes over five segments, see decode_unit; 881 whole), 48 ragged prompts 450 to 473 by their lengths.  The first kernel: waiting, for loads
+// and for its own warps, and memory, of which it reads and writes 0.45 GB (3.6 TB/s).  100 tokens: 24 us, half of it the first kernel.
 #include "tma.cuh"
 
 #include <cuda_fp16.h>
@@ -1687,8 +1687,8 @@ static bool make_rows_map(CUtensorMap* map, const void* base, uint64_t cols, uin
 // Segments of a sequence (1: none) and units of the first pass a CTA, for the least time, estimated for sequences of the average length: turns + 1
 // times a segment's chunks at 3 us each, and what the small kernel and the units' starts take, some 30 us and 8 a segment.  Each pass has an
 // SM for each of its CTAs: in the first one of every first segment and one for `turns` of the 2 (n - 2) others, in the second n - 1.
-// One prompt, a key head for each head, whole and split: 16384 tokens of 4 heads 791 and 235 us, of 32 952 and 646, of 64 1157 and 1050; 2048 of 16
-// heads 120 and 99.  16384 of 32 heads, a key head for two: 921, 692 with n = 3 and one turn, 580 with n = 5 and two.
+// One prompt, a key head for each head, whole and split: 16384 tokens of 4 heads 773 and 237 us, of 32 948 and 673, of 64 1169 and 1085; 2048 of 16
+// heads 120 and 102.  16384 of 32 heads, a key head for two: 881 and 606 (five segments, two turns; three and one took a sixth longer).
 struct Split {
     int segments, turns;
 };
@@ -1708,9 +1708,9 @@ static Split delta_split(long long sequences, long long heads, long long tokens,
     return best;
 }
 
-// Tokens of a batch up to which the CUDA cores are faster whatever the sequences are: 1 token of 4 heads in 6.7 us, 18.5 here; 16 sequences of 2
-// tokens, 32 heads, 27.6 and 47.3; one of 32 tokens, 32 heads, 13.4 and 18.9; but one of 64 22.5 and 18.4.  (More sequences of a few tokens would be faster
-// there too, 256 of 4, 4 heads, 45 and 81, but one long one among them would not, and the lengths are not known here.)
+// Tokens of a batch up to which the CUDA cores are faster whatever the sequences are: 1 token of 4 heads in 5.6 us, 19.5 here; 16 sequences of 2
+// tokens, 32 heads, 28.1 and 51.2; one of 32 tokens, 32 heads, 11.8 and 20.1; one of 64 19.9 and 20.1.  (More sequences of a few tokens would be faster
+// there too, 256 of 4, 4 heads, 45 and 86, but one long one among them would not, and the lengths are not known here.)
 constexpr long long kFewTokens = 32;
 
 // (The scratch's size is asked for without a device: it holds for so many SMs, and no more of them are counted on.)

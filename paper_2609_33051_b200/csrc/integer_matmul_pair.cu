@@ -8,10 +8,10 @@
 // BN / 16 warps take a tile's sums out (32 lanes, 64 columns each), times both scales, and store them through shared memory (TMA), or
 // directly where a row or the row stride is no multiple of 16 bytes.
 //
-// What bounds it: the operands' way from L2.  16384 x 12352 x 2048 to bf16 takes 293 us (L2 flushed before each call; 298 one after another):
-// 2.83 Pop/s, and 3136 tiles of 1 MB of operands are 11 TB/s, about what L2 gives.  The output's 405 MB are 63 us of memory.  With four
-// stages 320 us; five are what 227 KB hold beside the stores' staging.  Bands of 8 or 16 tiles of tokens, walked down a band first so that fewer
-// operand tiles are in use at a time: 301 and 294, no gain.
+// What bounds it: the operands' way from L2, and the power cap.  16384 x 12352 x 2048 to bf16 takes 331 us by itself (L2 flushed, the card idle before it) and
+// 350 one after another for a second, at 1430 to 1520 MHz of 1965: 2.50 and 2.37 Pop/s; 3136 tiles of 1 MB of operands are 9.0 to 9.5 TB/s.  (293 were
+// seen on a cooler card.)  The output's 405 MB are 63 us of memory.  With four stages 330 and 362; five are what 227 KB hold beside the stores'
+// staging.  Bands of 8 or 16 tiles of tokens, walked down a band first so that fewer operand tiles are in use at a time, gain nothing.
 #include "tma.cuh"
 
 namespace sketchssm {
