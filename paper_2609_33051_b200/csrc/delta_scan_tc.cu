@@ -1529,7 +1529,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 }
                 if (!ok || t >= rows.y) break;
                 // A chunk whose numbers may be too far apart.
-                if (x.outputs && o > 0) ok = warp_wait(bar + bOutFree + ((o - 1) & 1), ((o - 1) >> 1) & 1);
+                if (o > 0) ok = warp_wait(bar + bOutFree + ((o - 1) & 1), ((o - 1) >> 1) & 1);
                 if (!ok) break;
                 Alone c;
                 uint32_t* v = reinterpret_cast<uint32_t*>(smem + kYOff) + half * 16 * 128 + col;

@@ -56,7 +56,7 @@ def roles(units):
                 a("s0"), a("s1")
         w(*two("full", n))
         if looked or alone:
-            if outputs and o:
+            if o:
                 w(*two("out_free", o - 1))
             for _ in range(4 if alone else 1):
                 a("pair"), w("pair", met)
@@ -119,7 +119,8 @@ class Play:
             pass
 
 
-# whole sequences from zeros and from stored states, of one chunk and more; the first pass over segments, without outputs
+# whole sequences from zeros and from stored states, of one chunk and more; the first pass over segments, without outputs (a CTA's units have them all, or
+# none has)
 UNITS = [[(True, False, 1, (), ())], [(True, False, 2, (), (0,))], [(True, True, 5, (2, 3), (0, 1, 4))],
          [(True, False, 4, (), (2,)), (True, True, 1, (), (0,)), (True, False, 1, (0,), ()), (True, True, 3, (1,), ())],
          [(False, False, 4, (2,), (1, 3)), (False, True, 3, (0,), ())]]
