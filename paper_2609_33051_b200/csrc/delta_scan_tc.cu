@@ -16,8 +16,8 @@
 // bits each (the product of the second parts is left out), summed in fp32.  fp16 has the bits but not the range, so everything is scaled by
 // powers of two, which round nothing: keys and queries by one each, to lengths between a half and one (then one part holds all of their bits
 // but those below 2^-24 of the length), and a lane's state, X, U and W by one for the lane and chunk, from the largest value v in it and the length
-// of the state before it.  A token leaves the state's length |S|^2 at most d^2 |S|^2 + v^2 (a convex mean along its key), a chunk leaves it at
-// most 2^c_end |S| + 8 v; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are at most
+// of the state before it.  A token leaves the state's squared length at most at d^2 |S|^2 + v^2 (a convex mean along its key), a chunk at 2^(2 c_end) |S|^2
+// + 64 v^2, which bounds it from where it was measured on; so |U| is at most 9 v + |S|, |W| twice that, and is brought below 2^15.  T and P are at most
 // one as they are, T because the rows' step sizes are left to U (a part ends at 2^-24, and rows of small ones would lose their bits: with
 // b = -7 everywhere states were 4e-5 off), and are made kTile times as large, so that what has decayed to 2^-25 of a large value ends there, and not
 // that of one.  In bf16 the same accuracy took three parts, half as many products again and more than twice the time to split.
@@ -729,6 +729,11 @@ __device__ __forceinline__ void give_state(const uint64_t (&S)[32], int i, uint3
     tmem_st_wait();
     arrive_warp(bar, lane);
 }
+// Bounds sqrt(a^2 + b^2), a and b not negative.
+__device__ __forceinline__ float longer(float a, float b) {
+    const float m = fmaxf(a, b), n = fminf(a, b);
+    return fmaf(0.5f * n, __fdividef(n, fmaxf(m, 1e-30f)), m);
+}
 constexpr float kLength = 11.4f;                        // bounds the length of 128 elements of at most one
 
 // A chunk for the 32 columns of two warps, half of the channels each: whether its numbers are too far apart for one scale, and then the chunk, token by
@@ -770,6 +775,7 @@ __device__ __noinline__ bool token_by_token(Alone& g) {
     {
         float a = 0.f, last = fmaxf(g.most[0], g.most[128]);
         g.met = met;
+        g.length = fminf(g.length, kLength * last);
         if (__all_sync(0xffffffffu, last * beta[kKeep - kBeta] * up >= kFloor)) return false;      // (the state alone is large enough, up to the last token)
         bool nothing = g.zero, over = false, alone = false;      // neither a state nor a value so far; nothing behind it is finite
 #pragma unroll 1
@@ -1374,11 +1380,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                             X[i] = pack2(a, c);
                         }
                     }
-                    // What bounds the next chunk's state: this one's, from the state itself every eighth chunk (the halves meet behind the next
-                    // product), less what decays of it, and what the tokens add to it.
-                    const bool look = (n & 7) == 7;
                     if (more) {
-                        if (look) state_most(n);
                         fetch(n + 1);
                         if (!ok) break;
                     }
@@ -1503,7 +1505,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                     float r = down;
                     if (more) {
                         const float big = large[(n & 3) * 128].x;
-                        length = end * (look ? kLength * most_of(n) : length) + 8.f * big;
+                        length = longer(end * length, 8.f * big);
                         r = rescale(n + 1);
                     }
                     const uint64_t r2 = pack2(r, r), keep2 = pack2(keep * r, keep * r);
@@ -1568,10 +1570,10 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 if (!ok) break;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) S[i] = c.S[i];
+                length = c.length;                       // (measured now)
                 if (alone) {
                     up = c.up;
                     down = c.down;
-                    length = c.length;
                     if (c.live) ++m;
                     if (x.outputs) ++o;
                     t += kQ;

@@ -179,3 +179,19 @@ def test_infinite_gates_are_what_the_formulas_give(kind, od):
         x["dt"][t, h] = value
     starts, pr = batch_of([200, 20], None, [1, 5])
     check_scan(layer(8, 2, kind=kind), x, starts, pr, None, [1, 5], od)
+
+
+def test_a_long_sequence_without_decays():
+    """Nothing decays, and the bound behind a column's scale grows with every chunk while the state does not: 94 chunks of one sequence (among others, so
+    that it is not split) keep the accuracy of test_scan_keeps_fp32s_accuracy."""
+    lengths = [6000] + [10] * 18
+    x = scan_inputs("gdn", lengths, 4, 2, 128, 128, "bf16", 19, seed=22)
+    x["a"] = torch.tensor([0.0, -1e-5, -1e-3, 0.0])
+    x["k"][:, 1, 64:] = 0                                # half of the rows of the states of two heads stay zeros
+    starts, pr = batch_of(lengths)
+    m = layer(19, 4)
+    want, _, new, _ = dref.scan(starts, None, None, *(x[n] for n in NAMES), x["bias"], x["state"], 19)
+    out = torch.empty(sum(lengths), 4, 128, dtype=torch.bfloat16, device=DEV)
+    run_scan(m, pr, x, out)
+    assert (m.state.cpu().double() - new).norm() <= 1e-6 * new.norm()
+    assert (out.cpu().double() - want).norm() <= 2.0e-3 * want.norm()
