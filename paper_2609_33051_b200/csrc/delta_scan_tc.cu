@@ -54,10 +54,9 @@ constexpr uint32_t kCopied = kGOff + kGates * 4u, kBlock = kGOff + kFloats * 4u;
 // accuracy of its own column's numbers only while those, scaled, stay above some floor: the larger one of its value and the one before it (whose
 // weight the state has), or what earlier ones and the state were, less what has decayed since; and no value counts that beta keeps out.  Where they
 // do not (a value or a state 2^16 times as large as the others that a chunk meets, beta below 2^-12 throughout) the columns of a pair of warps go through
-// the chunk token by token, in fp32, and the products meet zeros: 50 to 100 us instead of 3.  It is looked at where a pair of tokens 2 i and 2 i + 1 is
-// below the floor (of normal numbers one in ten million columns and chunks), or the state that a unit begins with, or a beta below kLeastBeta; a look
-// takes 2 us, and 12 where nobody has run its instructions lately.  (Small tokens that stand beside a large one of their own pair, each of them, are
-// not seen: a small one behind another then has some bits less.)
+// the chunk token by token, in fp32, and the products meet zeros: 50 to 100 us instead of 3.  It is looked at where two neighbouring tokens are
+// below the floor (of normal numbers one in five million columns and chunks), or the state that a unit begins with, or a beta below kLeastBeta; a look
+// takes 2 us, and 12 where nobody has run its instructions lately.
 // (The floor: 2^-25 is 2^-18 of it, and what shows of it in outputs and states, measured where there was no floor, a twentieth of that: the tests' bound
 // is 2^-18.7.  With a floor of 1 / 32 there were looks in one of four calls of 16384 tokens.)
 constexpr float kFloor = 1.f / 128.f, kLeastBeta = 1.f / 4096.f;
@@ -929,7 +928,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
     int n = 0, m = 0;                                   // chunks so far, over all units of the CTA; those with a state before them
 
     if (warp == 0) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (lane == 0) {
             Unit x;
             for (int it = 0; ok && decode_unit(g, it, x); ++it) {
@@ -957,7 +956,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         __syncwarp();
     } else if (warp == 1) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         constexpr uint32_t kN64 = kTypes | ((64u >> 3) << 17), kProdDesc = kTypes | (1u << 16) | ((128u >> 3) << 17);
         Unit x;
         int o = 0, om = 0;                              // chunks with outputs; those of them with a state before them
@@ -1058,9 +1057,10 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 13);
         __syncwarp();
     } else if (warp == 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // V, copied a chunk ahead: four columns a lane; two rows at a time become one of pairs, in their place
         Unit next, x;
+        uint32_t last[2] = {0u, 0u};                    // the sizes of the token before
         int next_it = 0, next_n = 0, next_t = 0;
         bool there = decode_unit(g, 0, next);
         if (there) next_t = next.t0;
@@ -1089,45 +1089,63 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
                 ok = ok && warp_wait(bar + bRaw + b, (n / 2) & 1);
                 if (!ok) break;
                 unsigned char* v = smem + kVOff + b * 2 * kPart;
-                // The largest size, and the least of the larger ones of two neighbouring tokens, two columns at a time.  (As whole numbers: sizes in bf16
-                // are in their order, with what is not finite above all.)
+                // The largest size, and the least of all tokens' larger one of their size and that of the token before, two columns at a time.  (As whole
+                // numbers: sizes in bf16 are in their order, with what is not finite above all.  max(y, min(x, z)) is the lesser one of y's two pairs.)
                 uint32_t top[2] = {0u, 0u}, least[2] = {0x7f7f7f7fu, 0x7f7f7f7fu};
-#pragma unroll 1
-                for (int r = 0; r < 32; r += 4) {
-                    uint2 a[4], c[4];
+                if (t == x.t0) last[0] = last[1] = 0x7f7f7f7fu;          // (a unit's first token: see where it begins)
+                auto load = [&](uint2 (&a)[2], uint2 (&c)[2], int r) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
                         a[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + lane * 8);
                         c[i] = *reinterpret_cast<const uint2*>(v + (r + i) * 512 + 256 + lane * 8);
                     }
-                    if (2 * r + 8 > valid) {             // rows of the next sequence are no part of this one
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (2 * (r + i) >= valid) a[i] = make_uint2(0u, 0u);
-                            if (2 * (r + i) + 1 >= valid) c[i] = make_uint2(0u, 0u);
-                        }
-                    }
+                };
+                auto store = [&](const uint2& a, const uint2& c, int r) {
+                    *reinterpret_cast<uint4*>(v + r * 512 + lane * 16) =
+                        make_uint4(__byte_perm(a.x, c.x, 0x5410), __byte_perm(a.x, c.x, 0x7632), __byte_perm(a.y, c.y, 0x5410), __byte_perm(a.y, c.y, 0x7632));
+                };
+                auto take = [&](const uint2 (&a)[2], const uint2 (&c)[2], int r) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        uint32_t larger[4];
+                        const uint32_t y0 = (j ? a[0].y : a[0].x) & 0x7fff7fffu, z0 = (j ? c[0].y : c[0].x) & 0x7fff7fffu;
+                        const uint32_t y1 = (j ? a[1].y : a[1].x) & 0x7fff7fffu, z1 = (j ? c[1].y : c[1].x) & 0x7fff7fffu;
+                        top[j] = __vimax3_u16x2(__vimax3_u16x2(top[j], y0, z0), y1, z1);
+                        least[j] = __vimin3_u16x2(least[j], __vmaxu2(y0, __vminu2(last[j], z0)), __vmaxu2(y1, __vminu2(z0, z1)));
+                        last[j] = z1;
+                    }
+                    __syncwarp();                        // (rows are read by other lanes than write them)
+                    store(a[0], c[0], r);
+                    store(a[1], c[1], r + 1);
+                };
+                const int whole = valid / 8 * 4;         // pairs of rows that are all there, four at a time: two are loaded while two are worked on
+                {
+                    uint2 a[2], c[2], d[2], e[2];
+                    if (whole > 0) load(a, c, 0);
+#pragma unroll 1
+                    for (int r = 0; r < whole; r += 4) {
+                        load(d, e, r + 2);
+                        take(a, c, r);
+                        if (r + 4 < whole) load(a, c, r + 4);
+                        take(d, e, r + 2);
+                    }
+                }
+#pragma unroll 1
+                for (int r = whole; r < 32; ++r) {       // rows of the next sequence are no part of this one
+                    uint2 a = make_uint2(0u, 0u), c = a;
+                    if (2 * r < valid) {
+                        a = *reinterpret_cast<const uint2*>(v + r * 512 + lane * 8);
+                        if (2 * r + 1 < valid) c = *reinterpret_cast<const uint2*>(v + r * 512 + 256 + lane * 8);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) larger[i] = __vmaxu2((j ? a[i].y : a[i].x) & 0x7fff7fffu, (j ? c[i].y : c[i].x) & 0x7fff7fffu);
-                        top[j] = __vimax3_u16x2(__vimax3_u16x2(top[j], larger[0], larger[1]), larger[2], larger[3]);
-                        if (2 * r + 8 <= valid) {
-                            least[j] = __vimin3_u16x2(__vimin3_u16x2(least[j], larger[0], larger[1]), larger[2], larger[3]);
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)      // (the last one of an odd number is no pair, unless it is all there is)
-                                if (2 * (r + i) + 1 < valid || (r + i == 0 && valid == 1)) least[j] = __vminu2(least[j], larger[i]);
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t y = (j ? a.y : a.x) & 0x7fff7fffu, z = 2 * r + 1 < valid ? (j ? c.y : c.x) & 0x7fff7fffu : 0x7f7f7f7fu;
+                            top[j] = __vmaxu2(top[j], y);
+                            if (2 * r + 1 < valid) top[j] = __vmaxu2(top[j], z);
+                            least[j] = __vminu2(least[j], __vmaxu2(y, __vminu2(last[j], z)));
+                            last[j] = z;
                         }
+                        __syncwarp();
                     }
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint4 w = make_uint4(__byte_perm(a[i].x, c[i].x, 0x5410), __byte_perm(a[i].x, c[i].x, 0x7632), __byte_perm(a[i].y, c[i].y, 0x5410),
-                                                   __byte_perm(a[i].y, c[i].y, 0x7632));
-                        *reinterpret_cast<uint4*>(v + (r + i) * 512 + lane * 16) = w;
-                    }
+                    store(a, c, r);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -1157,7 +1175,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         for (int i = next_n < 2 ? 0 : next_n - 2; i < next_n; ++i) mbar_wait_bounded(bar + (ok ? bEmptyV : bRaw) + (i & 1), (i / 2) & 1, ok ? 1u << 22 : 1u << 16);
         __syncwarp();
     } else if (warp == 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         // Y: four columns a lane, two rows at a time
         Unit x;
         for (int it = 0; ok && decode_unit(g, it, x); ++it) {
@@ -1184,7 +1202,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 15);
         __syncwarp();
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // Y of a value column: Q S^T times its tokens' factors, and what U P has added to it
         const int col = (warp & 3) * 32 + lane;
         const uint32_t at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + cY;
@@ -1266,7 +1284,7 @@ __global__ void __launch_bounds__(kThreads, 1) delta_scan_tc_kernel(const __grid
         }
         if (!ok && lane == 0) record_fault(p.status, kFaultScanWait, 17);
     } else {
-        // (512 threads start with 128 registers: 128 x 48 + 256 x 192 + 128 x 80 are all 65536)
+        // (512 threads start with 128 registers: 128 x 56 + 256 x 192 + 128 x 72 are all 65536)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int quad = warp & 3, half = (warp - 4) >> 2, col = quad * 32 + lane;       // value column; half of the channels and tokens
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);

@@ -195,3 +195,32 @@ def test_a_long_sequence_without_decays():
     run_scan(m, pr, x, out)
     assert (m.state.cpu().double() - new).norm() <= 1e-6 * new.norm()
     assert (out.cpu().double() - want).norm() <= 2.0e-3 * want.norm()
+
+
+@pytest.mark.parametrize("a", [-16.0, -2.0])
+@pytest.mark.parametrize("phase", [0, 1, 2, 3])
+def test_small_neighbours_between_large_ones(phase, a):
+    """Two small values between two large ones, again and again, wherever the pairs begin."""
+    x = inputs([200, 67], seed=23)
+    t = (torch.arange(267) + phase) % 4
+    x["v"][t < 2] *= 2.0 ** -30
+    x["a"], x["bias"] = torch.full((2,), a), x["bias"] + 3
+    starts, pr = batch_of([200, 67], None, [1, -1])
+    check_scan(layer(8, 2), x, starts, pr, None, [1, -1], "bf16")
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_sizes_drawn_at_random(seed):
+    """Values, keys, states and gates over dozens of powers of two, drawn for every token and column, every token, every column."""
+    gen, lengths = torch.Generator().manual_seed(seed), [[200], [65, 130], [64, 1, 33]][seed % 3]
+    x, T = inputs(lengths, seed=30 + seed), sum(lengths)
+    powers = lambda spread, *shape: 2.0 ** (spread * torch.randn(*shape, generator=gen))  # noqa: E731
+    x["v"] = (x["v"].float() * powers(8, *((T, 2, 128), (T, 1, 1), (1, 1, 128))[seed // 2])).to(torch.bfloat16)
+    if seed % 2:
+        x["k"] = (x["k"].float() * powers(4, T, 1, 128)).to(torch.bfloat16)
+        x["state"] = x["state"] * powers(12, 8, 2, 128, 128)
+        x["b"], x["dt"] = x["b"] * 4, x["dt"] * 4
+    x["a"] = -torch.exp(3 * torch.rand(2, generator=gen) - 1)
+    resume = [1] + [-1] * (len(lengths) - 1)
+    starts, pr = batch_of(lengths, None, resume)
+    check_scan(layer(8, 2), x, starts, pr, None, resume, "bf16")
