@@ -24,8 +24,9 @@
 // Sums of log decays are made in 64 bits and kept as a whole number and a rest of at most a half.
 //
 // What bounds it.  The second kernel: a chunk's chain of products and of the warps' work between them, 3.0 to 3.3 us of which the products are less
-// than a third; a sequence's chunks follow one another.  16384 tokens of 32 heads (SM clock 1965 MHz): one prompt 600 us (125 the first kernel; 286, 21
-// and 167 the passes over five segments, see decode_unit; 881 whole), 48 ragged prompts 450 to 467 by their lengths.  The first kernel: waiting, for loads
+// than a third; a sequence's chunks follow one another.  16384 tokens of 32 heads (SM clock 1965 MHz): one prompt 604 us (126 the first kernel; 291, 22
+// and 160 the passes over five segments, see decode_unit; 881 whole), 48 ragged prompts 450 to 464 by their lengths.  The warp that lays out V needs
+// nearly as long for a chunk as the chain: without its look at the sizes the passes take 274 and 152.  The first kernel: waiting, for loads
 // and for its own warps, and memory, of which it reads and writes 0.45 GB (3.6 TB/s).  100 tokens: 24 us, half of it the first kernel.
 #include "tma.cuh"
 
