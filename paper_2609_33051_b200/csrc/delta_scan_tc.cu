@@ -56,7 +56,7 @@ constexpr uint32_t kCopied = kGOff + kGates * 4u, kBlock = kGOff + kFloats * 4u;
 // weight the state has), or what earlier ones and the state were, less what has decayed since; and no value counts that beta keeps out.  Where they
 // do not (a value or a state 2^16 times as large as the others that a chunk meets, beta below 2^-12 throughout) the columns of a pair of warps go through
 // the chunk token by token, in fp32, and the products meet zeros: 50 to 100 us instead of 3.  It is looked at where two neighbouring tokens are
-// below the floor (of normal numbers one in five million columns and chunks), or the state that a unit begins with, or a beta below kLeastBeta; a look
+// below the floor (of normal numbers one in ten million columns and chunks), or the state that a unit begins with, or a beta below kLeastBeta; a look
 // takes 2 us, and 12 where nobody has run its instructions lately.
 // (The floor: 2^-25 is 2^-18 of it, and what shows of it in outputs and states, measured where there was no floor, a twentieth of that: the tests' bound
 // is 2^-18.7.  With a floor of 1 / 32 there were looks in one of four calls of 16384 tokens.)
